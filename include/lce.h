@@ -53,8 +53,9 @@ typedef enum { LCE_PAD_VALID = 0, LCE_PAD_SAME_ONE = 1, LCE_PAD_SAME_ZERO = 2 } 
 typedef enum { LCE_OUT_FLOAT32 = 0, LCE_OUT_BITPACKED = 1, LCE_OUT_INT32 = 2 } lce_out_type;
 
 /* Fused activation of the float output transform (Section 3.2; Section 5: ReLU before
- * batch-norm in QuickNet).  Applied to the accumulator before multiplier and bias. */
-typedef enum { LCE_ACT_NONE = 0, LCE_ACT_RELU = 1 } lce_activation;
+ * batch-norm in QuickNet).  Applied to the accumulator before multiplier and bias.  SIGMOID is for the gate of
+ * lce_residual_norm only. */
+typedef enum { LCE_ACT_NONE = 0, LCE_ACT_RELU = 1, LCE_ACT_SIGMOID = 2 } lce_activation;
 
 /* Which kernel lce_bconv2d uses; every kernel gives the same, exact result.
  *   TILED  the XOR/POPC kernels on the integer pipes (1x1, 3x3, 5x5 filters, equal strides 1 or 2; a
@@ -278,6 +279,99 @@ lce_status lce_bmaxpool(const uint32_t *in, uint32_t *out, int32_t batch, int32_
 /* fp32 residual add out = a + b (one rounding), the shortcut pattern of Section 5.3
  * (float output -> Add -> LceQuantize).  n == 0 is a no-op; out may equal a or b. */
 lce_status lce_add_f32(const float *a, const float *b, float *out, int64_t n, void *stream);
+
+/* ---- Between the binary projections of a transformer (no counterpart in the paper) ----------------------------
+ * A projection whose weights are binarized is an LceBConv2d with a 1x1 filter over its tokens.  The calls below are
+ * what such a block does between two of them: the key/value cache in 4 bits, attention over it, and the norms, gate
+ * and residual add at the block's boundary with the next LceQuantize folded in. */
+
+/* Element types of their tensors.  Sums, softmax statistics and norms are held in 32 bits or more whatever the type;
+ * an output is rounded to it once. */
+typedef enum { LCE_TYPE_FLOAT32 = 0, LCE_TYPE_FLOAT16 = 1, LCE_TYPE_BFLOAT16 = 2 } lce_type;
+
+/* The cache: a pool of pages, each of page_size tokens (a multiple of 16) of kv_heads heads with head_dim (1 .. 256)
+ * channels of a key and of a value.  Slot s is token s % page_size of page s / page_size; there are fewer than 2^31.
+ * A head's channels are cut into blocks of 32 (the last may be shorter).  A block with values x is held as a scale
+ *   s = the smallest bf16 number with 7 s >= max |x|      (0 if the block is all zeros)
+ * and codes c = x / s rounded to the nearest integer, ties to even (-7 .. 7), that stand for c * s: both exact by
+ * that definition, from any input type.  A block with an infinity or a NaN reads back as NaN throughout, and one whose
+ * largest value is within 1/128 of its type's largest may read back as infinity there.
+ * The buffer holds 4.5 bits a channel in an order of its own: page, head, then tiles of 16 tokens, each
+ *   uint32 K[64 * blocks], V[64 * blocks], scales[16 * blocks]
+ * laid out as the attention kernel's matrix operands want them.  It is the caller's device memory, 16-byte aligned,
+ * lce_kv_cache_bytes(desc) bytes (0 for a malformed descriptor); it need not be cleared before use: what was never
+ * written never counts in lce_kv_attention, and reads back as arbitrary numbers. */
+typedef struct {
+    int32_t pages, page_size, kv_heads, head_dim;
+} lce_kv_desc;
+size_t lce_kv_cache_bytes(const lce_kv_desc *desc);
+
+/* Quantises the keys and values of `tokens` tokens into the cache, token i at slots[i].
+ *   k, v   [tokens][kv_heads][head_dim] of `type`, channels next to one another; strides in elements between tokens
+ *          and between heads, not negative (so k and v may be views into one projection's output)
+ *   slots  int32[tokens]: a slot outside the pool (say -1) skips its token.  No slot may come twice in a call: its
+ *          row would be a mixture of the two.
+ * tokens == 0 is a no-op.  Nothing but the rows of these slots changes. */
+lce_status lce_kv_quantize(const lce_kv_desc *desc, const void *k, const void *v, int32_t type, int64_t tokens, int64_t k_token_stride,
+                           int64_t k_head_stride, int64_t v_token_stride, int64_t v_head_stride, const int32_t *slots, void *cache, void *stream);
+
+/* Reads rows of the cache back: k, v [tokens][kv_heads][head_dim] of `type`, contiguous, row i from slots[i] (any order,
+ * repeats allowed; zeros for a slot outside the pool).  Either of k and v may be NULL.  tokens == 0 is a no-op. */
+lce_status lce_kv_dequantize(const lce_kv_desc *desc, const void *cache, const int32_t *slots, int64_t tokens, int32_t type, void *k, void *v,
+                             void *stream);
+
+/* Attention of each sequence's newest tokens over its pages of the cache.  Sequence b has lengths[b] tokens in the cache, token t
+ * at slot page_table[b][t / page_size] * page_size + t % page_size, and n = q_starts[b + 1] - q_starts[b] rows of q
+ * (q_starts NULL: one row each, tokens == batch).  Its row i stands at position p = lengths[b] - n + i, and for query head h
+ *   out = sum_t softmax_t(scale q . k_t) v_t   over tokens t < lengths[b],  t <= p if causal,  t > p - window if window > 0
+ * with keys and values of head h / (heads / kv_heads).  A row that sees no token (an empty sequence, p < 0) is 0.
+ *   q, out      [tokens][heads][head_dim] of `type`, strides in elements as above; out rows that belong to no sequence stay
+ *   page_table  int32[batch][table_pages]; tokens on a page outside the pool are masked, and so are those behind
+ *               table_pages * page_size
+ *   lengths     int32[batch], q_starts int32[batch + 1] from 0 to tokens, none decreasing; all on the device, so a captured
+ *               call serves growing sequences
+ *   workspace   lce_kv_attention_workspace_bytes(desc) bytes, 16-byte aligned; it needs no clearing and belongs to the call
+ *               until its kernels are done (calls that may overlap need one each)
+ * Long sequences are cut into pieces that are worked on side by side and joined in a fixed order: results repeat bit for bit. */
+typedef struct {
+    lce_kv_desc cache;
+    int32_t batch, heads, table_pages;
+    int32_t type;                  /* lce_type of q and out */
+    int32_t causal, window;        /* 0 or 1; 0: none */
+    float scale;
+    int64_t tokens;                /* rows of q */
+    int64_t q_token_stride, q_head_stride, out_token_stride, out_head_stride;
+} lce_kv_attention_desc;
+size_t lce_kv_attention_workspace_bytes(const lce_kv_attention_desc *desc);
+lce_status lce_kv_attention(const lce_kv_attention_desc *desc, const void *q, const void *cache, const int32_t *page_table,
+                            const int32_t *lengths, const int32_t *q_starts, void *out, void *workspace, size_t workspace_bytes, void *stream);
+
+/* The boundary between two blocks of a residual stream, row by row of `channels` (1 .. 16384):
+ *   u = post_norm(branch) * post_weight + post_bias          the norm behind a block
+ *   y = x + residual_scale * act(gate) * u                    gate and residual scale, the shortcut add
+ *   z = pre_norm(y) * pre_weight + pre_bias                   the norm in front of the next block
+ * RMS: v / sqrt(mean(v^2) + eps); LAYER: (v - mean) / sqrt(variance + eps); NONE: v.  z is taken from y before y is rounded.
+ *   x, y              [rows][channels] of stream_type; y may be x, or NULL
+ *   branch, gate      of `type`; branch NULL: y = x (post_norm NONE, no gate); gate NULL: 1; gate_stride 0: one row for all
+ *   weights, biases   fp32[channels] each, or NULL (1 and 0)
+ *   normed            [rows][channels] of `type`: z; or NULL
+ *   packed            uint32[rows][ceil(channels/32)]: bit (z < 0) of every channel, the next LceQuantize; or NULL.  The
+ *                     arithmetic is then in 64 bits, so that a sign next to 0 is the right one
+ * At least one of y, normed and packed.  Row strides in elements.  gate_activation: LCE_ACT_NONE or LCE_ACT_SIGMOID.
+ * rows == 0 is a no-op. */
+typedef enum { LCE_NORM_NONE = 0, LCE_NORM_RMS = 1, LCE_NORM_LAYER = 2 } lce_norm;
+typedef struct {
+    int64_t rows;
+    int32_t channels;
+    int32_t post_norm, pre_norm;   /* lce_norm */
+    int32_t gate_activation;
+    float eps, residual_scale;
+    int32_t stream_type, type;     /* lce_type */
+    int64_t x_stride, branch_stride, gate_stride, y_stride, normed_stride;
+} lce_residual_norm_desc;
+lce_status lce_residual_norm(const lce_residual_norm_desc *desc, const void *x, const void *branch, const void *gate,
+                             const float *post_weight, const float *post_bias, const float *pre_weight, const float *pre_bias,
+                             void *y, void *normed, uint32_t *packed, void *stream);
 
 /* Status of the bounded device-side waits.  The tensor-core kernel's warps meet through mbarriers
  * (operands ready, MMAs complete, accumulator read out); every such wait is limited to 0.2 s, after

@@ -12,8 +12,11 @@ _LIB_PATH = Path(__file__).resolve().parent / "liblce_b200.so"
 
 PAD_VALID, PAD_SAME_ONE, PAD_SAME_ZERO = 0, 1, 2
 OUT_FLOAT32, OUT_BITPACKED, OUT_INT32 = 0, 1, 2
-ACT_NONE, ACT_RELU = 0, 1
+ACT_NONE, ACT_RELU, ACT_SIGMOID = 0, 1, 2
 KERNEL_AUTO, KERNEL_DIRECT, KERNEL_TILED, KERNEL_TENSOR = 0, 1, 2, 3
+TYPE_FLOAT32, TYPE_FLOAT16, TYPE_BFLOAT16 = 0, 1, 2
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
+_TYPES = {torch.float32: TYPE_FLOAT32, torch.float16: TYPE_FLOAT16, torch.bfloat16: TYPE_BFLOAT16}
 
 
 class LceError(RuntimeError):
@@ -27,6 +30,25 @@ class BConv2dDesc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in (
         "batch", "in_h", "in_w", "in_c", "out_c", "kernel_h", "kernel_w", "stride_h", "stride_w",
         "padding", "out_type", "activation", "kernel", "weights_packed")]
+
+
+class KvDesc(ctypes.Structure):
+    """Mirror of lce_kv_desc."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("pages", "page_size", "kv_heads", "head_dim")]
+
+
+class KvAttentionDesc(ctypes.Structure):
+    """Mirror of lce_kv_attention_desc."""
+    _fields_ = [("cache", KvDesc)] + [(n, ctypes.c_int32) for n in ("batch", "heads", "table_pages", "type", "causal", "window")] + \
+               [("scale", ctypes.c_float)] + \
+               [(n, ctypes.c_int64) for n in ("tokens", "q_token_stride", "q_head_stride", "out_token_stride", "out_head_stride")]
+
+
+class ResidualNormDesc(ctypes.Structure):
+    """Mirror of lce_residual_norm_desc; types and strides are filled in from the tensors of a call."""
+    _fields_ = [("rows", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in ("channels", "post_norm", "pre_norm", "gate_activation")] + \
+               [("eps", ctypes.c_float), ("residual_scale", ctypes.c_float), ("stream_type", ctypes.c_int32), ("type", ctypes.c_int32)] + \
+               [(n, ctypes.c_int64) for n in ("x_stride", "branch_stride", "gate_stride", "y_stride", "normed_stride")]
 
 
 _lib = None
@@ -91,7 +113,16 @@ def library() -> ctypes.CDLL:
         lib.lce_plan_destroy.restype = None
         lib.lce_bmaxpool.argtypes = [vp, vp] + [i32] * 9 + [vp]
         lib.lce_add_f32.argtypes = [vp, vp, vp, i64, vp]
-        for name in ("lce_bitpack", "lce_unpack", "lce_bconv2d_out_shape", "lce_bconv2d", "lce_bconv2d_host",
+        kv, st = ctypes.POINTER(KvDesc), ctypes.c_size_t
+        lib.lce_kv_cache_bytes.argtypes = [kv]
+        lib.lce_kv_cache_bytes.restype = st
+        lib.lce_kv_quantize.argtypes = [kv, vp, vp, i32, i64, i64, i64, i64, i64, vp, vp, vp]
+        lib.lce_kv_dequantize.argtypes = [kv, vp, vp, i64, i32, vp, vp, vp]
+        lib.lce_kv_attention_workspace_bytes.argtypes = [ctypes.POINTER(KvAttentionDesc)]
+        lib.lce_kv_attention_workspace_bytes.restype = st
+        lib.lce_kv_attention.argtypes = [ctypes.POINTER(KvAttentionDesc), vp, vp, vp, vp, vp, vp, vp, st, vp]
+        lib.lce_residual_norm.argtypes = [ctypes.POINTER(ResidualNormDesc)] + [vp] * 11
+        for name in ("lce_kv_quantize", "lce_kv_dequantize", "lce_kv_attention", "lce_residual_norm", "lce_bitpack", "lce_unpack", "lce_bconv2d_out_shape", "lce_bconv2d", "lce_bconv2d_host",
                      "lce_bconv2d_pack_weights",
                      "lce_bmaxpool", "lce_add_f32"):
             getattr(lib, name).restype = ctypes.c_int
@@ -292,6 +323,60 @@ def lce_bmaxpool(words: torch.Tensor, channels: int, pool=(2, 2), stride=(2, 2),
 
 def lce_add_f32(a: torch.Tensor, b: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     return _native.add_f32(a, b, out)
+
+
+def make_kv_desc(pages, page_size, kv_heads, head_dim) -> KvDesc:
+    """A 4-bit key/value cache: a pool of pages of page_size tokens (a multiple of 16)."""
+    return KvDesc(pages, page_size, kv_heads, head_dim)
+
+
+def lce_kv_cache_bytes(desc: KvDesc) -> int:
+    """Bytes of the cache's buffer (a CUDA uint8 tensor); 0 for a malformed descriptor."""
+    return int(library().lce_kv_cache_bytes(ctypes.byref(desc)))
+
+
+def lce_kv_quantize(desc: KvDesc, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, cache: torch.Tensor) -> None:
+    """Quantises keys and values [tokens, kv_heads, head_dim] (fp32, fp16 or bf16; views with strides are fine) into the cache,
+    token i at slots[i] (int32); slots outside the pool are skipped, and no slot may come twice."""
+    _native.kv_quantize(desc, k, v, slots, cache)
+
+
+def lce_kv_dequantize(desc: KvDesc, cache: torch.Tensor, slots: torch.Tensor, dtype: torch.dtype = torch.float32,
+                      k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Reads the rows at `slots` back: (k, v) [tokens, kv_heads, head_dim] of `dtype`, zeros for a slot outside the pool."""
+    return _native.kv_dequantize(desc, cache, slots, _TYPES.get(dtype, -2), k, v)
+
+
+def lce_kv_attention_workspace_bytes(desc: KvDesc, batch: int, tokens: int, heads: int, table_pages: int,
+                                     dtype: torch.dtype = torch.float32) -> int:
+    """Bytes of lce_kv_attention's workspace for q [tokens, heads, head_dim] and a page table [batch, table_pages]."""
+    full = KvAttentionDesc(desc, batch, heads, table_pages, _TYPES.get(dtype, -2), 0, 0, 1.0, tokens, 0, 0, 0, 0)
+    return int(library().lce_kv_attention_workspace_bytes(ctypes.byref(full)))
+
+
+def lce_kv_attention(desc: KvDesc, q: torch.Tensor, cache: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor,
+                     q_starts: Optional[torch.Tensor] = None, scale: Optional[float] = None, causal: bool = True, window: int = 0,
+                     out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of q [tokens, heads, head_dim] over the 4-bit cache.  page_table int32 [sequences, pages]; lengths int32
+    [sequences], the new tokens included; q_starts int32 [sequences + 1] where a sequence's rows of q begin (None: one row for
+    each sequence).  scale: 1 / sqrt(head_dim) when None.  out and workspace (uint8, lce_kv_attention_workspace_bytes) are allocated with
+    torch when not given."""
+    return _native.kv_attention(desc, q, cache, page_table, lengths, q_starts, desc.head_dim ** -0.5 if scale is None else scale,
+                                causal, window, out, workspace)
+
+
+def make_norm_desc(rows, channels, post_norm=NORM_RMS, pre_norm=NORM_RMS, eps=1e-5, residual_scale=1.0,
+                   gate_activation=ACT_NONE) -> ResidualNormDesc:
+    return ResidualNormDesc(rows, channels, post_norm, pre_norm, gate_activation, eps, residual_scale, 0, 0, 0, 0, 0, 0, 0)
+
+
+def lce_residual_norm(desc: ResidualNormDesc, x: torch.Tensor, branch: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+                      post_weight: Optional[torch.Tensor] = None, post_bias: Optional[torch.Tensor] = None,
+                      pre_weight: Optional[torch.Tensor] = None, pre_bias: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
+                      normed: Optional[torch.Tensor] = None, packed: Optional[torch.Tensor] = None) -> None:
+    """y = x + residual_scale * act(gate) * post_norm(branch), z = pre_norm(y): the caller supplies whichever of y, normed (z) and
+    packed (LceQuantize of z) it wants.  x and y are fp32 or of the type of branch, gate and normed."""
+    _native.residual_norm(desc, x, branch, gate, post_weight, post_bias, pre_weight, pre_bias, y, normed, packed)
 
 
 def lce_device_status() -> int:

@@ -1,0 +1,765 @@
+// Attention over the 4-bit key/value cache.
+//
+// For the rows of one sequence that share a key/value head (its new tokens x the group's query heads: the "columns" here) the
+// keys and values are read once: S = K Q^T and O = V^T P, with the 4-bit operand on the 16-row side of m16n8k16 products and 8 or
+// 16 columns on the other.  What bounds a decode step is reading the cache, 4.5 bits a channel, so the arithmetic between the
+// 4-bit words and the matrix operands is kept to a minimum:
+//
+//   keys    a code n = c + 8 of four bits is, as it stands in a 16-bit half, the subnormal f16 number n 2^-24 (or 16 n 2^-24 in
+//           bits 4 .. 7): one AND makes a pair of operands, five instructions eight codes.  The 16 goes into Q, the 8 into the
+//           accumulators' initial value, -8 sum(q) over the block, and the block's scale multiplies the finished sums.
+//   values  want their sign (a sum over a long sequence would lose its last bits next to 8 sum(p)): f16 1024 + n by one
+//           AND-OR, less 1032 by one packed add: nine instructions eight codes.  The block's scale multiplies p, in fp32, before
+//           it is rounded to f16.
+//
+// Scores and the running softmax are fp32.  Q is f16 times a power of two chosen for each row, exact for f16 and bf16 rows up to
+// what lies 2^-29 below the row's largest; p is rounded to f16 (relative error 2^-11 of each weight, which is what an fp16
+// result has, and averages out).  fp32 rows take Q and p as two f16 numbers each (22 bits).
+#include "kv_common.cuh"
+
+#include <math.h>
+
+namespace lce {
+namespace {
+
+constexpr int kWarps = 4, kThreads = 32 * kWarps;
+constexpr int kStages = 4;                // tiles in flight of a warp
+constexpr float kRise = 4.0f;             // a running maximum is raised when a score passes it by 2^4
+constexpr float kHeadroom = 10.0f;        // weights are held times 2^10: 2^(10 + 4 + 1) is the most that meets f16
+constexpr float kLowest = -1e30f;
+
+struct AttnParams {
+    KvGeom g;
+    int32_t batch, group, table_pages, table_tokens;
+    int32_t causal, window, type;
+    int64_t tokens;
+    int64_t q_token, q_head, out_token, out_head;
+    float scale;                       // times log2(e)
+    const void *q;
+    const uint32_t *cache;
+    const int32_t *page_table, *lengths, *q_starts;
+    void *out;
+    float *parts;                      // [unit][kv head][column][32 blocks + 2]: sums, largest, weight
+    int32_t units, target, least_tiles;
+};
+
+// What a unit (a range of tiles for one tile of columns of a sequence) works on.
+struct Unit {
+    int32_t seq, column0, chunk, chunks, first_unit;  // first_unit: of this column tile
+    int32_t length, rows;                             // tokens of the sequence, its rows of q
+    int64_t row0;                                     // its first row of q
+    int32_t tile0, tile1;                             // the unit's tiles
+};
+
+struct Sequence {
+    int32_t length, rows, column_tiles, first_tile, tiles;
+    int64_t row0;
+};
+
+template <int COLUMNS>
+__device__ __forceinline__ Sequence sequence(const AttnParams &p, int b)
+{
+    Sequence s{};
+    if (b >= p.batch) return s;
+    s.length = min(max(__ldg(p.lengths + b), 0), p.table_tokens);
+    s.row0 = b;
+    s.rows = 1;
+    if (p.q_starts) {
+        const int64_t from = min(max((int64_t)__ldg(p.q_starts + b), (int64_t)0), p.tokens), to = min(max((int64_t)__ldg(p.q_starts + b + 1), from), p.tokens);
+        s.row0 = from;
+        s.rows = (int32_t)(to - from);
+    }
+    s.column_tiles = (int32_t)(((int64_t)s.rows * p.group + COLUMNS - 1) / COLUMNS);
+    // tiles that some row sees
+    int32_t low = 0;
+    if (p.window > 0) low = (int32_t)max((int64_t)s.length - s.rows + 1 - p.window, (int64_t)0);
+    s.first_tile = low / kKvTile;
+    s.tiles = max((s.length + kKvTile - 1) / kKvTile - s.first_tile, 0);
+    return s;
+}
+
+__device__ __forceinline__ int32_t warp_sum(int32_t v)
+{
+    return __reduce_add_sync(0xffffffffu, v);
+}
+
+// The work is cut evenly whatever the sequences' lengths: every column tile of a sequence into pieces of at most `most` tiles, where
+// `most` follows from the whole batch's tiles.  Every warp works this out for itself from the lengths (no launch in front, no host
+// copy of them).  False: there is no such unit.
+template <int COLUMNS>
+__device__ __forceinline__ bool find_unit(const AttnParams &p, int unit, Unit *u)
+{
+    const int lane = threadIdx.x & 31;
+    int64_t total = 0;
+    for (int b0 = 0; b0 < p.batch; b0 += 32) {
+        const Sequence s = sequence<COLUMNS>(p, b0 + lane);
+        int64_t t = (int64_t)s.column_tiles * s.tiles;
+#pragma unroll
+        for (int d = 16; d; d >>= 1) t += __shfl_xor_sync(0xffffffffu, t, d);
+        total += t;
+    }
+    const int32_t most = (int32_t)max((total + p.target - 1) / p.target, (int64_t)p.least_tiles);
+    int before = 0;
+    for (int b0 = 0; b0 < p.batch; b0 += 32) {
+        const Sequence s = sequence<COLUMNS>(p, b0 + lane);
+        const int32_t chunks = max((s.tiles + most - 1) / most, 1), mine = s.column_tiles * chunks;
+        int32_t upto = mine;  // units of this and the lanes below
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int32_t o = __shfl_up_sync(0xffffffffu, upto, d);
+            if (lane >= d) upto += o;
+        }
+        const uint32_t has = __ballot_sync(0xffffffffu, before + upto > unit);
+        if (has) {
+            const int from = __ffs(has) - 1;
+            const int32_t first = before + __shfl_sync(0xffffffffu, upto - mine, from);
+            u->seq = b0 + from;
+            u->chunks = __shfl_sync(0xffffffffu, chunks, from);
+            u->length = __shfl_sync(0xffffffffu, s.length, from);
+            u->rows = __shfl_sync(0xffffffffu, s.rows, from);
+            u->row0 = __shfl_sync(0xffffffffu, s.row0, from);
+            const int32_t tiles = __shfl_sync(0xffffffffu, s.tiles, from), first_tile = __shfl_sync(0xffffffffu, s.first_tile, from);
+            const int32_t at = unit - first, column_tile = at / u->chunks;
+            u->chunk = at - column_tile * u->chunks;
+            u->column0 = column_tile * COLUMNS;
+            u->first_unit = first + column_tile * u->chunks;
+            // equal pieces
+            u->tile0 = first_tile + (int32_t)((int64_t)tiles * u->chunk / u->chunks);
+            u->tile1 = first_tile + (int32_t)((int64_t)tiles * (u->chunk + 1) / u->chunks);
+            return true;
+        }
+        before += __shfl_sync(0xffffffffu, upto, 31);
+    }
+    return false;
+}
+
+// Tokens [lo, hi) that the row of a column sees; none for a column that does not exist.
+__device__ __forceinline__ void column_range(const AttnParams &p, const Unit &u, int column, int32_t *lo, int32_t *hi)
+{
+    const int32_t row = column / p.group;
+    *lo = *hi = 0;
+    if (row >= u.rows) return;
+    const int64_t position = (int64_t)u.length - u.rows + row;
+    *hi = p.causal ? (int32_t)min(max(position + 1, (int64_t)0), (int64_t)u.length) : u.length;
+    *lo = p.window > 0 ? (int32_t)min(max(position + 1 - p.window, (int64_t)0), (int64_t)u.length) : 0;
+}
+
+__device__ __forceinline__ float load_element(const void *p, int32_t type, int64_t i)
+{
+    switch (type) {
+        case LCE_TYPE_FLOAT32: return static_cast<const float *>(p)[i];
+        case LCE_TYPE_FLOAT16: return __half2float(static_cast<const __half *>(p)[i]);
+        default: return __bfloat162float(static_cast<const __nv_bfloat16 *>(p)[i]);
+    }
+}
+__device__ __forceinline__ void store_element(void *p, int32_t type, int64_t i, float v)
+{
+    switch (type) {
+        case LCE_TYPE_FLOAT32: static_cast<float *>(p)[i] = v; return;
+        case LCE_TYPE_FLOAT16: static_cast<__half *>(p)[i] = __float2half_rn(v); return;
+        default: static_cast<__nv_bfloat16 *>(p)[i] = __float2bfloat16_rn(v); return;
+    }
+}
+
+__device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t mask, uint32_t with)
+{
+    uint32_t d;
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(a), "r"(mask), "r"(with));
+    return d;
+}
+__device__ __forceinline__ uint32_t pack_half2(float lo, float hi)
+{
+    uint32_t d;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    return d;
+}
+__device__ __forceinline__ float half_low(uint32_t v) { return __half2float(__ushort_as_half((unsigned short)(v & 0xffffu))); }
+__device__ __forceinline__ float half_high(uint32_t v) { return __half2float(__ushort_as_half((unsigned short)(v >> 16))); }
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v)
+{
+    uint32_t d;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
+    return d;
+}
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float exp2_fast(float x)
+{
+    float d;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(d) : "f"(x));
+    return d;
+}
+
+// Pairs (low half, high half) of value codes 2 i, 2 i + 1 of a word as f16 numbers c = n - 8.
+__device__ __forceinline__ uint32_t value_even(uint32_t w)
+{
+    const __half2 v = __hadd2(*reinterpret_cast<const __half2 *>(&w), __half2half2(__ushort_as_half(0xe408)));  // - 1032
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+__device__ __forceinline__ uint32_t value_odd(uint32_t w)
+{
+    const __half2 v = __hfma2(*reinterpret_cast<const __half2 *>(&w), __half2half2(__ushort_as_half(0x2c00)), __half2half2(__ushort_as_half(0xd480)));  // / 16 - 72
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+
+// W words of a lane from shared memory.
+template <int W>
+__device__ __forceinline__ void load_words(const uint32_t *p, uint32_t (&w)[W])
+{
+    if (W == 4) {
+        const uint4 v = *reinterpret_cast<const uint4 *>(p);
+        w[0] = v.x; w[W > 1 ? 1 : 0] = v.y; w[W > 2 ? 2 : 0] = v.z; w[W > 3 ? 3 : 0] = v.w;
+    } else if (W == 2) {
+        const uint2 v = *reinterpret_cast<const uint2 *>(p);
+        w[0] = v.x; w[W > 1 ? 1 : 0] = v.y;
+    } else {
+        w[0] = *p;
+    }
+}
+
+__device__ __forceinline__ void cp_async16(uint32_t smem, const void *g)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(g) : "memory");
+}
+
+constexpr size_t ring_bytes(int blocks) { return (size_t)kWarps * kStages * kv_tile_words(blocks) * 4; }
+
+// B blocks of 32 channels, NT tiles of 8 columns, SPLIT: fp32 rows.
+template <int B, int NT, bool SPLIT>
+struct Warp {
+    float o[B][2][NT][4];        // sums of c p: channels 32 b + 4 (lane / 4) + 2 i + {0, 1}, columns 8 nt + 2 (lane % 4) + {0, 1}
+    float top[NT][2], weight[NT][2];  // of the lane's columns
+    float high;                  // scales above this want a higher reference
+    float shift;                 // kHeadroom - log2 of the scales' reference
+    uint32_t qf[B][2][NT][2];    // B operands of the keys' products
+    uint32_t ql[SPLIT ? B : 1][2][NT][2];
+    float init[B][NT][2];        // -8 sum(q) of the block, as the products count
+    float factor[NT][2];         // scores = factor * sum over blocks
+    int32_t lo[NT][2], hi[NT][2];
+};
+
+template <int B, int NT, bool SPLIT>
+__device__ __forceinline__ void load_queries(const AttnParams &p, const Unit &u, int head, Warp<B, NT, SPLIT> &w)
+{
+    const int lane = threadIdx.x & 31, n = lane >> 2, quarter = lane & 3;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int column = u.column0 + 8 * nt + n, row = column / p.group;
+        const bool there = row < u.rows;
+        const int64_t at = (u.row0 + row) * p.q_token + ((int64_t)head * p.group + (column - row * p.group)) * p.q_head;
+        float v[B][8];
+        float top = 0.0f;
+        bool finite = true;
+#pragma unroll
+        for (int b = 0; b < B; ++b)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int c = 32 * b + 8 * quarter + i;
+                v[b][i] = there && c < p.g.dim ? load_element(p.q, p.type, at + c) : 0.0f;
+                finite = finite && fabsf(v[b][i]) <= 3.4028234e38f;
+                top = fmaxf(top, fabsf(v[b][i]));
+            }
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        finite = __ballot_sync(0xffffffffu, !finite) >> (lane & 28) & 15 ? false : true;
+        // times 2^k, so that the largest is in [2^14, 2^15)
+        int e = 0;
+        if (top > 0.0f && finite) e = ilogbf(top);
+        const int k = 14 - e, k1 = k / 2, k2 = k - k1;
+        const float s1 = __uint_as_float((uint32_t)(127 + k1) << 23), s2 = __uint_as_float((uint32_t)(127 + k2) << 23);
+#pragma unroll
+        for (int b = 0; b < B; ++b) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                // codes 2 m and 2 m + 4 as they are, 2 m + 1 and 2 m + 5 times 16
+                const float x0 = v[b][2 * m] * s1 * s2, x1 = v[b][2 * m + 4] * s1 * s2, y0 = v[b][2 * m + 1] * s1 * s2 * 0.0625f,
+                            y1 = v[b][2 * m + 5] * s1 * s2 * 0.0625f;
+                const uint32_t a = pack_half2(x0, x1), c = pack_half2(y0, y1);
+                w.qf[b][m][nt][0] = a;
+                w.qf[b][m][nt][1] = c;
+                sum += half_low(a) + half_high(a) + 16.0f * (half_low(c) + half_high(c));
+                if (SPLIT) {
+                    const uint32_t al = pack_half2(x0 - half_low(a), x1 - half_high(a)), cl = pack_half2(y0 - half_low(c), y1 - half_high(c));
+                    w.ql[SPLIT ? b : 0][m][nt][0] = al;
+                    w.ql[SPLIT ? b : 0][m][nt][1] = cl;
+                    sum += half_low(al) + half_high(al) + 16.0f * (half_low(cl) + half_high(cl));
+                }
+            }
+            sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+            sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+            sum *= -8.0f * 0x1p-24f;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) w.init[b][nt][j] = __shfl_sync(0xffffffffu, sum, (2 * quarter + j) * 4);
+        }
+        // what the sums of 2^-24 2^k code * q are multiplied with (2^24 2^-k scale, in steps that stay in range)
+        const float f = finite ? p.scale : __uint_as_float(0x7fc00000u);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int from = (2 * quarter + j) * 4, kc = 24 - __shfl_sync(0xffffffffu, k, from), c1 = kc / 2, c2 = kc - c1;
+            w.factor[nt][j] = __shfl_sync(0xffffffffu, f, from) * __uint_as_float((uint32_t)(127 + c1) << 23) * __uint_as_float((uint32_t)(127 + c2) << 23);
+            column_range(p, u, u.column0 + 8 * nt + 2 * quarter + j, &w.lo[nt][j], &w.hi[nt][j]);
+        }
+    }
+}
+
+// Scores of tokens 8 r + lane / 4 of the tile for the lane's columns, the blocks of one plane.
+template <int B, int NT, bool SPLIT, int FIRST, int W>
+__device__ __forceinline__ void plane_scores(const uint32_t *tile, const Warp<B, NT, SPLIT> &w, const uint32_t (&sc)[2][B], float (&s)[2][NT][2])
+{
+    const int lane = threadIdx.x & 31;
+    uint32_t k[2][W];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) load_words<W>(tile + 64 * FIRST + (32 * h + lane) * W, k[h]);
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        constexpr uint32_t kEven = 0x000f000fu, kOdd = 0x00f000f0u;
+        const int b = FIRST + i;
+        const uint32_t u0 = k[0][i], u1 = k[1][i], v0 = u0 >> 8, v1 = u1 >> 8;
+        const float s0 = __uint_as_float(sc[0][b] << 16), s1 = __uint_as_float(sc[1][b] << 16);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            float d[4] = {w.init[b][nt][0], w.init[b][nt][1], w.init[b][nt][0], w.init[b][nt][1]};
+            mma(d, u0 & kEven, u1 & kEven, u0 & kOdd, u1 & kOdd, w.qf[b][0][nt][0], w.qf[b][0][nt][1]);
+            mma(d, v0 & kEven, v1 & kEven, v0 & kOdd, v1 & kOdd, w.qf[b][1][nt][0], w.qf[b][1][nt][1]);
+            if (SPLIT) {
+                mma(d, u0 & kEven, u1 & kEven, u0 & kOdd, u1 & kOdd, w.ql[SPLIT ? b : 0][0][nt][0], w.ql[SPLIT ? b : 0][0][nt][1]);
+                mma(d, v0 & kEven, v1 & kEven, v0 & kOdd, v1 & kOdd, w.ql[SPLIT ? b : 0][1][nt][0], w.ql[SPLIT ? b : 0][1][nt][1]);
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                s[0][nt][j] = fmaf(s0, d[j], s[0][nt][j]);
+                s[1][nt][j] = fmaf(s1, d[2 + j], s[1][nt][j]);
+            }
+        }
+    }
+}
+
+// O += V^T P over the tile, the blocks of one plane.  e: weights; shown: whether the column sees the token (only where MASKED).
+template <int B, int NT, bool SPLIT, int FIRST, int W, bool MASKED>
+__device__ __forceinline__ void plane_values(const uint32_t *tile, Warp<B, NT, SPLIT> &w, const uint32_t (&sc)[2][B], const float (&e)[2][NT][2],
+                                             const bool (&shown)[2][NT][2])
+{
+    const int lane = threadIdx.x & 31;
+    uint32_t v[2][W];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) load_words<W>(tile + 64 * B + 64 * FIRST + (32 * h + lane) * W, v[h]);
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        constexpr uint32_t kEven = 0x000f000fu, kOdd = 0x00f000f0u, kBase = 0x64006400u;
+        const int b = FIRST + i;
+        uint32_t a[2][4];  // [half][channel]
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t x = v[h][i], y = x >> 8;
+            a[h][0] = value_even(and_or(x, kEven, kBase));
+            a[h][1] = value_odd(and_or(x, kOdd, kBase));
+            a[h][2] = value_even(and_or(y, kEven, kBase));
+            a[h][3] = value_odd(and_or(y, kOdd, kBase));
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            uint32_t ph[2], pl[2];
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const float s = __uint_as_float(sc[r][b] & 0xffff0000u);
+                float x0 = e[r][nt][0] * s, x1 = e[r][nt][1] * s;
+                if (MASKED) {  // whatever stands behind a sequence's last token
+                    x0 = shown[r][nt][0] ? x0 : 0.0f;
+                    x1 = shown[r][nt][1] ? x1 : 0.0f;
+                }
+                const uint32_t packed = pack_half2(x0, x1);
+                ph[r] = transpose8x8(packed);
+                if (SPLIT) pl[r] = transpose8x8(pack_half2(x0 - half_low(packed), x1 - half_high(packed)));
+            }
+            mma(w.o[b][0][nt], a[0][0], a[0][1], a[1][0], a[1][1], ph[0], ph[1]);
+            mma(w.o[b][1][nt], a[0][2], a[0][3], a[1][2], a[1][3], ph[0], ph[1]);
+            if (SPLIT) {
+                mma(w.o[b][0][nt], a[0][0], a[0][1], a[1][0], a[1][1], pl[0], pl[1]);
+                mma(w.o[b][1][nt], a[0][2], a[0][3], a[1][2], a[1][3], pl[0], pl[1]);
+            }
+        }
+    }
+}
+
+template <int B, int NT, bool SPLIT, bool MASKED>
+__device__ __forceinline__ void tile_step(const uint32_t *tile, int32_t token0, Warp<B, NT, SPLIT> &w)
+{
+    constexpr int Q = B / 4 * 4;
+    constexpr bool T = (B & 2) != 0, S = (B & 1) != 0;
+    const int lane = threadIdx.x & 31;
+    uint32_t sc[2][B];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const uint32_t *at = tile + 128 * B;
+        const int token = 8 * r + (lane >> 2);
+#pragma unroll
+        for (int f = 0; f < Q; f += 4) {
+            uint32_t x[4];
+            load_words<4>(at + 16 * f + 4 * token, x);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sc[r][f + i] = x[i];
+        }
+        if (T) {
+            uint32_t x[2];
+            load_words<2>(at + 16 * Q + 2 * token, x);
+            sc[r][T ? Q : 0] = x[0];
+            sc[r][T ? Q + 1 : 0] = x[1];
+        }
+        if (S) sc[r][B - 1] = at[16 * (B - 1) + token];
+    }
+    float s[2][NT][2] = {};
+    if (Q > 0) plane_scores<B, NT, SPLIT, 0, 4>(tile, w, sc, s);
+    if (Q > 4) plane_scores<B, NT, SPLIT, (Q > 4 ? 4 : 0), 4>(tile, w, sc, s);
+    if (T) plane_scores<B, NT, SPLIT, (T ? Q : 0), 2>(tile, w, sc, s);
+    if (S) plane_scores<B, NT, SPLIT, B - 1, 1>(tile, w, sc, s);
+    bool shown[2][NT][2];
+    uint32_t largest = 0;  // scale of a value of the lane's tokens
+    bool some[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        some[r] = !MASKED;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                s[r][nt][j] *= w.factor[nt][j];
+                shown[r][nt][j] = true;
+                if (MASKED) {
+                    const int32_t token = token0 + 8 * r + (lane >> 2);
+                    shown[r][nt][j] = token >= w.lo[nt][j] && token < w.hi[nt][j];
+                    if (!shown[r][nt][j]) s[r][nt][j] = -INFINITY;
+                    some[r] = some[r] || shown[r][nt][j];
+                }
+            }
+#pragma unroll
+        for (int b = 0; b < B; ++b)
+            if (some[r] && sc[r][b] < 0x7f800000u) largest = max(largest, sc[r][b]);  // the value's scale is the high half; NaN aside
+    }
+    bool above = __uint_as_float(largest & 0xffff0000u) > w.high;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) above = above || fmaxf(s[0][nt][j], s[1][nt][j]) > w.top[nt][j] + kRise;
+    if (__any_sync(0xffffffffu, above)) {
+        // rare behind the first tiles: the references move up and the sums with them
+        float reference = __uint_as_float(largest & 0xffff0000u);
+#pragma unroll
+        for (int d = 16; d; d >>= 1) reference = fmaxf(reference, __shfl_xor_sync(0xffffffffu, reference, d));
+        const float old_shift = w.shift;
+        if (reference > w.high) {
+            const int e = max(ilogbf(reference) + 1, -100);  // reference < 2^e; the weights themselves stay in range
+            w.shift = kHeadroom - (float)e;
+            w.high = __uint_as_float((uint32_t)(127 + e) << 23);
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                float m = fmaxf(s[0][nt][j], s[1][nt][j]);
+                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
+                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
+                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
+                const float top = fmaxf(m, w.top[nt][j]);
+                const float f = exp2f((w.top[nt][j] - top) + (w.shift - old_shift));
+                w.top[nt][j] = top;
+                w.weight[nt][j] *= f;
+#pragma unroll
+                for (int b = 0; b < B; ++b)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        w.o[b][i][nt][j] *= f;
+                        w.o[b][i][nt][2 + j] *= f;
+                    }
+            }
+    }
+    float e[2][NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const float base = w.shift - w.top[nt][j];
+#pragma unroll
+            for (int r = 0; r < 2; ++r) e[r][nt][j] = exp2_fast(s[r][nt][j] + base);
+            w.weight[nt][j] += e[0][nt][j] + e[1][nt][j];
+        }
+    if (Q > 0) plane_values<B, NT, SPLIT, 0, 4, MASKED>(tile, w, sc, e, shown);
+    if (Q > 4) plane_values<B, NT, SPLIT, (Q > 4 ? 4 : 0), 4, MASKED>(tile, w, sc, e, shown);
+    if (T) plane_values<B, NT, SPLIT, (T ? Q : 0), 2, MASKED>(tile, w, sc, e, shown);
+    if (S) plane_values<B, NT, SPLIT, B - 1, 1, MASKED>(tile, w, sc, e, shown);
+}
+
+template <int B, int NT, bool SPLIT>
+__global__ void __launch_bounds__(kThreads) kv_attention_kernel(const __grid_constant__ AttnParams p)
+{
+    constexpr int COLUMNS = 8 * NT, TILE = kv_tile_words(B), PIECES = TILE / 4;
+    extern __shared__ __align__(128) uint32_t smem[];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    Unit u;
+    if (!find_unit<COLUMNS>(p, blockIdx.x, &u)) return;
+    const int head = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    Warp<B, NT, SPLIT> w;
+    load_queries(p, u, head, w);
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            w.top[nt][j] = kLowest;
+            w.weight[nt][j] = 0.0f;
+        }
+#pragma unroll
+    for (int b = 0; b < B; ++b)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w.o[b][i][nt][j] = 0.0f;
+    w.high = 0.0f;
+    w.shift = 0.0f;
+
+    // tokens that every column sees, and those that one sees at least
+    int32_t all_lo = 0, all_hi = 0x7fffffff, any_lo = 0x7fffffff, any_hi = 0;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            if (w.hi[nt][j] > w.lo[nt][j]) {
+                all_lo = max(all_lo, w.lo[nt][j]);
+                all_hi = min(all_hi, w.hi[nt][j]);
+                any_lo = min(any_lo, w.lo[nt][j]);
+                any_hi = max(any_hi, w.hi[nt][j]);
+            }
+        }
+    all_lo = __reduce_max_sync(0xffffffffu, all_lo);
+    all_hi = __reduce_min_sync(0xffffffffu, all_hi);
+    any_lo = __reduce_min_sync(0xffffffffu, any_lo);
+    any_hi = __reduce_max_sync(0xffffffffu, any_hi);
+    const int32_t tile0 = any_hi > 0 ? max(u.tile0, any_lo / kKvTile) : u.tile1, tile1 = min(u.tile1, (any_hi + kKvTile - 1) / kKvTile);
+
+    uint32_t *const ring = smem + warp * kStages * TILE;
+    const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
+    const int32_t *const table = p.page_table + (int64_t)u.seq * p.table_pages;
+    const int tiles_per_page = p.g.page_size / kKvTile;
+    // pages of the warp's next 32 tiles, one to a lane
+    int32_t pages = -1;
+    const int32_t mine = max((tile1 - tile0 - warp + kWarps - 1) / kWarps, 0);
+    auto fetch = [&](int i) {  // issues the copies of the warp's i-th tile
+        if ((i & 31) == 0) {
+            const int32_t t = tile0 + warp + (i + lane) * kWarps;
+            pages = t < tile1 ? __ldg(table + t / tiles_per_page) : -1;
+        }
+        const int32_t page = __shfl_sync(0xffffffffu, pages, i & 31);
+        if (i < mine && page >= 0 && page < p.g.pages) {
+            const int32_t t = tile0 + warp + i * kWarps;
+            const uint4 *from = reinterpret_cast<const uint4 *>(p.cache + (((int64_t)page * p.g.heads + head) * tiles_per_page + t % tiles_per_page) * TILE);
+            const uint32_t to = ring_at + (i % kStages) * TILE * 4;
+#pragma unroll
+            for (int c = 0; c < (PIECES + 31) / 32; ++c)
+                if (c * 32 + lane < PIECES) cp_async16(to + (c * 32 + lane) * 16, from + c * 32 + lane);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        return page >= 0 && page < p.g.pages;
+    };
+    uint32_t good = 0;  // whether the tile of a stage is there
+#pragma unroll
+    for (int i = 0; i < kStages - 1; ++i) good |= fetch(i) ? 1u << i : 0u;
+    for (int i = 0; i < mine; ++i) {
+        __syncwarp();  // everyone is done with the stage that comes next
+        const int next = (i + kStages - 1) % kStages;
+        good = (good & ~(1u << next)) | (fetch(i + kStages - 1) ? 1u << next : 0u);
+        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+        __syncwarp();
+        if (!(good >> (i % kStages) & 1)) continue;
+        const int32_t token0 = (tile0 + warp + i * kWarps) * kKvTile;
+        const uint32_t *const tile = ring + (i % kStages) * TILE;
+        if (token0 >= all_lo && token0 + kKvTile <= all_hi) tile_step<B, NT, SPLIT, false>(tile, token0, w);
+        else tile_step<B, NT, SPLIT, true>(tile, token0, w);
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncthreads();
+
+    // The warps' sums meet in shared memory: [warp][column][32 B], largest and weight of each behind them.
+    constexpr int D = 32 * B;
+    float *const sums = reinterpret_cast<float *>(smem), *const tops = sums + kWarps * COLUMNS * D, *const weights = tops + kWarps * COLUMNS;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int column = 8 * nt + 2 * (lane & 3) + j;
+            float l = w.weight[nt][j];
+            l += __shfl_xor_sync(0xffffffffu, l, 4);
+            l += __shfl_xor_sync(0xffffffffu, l, 8);
+            l += __shfl_xor_sync(0xffffffffu, l, 16);
+            if (lane < 4) {
+                tops[warp * COLUMNS + column] = w.top[nt][j] - w.shift;
+                weights[warp * COLUMNS + column] = l;
+            }
+            float *const to = sums + (warp * COLUMNS + column) * D + 4 * (lane >> 2);
+#pragma unroll
+            for (int b = 0; b < B; ++b)
+                *reinterpret_cast<float4 *>(to + 32 * b) = make_float4(w.o[b][0][nt][j], w.o[b][0][nt][2 + j], w.o[b][1][nt][j], w.o[b][1][nt][2 + j]);
+        }
+    __syncthreads();
+    for (int at = threadIdx.x; at < COLUMNS * D; at += kThreads) {
+        const int column = at / D, c = at % D;
+        float top = tops[column];
+#pragma unroll
+        for (int i = 1; i < kWarps; ++i) top = fmaxf(top, tops[i * COLUMNS + column]);
+        float sum = 0.0f, weight = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kWarps; ++i) {
+            const float f = exp2f(tops[i * COLUMNS + column] - top);
+            sum = fmaf(f, sums[(i * COLUMNS + column) * D + c], sum);
+            weight = fmaf(f, weights[i * COLUMNS + column], weight);
+        }
+        if (u.chunks > 1) {
+            float *const to = p.parts + (((int64_t)blockIdx.x * p.g.heads + head) * COLUMNS + column) * (D + 2);
+            to[c] = sum;
+            if (c == 0) {
+                to[D] = top;
+                to[D + 1] = weight;
+            }
+        } else {
+            const int q = u.column0 + column, row = q / p.group;
+            if (row < u.rows && c < p.g.dim)
+                store_element(p.out, p.type, (u.row0 + row) * p.out_token + ((int64_t)head * p.group + (q - row * p.group)) * p.out_head + c,
+                              weight == 0.0f ? 0.0f : sum / weight);
+        }
+    }
+}
+
+// Joins the pieces of a column, always in the same order.  A block to each column of a column tile.
+template <int NT>
+__global__ void __launch_bounds__(128) kv_attention_join_kernel(const __grid_constant__ AttnParams p)
+{
+    constexpr int COLUMNS = 8 * NT;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    Unit u;
+    if (!find_unit<COLUMNS>(p, blockIdx.x, &u)) return;
+    if (u.chunks == 1 || u.chunk != 0) return;
+    const int head = blockIdx.y, column = blockIdx.z, D = 32 * p.g.blocks;
+    const int q = u.column0 + column, row = q / p.group;
+    if (row >= u.rows) return;
+    const int64_t step = (int64_t)p.g.heads * COLUMNS * (D + 2);
+    const float *const from = p.parts + (((int64_t)blockIdx.x * p.g.heads + head) * COLUMNS + column) * (D + 2);
+    const int chunks = min(u.chunks, p.units - (int)blockIdx.x);
+    float top = -INFINITY;
+    for (int i = 0; i < chunks; ++i) top = fmaxf(top, from[i * step + D]);
+    for (int c = threadIdx.x; c < p.g.dim; c += 128) {
+        float sum = 0.0f, weight = 0.0f;
+        for (int i = 0; i < chunks; ++i) {
+            const float f = exp2f(from[i * step + D] - top);
+            sum = fmaf(f, from[i * step + c], sum);
+            weight = fmaf(f, from[i * step + D + 1], weight);
+        }
+        store_element(p.out, p.type, (u.row0 + row) * p.out_token + ((int64_t)head * p.group + (q - row * p.group)) * p.out_head + c,
+                      weight == 0.0f ? 0.0f : sum / weight);
+    }
+}
+
+constexpr size_t merge_bytes(int blocks, int nt) { return (size_t)kWarps * 8 * nt * (32 * blocks + 2) * 4; }
+
+template <int B, int NT, bool SPLIT>
+lce_status launch(const AttnParams &p, cudaStream_t s)
+{
+    constexpr size_t smem = ring_bytes(B) > merge_bytes(B, NT) ? ring_bytes(B) : merge_bytes(B, NT);
+    static SmemOptIn opt_in;
+    if (!opt_in.ensure(kv_attention_kernel<B, NT, SPLIT>, smem)) return LCE_ERR_CUDA;
+    const lce_status st = launch_dependent(kv_attention_kernel<B, NT, SPLIT>, dim3((unsigned)p.units, (unsigned)p.g.heads), kThreads, smem, s, p);
+    if (st != LCE_OK) return st;
+    return launch_dependent(kv_attention_join_kernel<NT>, dim3((unsigned)p.units, (unsigned)p.g.heads, 8 * NT), 128, 0, s, p);
+}
+
+// 16 columns where their sums and operands fit a thread's registers
+constexpr int kWideBlocks = 4;
+
+template <int NT, bool SPLIT>
+lce_status launch_blocks(const AttnParams &p, cudaStream_t s)
+{
+    constexpr int N = 1;
+    switch (p.g.blocks) {
+        case 1: return launch<1, NT, SPLIT>(p, s);
+        case 2: return launch<2, NT, SPLIT>(p, s);
+        case 3: return launch<3, NT, SPLIT>(p, s);
+        case 4: return launch<4, NT, SPLIT>(p, s);
+        case 5: return launch<5, N, SPLIT>(p, s);
+        case 6: return launch<6, N, SPLIT>(p, s);
+        case 7: return launch<7, N, SPLIT>(p, s);
+        default: return launch<8, N, SPLIT>(p, s);
+    }
+}
+
+int64_t column_tiles(const AttnParams &p, int columns) { return p.tokens * p.group / columns + p.batch; }
+
+lce_status make_params(const lce_kv_attention_desc *d, AttnParams *p, int *nt)
+{
+    if (!d) return LCE_ERR_INVALID_ARG;
+    const lce_status st = make_kv_geom(&d->cache, &p->g);
+    if (st != LCE_OK) return st;
+    if (d->batch <= 0 || d->heads <= 0 || d->table_pages <= 0 || d->tokens < 0 || d->window < 0 || !type_known(d->type)) return LCE_ERR_INVALID_ARG;
+    if (d->causal != 0 && d->causal != 1) return LCE_ERR_INVALID_ARG;
+    if (d->heads % d->cache.kv_heads != 0 || !isfinite(d->scale)) return LCE_ERR_INVALID_ARG;
+    for (const int64_t s : {d->q_token_stride, d->q_head_stride, d->out_token_stride, d->out_head_stride})
+        if (s < 0 || s >= (1ll << 40)) return LCE_ERR_INVALID_ARG;
+    p->batch = d->batch; p->group = d->heads / d->cache.kv_heads; p->table_pages = d->table_pages;
+    if (d->tokens * d->heads >= (1ll << 31) || (int64_t)d->table_pages * d->cache.page_size >= (1ll << 31) || d->batch >= (1 << 20)) return LCE_ERR_UNSUPPORTED;
+    p->table_tokens = d->table_pages * d->cache.page_size;
+    p->causal = d->causal; p->window = d->window; p->type = d->type;
+    p->tokens = d->tokens;
+    p->q_token = d->q_token_stride; p->q_head = d->q_head_stride; p->out_token = d->out_token_stride; p->out_head = d->out_head_stride;
+    p->scale = d->scale * 1.44269504088896341f;
+    *nt = p->g.blocks <= kWideBlocks && (d->tokens * p->group + d->batch - 1) / d->batch > 8 ? 2 : 1;
+    const int64_t tiles = column_tiles(*p, 8 * *nt);
+    const int64_t wanted = 148 * 8;  // blocks
+    int64_t target = (wanted + p->g.heads - 1) / p->g.heads;
+    // never more pieces than there are tiles
+    const int64_t most = (int64_t)((p->table_tokens + kKvTile - 1) / kKvTile) * tiles;
+    if (target > most) target = most;
+    p->target = (int32_t)target;
+    p->least_tiles = kWarps;
+    if (tiles + target >= (1ll << 31)) return LCE_ERR_UNSUPPORTED;
+    p->units = (int32_t)(tiles + target);
+    return LCE_OK;
+}
+
+size_t workspace_bytes(const AttnParams &p, int nt) { return (size_t)p.units * p.g.heads * 8 * nt * (32 * p.g.blocks + 2) * 4; }
+
+}  // namespace
+}  // namespace lce
+
+extern "C" size_t lce_kv_attention_workspace_bytes(const lce_kv_attention_desc *desc)
+{
+    using namespace lce;
+    AttnParams p{};
+    int nt;
+    if (make_params(desc, &p, &nt) != LCE_OK) return 0;
+    return workspace_bytes(p, nt);
+}
+
+extern "C" lce_status lce_kv_attention(const lce_kv_attention_desc *desc, const void *q, const void *cache, const int32_t *page_table,
+                                       const int32_t *lengths, const int32_t *q_starts, void *out, void *workspace, size_t workspace_size, void *stream)
+{
+    using namespace lce;
+    AttnParams p{};
+    int nt;
+    const lce_status st = make_params(desc, &p, &nt);
+    if (st != LCE_OK) return st;
+    if (!q_starts && desc->tokens != desc->batch) return LCE_ERR_INVALID_ARG;
+    if (desc->tokens == 0) return LCE_OK;
+    if (!q || !cache || !page_table || !lengths || !out || !workspace) return LCE_ERR_INVALID_ARG;
+    const size_t element = type_size(desc->type);
+    if (!aligned(q, element) || !aligned(out, element) || !aligned(cache, 16) || !aligned(page_table, 4) || !aligned(lengths, 4) || !aligned(q_starts, 4) ||
+        !aligned(workspace, 16))
+        return LCE_ERR_ALIGNMENT;
+    if (workspace_size < workspace_bytes(p, nt)) return LCE_ERR_WORKSPACE;
+    p.q = q; p.cache = static_cast<const uint32_t *>(cache); p.page_table = page_table; p.lengths = lengths; p.q_starts = q_starts;
+    p.out = out; p.parts = static_cast<float *>(workspace);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (desc->type == LCE_TYPE_FLOAT32) return nt == 2 ? launch_blocks<2, true>(p, s) : launch_blocks<1, true>(p, s);
+    return nt == 2 ? launch_blocks<2, false>(p, s) : launch_blocks<1, false>(p, s);
+}

@@ -1,0 +1,164 @@
+// The 4-bit key/value cache: its layout, the element types of its callers and the quantiser's arithmetic.
+//
+// A tile is 16 tokens of one head: with B = ceil(head_dim / 32) blocks, uint32 K[64 B], V[64 B], scales[16 B].  Its blocks come
+// in planes of 4, then 2, then 1 (6 = 4 + 2), W blocks each, so that a lane's words of a plane are one vector load:
+//   K       word (half h, lane l, block w) at (32 h + l) W + w: the 8 codes of token 8 h + l / 4, channels 8 (l % 4) .. + 7 of
+//           block w, lowest channel in the lowest nibble;
+//   V       word (h, l, w), same place: tokens 8 h + 2 (l % 4) in the low and the one behind it in the high half, channels
+//           4 (l / 4) .. + 3 of block w;
+//   scales  word (token, w) at W token + w: bf16 of the key in the low, of the value in the high half.
+// Lane l of a warp finds there exactly its part of the A operands of m16n8k16 products, 16 tokens x channels for the keys
+// and channels x 16 tokens for the values: no transposition, and shared memory is read lane by lane without bank conflicts.
+// Codes are stored as c + 8.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "common.cuh"
+
+namespace lce {
+
+constexpr int kKvTile = 16;     // tokens of a tile
+constexpr int kKvMaxDim = 256;
+
+__host__ __device__ __forceinline__ constexpr int kv_tile_words(int blocks) { return 144 * blocks; }
+
+struct KvGeom {
+    int32_t pages, page_size, heads, dim, blocks;
+    int32_t slots;
+};
+
+inline lce_status make_kv_geom(const lce_kv_desc *d, KvGeom *g)
+{
+    if (!d || d->pages <= 0 || d->page_size <= 0 || d->kv_heads <= 0 || d->head_dim <= 0) return LCE_ERR_INVALID_ARG;
+    if (d->page_size % kKvTile != 0) return LCE_ERR_INVALID_ARG;
+    if (d->head_dim > kKvMaxDim || d->kv_heads > 65535 || (int64_t)d->pages * d->page_size >= (1ll << 31)) return LCE_ERR_UNSUPPORTED;
+    g->pages = d->pages; g->page_size = d->page_size; g->heads = d->kv_heads; g->dim = d->head_dim;
+    g->blocks = (d->head_dim + 31) / 32;
+    g->slots = d->pages * d->page_size;
+    return LCE_OK;
+}
+
+inline bool type_known(int32_t t) { return t >= LCE_TYPE_FLOAT32 && t <= LCE_TYPE_BFLOAT16; }
+inline size_t type_size(int32_t t) { return t == LCE_TYPE_FLOAT32 ? 4 : 2; }
+
+// Where block `b` lies in a tile of `blocks`: its plane's first block and width.
+__host__ __device__ __forceinline__ void kv_plane(int blocks, int b, int *first, int *width)
+{
+    const int quads = blocks & ~3;
+    if (b < quads) { *first = b & ~3; *width = 4; }
+    else if ((blocks & 2) && b < quads + 2) { *first = quads; *width = 2; }
+    else { *first = blocks - 1; *width = 1; }
+}
+// Words of a tile: the keys' of (token, block, quarter of its channels), the values' of (token pair, block, eighth), the scales'.
+__host__ __device__ __forceinline__ int kv_key_word(int blocks, int token, int b, int quarter)
+{
+    int first, width;
+    kv_plane(blocks, b, &first, &width);
+    return 64 * first + ((token >> 3) * 32 + (token & 7) * 4 + quarter) * width + (b - first);
+}
+__host__ __device__ __forceinline__ int kv_value_word(int blocks, int pair, int b, int eighth)
+{
+    int first, width;
+    kv_plane(blocks, b, &first, &width);
+    return 64 * blocks + 64 * first + ((pair >> 2) * 32 + eighth * 4 + (pair & 3)) * width + (b - first);
+}
+__host__ __device__ __forceinline__ int kv_scale_word(int blocks, int token, int b)
+{
+    int first, width;
+    kv_plane(blocks, b, &first, &width);
+    return 128 * blocks + 16 * first + token * width + (b - first);
+}
+
+// --- elements of the callers' tensors ---------------------------------------------------------------
+
+template <typename T>
+__device__ __forceinline__ float to_float(T v);
+template <>
+__device__ __forceinline__ float to_float<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ float to_float<__half>(__half v) { return __half2float(v); }
+template <>
+__device__ __forceinline__ float to_float<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
+
+template <typename T>
+__device__ __forceinline__ T from_float(float v);
+template <>
+__device__ __forceinline__ float from_float<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+// Eight consecutive elements, in 16-byte accesses where VEC (the address is then a multiple of 16); `count` of them exist.
+template <typename T, bool VEC>
+__device__ __forceinline__ void load8(const T *p, int count, float (&v)[8])
+{
+    if (VEC && count >= 8) {
+        alignas(16) T e[8];
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4 *>(e)[i] = reinterpret_cast<const uint4 *>(p)[i];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = to_float(e[i]);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < count ? to_float(p[i]) : 0.0f;
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void store8(T *p, int count, const float (&v)[8])
+{
+    if (VEC && count >= 8) {
+        alignas(16) T e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = from_float<T>(v[i]);
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4 *>(p)[i] = reinterpret_cast<const uint4 *>(e)[i];
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < count) p[i] = from_float<T>(v[i]);
+}
+
+// --- the quantiser ------------------------------------------------------------------------------
+
+// The smallest bf16 s with 7 s >= a, a finite and not negative.  7 s is exact (3 + 8 bits).  The quotient rounded to fp32 lies
+// within half a step of a / 7, so cut to bf16 it is that s or the number before it.
+__device__ __forceinline__ float kv_scale(float a)
+{
+    const uint32_t cut = __float_as_uint(__fdiv_rn(a, 7.0f)) & 0xffff0000u;
+    return __uint_as_float(7.0f * __uint_as_float(cut) < a ? cut + 0x10000u : cut);
+}
+
+// round-half-even(x / s) for 0 <= x <= 7 s.  The product with the reciprocal is off by a few units of its last place, so the
+// code is the right one or, next to a tie, its neighbour; the remainder e = x - c s (exact: one rounding of a number of at most
+// 24 bits) tells.  s and 1 / s are normal numbers (kv_codes sees to it).
+__device__ __forceinline__ float kv_code(float x, float s, float r)
+{
+    float c = rintf(x * r);
+    const float e = fmaf(-c, s, x), twice = e + e;
+    const bool odd = (int)c & 1;
+    if (twice > s || (twice == s && odd)) c += 1.0f;
+    if (-twice > s || (-twice == s && odd)) c -= 1.0f;
+    return c;
+}
+
+// Codes (+ 8) of eight channels in a word, lowest channel in the lowest nibble, for the block's scale.
+__device__ __forceinline__ uint32_t kv_codes(const float (&v)[8], float s)
+{
+    if (!(s > 0.0f)) return 0x88888888u;  // all zeros, or NaN
+    const float up = s < 0x1p-100f ? 0x1p80f : 1.0f;  // away from subnormal numbers, exactly
+    const float t = s * up, r = __fdiv_rn(1.0f, t);
+    uint32_t word = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float c = kv_code(fabsf(v[i]) * up, t, r);
+        word |= (uint32_t)(8 + (int)(v[i] < 0.0f ? -c : c)) << (4 * i);
+    }
+    return word;
+}
+
+}  // namespace lce
