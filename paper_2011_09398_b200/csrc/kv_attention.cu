@@ -237,7 +237,7 @@ struct Warp {
     float shift;                 // kHeadroom - log2 of the scales' reference
     uint32_t qf[B][2][NT][2];    // B operands of the keys' products
     uint32_t ql[SPLIT ? B : 1][2][NT][2];
-    float init[B][NT][2];        // -8 sum(q) of the block, as the products count
+    float init[SPLIT ? 1 : B][NT][2];  // -8 sum(q) of the block, as the products count
     float factor[NT][2];         // scores = factor * sum over blocks
     int32_t lo[NT][2], hi[NT][2];
 };
@@ -274,33 +274,35 @@ __device__ __forceinline__ void load_queries(const AttnParams &p, const Unit &u,
 #pragma unroll
         for (int b = 0; b < B; ++b) {
             float sum = 0.0f;
+            constexpr float kOddFactor = SPLIT ? 1.0f : 0.0625f;
 #pragma unroll
             for (int m = 0; m < 2; ++m) {
-                // codes 2 m and 2 m + 4 as they are, 2 m + 1 and 2 m + 5 times 16
-                const float x0 = v[b][2 * m] * s1 * s2, x1 = v[b][2 * m + 4] * s1 * s2, y0 = v[b][2 * m + 1] * s1 * s2 * 0.0625f,
-                            y1 = v[b][2 * m + 5] * s1 * s2 * 0.0625f;
+                // channels 2 m and 2 m + 4, then 2 m + 1 and 2 m + 5, whose codes count 16 times as they stand
+                const float x0 = v[b][2 * m] * s1 * s2, x1 = v[b][2 * m + 4] * s1 * s2, y0 = v[b][2 * m + 1] * s1 * s2 * kOddFactor,
+                            y1 = v[b][2 * m + 5] * s1 * s2 * kOddFactor;
                 const uint32_t a = pack_half2(x0, x1), c = pack_half2(y0, y1);
                 w.qf[b][m][nt][0] = a;
                 w.qf[b][m][nt][1] = c;
-                sum += half_low(a) + half_high(a) + 16.0f * (half_low(c) + half_high(c));
                 if (SPLIT) {
-                    const uint32_t al = pack_half2(x0 - half_low(a), x1 - half_high(a)), cl = pack_half2(y0 - half_low(c), y1 - half_high(c));
-                    w.ql[SPLIT ? b : 0][m][nt][0] = al;
-                    w.ql[SPLIT ? b : 0][m][nt][1] = cl;
-                    sum += half_low(al) + half_high(al) + 16.0f * (half_low(cl) + half_high(cl));
+                    w.ql[SPLIT ? b : 0][m][nt][0] = pack_half2(x0 - half_low(a), x1 - half_high(a));
+                    w.ql[SPLIT ? b : 0][m][nt][1] = pack_half2(y0 - half_low(c), y1 - half_high(c));
+                } else {
+                    sum += half_low(a) + half_high(a) + 16.0f * (half_low(c) + half_high(c));
                 }
             }
-            sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-            sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-            sum *= -8.0f * 0x1p-24f;
+            if (!SPLIT) {
+                sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+                sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+                sum *= -8.0f * 0x1p-24f;
 #pragma unroll
-            for (int j = 0; j < 2; ++j) w.init[b][nt][j] = __shfl_sync(0xffffffffu, sum, (2 * quarter + j) * 4);
+                for (int j = 0; j < 2; ++j) w.init[SPLIT ? 0 : b][nt][j] = __shfl_sync(0xffffffffu, sum, (2 * quarter + j) * 4);
+            }
         }
-        // what the sums of 2^-24 2^k code * q are multiplied with (2^24 2^-k scale, in steps that stay in range)
+        // what the sums of 2^-24 2^k code * q are multiplied with (2^24 2^-k scale; fp32 rows 2^-k scale; in steps that stay in range)
         const float f = finite ? p.scale : __uint_as_float(0x7fc00000u);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const int from = (2 * quarter + j) * 4, kc = 24 - __shfl_sync(0xffffffffu, k, from), c1 = kc / 2, c2 = kc - c1;
+            const int from = (2 * quarter + j) * 4, kc = (SPLIT ? 0 : 24) - __shfl_sync(0xffffffffu, k, from), c1 = kc / 2, c2 = kc - c1;
             w.factor[nt][j] = __shfl_sync(0xffffffffu, f, from) * __uint_as_float((uint32_t)(127 + c1) << 23) * __uint_as_float((uint32_t)(127 + c2) << 23);
             column_range(p, u, u.column0 + 8 * nt + 2 * quarter + j, &w.lo[nt][j], &w.hi[nt][j]);
         }
@@ -317,19 +319,27 @@ __device__ __forceinline__ void plane_scores(const uint32_t *tile, const Warp<B,
     for (int h = 0; h < 2; ++h) load_words<W>(tile + 64 * FIRST + (32 * h + lane) * W, k[h]);
 #pragma unroll
     for (int i = 0; i < W; ++i) {
-        constexpr uint32_t kEven = 0x000f000fu, kOdd = 0x00f000f0u;
+        constexpr uint32_t kEven = 0x000f000fu, kOdd = 0x00f000f0u, kBase = 0x64006400u;
         const int b = FIRST + i;
         const uint32_t u0 = k[0][i], u1 = k[1][i], v0 = u0 >> 8, v1 = u1 >> 8;
         const float s0 = __uint_as_float(sc[0][b] << 16), s1 = __uint_as_float(sc[1][b] << 16);
+        uint32_t a[8] = {u0 & kEven, u1 & kEven, u0 & kOdd, u1 & kOdd, v0 & kEven, v1 & kEven, v0 & kOdd, v1 & kOdd};
+        if (SPLIT) {
+#pragma unroll
+            for (int x = 0; x < 8; ++x) a[x] = x & 2 ? value_odd(a[x] | kBase) : value_even(a[x] | kBase);
+        }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            float d[4] = {w.init[b][nt][0], w.init[b][nt][1], w.init[b][nt][0], w.init[b][nt][1]};
-            mma(d, u0 & kEven, u1 & kEven, u0 & kOdd, u1 & kOdd, w.qf[b][0][nt][0], w.qf[b][0][nt][1]);
-            mma(d, v0 & kEven, v1 & kEven, v0 & kOdd, v1 & kOdd, w.qf[b][1][nt][0], w.qf[b][1][nt][1]);
+            float d[4] = {};
             if (SPLIT) {
-                mma(d, u0 & kEven, u1 & kEven, u0 & kOdd, u1 & kOdd, w.ql[SPLIT ? b : 0][0][nt][0], w.ql[SPLIT ? b : 0][0][nt][1]);
-                mma(d, v0 & kEven, v1 & kEven, v0 & kOdd, v1 & kOdd, w.ql[SPLIT ? b : 0][1][nt][0], w.ql[SPLIT ? b : 0][1][nt][1]);
+                mma(d, a[0], a[1], a[2], a[3], w.ql[SPLIT ? b : 0][0][nt][0], w.ql[SPLIT ? b : 0][0][nt][1]);
+                mma(d, a[4], a[5], a[6], a[7], w.ql[SPLIT ? b : 0][1][nt][0], w.ql[SPLIT ? b : 0][1][nt][1]);
+            } else {
+                d[0] = d[2] = w.init[SPLIT ? 0 : b][nt][0];
+                d[1] = d[3] = w.init[SPLIT ? 0 : b][nt][1];
             }
+            mma(d, a[0], a[1], a[2], a[3], w.qf[b][0][nt][0], w.qf[b][0][nt][1]);
+            mma(d, a[4], a[5], a[6], a[7], w.qf[b][1][nt][0], w.qf[b][1][nt][1]);
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 s[0][nt][j] = fmaf(s0, d[j], s[0][nt][j]);
@@ -376,11 +386,17 @@ __device__ __forceinline__ void plane_values(const uint32_t *tile, Warp<B, NT, S
                 ph[r] = transpose8x8(packed);
                 if (SPLIT) pl[r] = transpose8x8(pack_half2(x0 - half_low(packed), x1 - half_high(packed)));
             }
-            mma(w.o[b][0][nt], a[0][0], a[0][1], a[1][0], a[1][1], ph[0], ph[1]);
-            mma(w.o[b][1][nt], a[0][2], a[0][3], a[1][2], a[1][3], ph[0], ph[1]);
-            if (SPLIT) {
-                mma(w.o[b][0][nt], a[0][0], a[0][1], a[1][0], a[1][1], pl[0], pl[1]);
-                mma(w.o[b][1][nt], a[0][2], a[0][3], a[1][2], a[1][3], pl[0], pl[1]);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                if (!SPLIT) {
+                    mma(w.o[b][c][nt], a[0][2 * c], a[0][2 * c + 1], a[1][2 * c], a[1][2 * c + 1], ph[0], ph[1]);
+                } else {
+                    float d[4] = {};  // the products cut their sums: a long one would drift by 2^-24 each
+                    mma(d, a[0][2 * c], a[0][2 * c + 1], a[1][2 * c], a[1][2 * c + 1], pl[0], pl[1]);
+                    mma(d, a[0][2 * c], a[0][2 * c + 1], a[1][2 * c], a[1][2 * c + 1], ph[0], ph[1]);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) w.o[b][c][nt][x] += d[x];
+                }
             }
         }
     }

@@ -229,12 +229,12 @@ extern "C" lce_status lce_residual_norm(const lce_residual_norm_desc *desc, cons
     if (!(desc->eps >= 0.0f) || !isfinite(desc->eps) || !isfinite(desc->residual_scale)) return LCE_ERR_INVALID_ARG;
     for (const int64_t s : {desc->x_stride, desc->branch_stride, desc->gate_stride, desc->y_stride, desc->normed_stride})
         if (s < 0 || s >= (1ll << 40)) return LCE_ERR_INVALID_ARG;
-    if (!branch && (gate || desc->post_norm != LCE_NORM_NONE || post_weight || post_bias)) return LCE_ERR_INVALID_ARG;
     if (desc->channels > kMaxChannels) return LCE_ERR_UNSUPPORTED;
     if (desc->stream_type != desc->type && desc->stream_type != LCE_TYPE_FLOAT32) return LCE_ERR_UNSUPPORTED;
     if (desc->rows >= (1ll << 31)) return LCE_ERR_UNSUPPORTED;
-    if (!y && !normed && !packed) return LCE_ERR_INVALID_ARG;
     if (desc->rows == 0) return LCE_OK;
+    if (!y && !normed && !packed) return LCE_ERR_INVALID_ARG;
+    if (!branch && (gate || desc->post_norm != LCE_NORM_NONE || post_weight || post_bias)) return LCE_ERR_INVALID_ARG;
     if (!x) return LCE_ERR_INVALID_ARG;
     // rows that are written do not run into one another
     if (desc->rows > 1 && ((y && desc->y_stride < desc->channels) || (normed && desc->normed_stride < desc->channels))) return LCE_ERR_INVALID_ARG;
