@@ -39,13 +39,14 @@ struct AttnParams {
     const uint32_t *cache;
     const int32_t *page_table, *lengths, *q_starts;
     void *out;
-    float *parts;                      // [unit][kv head][column][32 blocks + 2]: sums, largest, weight
-    int32_t units, target, least_tiles;
+    float *parts;                      // [unit][kv head][column][32 blocks + 4]: sums, largest, weight
+    int32_t units, column_tiles, target, least_tiles;
+    int32_t one_row;                   // each sequence has one row of q
 };
 
 // What a unit (a range of tiles for one tile of columns of a sequence) works on.
 struct Unit {
-    int32_t seq, column0, chunk, chunks, first_unit;  // first_unit: of this column tile
+    int32_t seq, column0, chunks;
     int32_t length, rows;                             // tokens of the sequence, its rows of q
     int64_t row0;                                     // its first row of q
     int32_t tile0, tile1;                             // the unit's tiles
@@ -78,57 +79,56 @@ __device__ __forceinline__ Sequence sequence(const AttnParams &p, int b)
     return s;
 }
 
-__device__ __forceinline__ int32_t warp_sum(int32_t v)
-{
-    return __reduce_add_sync(0xffffffffu, v);
-}
-
 // The work is cut evenly whatever the sequences' lengths: every column tile of a sequence into pieces of at most `most` tiles, where
 // `most` follows from the whole batch's tiles.  Every warp works this out for itself from the lengths (no launch in front, no host
-// copy of them).  False: there is no such unit.
-template <int COLUMNS>
-__device__ __forceinline__ bool find_unit(const AttnParams &p, int unit, Unit *u)
+// copy of them).  Finds the `at`-th unit, or the first unit of the `at`-th column tile; false: there is no such one.
+template <int COLUMNS, bool BY_COLUMN_TILE>
+__device__ __forceinline__ bool find_unit(const AttnParams &p, int at, Unit *u, int *first_unit)
 {
     const int lane = threadIdx.x & 31;
+    const Sequence first = sequence<COLUMNS>(p, lane);
     int64_t total = 0;
     for (int b0 = 0; b0 < p.batch; b0 += 32) {
-        const Sequence s = sequence<COLUMNS>(p, b0 + lane);
+        const Sequence s = b0 ? sequence<COLUMNS>(p, b0 + lane) : first;
         int64_t t = (int64_t)s.column_tiles * s.tiles;
 #pragma unroll
         for (int d = 16; d; d >>= 1) t += __shfl_xor_sync(0xffffffffu, t, d);
         total += t;
     }
     const int32_t most = (int32_t)max((total + p.target - 1) / p.target, (int64_t)p.least_tiles);
-    int before = 0;
+    int before = 0, units_before = 0;
     for (int b0 = 0; b0 < p.batch; b0 += 32) {
-        const Sequence s = sequence<COLUMNS>(p, b0 + lane);
-        const int32_t chunks = max((s.tiles + most - 1) / most, 1), mine = s.column_tiles * chunks;
-        int32_t upto = mine;  // units of this and the lanes below
+        const Sequence s = b0 ? sequence<COLUMNS>(p, b0 + lane) : first;
+        const int32_t chunks = max((s.tiles + most - 1) / most, 1), units = s.column_tiles * chunks, mine = BY_COLUMN_TILE ? s.column_tiles : units;
+        int32_t upto = mine, units_upto = units;  // of this and the lanes below
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
-            const int32_t o = __shfl_up_sync(0xffffffffu, upto, d);
-            if (lane >= d) upto += o;
+            const int32_t o = __shfl_up_sync(0xffffffffu, upto, d), n = __shfl_up_sync(0xffffffffu, units_upto, d);
+            if (lane >= d) {
+                upto += o;
+                units_upto += n;
+            }
         }
-        const uint32_t has = __ballot_sync(0xffffffffu, before + upto > unit);
+        const uint32_t has = __ballot_sync(0xffffffffu, before + upto > at);
         if (has) {
             const int from = __ffs(has) - 1;
-            const int32_t first = before + __shfl_sync(0xffffffffu, upto - mine, from);
+            const int32_t local = at - (before + __shfl_sync(0xffffffffu, upto - mine, from));
             u->seq = b0 + from;
             u->chunks = __shfl_sync(0xffffffffu, chunks, from);
             u->length = __shfl_sync(0xffffffffu, s.length, from);
             u->rows = __shfl_sync(0xffffffffu, s.rows, from);
             u->row0 = __shfl_sync(0xffffffffu, s.row0, from);
             const int32_t tiles = __shfl_sync(0xffffffffu, s.tiles, from), first_tile = __shfl_sync(0xffffffffu, s.first_tile, from);
-            const int32_t at = unit - first, column_tile = at / u->chunks;
-            u->chunk = at - column_tile * u->chunks;
+            const int32_t column_tile = BY_COLUMN_TILE ? local : local / u->chunks, chunk = BY_COLUMN_TILE ? 0 : local - column_tile * u->chunks;
             u->column0 = column_tile * COLUMNS;
-            u->first_unit = first + column_tile * u->chunks;
+            *first_unit = units_before + __shfl_sync(0xffffffffu, units_upto - units, from) + column_tile * u->chunks;
             // equal pieces
-            u->tile0 = first_tile + (int32_t)((int64_t)tiles * u->chunk / u->chunks);
-            u->tile1 = first_tile + (int32_t)((int64_t)tiles * (u->chunk + 1) / u->chunks);
+            u->tile0 = first_tile + (int32_t)((int64_t)tiles * chunk / u->chunks);
+            u->tile1 = first_tile + (int32_t)((int64_t)tiles * (chunk + 1) / u->chunks);
             return true;
         }
         before += __shfl_sync(0xffffffffu, upto, 31);
+        units_before += __shfl_sync(0xffffffffu, units_upto, 31);
     }
     return false;
 }
@@ -181,11 +181,17 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t v)
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
     return d;
 }
+// d = A B + c
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, float c0, float c1,
+                                    float c2, float c3)
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%12,%13};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
+}
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    mma(d, a0, a1, a2, a3, b0, b1, d[0], d[1], d[2], d[3]);
 }
 __device__ __forceinline__ float exp2_fast(float x)
 {
@@ -228,12 +234,22 @@ __device__ __forceinline__ void cp_async16(uint32_t smem, const void *g)
 
 constexpr size_t ring_bytes(int blocks) { return (size_t)kWarps * kStages * kv_tile_words(blocks) * 4; }
 
+// Blocks that a variant's registers let an SM hold.
+__host__ __device__ constexpr int blocks_per_sm(int blocks, int nt, bool split)
+{
+    return blocks * nt <= (split ? 3 : 4) ? 4 : blocks * nt <= (split ? 4 : 6) ? 3 : 2;
+}
+
+// Lets the join, which this call launches behind, take its place while this kernel runs.  It waits for all of it, and nothing
+// that a caller launches can start before the join is done.
+__device__ __forceinline__ void release_join() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // B blocks of 32 channels, NT tiles of 8 columns, SPLIT: fp32 rows.
 template <int B, int NT, bool SPLIT>
 struct Warp {
     float o[B][2][NT][4];        // sums of c p: channels 32 b + 4 (lane / 4) + 2 i + {0, 1}, columns 8 nt + 2 (lane % 4) + {0, 1}
     float top[NT][2], weight[NT][2];  // of the lane's columns
-    float high;                  // scales above this want a higher reference
+    uint32_t high;               // words of scales above this want a higher reference
     float shift;                 // kHeadroom - log2 of the scales' reference
     uint32_t qf[B][2][NT][2];    // B operands of the keys' products
     uint32_t ql[SPLIT ? B : 1][2][NT][2];
@@ -330,15 +346,15 @@ __device__ __forceinline__ void plane_scores(const uint32_t *tile, const Warp<B,
         }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            float d[4] = {};
+            float d[4];
             if (SPLIT) {
-                mma(d, a[0], a[1], a[2], a[3], w.ql[SPLIT ? b : 0][0][nt][0], w.ql[SPLIT ? b : 0][0][nt][1]);
+                mma(d, a[0], a[1], a[2], a[3], w.ql[SPLIT ? b : 0][0][nt][0], w.ql[SPLIT ? b : 0][0][nt][1], 0.0f, 0.0f, 0.0f, 0.0f);
                 mma(d, a[4], a[5], a[6], a[7], w.ql[SPLIT ? b : 0][1][nt][0], w.ql[SPLIT ? b : 0][1][nt][1]);
+                mma(d, a[0], a[1], a[2], a[3], w.qf[b][0][nt][0], w.qf[b][0][nt][1]);
             } else {
-                d[0] = d[2] = w.init[SPLIT ? 0 : b][nt][0];
-                d[1] = d[3] = w.init[SPLIT ? 0 : b][nt][1];
+                const float c0 = w.init[SPLIT ? 0 : b][nt][0], c1 = w.init[SPLIT ? 0 : b][nt][1];
+                mma(d, a[0], a[1], a[2], a[3], w.qf[b][0][nt][0], w.qf[b][0][nt][1], c0, c1, c0, c1);
             }
-            mma(d, a[0], a[1], a[2], a[3], w.qf[b][0][nt][0], w.qf[b][0][nt][1]);
             mma(d, a[4], a[5], a[6], a[7], w.qf[b][1][nt][0], w.qf[b][1][nt][1]);
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
@@ -391,8 +407,8 @@ __device__ __forceinline__ void plane_values(const uint32_t *tile, Warp<B, NT, S
                 if (!SPLIT) {
                     mma(w.o[b][c][nt], a[0][2 * c], a[0][2 * c + 1], a[1][2 * c], a[1][2 * c + 1], ph[0], ph[1]);
                 } else {
-                    float d[4] = {};  // the products cut their sums: a long one would drift by 2^-24 each
-                    mma(d, a[0][2 * c], a[0][2 * c + 1], a[1][2 * c], a[1][2 * c + 1], pl[0], pl[1]);
+                    float d[4];  // the products cut their sums: a long one would drift by 2^-24 each
+                    mma(d, a[0][2 * c], a[0][2 * c + 1], a[1][2 * c], a[1][2 * c + 1], pl[0], pl[1], 0.0f, 0.0f, 0.0f, 0.0f);
                     mma(d, a[0][2 * c], a[0][2 * c + 1], a[1][2 * c], a[1][2 * c + 1], ph[0], ph[1]);
 #pragma unroll
                     for (int x = 0; x < 4; ++x) w.o[b][c][nt][x] += d[x];
@@ -434,11 +450,10 @@ __device__ __forceinline__ void tile_step(const uint32_t *tile, int32_t token0, 
     if (T) plane_scores<B, NT, SPLIT, (T ? Q : 0), 2>(tile, w, sc, s);
     if (S) plane_scores<B, NT, SPLIT, B - 1, 1>(tile, w, sc, s);
     bool shown[2][NT][2];
-    uint32_t largest = 0;  // scale of a value of the lane's tokens
-    bool some[2];
+    uint32_t largest = 0;  // scale of a value of the lane's tokens, in the high half
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-        some[r] = !MASKED;
+        bool some = !MASKED;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -449,28 +464,25 @@ __device__ __forceinline__ void tile_step(const uint32_t *tile, int32_t token0, 
                     const int32_t token = token0 + 8 * r + (lane >> 2);
                     shown[r][nt][j] = token >= w.lo[nt][j] && token < w.hi[nt][j];
                     if (!shown[r][nt][j]) s[r][nt][j] = -INFINITY;
-                    some[r] = some[r] || shown[r][nt][j];
+                    some = some || shown[r][nt][j];
                 }
             }
 #pragma unroll
-        for (int b = 0; b < B; ++b)
-            if (some[r] && sc[r][b] < 0x7f800000u) largest = max(largest, sc[r][b]);  // the value's scale is the high half; NaN aside
+        for (int b = 0; b < B; ++b) largest = max(largest, some ? sc[r][b] : 0u);
     }
-    bool above = __uint_as_float(largest & 0xffff0000u) > w.high;
+    bool above = largest > w.high;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int j = 0; j < 2; ++j) above = above || fmaxf(s[0][nt][j], s[1][nt][j]) > w.top[nt][j] + kRise;
     if (__any_sync(0xffffffffu, above)) {
         // rare behind the first tiles: the references move up and the sums with them
-        float reference = __uint_as_float(largest & 0xffff0000u);
-#pragma unroll
-        for (int d = 16; d; d >>= 1) reference = fmaxf(reference, __shfl_xor_sync(0xffffffffu, reference, d));
         const float old_shift = w.shift;
-        if (reference > w.high) {
-            const int e = max(ilogbf(reference) + 1, -100);  // reference < 2^e; the weights themselves stay in range
+        largest = __reduce_max_sync(0xffffffffu, largest);
+        if (largest > w.high && largest < 0x7f800000u) {  // a NaN moves nothing
+            const int e = max((int)(largest >> 23) - 126, -100);  // scales < 2^e; the weights themselves stay in range
             w.shift = kHeadroom - (float)e;
-            w.high = __uint_as_float((uint32_t)(127 + e) << 23);
+            w.high = (uint32_t)(127 + e) << 23 | 0xffffu;
         }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -510,13 +522,15 @@ __device__ __forceinline__ void tile_step(const uint32_t *tile, int32_t token0, 
 }
 
 template <int B, int NT, bool SPLIT>
-__global__ void __launch_bounds__(kThreads) kv_attention_kernel(const __grid_constant__ AttnParams p)
+__global__ void __launch_bounds__(kThreads, blocks_per_sm(B, NT, SPLIT)) kv_attention_kernel(const __grid_constant__ AttnParams p)
 {
     constexpr int COLUMNS = 8 * NT, TILE = kv_tile_words(B), PIECES = TILE / 4;
     extern __shared__ __align__(128) uint32_t smem[];
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    release_join();
     Unit u;
-    if (!find_unit<COLUMNS>(p, blockIdx.x, &u)) return;
+    int first_unit;
+    if (!find_unit<COLUMNS, false>(p, blockIdx.x, &u, &first_unit)) return;
     const int head = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     Warp<B, NT, SPLIT> w;
     load_queries(p, u, head, w);
@@ -535,7 +549,7 @@ __global__ void __launch_bounds__(kThreads) kv_attention_kernel(const __grid_con
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) w.o[b][i][nt][j] = 0.0f;
-    w.high = 0.0f;
+    w.high = 0xffffu;
     w.shift = 0.0f;
 
     // tokens that every column sees, and those that one sees at least
@@ -561,25 +575,25 @@ __global__ void __launch_bounds__(kThreads) kv_attention_kernel(const __grid_con
     const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
     const int32_t *const table = p.page_table + (int64_t)u.seq * p.table_pages;
     const int tiles_per_page = p.g.page_size / kKvTile;
-    // pages of the warp's next 32 tiles, one to a lane
-    int32_t pages = -1;
+    // places of the warp's next 32 tiles in the cache, one to a lane; negative: not in the pool
+    int64_t places = -1;
     const int32_t mine = max((tile1 - tile0 - warp + kWarps - 1) / kWarps, 0);
+    const char *const cache = reinterpret_cast<const char *>(p.cache) + lane * 16;
     auto fetch = [&](int i) {  // issues the copies of the warp's i-th tile
         if ((i & 31) == 0) {
-            const int32_t t = tile0 + warp + (i + lane) * kWarps;
-            pages = t < tile1 ? __ldg(table + t / tiles_per_page) : -1;
+            const int32_t t = tile0 + warp + (i + lane) * kWarps, in_table = t / tiles_per_page;
+            const int32_t page = t < tile1 ? __ldg(table + in_table) : -1;
+            places = page >= 0 && page < p.g.pages ? (((int64_t)page * p.g.heads + head) * tiles_per_page + (t - in_table * tiles_per_page)) * (TILE * 4) : -1;
         }
-        const int32_t page = __shfl_sync(0xffffffffu, pages, i & 31);
-        if (i < mine && page >= 0 && page < p.g.pages) {
-            const int32_t t = tile0 + warp + i * kWarps;
-            const uint4 *from = reinterpret_cast<const uint4 *>(p.cache + (((int64_t)page * p.g.heads + head) * tiles_per_page + t % tiles_per_page) * TILE);
-            const uint32_t to = ring_at + (i % kStages) * TILE * 4;
+        const int64_t place = __shfl_sync(0xffffffffu, places, i & 31);
+        if (place >= 0) {
+            const uint32_t to = ring_at + (i % kStages) * (TILE * 4) + lane * 16;
 #pragma unroll
             for (int c = 0; c < (PIECES + 31) / 32; ++c)
-                if (c * 32 + lane < PIECES) cp_async16(to + (c * 32 + lane) * 16, from + c * 32 + lane);
+                if (c * 32 + 32 <= PIECES || c * 32 + lane < PIECES) cp_async16(to + c * 512, cache + place + c * 512);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
-        return page >= 0 && page < p.g.pages;
+        return place >= 0;
     };
     uint32_t good = 0;  // whether the tile of a stage is there
 #pragma unroll
@@ -634,7 +648,7 @@ __global__ void __launch_bounds__(kThreads) kv_attention_kernel(const __grid_con
             weight = fmaf(f, weights[i * COLUMNS + column], weight);
         }
         if (u.chunks > 1) {
-            float *const to = p.parts + (((int64_t)blockIdx.x * p.g.heads + head) * COLUMNS + column) * (D + 2);
+            float *const to = p.parts + (((int64_t)blockIdx.x * p.g.heads + head) * COLUMNS + column) * (D + 4);
             to[c] = sum;
             if (c == 0) {
                 to[D] = top;
@@ -649,32 +663,67 @@ __global__ void __launch_bounds__(kThreads) kv_attention_kernel(const __grid_con
     }
 }
 
-// Joins the pieces of a column, always in the same order.  A block to each column of a column tile.
+// Joins the pieces of a column, always in the same order: a block to a column, its warps' share of the pieces first, then the
+// warps.  It is there before the pieces are (release_join) and has found its own by then.
+constexpr int kJoinWarps = 8;
+
 template <int NT>
-__global__ void __launch_bounds__(128) kv_attention_join_kernel(const __grid_constant__ AttnParams p)
+__global__ void __launch_bounds__(32 * kJoinWarps) kv_attention_join_kernel(const __grid_constant__ AttnParams p)
 {
     constexpr int COLUMNS = 8 * NT;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    __shared__ float4 sums[kJoinWarps][2][32];
+    __shared__ float tops[kJoinWarps], weights[kJoinWarps];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     Unit u;
-    if (!find_unit<COLUMNS>(p, blockIdx.x, &u)) return;
-    if (u.chunks == 1 || u.chunk != 0) return;
+    int first_unit;
+    // the lengths are what the kernel in front read: nothing has written them since
+    const bool found = find_unit<COLUMNS, true>(p, blockIdx.x, &u, &first_unit);
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // every block: what comes behind this kernel relies on the one in front, too
     const int head = blockIdx.y, column = blockIdx.z, D = 32 * p.g.blocks;
+    if (!found || u.chunks == 1) return;
     const int q = u.column0 + column, row = q / p.group;
     if (row >= u.rows) return;
-    const int64_t step = (int64_t)p.g.heads * COLUMNS * (D + 2);
-    const float *const from = p.parts + (((int64_t)blockIdx.x * p.g.heads + head) * COLUMNS + column) * (D + 2);
-    const int chunks = min(u.chunks, p.units - (int)blockIdx.x);
+    const int64_t step = (int64_t)p.g.heads * COLUMNS * (D + 4);
+    const float *const from = p.parts + (((int64_t)first_unit * p.g.heads + head) * COLUMNS + column) * (D + 4);
+    const int chunks = min(u.chunks, p.units - first_unit);
     float top = -INFINITY;
-    for (int i = 0; i < chunks; ++i) top = fmaxf(top, from[i * step + D]);
-    for (int c = threadIdx.x; c < p.g.dim; c += 128) {
-        float sum = 0.0f, weight = 0.0f;
-        for (int i = 0; i < chunks; ++i) {
-            const float f = exp2f(from[i * step + D] - top);
-            sum = fmaf(f, from[i * step + c], sum);
-            weight = fmaf(f, from[i * step + D + 1], weight);
+    for (int i = warp * 32 + lane; i < chunks; i += 32 * kJoinWarps) top = fmaxf(top, from[i * step + D]);
+#pragma unroll
+    for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+    if (lane == 0) tops[warp] = top;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kJoinWarps; ++i) top = fmaxf(top, tops[i]);
+    float weight = 0.0f;
+    float4 sum[2] = {};
+#pragma unroll 4
+    for (int i = warp; i < chunks; i += kJoinWarps) {
+        const float f = exp2f(from[i * step + D] - top);
+        weight = fmaf(f, from[i * step + D + 1], weight);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int c = 4 * (lane + 32 * h);
+            if (c >= D) break;
+            const float4 v = *reinterpret_cast<const float4 *>(from + i * step + c);
+            sum[h].x = fmaf(f, v.x, sum[h].x);
+            sum[h].y = fmaf(f, v.y, sum[h].y);
+            sum[h].z = fmaf(f, v.z, sum[h].z);
+            sum[h].w = fmaf(f, v.w, sum[h].w);
+        }
+    }
+    sums[warp][0][lane] = sum[0];
+    sums[warp][1][lane] = sum[1];
+    if (lane == 0) weights[warp] = weight;
+    __syncthreads();
+    for (int c = threadIdx.x; c < p.g.dim; c += 32 * kJoinWarps) {
+        float s = 0.0f, l = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kJoinWarps; ++i) {
+            s += reinterpret_cast<const float *>(sums[i])[c];
+            l += weights[i];
         }
         store_element(p.out, p.type, (u.row0 + row) * p.out_token + ((int64_t)head * p.group + (q - row * p.group)) * p.out_head + c,
-                      weight == 0.0f ? 0.0f : sum / weight);
+                      l == 0.0f ? 0.0f : s / l);
     }
 }
 
@@ -688,7 +737,9 @@ lce_status launch(const AttnParams &p, cudaStream_t s)
     if (!opt_in.ensure(kv_attention_kernel<B, NT, SPLIT>, smem)) return LCE_ERR_CUDA;
     const lce_status st = launch_dependent(kv_attention_kernel<B, NT, SPLIT>, dim3((unsigned)p.units, (unsigned)p.g.heads), kThreads, smem, s, p);
     if (st != LCE_OK) return st;
-    return launch_dependent(kv_attention_join_kernel<NT>, dim3((unsigned)p.units, (unsigned)p.g.heads, 8 * NT), 128, 0, s, p);
+    // columns that there can be in a tile
+    const int64_t columns = p.tokens * p.group < 8 * NT ? p.tokens * p.group : p.one_row && p.group < 8 * NT ? p.group : 8 * NT;
+    return launch_dependent(kv_attention_join_kernel<NT>, dim3((unsigned)p.column_tiles, (unsigned)p.g.heads, (unsigned)columns), 32 * kJoinWarps, 0, s, p);
 }
 
 // 16 columns where their sums and operands fit a thread's registers
@@ -731,7 +782,7 @@ lce_status make_params(const lce_kv_attention_desc *d, AttnParams *p, int *nt)
     p->scale = d->scale * 1.44269504088896341f;
     *nt = p->g.blocks <= kWideBlocks && (d->tokens * p->group + d->batch - 1) / d->batch > 8 ? 2 : 1;
     const int64_t tiles = column_tiles(*p, 8 * *nt);
-    const int64_t wanted = 148 * 8;  // blocks
+    const int64_t wanted = 148 * blocks_per_sm(p->g.blocks, *nt, p->type == LCE_TYPE_FLOAT32);  // blocks: what the GPU holds at a time
     int64_t target = (wanted + p->g.heads - 1) / p->g.heads;
     // never more pieces than there are tiles
     const int64_t most = (int64_t)((p->table_tokens + kKvTile - 1) / kKvTile) * tiles;
@@ -740,10 +791,11 @@ lce_status make_params(const lce_kv_attention_desc *d, AttnParams *p, int *nt)
     p->least_tiles = kWarps;
     if (tiles + target >= (1ll << 31)) return LCE_ERR_UNSUPPORTED;
     p->units = (int32_t)(tiles + target);
+    p->column_tiles = (int32_t)tiles;
     return LCE_OK;
 }
 
-size_t workspace_bytes(const AttnParams &p, int nt) { return (size_t)p.units * p.g.heads * 8 * nt * (32 * p.g.blocks + 2) * 4; }
+size_t workspace_bytes(const AttnParams &p, int nt) { return (size_t)p.units * p.g.heads * 8 * nt * (32 * p.g.blocks + 4) * 4; }
 
 }  // namespace
 }  // namespace lce
@@ -773,6 +825,7 @@ extern "C" lce_status lce_kv_attention(const lce_kv_attention_desc *desc, const 
         !aligned(workspace, 16))
         return LCE_ERR_ALIGNMENT;
     if (workspace_size < workspace_bytes(p, nt)) return LCE_ERR_WORKSPACE;
+    p.one_row = !q_starts;
     p.q = q; p.cache = static_cast<const uint32_t *>(cache); p.page_table = page_table; p.lengths = lengths; p.q_starts = q_starts;
     p.out = out; p.parts = static_cast<float *>(workspace);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
