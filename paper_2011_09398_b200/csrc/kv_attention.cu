@@ -8,13 +8,14 @@
 //   keys    a code n = c + 8 of four bits is, as it stands in a 16-bit half, the subnormal f16 number n 2^-24 (or 16 n 2^-24 in
 //           bits 4 .. 7): one AND makes a pair of operands, five instructions eight codes.  The 16 goes into Q, the 8 into the
 //           accumulators' initial value, -8 sum(q) over the block, and the block's scale multiplies the finished sums.
-//   values  want their sign (a sum over a long sequence would lose its last bits next to 8 sum(p)): f16 1024 + n by one
-//           AND-OR, less 1032 by one packed add: nine instructions eight codes.  The block's scale multiplies p, in fp32, before
-//           it is rounded to f16.
+//   values  likewise; the 8 leaves by a second product, of a constant matrix and the same p, tile by tile (left to the end,
+//           the sums over a long sequence would lose their last bits next to 8 sum(p)): the tensor cores have the time.  The
+//           block's scale multiplies p, in fp32, before it is rounded to f16.
 //
 // Scores and the running softmax are fp32.  Q is f16 times a power of two chosen for each row, exact for f16 and bf16 rows up to
 // what lies 2^-29 below the row's largest; p is rounded to f16 (relative error 2^-11 of each weight, which is what an fp16
-// result has, and averages out).  fp32 rows take Q and p as two f16 numbers each (22 bits).
+// result has, and averages out).  fp32 rows take Q and p as two f16 numbers each (22 bits), and codes as f16 c = n - 8: 1024 + n by
+// one AND-OR, less 1032 by one packed add.
 #include "kv_common.cuh"
 
 #include <math.h>
@@ -32,6 +33,7 @@ struct AttnParams {
     KvGeom g;
     int32_t batch, group, table_pages, table_tokens;
     int32_t causal, window, type;
+    int32_t q_vectors;                 // rows of q allow 16-byte loads
     int64_t tokens;
     int64_t q_token, q_head, out_token, out_head;
     float scale;                       // times log2(e)
@@ -41,6 +43,8 @@ struct AttnParams {
     void *out;
     float *parts;                      // [unit][kv head][column][32 blocks + 4]: sums, largest, weight
     int32_t units, column_tiles, target, least_tiles;
+    int32_t cluster;                   // blocks that share a unit
+    int32_t join;                      // there may be units that are not a whole column tile
     int32_t one_row;                   // each sequence has one row of q
 };
 
@@ -95,7 +99,11 @@ __device__ __forceinline__ bool find_unit(const AttnParams &p, int at, Unit *u, 
         for (int d = 16; d; d >>= 1) t += __shfl_xor_sync(0xffffffffu, t, d);
         total += t;
     }
-    const int32_t most = (int32_t)max((total + p.target - 1) / p.target, (int64_t)p.least_tiles);
+    int32_t most = 1 << 30;
+    if (p.join) {
+        most = total < (1ll << 31) ? (int32_t)(((uint32_t)total + p.target - 1) / p.target) : (int32_t)min((total + p.target - 1) / p.target, (int64_t)most);
+        most = max(most, p.least_tiles);
+    }
     int before = 0, units_before = 0;
     for (int b0 = 0; b0 < p.batch; b0 += 32) {
         const Sequence s = b0 ? sequence<COLUMNS>(p, b0 + lane) : first;
@@ -123,8 +131,9 @@ __device__ __forceinline__ bool find_unit(const AttnParams &p, int at, Unit *u, 
             u->column0 = column_tile * COLUMNS;
             *first_unit = units_before + __shfl_sync(0xffffffffu, units_upto - units, from) + column_tile * u->chunks;
             // equal pieces
-            u->tile0 = first_tile + (int32_t)((int64_t)tiles * chunk / u->chunks);
-            u->tile1 = first_tile + (int32_t)((int64_t)tiles * (chunk + 1) / u->chunks);
+            const int32_t each = tiles / u->chunks, more = tiles - each * u->chunks;
+            u->tile0 = first_tile + chunk * each + min(chunk, more);
+            u->tile1 = u->tile0 + each + (chunk < more ? 1 : 0);
             return true;
         }
         before += __shfl_sync(0xffffffffu, upto, 31);
@@ -144,12 +153,22 @@ __device__ __forceinline__ void column_range(const AttnParams &p, const Unit &u,
     *lo = p.window > 0 ? (int32_t)min(max(position + 1 - p.window, (int64_t)0), (int64_t)u.length) : 0;
 }
 
-__device__ __forceinline__ float load_element(const void *p, int32_t type, int64_t i)
+// Eight channels of a row of q; `count` of them exist.  SPLIT: fp32, otherwise f16 or bf16.
+template <bool SPLIT>
+__device__ __forceinline__ void load_row(const AttnParams &p, int64_t at, int count, float (&v)[8])
 {
-    switch (type) {
-        case LCE_TYPE_FLOAT32: return static_cast<const float *>(p)[i];
-        case LCE_TYPE_FLOAT16: return __half2float(static_cast<const __half *>(p)[i]);
-        default: return __bfloat162float(static_cast<const __nv_bfloat16 *>(p)[i]);
+    if (SPLIT) {
+        const float *const q = static_cast<const float *>(p.q) + at;
+        if (p.q_vectors) load8<float, true>(q, count, v);
+        else load8<float, false>(q, count, v);
+    } else if (p.type == LCE_TYPE_FLOAT16) {
+        const __half *const q = static_cast<const __half *>(p.q) + at;
+        if (p.q_vectors) load8<__half, true>(q, count, v);
+        else load8<__half, false>(q, count, v);
+    } else {
+        const __nv_bfloat16 *const q = static_cast<const __nv_bfloat16 *>(p.q) + at;
+        if (p.q_vectors) load8<__nv_bfloat16, true>(q, count, v);
+        else load8<__nv_bfloat16, false>(q, count, v);
     }
 }
 __device__ __forceinline__ void store_element(void *p, int32_t type, int64_t i, float v)
@@ -181,6 +200,13 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t v)
     asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
     return d;
 }
+// The same of bf16 numbers, c = 0.
+__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
 // d = A B + c
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, float c0, float c1,
                                     float c2, float c3)
@@ -200,17 +226,16 @@ __device__ __forceinline__ float exp2_fast(float x)
     return d;
 }
 
-// Pairs (low half, high half) of value codes 2 i, 2 i + 1 of a word as f16 numbers c = n - 8.
-__device__ __forceinline__ uint32_t value_even(uint32_t w)
+// Bytes exchanged in either half.
+__device__ __forceinline__ uint32_t swap_bytes(uint32_t w) { return __byte_perm(w, 0, 0x2301); }
+// A pair of codes on the mantissa of 1024, 1024 + 4 n or 1024 + 64 n, as f16 numbers c = n - 8.
+__device__ __forceinline__ uint32_t half_fma(uint32_t w, unsigned short by, unsigned short plus)
 {
-    const __half2 v = __hadd2(*reinterpret_cast<const __half2 *>(&w), __half2half2(__ushort_as_half(0xe408)));  // - 1032
+    const __half2 v = __hfma2(*reinterpret_cast<const __half2 *>(&w), __half2half2(__ushort_as_half(by)), __half2half2(__ushort_as_half(plus)));
     return *reinterpret_cast<const uint32_t *>(&v);
 }
-__device__ __forceinline__ uint32_t value_odd(uint32_t w)
-{
-    const __half2 v = __hfma2(*reinterpret_cast<const __half2 *>(&w), __half2half2(__ushort_as_half(0x2c00)), __half2half2(__ushort_as_half(0xd480)));  // / 16 - 72
-    return *reinterpret_cast<const uint32_t *>(&v);
-}
+__device__ __forceinline__ uint32_t signed_even(uint32_t w) { return half_fma(w, 0x3400, 0xdc20); }  // / 4 - 264
+__device__ __forceinline__ uint32_t signed_odd(uint32_t w) { return half_fma(w, 0x2400, 0xce00); }   // / 64 - 24
 
 // W words of a lane from shared memory.
 template <int W>
@@ -232,6 +257,30 @@ __device__ __forceinline__ void cp_async16(uint32_t smem, const void *g)
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem), "l"(g) : "memory");
 }
 
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+}
+// The same place in the shared memory of block `rank` of the cluster.
+__device__ __forceinline__ uint32_t remote_place(const void *p, int rank)
+{
+    uint32_t at;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+    return at;
+}
+__device__ __forceinline__ float remote(const float *p, int rank)
+{
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote_place(p, rank)) : "memory");
+    return v;
+}
+__device__ __forceinline__ float4 remote4(const float *p, int rank)
+{
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(remote_place(p, rank)) : "memory");
+    return v;
+}
+
 constexpr size_t ring_bytes(int blocks) { return (size_t)kWarps * kStages * kv_tile_words(blocks) * 4; }
 
 // Blocks that a variant's registers let an SM hold.
@@ -248,12 +297,12 @@ __device__ __forceinline__ void release_join() { asm volatile("griddepcontrol.la
 template <int B, int NT, bool SPLIT>
 struct Warp {
     float o[B][2][NT][4];        // sums of c p: channels 32 b + 4 (lane / 4) + 2 i + {0, 1}, columns 8 nt + 2 (lane % 4) + {0, 1}
-    float top[NT][2], weight[NT][2];  // of the lane's columns
+    float base[NT][2], weight[NT][2];  // of the lane's columns: what is added to a score, shift - largest so far; sum of weights
     uint32_t high;               // words of scales above this want a higher reference
-    float shift;                 // kHeadroom - log2 of the scales' reference
+    float shift, limit;          // kHeadroom - log2 of the scales' reference; shift + kRise
     uint32_t qf[B][2][NT][2];    // B operands of the keys' products
     uint32_t ql[SPLIT ? B : 1][2][NT][2];
-    float init[SPLIT ? 1 : B][NT][2];  // -8 sum(q) of the block, as the products count
+    uint32_t eights[(B + 3) / 4][NT][2];  // -8 sum(q) of block lane % 4 of each four, for column lane / 4, in three bf16 parts
     float factor[NT][2];         // scores = factor * sum over blocks
     int32_t lo[NT][2], hi[NT][2];
 };
@@ -268,25 +317,24 @@ __device__ __forceinline__ void load_queries(const AttnParams &p, const Unit &u,
         const bool there = row < u.rows;
         const int64_t at = (u.row0 + row) * p.q_token + ((int64_t)head * p.group + (column - row * p.group)) * p.q_head;
         float v[B][8];
-        float top = 0.0f;
-        bool finite = true;
+        uint32_t magnitude = 0;  // magnitudes compare like integers, infinity and NaN above all others
 #pragma unroll
-        for (int b = 0; b < B; ++b)
+        for (int b = 0; b < B; ++b) {
+            const int c = 32 * b + 8 * quarter;
+            load_row<SPLIT>(p, at + c, there ? p.g.dim - c : 0, v[b]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int c = 32 * b + 8 * quarter + i;
-                v[b][i] = there && c < p.g.dim ? load_element(p.q, p.type, at + c) : 0.0f;
-                finite = finite && fabsf(v[b][i]) <= 3.4028234e38f;
-                top = fmaxf(top, fabsf(v[b][i]));
-            }
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        finite = __ballot_sync(0xffffffffu, !finite) >> (lane & 28) & 15 ? false : true;
+            for (int i = 0; i < 8; ++i) magnitude = max(magnitude, __float_as_uint(v[b][i]) & 0x7fffffffu);
+        }
+        magnitude = max(magnitude, __shfl_xor_sync(0xffffffffu, magnitude, 1));
+        magnitude = max(magnitude, __shfl_xor_sync(0xffffffffu, magnitude, 2));
+        const bool finite = magnitude < 0x7f800000u;
+        const float top = __uint_as_float(magnitude);
         // times 2^k, so that the largest is in [2^14, 2^15)
         int e = 0;
         if (top > 0.0f && finite) e = ilogbf(top);
         const int k = 14 - e, k1 = k / 2, k2 = k - k1;
         const float s1 = __uint_as_float((uint32_t)(127 + k1) << 23), s2 = __uint_as_float((uint32_t)(127 + k2) << 23);
+        float eights[(B + 3) / 4] = {};
 #pragma unroll
         for (int b = 0; b < B; ++b) {
             float sum = 0.0f;
@@ -309,16 +357,23 @@ __device__ __forceinline__ void load_queries(const AttnParams &p, const Unit &u,
             if (!SPLIT) {
                 sum += __shfl_xor_sync(0xffffffffu, sum, 1);
                 sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-                sum *= -8.0f * 0x1p-24f;
-#pragma unroll
-                for (int j = 0; j < 2; ++j) w.init[SPLIT ? 0 : b][nt][j] = __shfl_sync(0xffffffffu, sum, (2 * quarter + j) * 4);
+                if ((b & 3) == quarter) eights[b / 4] = sum * (-8.0f * 0x1p-22f);
             }
         }
-        // what the sums of 2^-24 2^k code * q are multiplied with (2^24 2^-k scale; fp32 rows 2^-k scale; in steps that stay in range)
+        if (!SPLIT) {
+#pragma unroll
+            for (int x = 0; x < (B + 3) / 4; ++x) {
+                const __nv_bfloat16 a = __float2bfloat16_rn(eights[x]), c = __float2bfloat16_rn(eights[x] - __bfloat162float(a)),
+                                    d = __float2bfloat16_rn(eights[x] - __bfloat162float(a) - __bfloat162float(c));
+                w.eights[x][nt][0] = (uint32_t)__bfloat16_as_ushort(a) | (uint32_t)__bfloat16_as_ushort(c) << 16;
+                w.eights[x][nt][1] = (uint32_t)__bfloat16_as_ushort(d);
+            }
+        }
+        // what the sums of 2^-22 2^k code * q are multiplied with (2^22 2^-k scale; fp32 rows 2^-k scale; in steps that stay in range)
         const float f = finite ? p.scale : __uint_as_float(0x7fc00000u);
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const int from = (2 * quarter + j) * 4, kc = (SPLIT ? 0 : 24) - __shfl_sync(0xffffffffu, k, from), c1 = kc / 2, c2 = kc - c1;
+            const int from = (2 * quarter + j) * 4, kc = (SPLIT ? 0 : 22) - __shfl_sync(0xffffffffu, k, from), c1 = kc / 2, c2 = kc - c1;
             w.factor[nt][j] = __shfl_sync(0xffffffffu, f, from) * __uint_as_float((uint32_t)(127 + c1) << 23) * __uint_as_float((uint32_t)(127 + c2) << 23);
             column_range(p, u, u.column0 + 8 * nt + 2 * quarter + j, &w.lo[nt][j], &w.hi[nt][j]);
         }
@@ -327,7 +382,7 @@ __device__ __forceinline__ void load_queries(const AttnParams &p, const Unit &u,
 
 // Scores of tokens 8 r + lane / 4 of the tile for the lane's columns, the blocks of one plane.
 template <int B, int NT, bool SPLIT, int FIRST, int W>
-__device__ __forceinline__ void plane_scores(const uint32_t *tile, const Warp<B, NT, SPLIT> &w, const uint32_t (&sc)[2][B], float (&s)[2][NT][2])
+__device__ __forceinline__ void plane_scores(const uint32_t *tile, const Warp<B, NT, SPLIT> &w, const uint32_t (&sc)[2][B], float (&s)[NT][4])
 {
     const int lane = threadIdx.x & 31;
     uint32_t k[2][W];
@@ -335,14 +390,14 @@ __device__ __forceinline__ void plane_scores(const uint32_t *tile, const Warp<B,
     for (int h = 0; h < 2; ++h) load_words<W>(tile + 64 * FIRST + (32 * h + lane) * W, k[h]);
 #pragma unroll
     for (int i = 0; i < W; ++i) {
-        constexpr uint32_t kEven = 0x000f000fu, kOdd = 0x00f000f0u, kBase = 0x64006400u;
+        constexpr uint32_t kEven = 0x003c003cu, kOdd = 0x03c003c0u, kBase = 0x64006400u;
         const int b = FIRST + i;
-        const uint32_t u0 = k[0][i], u1 = k[1][i], v0 = u0 >> 8, v1 = u1 >> 8;
+        const uint32_t u0 = k[0][i], u1 = k[1][i], v0 = swap_bytes(u0), v1 = swap_bytes(u1);
         const float s0 = __uint_as_float(sc[0][b] << 16), s1 = __uint_as_float(sc[1][b] << 16);
         uint32_t a[8] = {u0 & kEven, u1 & kEven, u0 & kOdd, u1 & kOdd, v0 & kEven, v1 & kEven, v0 & kOdd, v1 & kOdd};
         if (SPLIT) {
 #pragma unroll
-            for (int x = 0; x < 8; ++x) a[x] = x & 2 ? value_odd(a[x] | kBase) : value_even(a[x] | kBase);
+            for (int x = 0; x < 8; ++x) a[x] = x & 2 ? signed_odd(a[x] | kBase) : signed_even(a[x] | kBase);
         }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -352,14 +407,13 @@ __device__ __forceinline__ void plane_scores(const uint32_t *tile, const Warp<B,
                 mma(d, a[4], a[5], a[6], a[7], w.ql[SPLIT ? b : 0][1][nt][0], w.ql[SPLIT ? b : 0][1][nt][1]);
                 mma(d, a[0], a[1], a[2], a[3], w.qf[b][0][nt][0], w.qf[b][0][nt][1]);
             } else {
-                const float c0 = w.init[SPLIT ? 0 : b][nt][0], c1 = w.init[SPLIT ? 0 : b][nt][1];
-                mma(d, a[0], a[1], a[2], a[3], w.qf[b][0][nt][0], w.qf[b][0][nt][1], c0, c1, c0, c1);
+                mma(d, a[0], a[1], a[2], a[3], w.qf[b][0][nt][0], w.qf[b][0][nt][1], 0.0f, 0.0f, 0.0f, 0.0f);
             }
             mma(d, a[4], a[5], a[6], a[7], w.qf[b][1][nt][0], w.qf[b][1][nt][1]);
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                s[0][nt][j] = fmaf(s0, d[j], s[0][nt][j]);
-                s[1][nt][j] = fmaf(s1, d[2 + j], s[1][nt][j]);
+                s[nt][j] = fmaf(s0, d[j], s[nt][j]);
+                s[nt][2 + j] = fmaf(s1, d[2 + j], s[nt][2 + j]);
             }
         }
     }
@@ -376,16 +430,17 @@ __device__ __forceinline__ void plane_values(const uint32_t *tile, Warp<B, NT, S
     for (int h = 0; h < 2; ++h) load_words<W>(tile + 64 * B + 64 * FIRST + (32 * h + lane) * W, v[h]);
 #pragma unroll
     for (int i = 0; i < W; ++i) {
-        constexpr uint32_t kEven = 0x000f000fu, kOdd = 0x00f000f0u, kBase = 0x64006400u;
+        constexpr uint32_t kEven = 0x003c003cu, kOdd = 0x03c003c0u, kBase = 0x64006400u;
+        constexpr uint32_t kEven8 = 0x80208020u, kOdd8 = 0x82008200u;  // of the even and of the odd codes, as they stand
         const int b = FIRST + i;
         uint32_t a[2][4];  // [half][channel]
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const uint32_t x = v[h][i], y = x >> 8;
-            a[h][0] = value_even(and_or(x, kEven, kBase));
-            a[h][1] = value_odd(and_or(x, kOdd, kBase));
-            a[h][2] = value_even(and_or(y, kEven, kBase));
-            a[h][3] = value_odd(and_or(y, kOdd, kBase));
+            const uint32_t x = v[h][i], y = swap_bytes(x);
+            a[h][0] = SPLIT ? signed_even(and_or(x, kEven, kBase)) : x & kEven;
+            a[h][1] = SPLIT ? signed_odd(and_or(x, kOdd, kBase)) : x & kOdd;
+            a[h][2] = SPLIT ? signed_even(and_or(y, kEven, kBase)) : y & kEven;
+            a[h][3] = SPLIT ? signed_odd(and_or(y, kOdd, kBase)) : y & kOdd;
         }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -405,6 +460,7 @@ __device__ __forceinline__ void plane_values(const uint32_t *tile, Warp<B, NT, S
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 if (!SPLIT) {
+                    mma(w.o[b][c][nt], kEven8, kOdd8, kEven8, kOdd8, ph[0], ph[1]);
                     mma(w.o[b][c][nt], a[0][2 * c], a[0][2 * c + 1], a[1][2 * c], a[1][2 * c + 1], ph[0], ph[1]);
                 } else {
                     float d[4];  // the products cut their sums: a long one would drift by 2^-24 each
@@ -444,13 +500,29 @@ __device__ __forceinline__ void tile_step(const uint32_t *tile, int32_t token0, 
         }
         if (S) sc[r][B - 1] = at[16 * (B - 1) + token];
     }
-    float s[2][NT][2] = {};
+    float s[NT][4] = {};
+    if (!SPLIT) {
+        // what the 8 in every code adds, taken off: -8 sum(q) of each block times the key's scale, a product of its own
+#pragma unroll
+        for (int x = 0; x < (B + 3) / 4; ++x) {
+            const int b = 4 * x + (lane & 3);
+            uint32_t a[2] = {0, 0};
+            if (4 * x + 4 <= B || b < B) {
+#pragma unroll
+                for (int r = 0; r < 2; ++r) a[r] = __byte_perm(tile[kv_scale_word(B, 8 * r + (lane >> 2), b)], 0, 0x1010);
+            }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) mma_bf16(s[nt], a[0], a[1], a[0], a[1], w.eights[x][nt][0], w.eights[x][nt][1]);
+        }
+    }
     if (Q > 0) plane_scores<B, NT, SPLIT, 0, 4>(tile, w, sc, s);
     if (Q > 4) plane_scores<B, NT, SPLIT, (Q > 4 ? 4 : 0), 4>(tile, w, sc, s);
     if (T) plane_scores<B, NT, SPLIT, (T ? Q : 0), 2>(tile, w, sc, s);
     if (S) plane_scores<B, NT, SPLIT, B - 1, 1>(tile, w, sc, s);
     bool shown[2][NT][2];
     uint32_t largest = 0;  // scale of a value of the lane's tokens, in the high half
+    float highest = -INFINITY;
+    float e[2][NT][2];     // log2 of the weights first
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
         bool some = !MASKED;
@@ -458,44 +530,46 @@ __device__ __forceinline__ void tile_step(const uint32_t *tile, int32_t token0, 
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                s[r][nt][j] *= w.factor[nt][j];
+                e[r][nt][j] = fmaf(s[nt][2 * r + j], w.factor[nt][j], w.base[nt][j]);
                 shown[r][nt][j] = true;
                 if (MASKED) {
                     const int32_t token = token0 + 8 * r + (lane >> 2);
                     shown[r][nt][j] = token >= w.lo[nt][j] && token < w.hi[nt][j];
-                    if (!shown[r][nt][j]) s[r][nt][j] = -INFINITY;
+                    if (!shown[r][nt][j]) e[r][nt][j] = -INFINITY;
                     some = some || shown[r][nt][j];
                 }
+                highest = fmaxf(highest, e[r][nt][j]);
             }
 #pragma unroll
         for (int b = 0; b < B; ++b) largest = max(largest, some ? sc[r][b] : 0u);
     }
-    bool above = largest > w.high;
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) above = above || fmaxf(s[0][nt][j], s[1][nt][j]) > w.top[nt][j] + kRise;
-    if (__any_sync(0xffffffffu, above)) {
+    if (__any_sync(0xffffffffu, largest > w.high || highest > w.limit)) {
         // rare behind the first tiles: the references move up and the sums with them
         const float old_shift = w.shift;
         largest = __reduce_max_sync(0xffffffffu, largest);
         if (largest > w.high && largest < 0x7f800000u) {  // a NaN moves nothing
-            const int e = max((int)(largest >> 23) - 126, -100);  // scales < 2^e; the weights themselves stay in range
-            w.shift = kHeadroom - (float)e;
-            w.high = (uint32_t)(127 + e) << 23 | 0xffffu;
+            const int x = max((int)(largest >> 23) - 126, -100);  // scales < 2^x; the weights themselves stay in range
+            w.shift = kHeadroom - (float)x;
+            w.high = (uint32_t)(127 + x) << 23 | 0xffffu;
+            w.limit = w.shift + kRise;
         }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                float m = fmaxf(s[0][nt][j], s[1][nt][j]);
+                // scores again, the largest among them and so far
+                float x[2];
+#pragma unroll
+                for (int r = 0; r < 2; ++r) x[r] = shown[r][nt][j] ? s[nt][2 * r + j] * w.factor[nt][j] : -INFINITY;
+                float m = fmaxf(x[0], x[1]);
                 m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
                 m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
                 m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16));
-                const float top = fmaxf(m, w.top[nt][j]);
-                const float f = exp2f((w.top[nt][j] - top) + (w.shift - old_shift));
-                w.top[nt][j] = top;
+                const float base = w.shift - fmaxf(m, old_shift - w.base[nt][j]), f = exp2f(base - w.base[nt][j]);
+                w.base[nt][j] = base;
                 w.weight[nt][j] *= f;
+#pragma unroll
+                for (int r = 0; r < 2; ++r) e[r][nt][j] = x[r] + base;
 #pragma unroll
                 for (int b = 0; b < B; ++b)
 #pragma unroll
@@ -505,14 +579,12 @@ __device__ __forceinline__ void tile_step(const uint32_t *tile, int32_t token0, 
                     }
             }
     }
-    float e[2][NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            const float base = w.shift - w.top[nt][j];
 #pragma unroll
-            for (int r = 0; r < 2; ++r) e[r][nt][j] = exp2_fast(s[r][nt][j] + base);
+            for (int r = 0; r < 2; ++r) e[r][nt][j] = exp2_fast(e[r][nt][j]);
             w.weight[nt][j] += e[0][nt][j] + e[1][nt][j];
         }
     if (Q > 0) plane_values<B, NT, SPLIT, 0, 4, MASKED>(tile, w, sc, e, shown);
@@ -527,10 +599,11 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(B, NT, SPLIT)) kv_atte
     constexpr int COLUMNS = 8 * NT, TILE = kv_tile_words(B), PIECES = TILE / 4;
     extern __shared__ __align__(128) uint32_t smem[];
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    release_join();
+    if (p.join) release_join();
     Unit u;
     int first_unit;
-    if (!find_unit<COLUMNS, false>(p, blockIdx.x, &u, &first_unit)) return;
+    const int unit = blockIdx.x / p.cluster, rank = blockIdx.x - unit * p.cluster;
+    if (!find_unit<COLUMNS, false>(p, unit, &u, &first_unit)) return;
     const int head = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     Warp<B, NT, SPLIT> w;
     load_queries(p, u, head, w);
@@ -538,7 +611,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(B, NT, SPLIT)) kv_atte
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            w.top[nt][j] = kLowest;
+            w.base[nt][j] = -kLowest;
             w.weight[nt][j] = 0.0f;
         }
 #pragma unroll
@@ -551,6 +624,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(B, NT, SPLIT)) kv_atte
                 for (int j = 0; j < 4; ++j) w.o[b][i][nt][j] = 0.0f;
     w.high = 0xffffu;
     w.shift = 0.0f;
+    w.limit = kRise;
 
     // tokens that every column sees, and those that one sees at least
     int32_t all_lo = 0, all_hi = 0x7fffffff, any_lo = 0x7fffffff, any_hi = 0;
@@ -572,41 +646,42 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(B, NT, SPLIT)) kv_atte
     const int32_t tile0 = any_hi > 0 ? max(u.tile0, any_lo / kKvTile) : u.tile1, tile1 = min(u.tile1, (any_hi + kKvTile - 1) / kKvTile);
 
     uint32_t *const ring = smem + warp * kStages * TILE;
-    const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
     const int32_t *const table = p.page_table + (int64_t)u.seq * p.table_pages;
     const int tiles_per_page = p.g.page_size / kKvTile;
-    // places of the warp's next 32 tiles in the cache, one to a lane; negative: not in the pool
-    int64_t places = -1;
-    const int32_t mine = max((tile1 - tile0 - warp + kWarps - 1) / kWarps, 0);
+    // a cluster's warps take its tiles in turn
+    const int first_warp = rank * kWarps + warp, step = kWarps * p.cluster;
+    // the warp's next 32 tiles in the cache, one to a lane; negative: not in the pool
+    int32_t places = -1;
+    const int32_t mine = max((tile1 - tile0 - first_warp + step - 1) / step, 0);
     const char *const cache = reinterpret_cast<const char *>(p.cache) + lane * 16;
-    auto fetch = [&](int i) {  // issues the copies of the warp's i-th tile
+    auto fetch = [&](int i, uint32_t to) {  // issues the copies of the warp's i-th tile
         if ((i & 31) == 0) {
-            const int32_t t = tile0 + warp + (i + lane) * kWarps, in_table = t / tiles_per_page;
+            const int32_t t = tile0 + first_warp + (i + lane) * step, in_table = t / tiles_per_page;
             const int32_t page = t < tile1 ? __ldg(table + in_table) : -1;
-            places = page >= 0 && page < p.g.pages ? (((int64_t)page * p.g.heads + head) * tiles_per_page + (t - in_table * tiles_per_page)) * (TILE * 4) : -1;
+            places = page >= 0 && page < p.g.pages ? (page * p.g.heads + head) * tiles_per_page + (t - in_table * tiles_per_page) : -1;
         }
-        const int64_t place = __shfl_sync(0xffffffffu, places, i & 31);
+        const int32_t place = __shfl_sync(0xffffffffu, places, i & 31);
         if (place >= 0) {
-            const uint32_t to = ring_at + (i % kStages) * (TILE * 4) + lane * 16;
+            const char *const from = cache + (int64_t)place * (TILE * 4);
 #pragma unroll
             for (int c = 0; c < (PIECES + 31) / 32; ++c)
-                if (c * 32 + 32 <= PIECES || c * 32 + lane < PIECES) cp_async16(to + c * 512, cache + place + c * 512);
+                if (c * 32 + 32 <= PIECES || c * 32 + lane < PIECES) cp_async16(to + c * 512, from + c * 512);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
         return place >= 0;
     };
-    uint32_t good = 0;  // whether the tile of a stage is there
+    uint32_t good = 0;  // whether the warp's next tiles are there, the next one in bit 0
+    const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring) + lane * 16;
 #pragma unroll
-    for (int i = 0; i < kStages - 1; ++i) good |= fetch(i) ? 1u << i : 0u;
-    for (int i = 0; i < mine; ++i) {
+    for (int i = 0; i < kStages - 1; ++i) good |= fetch(i, ring_at + i * (TILE * 4)) ? 1u << i : 0u;
+    int32_t token0 = (tile0 + first_warp) * kKvTile;
+    for (int i = 0, stage = 0; i < mine; ++i, token0 += step * kKvTile, good >>= 1, stage = stage + 1 == kStages ? 0 : stage + 1) {
         __syncwarp();  // everyone is done with the stage that comes next
-        const int next = (i + kStages - 1) % kStages;
-        good = (good & ~(1u << next)) | (fetch(i + kStages - 1) ? 1u << next : 0u);
+        good |= fetch(i + kStages - 1, ring_at + (stage ? stage - 1 : kStages - 1) * (TILE * 4)) ? 1u << (kStages - 1) : 0u;
         asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
         __syncwarp();
-        if (!(good >> (i % kStages) & 1)) continue;
-        const int32_t token0 = (tile0 + warp + i * kWarps) * kKvTile;
-        const uint32_t *const tile = ring + (i % kStages) * TILE;
+        if (!(good & 1)) continue;
+        const uint32_t *const tile = ring + stage * TILE;
         if (token0 >= all_lo && token0 + kKvTile <= all_hi) tile_step<B, NT, SPLIT, false>(tile, token0, w);
         else tile_step<B, NT, SPLIT, true>(tile, token0, w);
     }
@@ -626,41 +701,87 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(B, NT, SPLIT)) kv_atte
             l += __shfl_xor_sync(0xffffffffu, l, 8);
             l += __shfl_xor_sync(0xffffffffu, l, 16);
             if (lane < 4) {
-                tops[warp * COLUMNS + column] = w.top[nt][j] - w.shift;
+                tops[warp * COLUMNS + column] = -w.base[nt][j];
                 weights[warp * COLUMNS + column] = l;
             }
             float *const to = sums + (warp * COLUMNS + column) * D + 4 * (lane >> 2);
 #pragma unroll
-            for (int b = 0; b < B; ++b)
-                *reinterpret_cast<float4 *>(to + 32 * b) = make_float4(w.o[b][0][nt][j], w.o[b][0][nt][2 + j], w.o[b][1][nt][j], w.o[b][1][nt][2 + j]);
+            for (int b = 0; b < B; ++b) {
+                constexpr float kEven = SPLIT ? 1.0f : 0x1p22f, kOdd = SPLIT ? 1.0f : 0x1p18f;  // what the codes stood for
+                *reinterpret_cast<float4 *>(to + 32 * b) = make_float4(kEven * w.o[b][0][nt][j], kOdd * w.o[b][0][nt][2 + j], kEven * w.o[b][1][nt][j],
+                                                                       kOdd * w.o[b][1][nt][2 + j]);
+            }
         }
     __syncthreads();
-    for (int at = threadIdx.x; at < COLUMNS * D; at += kThreads) {
-        const int column = at / D, c = at % D;
-        float top = tops[column];
+    // [warp][column]: by what a warp's sums and weight count; the largest and the weight of all
+    float *const factors = weights + kWarps * COLUMNS, *const all_top = factors + kWarps * COLUMNS, *const all_weight = all_top + COLUMNS;
+    if (threadIdx.x < COLUMNS) {
+        const int column = threadIdx.x;
+        float top = tops[column], weight = 0.0f;
 #pragma unroll
         for (int i = 1; i < kWarps; ++i) top = fmaxf(top, tops[i * COLUMNS + column]);
-        float sum = 0.0f, weight = 0.0f;
 #pragma unroll
         for (int i = 0; i < kWarps; ++i) {
             const float f = exp2f(tops[i * COLUMNS + column] - top);
-            sum = fmaf(f, sums[(i * COLUMNS + column) * D + c], sum);
+            factors[i * COLUMNS + column] = f;
             weight = fmaf(f, weights[i * COLUMNS + column], weight);
         }
-        if (u.chunks > 1) {
-            float *const to = p.parts + (((int64_t)blockIdx.x * p.g.heads + head) * COLUMNS + column) * (D + 4);
-            to[c] = sum;
-            if (c == 0) {
-                to[D] = top;
-                to[D + 1] = weight;
-            }
-        } else {
-            const int q = u.column0 + column, row = q / p.group;
-            if (row < u.rows && c < p.g.dim)
-                store_element(p.out, p.type, (u.row0 + row) * p.out_token + ((int64_t)head * p.group + (q - row * p.group)) * p.out_head + c,
-                              weight == 0.0f ? 0.0f : sum / weight);
-        }
+        all_top[column] = top;
+        all_weight[column] = weight;
     }
+    __syncthreads();
+    // four channels at a time
+    auto put = [&](int column, int c, float4 sum, float top, float weight) {
+        if (u.chunks > 1) {
+            float *const to = p.parts + (((int64_t)unit * p.g.heads + head) * COLUMNS + column) * (D + 4);
+            *reinterpret_cast<float4 *>(to + c) = sum;
+            if (c == 0) *reinterpret_cast<float2 *>(to + D) = make_float2(top, weight);
+            return;
+        }
+        const int q = u.column0 + column, row = q / p.group;
+        if (row >= u.rows) return;
+        const float by = weight == 0.0f ? 0.0f : 1.0f / weight;
+        const int64_t at = (u.row0 + row) * p.out_token + ((int64_t)head * p.group + (q - row * p.group)) * p.out_head + c;
+        const float v[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (c + i < p.g.dim) store_element(p.out, p.type, at + i, weight == 0.0f ? 0.0f : v[i] * by);
+    };
+    for (int at = threadIdx.x; at < COLUMNS * D / 4; at += kThreads) {
+        const int column = at / (D / 4), c = at % (D / 4) * 4;
+        float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int i = 0; i < kWarps; ++i) {
+            const float f = factors[i * COLUMNS + column];
+            const float4 v = *reinterpret_cast<const float4 *>(sums + (i * COLUMNS + column) * D + c);
+            sum.x = fmaf(f, v.x, sum.x);
+            sum.y = fmaf(f, v.y, sum.y);
+            sum.z = fmaf(f, v.z, sum.z);
+            sum.w = fmaf(f, v.w, sum.w);
+        }
+        if (p.cluster == 1) put(column, c, sum, all_top[column], all_weight[column]);
+        else *reinterpret_cast<float4 *>(sums + column * D + c) = sum;  // in warp 0's place, which nobody else reads
+    }
+    if (p.cluster == 1) return;
+    // The blocks of a cluster read each other's sums where they are; each finishes its share of the columns' channels.
+    cluster_sync();
+    for (int at = rank * kThreads + threadIdx.x; at < COLUMNS * D / 4; at += p.cluster * kThreads) {
+        const int column = at / (D / 4), c = at % (D / 4) * 4;
+        float top = -INFINITY, weight = 0.0f;
+        for (int r = 0; r < p.cluster; ++r) top = fmaxf(top, remote(all_top + column, r));
+        float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int r = 0; r < p.cluster; ++r) {
+            const float f = exp2f(remote(all_top + column, r) - top);
+            weight = fmaf(f, remote(all_weight + column, r), weight);
+            const float4 v = remote4(sums + column * D + c, r);
+            sum.x = fmaf(f, v.x, sum.x);
+            sum.y = fmaf(f, v.y, sum.y);
+            sum.z = fmaf(f, v.z, sum.z);
+            sum.w = fmaf(f, v.w, sum.w);
+        }
+        put(column, c, sum, top, weight);
+    }
+    cluster_sync();  // nobody leaves while its sums are read
 }
 
 // Joins the pieces of a column, always in the same order: a block to a column, its warps' share of the pieces first, then the
@@ -727,7 +848,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) kv_attention_join_kernel(cons
     }
 }
 
-constexpr size_t merge_bytes(int blocks, int nt) { return (size_t)kWarps * 8 * nt * (32 * blocks + 2) * 4; }
+constexpr size_t merge_bytes(int blocks, int nt) { return ((size_t)kWarps * 8 * nt * (32 * blocks + 3) + 2 * 8 * nt) * 4; }
 
 template <int B, int NT, bool SPLIT>
 lce_status launch(const AttnParams &p, cudaStream_t s)
@@ -735,8 +856,24 @@ lce_status launch(const AttnParams &p, cudaStream_t s)
     constexpr size_t smem = ring_bytes(B) > merge_bytes(B, NT) ? ring_bytes(B) : merge_bytes(B, NT);
     static SmemOptIn opt_in;
     if (!opt_in.ensure(kv_attention_kernel<B, NT, SPLIT>, smem)) return LCE_ERR_CUDA;
-    const lce_status st = launch_dependent(kv_attention_kernel<B, NT, SPLIT>, dim3((unsigned)p.units, (unsigned)p.g.heads), kThreads, smem, s, p);
-    if (st != LCE_OK) return st;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(p.units * p.cluster), (unsigned)p.g.heads, 1);
+    cfg.blockDim = dim3(kThreads, 1, 1);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)p.cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = p.cluster > 1 ? 2 : 1;
+    if (cudaLaunchKernelEx(&cfg, kv_attention_kernel<B, NT, SPLIT>, p) != cudaSuccess) {
+        cudaGetLastError();
+        return LCE_ERR_CUDA;
+    }
+    if (!p.join) return LCE_OK;
     // columns that there can be in a tile
     const int64_t columns = p.tokens * p.group < 8 * NT ? p.tokens * p.group : p.one_row && p.group < 8 * NT ? p.group : 8 * NT;
     return launch_dependent(kv_attention_join_kernel<NT>, dim3((unsigned)p.column_tiles, (unsigned)p.g.heads, (unsigned)columns), 32 * kJoinWarps, 0, s, p);
@@ -761,9 +898,10 @@ lce_status launch_blocks(const AttnParams &p, cudaStream_t s)
     }
 }
 
-int64_t column_tiles(const AttnParams &p, int columns) { return p.tokens * p.group / columns + p.batch; }
+constexpr int kLeastTiles = 16;  // tiles of a warp that a piece is worth
 
-lce_status make_params(const lce_kv_attention_desc *d, AttnParams *p, int *nt)
+// one_row: without q_starts
+lce_status make_params(const lce_kv_attention_desc *d, bool one_row, AttnParams *p, int *nt)
 {
     if (!d) return LCE_ERR_INVALID_ARG;
     const lce_status st = make_kv_geom(&d->cache, &p->g);
@@ -774,6 +912,7 @@ lce_status make_params(const lce_kv_attention_desc *d, AttnParams *p, int *nt)
     for (const int64_t s : {d->q_token_stride, d->q_head_stride, d->out_token_stride, d->out_head_stride})
         if (s < 0 || s >= (1ll << 40)) return LCE_ERR_INVALID_ARG;
     p->batch = d->batch; p->group = d->heads / d->cache.kv_heads; p->table_pages = d->table_pages;
+    p->one_row = one_row;
     if (d->tokens * d->heads >= (1ll << 31) || (int64_t)d->table_pages * d->cache.page_size >= (1ll << 31) || d->batch >= (1 << 20)) return LCE_ERR_UNSUPPORTED;
     p->table_tokens = d->table_pages * d->cache.page_size;
     p->causal = d->causal; p->window = d->window; p->type = d->type;
@@ -781,21 +920,27 @@ lce_status make_params(const lce_kv_attention_desc *d, AttnParams *p, int *nt)
     p->q_token = d->q_token_stride; p->q_head = d->q_head_stride; p->out_token = d->out_token_stride; p->out_head = d->out_head_stride;
     p->scale = d->scale * 1.44269504088896341f;
     *nt = p->g.blocks <= kWideBlocks && (d->tokens * p->group + d->batch - 1) / d->batch > 8 ? 2 : 1;
-    const int64_t tiles = column_tiles(*p, 8 * *nt);
-    const int64_t wanted = 148 * blocks_per_sm(p->g.blocks, *nt, p->type == LCE_TYPE_FLOAT32);  // blocks: what the GPU holds at a time
-    int64_t target = (wanted + p->g.heads - 1) / p->g.heads;
-    // never more pieces than there are tiles
-    const int64_t most = (int64_t)((p->table_tokens + kKvTile - 1) / kKvTile) * tiles;
-    if (target > most) target = most;
-    p->target = (int32_t)target;
-    p->least_tiles = kWarps;
-    if (tiles + target >= (1ll << 31)) return LCE_ERR_UNSUPPORTED;
+    const int columns = 8 * *nt;
+    const int64_t tiles = one_row ? (int64_t)p->batch * ((p->group + columns - 1) / columns) : p->tokens * p->group / columns + p->batch;
+    // A cluster of up to eight blocks shares a unit, as many as the GPU has room for and as there are tiles for their warps.
+    const int64_t blocks = 148 * blocks_per_sm(p->g.blocks, *nt, p->type == LCE_TYPE_FLOAT32);
+    int64_t most = (p->table_tokens + kKvTile - 1) / kKvTile;  // tiles that a sequence can have in view
+    if (p->window > 0 && one_row && p->window / kKvTile + 2 < most) most = p->window / kKvTile + 2;
+    p->cluster = 1;
+    while (p->cluster < 8 && most <= kWarps * 8 * kLeastTiles && tiles * p->g.heads * p->cluster * 2 <= blocks && p->cluster * kWarps < most) p->cluster *= 2;
+    // Sequences longer than that pays for are cut further.
+    p->least_tiles = kWarps * p->cluster * kLeastTiles;
+    p->join = most > p->least_tiles;
+    const int waves = p->batch > 1 ? 2 : 1;  // pieces of one sequence are all alike
+    const int64_t target = p->join ? (blocks * waves / p->cluster + p->g.heads - 1) / p->g.heads : 0;
+    p->target = (int32_t)(target > 0 ? target : 1);
+    if ((tiles + target) * p->cluster >= (1ll << 31) || (int64_t)p->g.slots / kKvTile * p->g.heads >= (1ll << 31)) return LCE_ERR_UNSUPPORTED;
     p->units = (int32_t)(tiles + target);
     p->column_tiles = (int32_t)tiles;
     return LCE_OK;
 }
 
-size_t workspace_bytes(const AttnParams &p, int nt) { return (size_t)p.units * p.g.heads * 8 * nt * (32 * p.g.blocks + 4) * 4; }
+size_t workspace_bytes(const AttnParams &p, int nt) { return !p.join ? 16 : (size_t)p.units * p.g.heads * 8 * nt * (32 * p.g.blocks + 4) * 4; }
 
 }  // namespace
 }  // namespace lce
@@ -805,8 +950,15 @@ extern "C" size_t lce_kv_attention_workspace_bytes(const lce_kv_attention_desc *
     using namespace lce;
     AttnParams p{};
     int nt;
-    if (make_params(desc, &p, &nt) != LCE_OK) return 0;
-    return workspace_bytes(p, nt);
+    // the room that the call wants with and without q_starts
+    size_t bytes = 0;
+    for (const bool one_row : {false, true}) {
+        if (one_row && desc && desc->tokens != desc->batch) continue;
+        if (make_params(desc, one_row, &p, &nt) != LCE_OK) return 0;
+        const size_t b = workspace_bytes(p, nt);
+        if (b > bytes) bytes = b;
+    }
+    return bytes;
 }
 
 extern "C" lce_status lce_kv_attention(const lce_kv_attention_desc *desc, const void *q, const void *cache, const int32_t *page_table,
@@ -815,7 +967,7 @@ extern "C" lce_status lce_kv_attention(const lce_kv_attention_desc *desc, const 
     using namespace lce;
     AttnParams p{};
     int nt;
-    const lce_status st = make_params(desc, &p, &nt);
+    const lce_status st = make_params(desc, !q_starts, &p, &nt);
     if (st != LCE_OK) return st;
     if (!q_starts && desc->tokens != desc->batch) return LCE_ERR_INVALID_ARG;
     if (desc->tokens == 0) return LCE_OK;
@@ -825,7 +977,7 @@ extern "C" lce_status lce_kv_attention(const lce_kv_attention_desc *desc, const 
         !aligned(workspace, 16))
         return LCE_ERR_ALIGNMENT;
     if (workspace_size < workspace_bytes(p, nt)) return LCE_ERR_WORKSPACE;
-    p.one_row = !q_starts;
+    p.q_vectors = p.g.dim % 8 == 0 && aligned(q, 16) && p.q_token * element % 16 == 0 && p.q_head * element % 16 == 0;
     p.q = q; p.cache = static_cast<const uint32_t *>(cache); p.page_table = page_table; p.lengths = lengths; p.q_starts = q_starts;
     p.out = out; p.parts = static_cast<float *>(workspace);
     cudaStream_t s = static_cast<cudaStream_t>(stream);

@@ -80,6 +80,7 @@ __global__ void __launch_bounds__(kThreads) kv_quantize_kernel(const __grid_cons
 
 __device__ __forceinline__ void kv_values(uint32_t word, float s, float (&v)[8])
 {
+    word = kv_rotate_back(word);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = (float)((int)((word >> (4 * i)) & 15u) - 8) * s;
 }

@@ -9,7 +9,8 @@
 //   scales  word (token, w) at W token + w: bf16 of the key in the low, of the value in the high half.
 // Lane l of a warp finds there exactly its part of the A operands of m16n8k16 products, 16 tokens x channels for the keys
 // and channels x 16 tokens for the values: no transposition, and shared memory is read lane by lane without bank conflicts.
-// Codes are stored as c + 8.
+// Codes are stored as n = c + 8, in either half of a word rotated left by two bits: bits 2 .. 5 and 6 .. 9 of a half, and of one with
+// its bytes exchanged, are then codes as high in the ten mantissa bits of an f16 number as two of them can stand.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -146,10 +147,13 @@ __device__ __forceinline__ float kv_code(float x, float s, float r)
     return c;
 }
 
-// Codes (+ 8) of eight channels in a word, lowest channel in the lowest nibble, for the block's scale.
+__device__ __forceinline__ uint32_t kv_rotate(uint32_t w) { return (w & 0x3fff3fffu) << 2 | (w >> 14 & 0x00030003u); }
+__device__ __forceinline__ uint32_t kv_rotate_back(uint32_t w) { return (w >> 2 & 0x3fff3fffu) | (w & 0x00030003u) << 14; }
+
+// Codes of eight channels as a word holds them, for the block's scale.
 __device__ __forceinline__ uint32_t kv_codes(const float (&v)[8], float s)
 {
-    if (!(s > 0.0f)) return 0x88888888u;  // all zeros, or NaN
+    if (!(s > 0.0f)) return kv_rotate(0x88888888u);  // all zeros, or NaN
     const float up = s < 0x1p-100f ? 0x1p80f : 1.0f;  // away from subnormal numbers, exactly
     const float t = s * up, r = __fdiv_rn(1.0f, t);
     uint32_t word = 0;
@@ -158,7 +162,7 @@ __device__ __forceinline__ uint32_t kv_codes(const float (&v)[8], float s)
         const float c = kv_code(fabsf(v[i]) * up, t, r);
         word |= (uint32_t)(8 + (int)(v[i] < 0.0f ? -c : c)) << (4 * i);
     }
-    return word;
+    return kv_rotate(word);
 }
 
 }  // namespace lce

@@ -49,7 +49,7 @@ class Setup:
 
     def expected(self, scale=None, causal=True, window=0, bad_tokens=()):
         scale = self.dim ** -0.5 if scale is None else scale
-        (k, ks), (v, _) = (ref.quantized(t.double().cpu().numpy()) for t in (self.k, self.v))
+        (k, ks), (v, vs) = (ref.quantized(t.double().cpu().numpy()) for t in (self.k, self.v))
         q = self.q.double().cpu().numpy()
         out, bound = np.zeros(q.shape), np.zeros(q.shape)
         row = token = 0
@@ -65,7 +65,7 @@ class Setup:
                 for s, bad in bad_tokens:
                     if s == b:
                         shown[bad] = False
-                out[row], bound[row] = ref.attention(q[row], k[token:token + n], v[token:token + n], ks[token:token + n], shown, scale, NAMES[self.dtype])
+                out[row], bound[row] = ref.attention(q[row], k[token:token + n], v[token:token + n], ks[token:token + n], vs[token:token + n], shown, scale, NAMES[self.dtype])
                 row += 1
             token += n
         return out, bound
@@ -253,8 +253,8 @@ def test_streams_graphs_and_growing_sequences():
         for b, n in enumerate(lengths):
             keep = list(range(sum(t.lengths[:b]), sum(t.lengths[:b]) + n))
             q = t.q[b].double().cpu().numpy()
-            (k, ks), (v, _) = (ref.quantized(x[keep].double().cpu().numpy()) for x in (t.k, t.v))
-            want = ref.attention(q, k, v, ks, np.ones(n, bool), 128 ** -0.5, "bfloat16")
+            (k, ks), (v, vs) = (ref.quantized(x[keep].double().cpu().numpy()) for x in (t.k, t.v))
+            want = ref.attention(q, k, v, ks, vs, np.ones(n, bool), 128 ** -0.5, "bfloat16")
             check(out[b], want)
             assert torch.equal(out[b], out2[b])
 
@@ -281,7 +281,8 @@ def test_binding_refuses_what_does_not_fit():
         with pytest.raises(ValueError):
             lce.lce_kv_attention(desc, **{**good, **change})
     with pytest.raises(lce.LceError) as e:
-        lce.lce_kv_attention(desc, **good, workspace=torch.empty(16, dtype=torch.uint8, device=DEV))
+        small = lce.lce_kv_attention_workspace_bytes(desc, 2, 2, 4, table.shape[1], BF16) - 1
+        lce.lce_kv_attention(desc, **good, workspace=torch.empty(small, dtype=torch.uint8, device=DEV))
     assert e.value.status == 6
     with pytest.raises(lce.LceError) as e:
         lce.lce_kv_attention(desc, q[:, :3], cache, table, lengths)

@@ -70,10 +70,10 @@ def test_prompt_then_single_tokens():
         want, bound = np.zeros(o.shape), np.zeros(o.shape)
         at = 0
         for b, n in enumerate(news):
-            (kq, ks), (vq, _) = ref.quantized(keys[b]), ref.quantized(values[b])
+            (kq, ks), (vq, vs) = ref.quantized(keys[b]), ref.quantized(values[b])
             for i in range(n):
                 shown = np.arange(lengths[b]) <= lengths[b] - n + i
-                want[at], bound[at] = ref.attention(q[at].double().cpu().numpy(), kq, vq, ks, shown, DIM ** -0.5, "float32")
+                want[at], bound[at] = ref.attention(q[at].double().cpu().numpy(), kq, vq, ks, vs, shown, DIM ** -0.5, "float32")
                 at += 1
         check(o, (want, bound))
         o_bits = lce.lce_bitpack(o.view(tokens, HEADS * DIM))
