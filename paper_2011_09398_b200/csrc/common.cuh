@@ -93,6 +93,14 @@ inline void fast_div_constants(uint32_t d, uint32_t *mul, uint32_t *sh)
     *mul = (uint32_t)(((1ull << (31 + l)) / d) + 1);
 }
 
+#ifdef __CUDACC__
+// n / d for 0 <= n < 2^31 (fast_div_constants)
+struct FastDiv {
+    uint32_t mul, sh;
+    __device__ __forceinline__ int32_t operator()(int32_t n) const { return (int32_t)(((uint64_t)(uint32_t)n * mul) >> sh); }
+};
+#endif
+
 inline lce_status launch_status()
 {
     return cudaGetLastError() == cudaSuccess ? LCE_OK : LCE_ERR_CUDA;

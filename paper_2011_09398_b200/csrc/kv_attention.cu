@@ -605,44 +605,10 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(B, NT, SPLIT)) kv_atte
     const int unit = blockIdx.x / p.cluster, rank = blockIdx.x - unit * p.cluster;
     if (!find_unit<COLUMNS, false>(p, unit, &u, &first_unit)) return;
     const int head = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    Warp<B, NT, SPLIT> w;
-    load_queries(p, u, head, w);
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            w.base[nt][j] = -kLowest;
-            w.weight[nt][j] = 0.0f;
-        }
-#pragma unroll
-    for (int b = 0; b < B; ++b)
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) w.o[b][i][nt][j] = 0.0f;
-    w.high = 0xffffu;
-    w.shift = 0.0f;
-    w.limit = kRise;
-
-    // tokens that every column sees, and those that one sees at least
-    int32_t all_lo = 0, all_hi = 0x7fffffff, any_lo = 0x7fffffff, any_hi = 0;
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            if (w.hi[nt][j] > w.lo[nt][j]) {
-                all_lo = max(all_lo, w.lo[nt][j]);
-                all_hi = min(all_hi, w.hi[nt][j]);
-                any_lo = min(any_lo, w.lo[nt][j]);
-                any_hi = max(any_hi, w.hi[nt][j]);
-            }
-        }
-    all_lo = __reduce_max_sync(0xffffffffu, all_lo);
-    all_hi = __reduce_min_sync(0xffffffffu, all_hi);
-    any_lo = __reduce_min_sync(0xffffffffu, any_lo);
-    any_hi = __reduce_max_sync(0xffffffffu, any_hi);
+    // tokens that every column sees, and those that one sees at least: the ranges' ends grow with the rows
+    int32_t any_lo, all_hi, all_lo, any_hi;
+    column_range(p, u, u.column0, &any_lo, &all_hi);
+    column_range(p, u, min(u.column0 + COLUMNS, u.rows * p.group) - 1, &all_lo, &any_hi);
     const int32_t tile0 = any_hi > 0 ? max(u.tile0, any_lo / kKvTile) : u.tile1, tile1 = min(u.tile1, (any_hi + kKvTile - 1) / kKvTile);
 
     uint32_t *const ring = smem + warp * kStages * TILE;
@@ -674,6 +640,27 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(B, NT, SPLIT)) kv_atte
     const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring) + lane * 16;
 #pragma unroll
     for (int i = 0; i < kStages - 1; ++i) good |= fetch(i, ring_at + i * (TILE * 4)) ? 1u << i : 0u;
+    Warp<B, NT, SPLIT> w;
+    load_queries(p, u, head, w);  // while the first tiles are on their way
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            w.base[nt][j] = -kLowest;
+            w.weight[nt][j] = 0.0f;
+        }
+#pragma unroll
+    for (int b = 0; b < B; ++b)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w.o[b][i][nt][j] = 0.0f;
+    w.high = 0xffffu;
+    w.shift = 0.0f;
+    w.limit = kRise;
+
     int32_t token0 = (tile0 + first_warp) * kKvTile;
     for (int i = 0, stage = 0; i < mine; ++i, token0 += step * kKvTile, good >>= 1, stage = stage + 1 == kStages ? 0 : stage + 1) {
         __syncwarp();  // everyone is done with the stage that comes next

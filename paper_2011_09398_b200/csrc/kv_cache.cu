@@ -1,7 +1,9 @@
 // Quantising keys and values into the 4-bit cache as they are written, and reading them back.
 //
-// Both kernels move memory: a thread takes eight channels of the key and of the value of one (token, head), four threads a
-// block of 32 channels, whose largest value they find with two shuffles; no value is read twice.
+// Both kernels move memory.  A thread takes eight channels of the key and of the value of one (token, head), four threads a block of
+// 32 channels, whose largest value they find with two shuffles; no value is read twice.  A block of threads works on sixteen
+// consecutive tokens of a head, because that is what shares the cache's sectors: a token's values lie in two bytes each all over
+// its tile.  Where the sixteen are a whole tile (a prompt) they are put together in shared memory and leave in 16-byte stores.
 #include "kv_common.cuh"
 
 namespace lce {
@@ -11,112 +13,177 @@ constexpr int kThreads = 256;
 
 struct KvRows {
     KvGeom g;
-    int64_t items;            // (token, head, block, quarter), the quarter fastest
+    int64_t tokens;
+    int32_t groups;           // of sixteen tokens
+    FastDiv by_heads, by_page;
     int64_t k_token, k_head, v_token, v_head;
     const int32_t *slots;
     uint32_t *cache;
 };
 
-struct KvItem {
-    int64_t token;
-    int head, block, quarter, slot;
-};
-
-__device__ __forceinline__ KvItem kv_item(const KvRows &p, int64_t at)
+// The tile that a slot of the pool lies in.
+__device__ __forceinline__ uint32_t *kv_tile_of(const KvRows &p, int slot, int head)
 {
-    KvItem it;
-    it.quarter = (int)(at & 3);
-    const int64_t row = (at >> 2) / p.g.blocks;
-    it.block = (int)((at >> 2) - row * p.g.blocks);
-    it.token = row / p.g.heads;
-    it.head = (int)(row - it.token * p.g.heads);
-    it.slot = __ldg(p.slots + it.token);
-    return it;
+    const int page = p.by_page(slot), in_page = slot - page * p.g.page_size;
+    const int64_t tile = ((int64_t)page * p.g.heads + head) * (p.g.page_size / kKvTile) + in_page / kKvTile;
+    return p.cache + tile * kv_tile_words(p.g.blocks);
 }
 
-__device__ __forceinline__ uint32_t *kv_tile_of(const KvRows &p, const KvItem &it)
+__device__ __forceinline__ float max_or_nan(float a, float b)
 {
-    const int page = it.slot / p.g.page_size, in_page = it.slot - page * p.g.page_size;
-    const int64_t tile = ((int64_t)page * p.g.heads + it.head) * (p.g.page_size / kKvTile) + in_page / kKvTile;
-    return p.cache + tile * kv_tile_words(p.g.blocks);
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
 }
 
 // Scale of the block that four neighbouring lanes hold, NaN where a value is not finite.
 __device__ __forceinline__ float block_scale(const float (&v)[8])
 {
-    uint32_t a = 0;  // magnitudes compare like integers, NaN and infinity above all others
+    float a = fabsf(v[0]);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) a = max(a, __float_as_uint(v[i]) & 0x7fffffffu);
-    a = max(a, __shfl_xor_sync(0xffffffffu, a, 1));
-    a = max(a, __shfl_xor_sync(0xffffffffu, a, 2));
-    return a >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : kv_scale(__uint_as_float(a));
+    for (int i = 1; i < 8; ++i) a = max_or_nan(a, fabsf(v[i]));
+    a = max_or_nan(a, __shfl_xor_sync(0xffffffffu, a, 1));
+    a = max_or_nan(a, __shfl_xor_sync(0xffffffffu, a, 2));
+    return a < __uint_as_float(0x7f800000u) ? kv_scale(a) : __uint_as_float(0x7fc00000u);
 }
+
+template <typename T>
+constexpr bool kShort = sizeof(T) == 2;
 
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kThreads) kv_quantize_kernel(const __grid_constant__ KvRows p, const T *k, const T *v)
 {
+    __shared__ __align__(16) uint32_t staged[kv_tile_words(kKvMaxDim / 32)];
+    __shared__ int32_t slots[kKvTile];
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int64_t step = (int64_t)gridDim.x * kThreads;
+    const int group = p.by_heads((int)blockIdx.x), head = blockIdx.x - group * p.g.heads;
+    const int64_t token0 = (int64_t)group * kKvTile;
+    const int tokens = (int)min(p.tokens - token0, (int64_t)kKvTile);
+    if (threadIdx.x < kKvTile) slots[threadIdx.x] = threadIdx.x < tokens ? __ldg(p.slots + token0 + threadIdx.x) : -1;
+    __syncthreads();
+    // a whole tile, in order
+    const int first = slots[0];
+    const bool whole = __syncthreads_and(threadIdx.x >= kKvTile || (first >= 0 && (first & 15) == 0 && first < p.g.slots && slots[threadIdx.x] == first + (int)threadIdx.x));
+    const int threads_per_token = 4 * p.g.blocks, items = tokens * threads_per_token;
     // whole warps go round together: the shuffles need every lane
-    for (int64_t at = (int64_t)blockIdx.x * kThreads + threadIdx.x; at - (threadIdx.x & 31) < p.items; at += step) {
-        const bool there = at < p.items;
-        const KvItem it = kv_item(p, there ? at : p.items - 1);
-        const int channel = it.block * 32 + it.quarter * 8;
+    for (int at = threadIdx.x; at - (int)(threadIdx.x & 31) < items; at += kThreads) {
+        const bool there = at < items;
+        const int token = (there ? at : items - 1) / threads_per_token, in_row = (there ? at : items - 1) - token * threads_per_token;
+        const int block = in_row >> 2, quarter = in_row & 3, channel = in_row * 8, slot = slots[token];
         float kx[8], vx[8];
-        load8<T, VEC>(k + it.token * p.k_token + it.head * p.k_head + channel, p.g.dim - channel, kx);
-        load8<T, VEC>(v + it.token * p.v_token + it.head * p.v_head + channel, p.g.dim - channel, vx);
+        load8<T, VEC>(k + (token0 + token) * p.k_token + head * p.k_head + channel, p.g.dim - channel, kx);
+        load8<T, VEC>(v + (token0 + token) * p.v_token + head * p.v_head + channel, p.g.dim - channel, vx);
         const float ks = block_scale(kx), vs = block_scale(vx);
-        if (!there || it.slot < 0 || it.slot >= p.g.slots) continue;
-        uint32_t *const tile = kv_tile_of(p, it);
-        const int token = it.slot % kKvTile;
-        tile[kv_key_word(p.g.blocks, token, it.block, it.quarter)] = kv_codes(kx, ks);
-        const uint32_t codes = kv_codes(vx, vs);
-        uint16_t *const halves = reinterpret_cast<uint16_t *>(tile) + (token & 1);
-        halves[2 * kv_value_word(p.g.blocks, token >> 1, it.block, 2 * it.quarter)] = (uint16_t)codes;
-        halves[2 * kv_value_word(p.g.blocks, token >> 1, it.block, 2 * it.quarter + 1)] = (uint16_t)(codes >> 16);
-        if (it.quarter == 0) tile[kv_scale_word(p.g.blocks, token, it.block)] = (__float_as_uint(ks) >> 16) | (__float_as_uint(vs) & 0xffff0000u);
+        if (!there || slot < 0 || slot >= p.g.slots) continue;
+        uint32_t *const tile = whole ? staged : kv_tile_of(p, slot, head);
+        const int in_tile = slot % kKvTile;
+        tile[kv_key_word(p.g.blocks, in_tile, block, quarter)] = kv_codes<kShort<T>>(kx, ks);
+        const uint32_t codes = kv_codes<kShort<T>>(vx, vs);
+        uint16_t *const halves = reinterpret_cast<uint16_t *>(tile) + (in_tile & 1);
+        halves[2 * kv_value_word(p.g.blocks, in_tile >> 1, block, 2 * quarter)] = (uint16_t)codes;
+        halves[2 * kv_value_word(p.g.blocks, in_tile >> 1, block, 2 * quarter + 1)] = (uint16_t)(codes >> 16);
+        if (quarter == 0) tile[kv_scale_word(p.g.blocks, in_tile, block)] = (__float_as_uint(ks) >> 16) | (__float_as_uint(vs) & 0xffff0000u);
     }
+    if (!whole) return;
+    __syncthreads();
+    uint4 *const to = reinterpret_cast<uint4 *>(kv_tile_of(p, first, head));
+    for (int i = threadIdx.x; i < kv_tile_words(p.g.blocks) / 4; i += kThreads) to[i] = reinterpret_cast<const uint4 *>(staged)[i];
 }
 
-__device__ __forceinline__ void kv_values(uint32_t word, float s, float (&v)[8])
-{
-    word = kv_rotate_back(word);
+// Eight values c * s, rounded to T once; the product itself is exact in fp32.
+template <typename T>
+struct Values {
+    T e[8];
+    __device__ __forceinline__ void set(uint32_t word, uint32_t scale)  // a bf16 number in the high half
+    {
+        word = kv_rotate_back(word);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = (float)((int)((word >> (4 * i)) & 15u) - 8) * s;
+        for (int i = 0; i < 8; ++i) e[i] = from_float<T>((__uint_as_float((word >> (4 * i) & 15u) | 0x4b400000u) - 12582920.0f) * __uint_as_float(scale));
+    }
+};
+template <>
+struct Values<__nv_bfloat16> {
+    // two at a time: 128 + n by one AND-OR, less 136, times s in bf16, which is the one rounding
+    __nv_bfloat16 e[8];
+    __device__ __forceinline__ void set(uint32_t word, uint32_t scale)
+    {
+        word = kv_rotate_back(word);
+        const __nv_bfloat162 s = __bfloat162bfloat162(__ushort_as_bfloat16((unsigned short)(scale >> 16))), less = __bfloat162bfloat162(__ushort_as_bfloat16(0x4308));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t n = (word >> (4 * i) & 0x000f000fu) | 0x43004300u;
+            const __nv_bfloat162 v = __hmul2(__hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&n), less), s);
+            e[i] = v.x;
+            e[i + 4] = v.y;
+        }
+    }
+};
+
+template <typename T, bool VEC>
+__device__ __forceinline__ void store_values(T *p, int count, const Values<T> &v)
+{
+    if (VEC) {
+        alignas(16) T e[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = v.e[i];
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4 *>(p)[i] = reinterpret_cast<const uint4 *>(e)[i];
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < count) p[i] = v.e[i];
 }
 
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kThreads) kv_dequantize_kernel(const __grid_constant__ KvRows p, T *k, T *v)
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int64_t step = (int64_t)gridDim.x * kThreads;
-    for (int64_t at = (int64_t)blockIdx.x * kThreads + threadIdx.x; at < p.items; at += step) {
-        const KvItem it = kv_item(p, at);
-        const int channel = it.block * 32 + it.quarter * 8;
+    const int group = p.by_heads((int)blockIdx.x), head = blockIdx.x - group * p.g.heads;
+    const int64_t token0 = (int64_t)group * kKvTile;
+    const int tokens = (int)min(p.tokens - token0, (int64_t)kKvTile);
+    const int threads_per_token = 4 * p.g.blocks, items = tokens * threads_per_token;
+    for (int at = threadIdx.x; at < items; at += kThreads) {
+        const int token = at / threads_per_token, in_row = at - token * threads_per_token;
+        const int block = in_row >> 2, quarter = in_row & 3, channel = in_row * 8, slot = __ldg(p.slots + token0 + token);
         if (channel >= p.g.dim) continue;
-        float kx[8] = {}, vx[8] = {};
-        if (it.slot >= 0 && it.slot < p.g.slots) {
-            const uint32_t *const tile = kv_tile_of(p, it);
-            const int token = it.slot % kKvTile;
-            const uint32_t s = __ldg(tile + kv_scale_word(p.g.blocks, token, it.block));
-            if (k) kv_values(__ldg(tile + kv_key_word(p.g.blocks, token, it.block, it.quarter)), __uint_as_float(s << 16), kx);
+        uint32_t kw = kv_rotate(0x88888888u), vw = kw, s = 0;  // zeros for a slot outside the pool
+        if (slot >= 0 && slot < p.g.slots) {
+            const uint32_t *const tile = kv_tile_of(p, slot, head);
+            const int in_tile = slot % kKvTile;
+            s = __ldg(tile + kv_scale_word(p.g.blocks, in_tile, block));
+            if (k) kw = __ldg(tile + kv_key_word(p.g.blocks, in_tile, block, quarter));
             if (v) {
-                const uint16_t *const halves = reinterpret_cast<const uint16_t *>(tile) + (token & 1);
-                const uint32_t lo = __ldg(halves + 2 * kv_value_word(p.g.blocks, token >> 1, it.block, 2 * it.quarter));
-                const uint32_t hi = __ldg(halves + 2 * kv_value_word(p.g.blocks, token >> 1, it.block, 2 * it.quarter + 1));
-                kv_values(lo | hi << 16, __uint_as_float(s & 0xffff0000u), vx);
+                const uint16_t *const halves = reinterpret_cast<const uint16_t *>(tile) + (in_tile & 1);
+                vw = __ldg(halves + 2 * kv_value_word(p.g.blocks, in_tile >> 1, block, 2 * quarter)) |
+                     (uint32_t)__ldg(halves + 2 * kv_value_word(p.g.blocks, in_tile >> 1, block, 2 * quarter + 1)) << 16;
             }
         }
-        const int64_t out = (it.token * p.g.heads + it.head) * p.g.dim + channel;
-        if (k) store8<T, VEC>(k + out, p.g.dim - channel, kx);
-        if (v) store8<T, VEC>(v + out, p.g.dim - channel, vx);
+        const int64_t out = ((token0 + token) * p.g.heads + head) * p.g.dim + channel;
+        Values<T> x;
+        if (k) {
+            x.set(kw, s << 16);
+            store_values<T, VEC>(k + out, p.g.dim - channel, x);
+        }
+        if (v) {
+            x.set(vw, s & 0xffff0000u);
+            store_values<T, VEC>(v + out, p.g.dim - channel, x);
+        }
     }
 }
 
-int grid_for(int64_t items)
+// A block to a head of sixteen tokens.
+lce_status set_rows(KvRows *p, int64_t tokens, const int32_t *slots, const void *cache)
 {
-    const int64_t blocks = (items + kThreads - 1) / kThreads;
-    return (int)(blocks < 148 * 8 ? blocks : 148 * 8);
+    const int64_t groups = (tokens + kKvTile - 1) / kKvTile;
+    if (groups * p->g.heads >= (1ll << 31)) return LCE_ERR_UNSUPPORTED;
+    p->tokens = tokens;
+    p->groups = (int32_t)groups;
+    fast_div_constants((uint32_t)p->g.heads, &p->by_heads.mul, &p->by_heads.sh);
+    fast_div_constants((uint32_t)p->g.page_size, &p->by_page.mul, &p->by_page.sh);
+    p->slots = slots;
+    p->cache = static_cast<uint32_t *>(const_cast<void *>(cache));
+    return LCE_OK;
 }
 
 bool stride_ok(int64_t s) { return s >= 0 && s < (1ll << 40); }
@@ -131,7 +198,7 @@ template <typename T>
 lce_status quantize(const KvRows &p, const void *k, const void *v, cudaStream_t s)
 {
     const bool vec = p.g.dim % 8 == 0 && rows_on_16(k, p.k_token, p.k_head, sizeof(T)) && rows_on_16(v, p.v_token, p.v_head, sizeof(T));
-    return launch_dependent(vec ? kv_quantize_kernel<T, true> : kv_quantize_kernel<T, false>, dim3(grid_for(p.items)), kThreads, 0, s, p,
+    return launch_dependent(vec ? kv_quantize_kernel<T, true> : kv_quantize_kernel<T, false>, dim3((unsigned)(p.groups * p.g.heads)), kThreads, 0, s, p,
                             static_cast<const T *>(k), static_cast<const T *>(v));
 }
 
@@ -139,7 +206,7 @@ template <typename T>
 lce_status dequantize(const KvRows &p, void *k, void *v, cudaStream_t s)
 {
     const bool vec = p.g.dim % 8 == 0 && aligned(k, 16) && aligned(v, 16);
-    return launch_dependent(vec ? kv_dequantize_kernel<T, true> : kv_dequantize_kernel<T, false>, dim3(grid_for(p.items)), kThreads, 0, s, p,
+    return launch_dependent(vec ? kv_dequantize_kernel<T, true> : kv_dequantize_kernel<T, false>, dim3((unsigned)(p.groups * p.g.heads)), kThreads, 0, s, p,
                             static_cast<T *>(k), static_cast<T *>(v));
 }
 
@@ -168,10 +235,8 @@ extern "C" lce_status lce_kv_quantize(const lce_kv_desc *desc, const void *k, co
     if (tokens == 0) return LCE_OK;
     if (!k || !v || !slots || !cache) return LCE_ERR_INVALID_ARG;
     if (!aligned(k, type_size(type)) || !aligned(v, type_size(type)) || !aligned(slots, 4) || !aligned(cache, 16)) return LCE_ERR_ALIGNMENT;
-    p.items = tokens * p.g.heads * p.g.blocks * 4;
+    if (set_rows(&p, tokens, slots, cache) != LCE_OK) return LCE_ERR_UNSUPPORTED;
     p.k_token = k_token_stride; p.k_head = k_head_stride; p.v_token = v_token_stride; p.v_head = v_head_stride;
-    p.slots = slots;
-    p.cache = static_cast<uint32_t *>(cache);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     switch (type) {
         case LCE_TYPE_FLOAT32: return quantize<float>(p, k, v, s);
@@ -192,9 +257,7 @@ extern "C" lce_status lce_kv_dequantize(const lce_kv_desc *desc, const void *cac
     if (tokens == 0) return LCE_OK;
     if ((!k && !v) || !slots || !cache) return LCE_ERR_INVALID_ARG;
     if (!aligned(k, type_size(type)) || !aligned(v, type_size(type)) || !aligned(slots, 4) || !aligned(cache, 16)) return LCE_ERR_ALIGNMENT;
-    p.items = tokens * p.g.heads * p.g.blocks * 4;
-    p.slots = slots;
-    p.cache = static_cast<uint32_t *>(const_cast<void *>(cache));
+    if (set_rows(&p, tokens, slots, cache) != LCE_OK) return LCE_ERR_UNSUPPORTED;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     switch (type) {
         case LCE_TYPE_FLOAT32: return dequantize<float>(p, k, v, s);

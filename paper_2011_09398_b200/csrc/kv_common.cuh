@@ -151,9 +151,9 @@ __device__ __forceinline__ uint32_t kv_rotate(uint32_t w) { return (w & 0x3fff3f
 __device__ __forceinline__ uint32_t kv_rotate_back(uint32_t w) { return (w >> 2 & 0x3fff3fffu) | (w & 0x00030003u) << 14; }
 
 // Codes of eight channels as a word holds them, for the block's scale.
-__device__ __forceinline__ uint32_t kv_codes(const float (&v)[8], float s)
+__device__ __noinline__ static uint32_t kv_codes_any(float v0, float v1, float v2, float v3, float v4, float v5, float v6, float v7, float s)
 {
-    if (!(s > 0.0f)) return kv_rotate(0x88888888u);  // all zeros, or NaN
+    const float v[8] = {v0, v1, v2, v3, v4, v5, v6, v7};
     const float up = s < 0x1p-100f ? 0x1p80f : 1.0f;  // away from subnormal numbers, exactly
     const float t = s * up, r = __fdiv_rn(1.0f, t);
     uint32_t word = 0;
@@ -162,7 +162,32 @@ __device__ __forceinline__ uint32_t kv_codes(const float (&v)[8], float s)
         const float c = kv_code(fabsf(v[i]) * up, t, r);
         word |= (uint32_t)(8 + (int)(v[i] < 0.0f ? -c : c)) << (4 * i);
     }
-    return kv_rotate(word);
+    return word;
+}
+
+// The same of f16 or bf16 values: x and s have 11 and 8 significant bits, so a quotient that is no tie is 2^-13 away from one at least
+// and rounding it to fp32 first (a product with the reciprocal and one correction by the remainder is that rounding) changes
+// nothing.  The sum with 1.5 * 2^23 + 8 rounds half to even and leaves n in its lowest bits; what stands above them adds up to a
+// constant.  Five operations a value where the general form takes twelve.
+__device__ __forceinline__ uint32_t kv_codes_short(const float (&v)[8], float s)
+{
+    const float r = __fdiv_rn(1.0f, s);
+    uint32_t word = 0;
+#pragma unroll
+    for (int i = 7; i >= 0; --i) {
+        const float q = v[i] * r, exact = fmaf(fmaf(-q, s, v[i]), r, q);
+        word = word * 16 + __float_as_uint(exact + 12582920.0f);
+    }
+    return word - 0x4b400000u * 0x11111111u;
+}
+
+// SHORT: the values are f16 or bf16 numbers
+template <bool SHORT>
+__device__ __forceinline__ uint32_t kv_codes(const float (&v)[8], float s)
+{
+    if (!(s > 0.0f)) return kv_rotate(0x88888888u);  // all zeros, or NaN
+    if (SHORT && s >= 0x1p-100f) return kv_rotate(kv_codes_short(v, s));
+    return kv_rotate(kv_codes_any(v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7], s));
 }
 
 }  // namespace lce

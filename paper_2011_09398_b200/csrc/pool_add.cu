@@ -11,12 +11,6 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// n / d for 0 <= n < 2^31 (fast_div_constants)
-struct FastDiv {
-    uint32_t mul, sh;
-    __device__ __forceinline__ int32_t operator()(int32_t n) const { return (int32_t)(((uint64_t)(uint32_t)n * mul) >> sh); }
-};
-
 struct PoolParams {
     const uint32_t *in;
     uint32_t *out;
