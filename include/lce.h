@@ -355,8 +355,8 @@ lce_status lce_kv_attention(const lce_kv_attention_desc *desc, const void *q, co
  *   branch, gate      of `type`; branch NULL: y = x (post_norm NONE, no gate); gate NULL: 1; gate_stride 0: one row for all
  *   weights, biases   fp32[channels] each, or NULL (1 and 0)
  *   normed            [rows][channels] of `type`: z; or NULL
- *   packed            uint32[rows][ceil(channels/32)]: bit (z < 0) of every channel, the next LceQuantize; or NULL.  Rows
- *                     with a z that fp32 leaves in doubt are done again in 64 bits, so that a sign next to 0 is right
+ *   packed            uint32[rows][ceil(channels/32)]: bit (z < 0) of every channel, the next LceQuantize; or NULL.  The
+ *                     arithmetic is then in 64 bits, so that a sign next to 0 is the right one
  * At least one of y, normed and packed.  Row strides in elements.  gate_activation: LCE_ACT_NONE or LCE_ACT_SIGMOID.
  * rows == 0 is a no-op. */
 typedef enum { LCE_NORM_NONE = 0, LCE_NORM_RMS = 1, LCE_NORM_LAYER = 2 } lce_norm;

@@ -33,7 +33,7 @@ struct AttnParams {
     KvGeom g;
     int32_t batch, group, table_pages, table_tokens;
     int32_t causal, window, type;
-    int32_t q_vectors;                 // rows of q allow 16-byte loads
+    int32_t q_vectors;                 // eight channels of q are one load
     int64_t tokens;
     int64_t q_token, q_head, out_token, out_head;
     float scale;                       // times log2(e)
@@ -964,7 +964,7 @@ extern "C" lce_status lce_kv_attention(const lce_kv_attention_desc *desc, const 
         !aligned(workspace, 16))
         return LCE_ERR_ALIGNMENT;
     if (workspace_size < workspace_bytes(p, nt)) return LCE_ERR_WORKSPACE;
-    p.q_vectors = p.g.dim % 8 == 0 && aligned(q, 16) && p.q_token * element % 16 == 0 && p.q_head * element % 16 == 0;
+    p.q_vectors = p.g.dim % 8 == 0 && aligned(q, 8 * element) && p.q_token % 8 == 0 && p.q_head % 8 == 0;
     p.q = q; p.cache = static_cast<const uint32_t *>(cache); p.page_table = page_table; p.lengths = lengths; p.q_starts = q_starts;
     p.out = out; p.parts = static_cast<float *>(workspace);
     cudaStream_t s = static_cast<cudaStream_t>(stream);

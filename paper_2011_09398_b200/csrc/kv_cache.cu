@@ -6,6 +6,8 @@
 // its tile.  Where the sixteen are a whole tile (a prompt) they are put together in shared memory and leave in 16-byte stores.
 #include "kv_common.cuh"
 
+#include <type_traits>
+
 namespace lce {
 namespace {
 
@@ -50,44 +52,56 @@ __device__ __forceinline__ float block_scale(const float (&v)[8])
 template <typename T>
 constexpr bool kShort = sizeof(T) == 2;
 
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(kThreads) kv_quantize_kernel(const __grid_constant__ KvRows p, const T *k, const T *v)
+// BLOCKS of 32 channels; 0: p.g.blocks.
+template <typename T, bool VEC, int BLOCKS>
+__global__ void __launch_bounds__(kThreads, 5) kv_quantize_kernel(const __grid_constant__ KvRows p, const T *k, const T *v)
 {
     __shared__ __align__(16) uint32_t staged[kv_tile_words(kKvMaxDim / 32)];
     __shared__ int32_t slots[kKvTile];
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int blocks = BLOCKS ? BLOCKS : p.g.blocks;
     const int group = p.by_heads((int)blockIdx.x), head = blockIdx.x - group * p.g.heads;
     const int64_t token0 = (int64_t)group * kKvTile;
     const int tokens = (int)min(p.tokens - token0, (int64_t)kKvTile);
-    if (threadIdx.x < kKvTile) slots[threadIdx.x] = threadIdx.x < tokens ? __ldg(p.slots + token0 + threadIdx.x) : -1;
-    __syncthreads();
-    // a whole tile, in order
-    const int first = slots[0];
-    const bool whole = __syncthreads_and(threadIdx.x >= kKvTile || (first >= 0 && (first & 15) == 0 && first < p.g.slots && slots[threadIdx.x] == first + (int)threadIdx.x));
-    const int threads_per_token = 4 * p.g.blocks, items = tokens * threads_per_token;
+    const int threads_per_token = 4 * blocks, items = tokens * threads_per_token;
+    Eight<T> ke, ve;
+    const auto load = [&](int at) {
+        const int token = at / threads_per_token, channel = 8 * (at - token * threads_per_token);
+        ke = load_eight<T, VEC>(k + (token0 + token) * p.k_token + head * p.k_head + channel, p.g.dim - channel);
+        ve = load_eight<T, VEC>(v + (token0 + token) * p.v_token + head * p.v_head + channel, p.g.dim - channel);
+    };
+    load(min((int)threadIdx.x, items - 1));  // on their way while the slots are
+    bool whole = false;  // a whole tile, in order
+    if (tokens == kKvTile) {
+        if (threadIdx.x < kKvTile) slots[threadIdx.x] = __ldg(p.slots + token0 + threadIdx.x);
+        __syncthreads();
+        const int first = slots[0];
+        whole = __syncthreads_and(threadIdx.x >= kKvTile || (first >= 0 && (first & 15) == 0 && first < p.g.slots && slots[threadIdx.x] == first + (int)threadIdx.x));
+    }
     // whole warps go round together: the shuffles need every lane
     for (int at = threadIdx.x; at - (int)(threadIdx.x & 31) < items; at += kThreads) {
         const bool there = at < items;
-        const int token = (there ? at : items - 1) / threads_per_token, in_row = (there ? at : items - 1) - token * threads_per_token;
-        const int block = in_row >> 2, quarter = in_row & 3, channel = in_row * 8, slot = slots[token];
+        const int token = min(at, items - 1) / threads_per_token, in_row = min(at, items - 1) - token * threads_per_token;
+        const int block = in_row >> 2, quarter = in_row & 3, slot = __ldg(p.slots + token0 + token);
+        if (at >= kThreads) load(min(at, items - 1));
         float kx[8], vx[8];
-        load8<T, VEC>(k + (token0 + token) * p.k_token + head * p.k_head + channel, p.g.dim - channel, kx);
-        load8<T, VEC>(v + (token0 + token) * p.v_token + head * p.v_head + channel, p.g.dim - channel, vx);
+        ke.expand(kx);
+        ve.expand(vx);
         const float ks = block_scale(kx), vs = block_scale(vx);
         if (!there || slot < 0 || slot >= p.g.slots) continue;
         uint32_t *const tile = whole ? staged : kv_tile_of(p, slot, head);
         const int in_tile = slot % kKvTile;
-        tile[kv_key_word(p.g.blocks, in_tile, block, quarter)] = kv_codes<kShort<T>>(kx, ks);
+        tile[kv_key_word(blocks, in_tile, block, quarter)] = kv_codes<kShort<T>>(kx, ks);
         const uint32_t codes = kv_codes<kShort<T>>(vx, vs);
         uint16_t *const halves = reinterpret_cast<uint16_t *>(tile) + (in_tile & 1);
-        halves[2 * kv_value_word(p.g.blocks, in_tile >> 1, block, 2 * quarter)] = (uint16_t)codes;
-        halves[2 * kv_value_word(p.g.blocks, in_tile >> 1, block, 2 * quarter + 1)] = (uint16_t)(codes >> 16);
-        if (quarter == 0) tile[kv_scale_word(p.g.blocks, in_tile, block)] = (__float_as_uint(ks) >> 16) | (__float_as_uint(vs) & 0xffff0000u);
+        halves[2 * kv_value_word(blocks, in_tile >> 1, block, 2 * quarter)] = (uint16_t)codes;
+        halves[2 * kv_value_word(blocks, in_tile >> 1, block, 2 * quarter + 1)] = (uint16_t)(codes >> 16);
+        if (quarter == 0) tile[kv_scale_word(blocks, in_tile, block)] = (__float_as_uint(ks) >> 16) | (__float_as_uint(vs) & 0xffff0000u);
     }
     if (!whole) return;
     __syncthreads();
-    uint4 *const to = reinterpret_cast<uint4 *>(kv_tile_of(p, first, head));
-    for (int i = threadIdx.x; i < kv_tile_words(p.g.blocks) / 4; i += kThreads) to[i] = reinterpret_cast<const uint4 *>(staged)[i];
+    uint4 *const to = reinterpret_cast<uint4 *>(kv_tile_of(p, slots[0], head));
+    for (int i = threadIdx.x; i < kv_tile_words(blocks) / 4; i += kThreads) to[i] = reinterpret_cast<const uint4 *>(staged)[i];
 }
 
 // Eight values c * s, rounded to T once; the product itself is exact in fp32.
@@ -123,26 +137,26 @@ template <typename T, bool VEC>
 __device__ __forceinline__ void store_values(T *p, int count, const Values<T> &v)
 {
     if (VEC) {
-        alignas(16) T e[8];
+        Eight<T> e;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = v.e[i];
+        for (int i = 0; i < 8; ++i) e.e[i] = v.e[i];
+        store_eight(p, e);
+    } else {
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4 *>(p)[i] = reinterpret_cast<const uint4 *>(e)[i];
-        return;
+        for (int i = 0; i < 8; ++i)
+            if (i < count) p[i] = v.e[i];
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (i < count) p[i] = v.e[i];
 }
 
-template <typename T, bool VEC>
+template <typename T, bool VEC, int BLOCKS>
 __global__ void __launch_bounds__(kThreads) kv_dequantize_kernel(const __grid_constant__ KvRows p, T *k, T *v)
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int blocks = BLOCKS ? BLOCKS : p.g.blocks;
     const int group = p.by_heads((int)blockIdx.x), head = blockIdx.x - group * p.g.heads;
     const int64_t token0 = (int64_t)group * kKvTile;
     const int tokens = (int)min(p.tokens - token0, (int64_t)kKvTile);
-    const int threads_per_token = 4 * p.g.blocks, items = tokens * threads_per_token;
+    const int threads_per_token = 4 * blocks, items = tokens * threads_per_token;
     for (int at = threadIdx.x; at < items; at += kThreads) {
         const int token = at / threads_per_token, in_row = at - token * threads_per_token;
         const int block = in_row >> 2, quarter = in_row & 3, channel = in_row * 8, slot = __ldg(p.slots + token0 + token);
@@ -151,12 +165,12 @@ __global__ void __launch_bounds__(kThreads) kv_dequantize_kernel(const __grid_co
         if (slot >= 0 && slot < p.g.slots) {
             const uint32_t *const tile = kv_tile_of(p, slot, head);
             const int in_tile = slot % kKvTile;
-            s = __ldg(tile + kv_scale_word(p.g.blocks, in_tile, block));
-            if (k) kw = __ldg(tile + kv_key_word(p.g.blocks, in_tile, block, quarter));
+            s = __ldg(tile + kv_scale_word(blocks, in_tile, block));
+            if (k) kw = __ldg(tile + kv_key_word(blocks, in_tile, block, quarter));
             if (v) {
                 const uint16_t *const halves = reinterpret_cast<const uint16_t *>(tile) + (in_tile & 1);
-                vw = __ldg(halves + 2 * kv_value_word(p.g.blocks, in_tile >> 1, block, 2 * quarter)) |
-                     (uint32_t)__ldg(halves + 2 * kv_value_word(p.g.blocks, in_tile >> 1, block, 2 * quarter + 1)) << 16;
+                vw = __ldg(halves + 2 * kv_value_word(blocks, in_tile >> 1, block, 2 * quarter)) |
+                     (uint32_t)__ldg(halves + 2 * kv_value_word(blocks, in_tile >> 1, block, 2 * quarter + 1)) << 16;
             }
         }
         const int64_t out = ((token0 + token) * p.g.heads + head) * p.g.dim + channel;
@@ -186,27 +200,43 @@ lce_status set_rows(KvRows *p, int64_t tokens, const int32_t *slots, const void 
     return LCE_OK;
 }
 
+// The kernel for so many blocks.
+template <typename Kernel>
+auto with_blocks(int blocks, Kernel kernel) -> decltype(kernel(std::integral_constant<int, 1>()))
+{
+    switch (blocks) {
+        case 1: return kernel(std::integral_constant<int, 1>());
+        case 2: return kernel(std::integral_constant<int, 2>());
+        case 3: return kernel(std::integral_constant<int, 3>());
+        case 4: return kernel(std::integral_constant<int, 4>());
+        case 5: return kernel(std::integral_constant<int, 5>());
+        case 6: return kernel(std::integral_constant<int, 6>());
+        case 7: return kernel(std::integral_constant<int, 7>());
+        default: return kernel(std::integral_constant<int, 8>());
+    }
+}
+
 bool stride_ok(int64_t s) { return s >= 0 && s < (1ll << 40); }
 
-// 16-byte accesses: whole groups of eight channels, rows on 16 bytes
-bool rows_on_16(const void *p, int64_t token_stride, int64_t head_stride, size_t size)
+// Whole groups of eight channels in one access: rows on 16 bytes, fp32 rows on 32
+bool rows_aligned(const void *p, int64_t token_stride, int64_t head_stride, size_t size)
 {
-    return aligned(p, 16) && token_stride * size % 16 == 0 && head_stride * size % 16 == 0;
+    return aligned(p, 8 * size) && token_stride % 8 == 0 && head_stride % 8 == 0;
 }
 
 template <typename T>
 lce_status quantize(const KvRows &p, const void *k, const void *v, cudaStream_t s)
 {
-    const bool vec = p.g.dim % 8 == 0 && rows_on_16(k, p.k_token, p.k_head, sizeof(T)) && rows_on_16(v, p.v_token, p.v_head, sizeof(T));
-    return launch_dependent(vec ? kv_quantize_kernel<T, true> : kv_quantize_kernel<T, false>, dim3((unsigned)(p.groups * p.g.heads)), kThreads, 0, s, p,
+    const bool vec = p.g.dim % 8 == 0 && rows_aligned(k, p.k_token, p.k_head, sizeof(T)) && rows_aligned(v, p.v_token, p.v_head, sizeof(T));
+    return launch_dependent(vec ? with_blocks(p.g.blocks, [](auto b) { return kv_quantize_kernel<T, true, b.value>; }) : kv_quantize_kernel<T, false, 0>, dim3((unsigned)(p.groups * p.g.heads)), kThreads, 0, s, p,
                             static_cast<const T *>(k), static_cast<const T *>(v));
 }
 
 template <typename T>
 lce_status dequantize(const KvRows &p, void *k, void *v, cudaStream_t s)
 {
-    const bool vec = p.g.dim % 8 == 0 && aligned(k, 16) && aligned(v, 16);
-    return launch_dependent(vec ? kv_dequantize_kernel<T, true> : kv_dequantize_kernel<T, false>, dim3((unsigned)(p.groups * p.g.heads)), kThreads, 0, s, p,
+    const bool vec = p.g.dim % 8 == 0 && aligned(k, 8 * sizeof(T)) && aligned(v, 8 * sizeof(T));
+    return launch_dependent(vec ? with_blocks(p.g.blocks, [](auto b) { return kv_dequantize_kernel<T, true, b.value>; }) : kv_dequantize_kernel<T, false, 0>, dim3((unsigned)(p.groups * p.g.heads)), kThreads, 0, s, p,
                             static_cast<T *>(k), static_cast<T *>(v));
 }
 

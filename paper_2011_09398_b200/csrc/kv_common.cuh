@@ -93,35 +93,71 @@ __device__ __forceinline__ __half from_float<__half>(float v) { return __float2h
 template <>
 __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
-// Eight consecutive elements, in 16-byte accesses where VEC (the address is then a multiple of 16); `count` of them exist.
-template <typename T, bool VEC>
-__device__ __forceinline__ void load8(const T *p, int count, float (&v)[8])
-{
-    if (VEC && count >= 8) {
-        alignas(16) T e[8];
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4 *>(e)[i] = reinterpret_cast<const uint4 *>(p)[i];
+// Eight consecutive elements as they come from memory, in one access where VEC (the address is then a multiple of their size, 16 or 32
+// bytes, and either all eight exist or none; fp32 in two accesses of 16 bytes asks for every sector twice); `count` of them exist, zeros
+// stand for the others.  Nothing is done to them here, so that many loads can be on their way at once.
+template <typename T>
+struct alignas(8 * sizeof(T)) Eight {
+    T e[8];
+    __device__ __forceinline__ void expand(float (&v)[8]) const
+    {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = to_float(e[i]);
-        return;
     }
+};
+template <typename T, bool VEC>
+__device__ __forceinline__ Eight<T> load_eight(const T *p, int count)
+{
+    Eight<T> r;
+    if (VEC && sizeof(T) == 4) {
+        uint32_t q[8] = {};
+        if (count > 0)
+            asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                         : "=r"(q[0]), "=r"(q[1]), "=r"(q[2]), "=r"(q[3]), "=r"(q[4]), "=r"(q[5]), "=r"(q[6]), "=r"(q[7])
+                         : "l"(p)
+                         : "memory");
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < count ? to_float(p[i]) : 0.0f;
+        for (int i = 0; i < 8; ++i) reinterpret_cast<uint32_t *>(r.e)[i] = q[i];
+    } else if (VEC) {
+        uint4 q = make_uint4(0, 0, 0, 0);
+        if (count > 0) q = *reinterpret_cast<const uint4 *>(p);
+        *reinterpret_cast<uint4 *>(r.e) = q;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            r.e[i] = from_float<T>(0.0f);
+            if (i < count) r.e[i] = p[i];
+        }
+    }
+    return r;
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void load8(const T *p, int count, float (&v)[8]) { load_eight<T, VEC>(p, count).expand(v); }
+template <typename T>
+__device__ __forceinline__ void store_eight(T *p, const Eight<T> &r)
+{
+    const uint32_t *const q = reinterpret_cast<const uint32_t *>(r.e);
+    if (sizeof(T) == 4)
+        asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(q[0]), "r"(q[1]), "r"(q[2]), "r"(q[3]), "r"(q[sizeof(T)]), "r"(q[sizeof(T) + 1]),
+                     "r"(q[2 * sizeof(T) - 2]), "r"(q[2 * sizeof(T) - 1])
+                     : "memory");
+    else
+        *reinterpret_cast<uint4 *>(p) = make_uint4(q[0], q[1], q[2], q[3]);
 }
 template <typename T, bool VEC>
 __device__ __forceinline__ void store8(T *p, int count, const float (&v)[8])
 {
-    if (VEC && count >= 8) {
-        alignas(16) T e[8];
+    if (VEC) {
+        if (count <= 0) return;
+        Eight<T> r;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = from_float<T>(v[i]);
+        for (int i = 0; i < 8; ++i) r.e[i] = from_float<T>(v[i]);
+        store_eight(p, r);
+    } else {
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4 *>(p)[i] = reinterpret_cast<const uint4 *>(e)[i];
-        return;
+        for (int i = 0; i < 8; ++i)
+            if (i < count) p[i] = from_float<T>(v[i]);
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (i < count) p[i] = from_float<T>(v[i]);
 }
 
 // --- the quantiser ------------------------------------------------------------------------------

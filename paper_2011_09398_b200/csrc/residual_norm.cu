@@ -2,15 +2,17 @@
 // shortcut add, the norm in front of the next block and that block's LceQuantize.
 //
 // What bounds it is reading x, the block's output and the gate and writing y and the result once each: a row stays in the
-// registers of the threads that loaded it, eight channels to a thread and vector, through up to four sums over the row (both
-// norms, variances from the differences to the mean), all in fp32.
+// registers of its threads, eight channels to a thread and vector, through up to four sums over the row (both norms, variances from the
+// differences to the mean).  A block takes row after row, and while it works on one the next one is on its way to shared memory.
 //
-// Sign bits want more: a bit is the sign of a difference of rounded numbers, and next to zero fp32 gets it wrong.  So with them a
-// bound on every result's error is worked out beside it, and a row in which some result is not clear of zero by it (7% of rows of
-// 4000 channels) goes through once more in fp64.  (Everything in fp64 at once: 188 us for 8000 x 4000 fp32, most of it conversions.)
+// The arithmetic is fp32, or fp64 where sign bits are asked for: a bit is the sign of a difference of rounded numbers, and next to zero
+// only a far finer arithmetic gets it right.  (fp32 with a bound on its error, and fp64 for the rows in doubt, was slower: 6% of rows
+// of 4000 channels are, and each holds its block up.)
 #include "kv_common.cuh"
 
 #include <math.h>
+
+#include <algorithm>
 
 namespace lce {
 namespace {
@@ -21,6 +23,7 @@ struct NormParams {
     int64_t rows;
     int32_t channels, vectors;         // vectors of eight channels, whole words of 32
     int32_t post_norm, pre_norm, sigmoid, row_threads;
+    int32_t stages, stage_places;      // rows in shared memory at a time; pieces of 16 bytes to a row of the block
     float eps, residual_scale;
     int64_t x_stride, branch_stride, gate_stride, y_stride, normed_stride;
     const float *post_weight, *post_bias, *pre_weight, *pre_bias;
@@ -32,27 +35,21 @@ __device__ __forceinline__ double sigmoid_of(double g) { return 1.0 / (1.0 + exp
 __device__ __forceinline__ float inverse_root(float v) { return 1.0f / sqrtf(v); }
 __device__ __forceinline__ double inverse_root(double v) { return 1.0 / sqrt(v); }
 
-// Sums over the threads of a row, in every one of them.
-template <typename A, int M>
-__device__ __forceinline__ void row_sums(A (&v)[M], int row_threads, A (*warps)[32])
+// Sum over the threads of a row, in every one of them.  `warps`: shared memory of this sum alone, so that one barrier does.
+template <typename A>
+__device__ __forceinline__ A row_sum(A v, int row_threads, A *warps)
 {
 #pragma unroll
-    for (int d = 16; d; d >>= 1)
-#pragma unroll
-        for (int m = 0; m < M; ++m) v[m] += __shfl_xor_sync(0xffffffffu, v[m], d);
-    if (row_threads == 32) return;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    __syncthreads();  // the last sums have been read
-    if (lane == 0)
-#pragma unroll
-        for (int m = 0; m < M; ++m) warps[m][warp] = v[m];
+    for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    if (row_threads == 32) return v;
+    const int lane = threadIdx.x & 31, row_warps = row_threads / 32;
+    if (lane == 0) warps[threadIdx.x >> 5] = v;
     __syncthreads();
+    v = lane < row_warps ? warps[lane] : A(0);
+    // at most sixteen warps: lanes 0 .. 15 hold all there is
 #pragma unroll
-    for (int m = 0; m < M; ++m) v[m] = lane < row_threads / 32 ? warps[m][lane] : A(0);
-#pragma unroll
-    for (int d = 16; d; d >>= 1)
-#pragma unroll
-        for (int m = 0; m < M; ++m) v[m] += __shfl_xor_sync(0xffffffffu, v[m], d);
+    for (int d = 8; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    return __shfl_sync(0xffffffffu, v, 0);
 }
 
 // Sum of a thread's values, in pairs: few roundings deep
@@ -62,50 +59,43 @@ __device__ __forceinline__ A sum_of(const A (&v)[N][8])
     A s[N];
 #pragma unroll
     for (int k = 0; k < N; ++k) s[k] = ((v[k][0] + v[k][1]) + (v[k][2] + v[k][3])) + ((v[k][4] + v[k][5]) + (v[k][6] + v[k][7]));
-    return N == 2 ? s[0] + s[N - 1] : s[0];
+#pragma unroll
+    for (int d = 1; d < N; d *= 2)
+#pragma unroll
+        for (int k = 0; k + d < N; k += 2 * d) s[k] += s[k + d];
+    return s[0];
 }
 template <typename A, int N>
 __device__ __forceinline__ A squares_of(const A (&v)[N][8])
 {
-    A q[N][8];
+    A s[N];
 #pragma unroll
-    for (int k = 0; k < N; ++k)
+    for (int k = 0; k < N; ++k) {
+        A q[4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) q[k][i] = v[k][i] * v[k][i];
-    return sum_of(q);
+        for (int i = 0; i < 4; ++i) q[i] = v[k][2 * i] * v[k][2 * i] + v[k][2 * i + 1] * v[k][2 * i + 1];
+        s[k] = (q[0] + q[1]) + (q[2] + q[3]);
+    }
+#pragma unroll
+    for (int d = 1; d < N; d *= 2)
+#pragma unroll
+        for (int k = 0; k + d < N; k += 2 * d) s[k] += s[k + d];
+    return s[0];
 }
 
-template <typename A>
-struct RowNorm {
-    A mean, factor;  // (v - mean) * factor
-};
-
-// v := v - mean (LAYER), and the factor that norms it.  `more` is summed over the row along the way.
+// v := v - mean (LAYER); returns the factor that norms it.  Squares are of the differences to the mean.
 template <typename A, int N>
-__device__ __forceinline__ RowNorm<A> row_norm(A (&v)[N][8], int kind, const NormParams &p, const int (&channel)[N], A (*warps)[32], A *more = nullptr)
+__device__ __forceinline__ A row_norm(A (&v)[N][8], int kind, const NormParams &p, const int (&channel)[N], A (*warps)[32])
 {
     const A each = A(1) / A(p.channels);
-    RowNorm<A> n{A(0), A(1)};
     if (kind == LCE_NORM_LAYER) {
-        A sum[1] = {sum_of(v)};  // 0 behind the last channel
-        row_sums(sum, p.row_threads, warps);
-        n.mean = sum[0] * each;
+        const A mean = row_sum(sum_of(v), p.row_threads, warps[0]) * each;  // 0 behind the last channel
 #pragma unroll
         for (int k = 0; k < N; ++k)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[k][i] = channel[k] + i < p.channels ? v[k][i] - n.mean : A(0);
+            for (int i = 0; i < 8; ++i) v[k][i] = channel[k] + i < p.channels ? v[k][i] - mean : A(0);
     }
-    if (more) {
-        A sums[2] = {squares_of(v), *more};
-        row_sums(sums, p.row_threads, warps);
-        if (kind != LCE_NORM_NONE) n.factor = inverse_root(sums[0] * each + A(p.eps));
-        *more = sums[1];
-    } else if (kind != LCE_NORM_NONE) {
-        A sums[1] = {squares_of(v)};
-        row_sums(sums, p.row_threads, warps);
-        n.factor = inverse_root(sums[0] * each + A(p.eps));
-    }
-    return n;
+    return inverse_root(row_sum(squares_of(v), p.row_threads, warps[1]) * each + A(p.eps));
 }
 
 template <typename TS, typename TB>
@@ -117,92 +107,111 @@ struct NormRow {  // one row's tensors
     uint8_t *packed;
 };
 
-// Errors of the fp32 arithmetic are below kUnsure times the sizes that meet in a value: sums of 14 levels of roundings, twice
-// (mean and variance), and a dozen roundings, of 2^-24 each.
-constexpr float kUnsure = 0x1p-18f;
-
-// The row in the arithmetic A.  CHECKED: writes nothing and returns false where a sign is in doubt.
-template <typename TS, typename TB, typename A, int N, bool VEC, bool CHECKED>
-__device__ __forceinline__ bool norm_row(const NormParams &p, const NormRow<TS, TB> &row, int thread, A (*warps)[32])
+// A row comes by asynchronous copies to shared memory.  A warp's vectors of a tensor are one run of memory, which its lanes copy 16 bytes
+// next to 16 bytes and read as they need them: what a warp copies is its own, so no other barrier is needed.
+template <typename T>
+__device__ __forceinline__ void fetch_run(const T *row, int channels, int channel0, uint4 *to)
 {
+    constexpr int W = sizeof(T) / 2, PIECE = 16 / sizeof(T);
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        const int channel = channel0 + (i * 32 + lane) * PIECE;
+        const bool there = channel < channels;  // whole pieces: channels is a multiple of eight
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to + i * 32 + lane)), "l"(row + (there ? channel : 0)),
+                     "r"(there ? 16 : 0)
+                     : "memory");
+    }
+}
+template <typename T>
+__device__ __forceinline__ Eight<T> take(const uint4 *from)
+{
+    constexpr int W = sizeof(T) / 2;
+    const int lane = threadIdx.x & 31;
+    Eight<T> to;
+#pragma unroll
+    for (int i = 0; i < W; ++i) reinterpret_cast<uint4 *>(to.e)[i] = from[lane * W + i];
+    return to;
+}
+// `places`: a warp's, 32 N (2 sizeof(TB) + sizeof(TS)) / 2 pieces of 16 bytes: of each vector the branch's, the gate's, the stream's.
+template <typename TS, typename TB, int N>
+__device__ __forceinline__ void fetch_share(const NormParams &p, const NormRow<TS, TB> &row, int thread, uint4 *places)
+{
+    constexpr int WB = 32 * sizeof(TB) / 2, WS = 32 * sizeof(TS) / 2;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const int channel0 = 8 * ((thread & ~31) + k * p.row_threads);
+        uint4 *const at = places + k * (2 * WB + WS);
+        if (row.branch) fetch_run(row.branch, p.channels, channel0, at);
+        if (row.gate) fetch_run(row.gate, p.channels, channel0, at + WB);
+        fetch_run(row.x, p.channels, channel0, at + 2 * WB);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+}
+// The row in the arithmetic A.  VEC: it lies in `places`.
+template <typename TS, typename TB, typename A, int N, bool VEC>
+__device__ __forceinline__ void norm_row(const NormParams &p, const NormRow<TS, TB> &row, const uint4 *places, int thread, A (*warps)[32])
+{
+    constexpr int WB = 32 * sizeof(TB) / 2, WS = 32 * sizeof(TS) / 2;
     A v[N][8];
     int channel[N];
 #pragma unroll
     for (int k = 0; k < N; ++k) channel[k] = 8 * (thread + k * p.row_threads);
     float f[8];
-    float size[CHECKED ? N : 1][8];  // of what meets in y
+    const auto block_values = [&](int k, const TB *from, int place) {
+        const Eight<TB> e = VEC ? take<TB>(places + k * (2 * WB + WS) + place) : load_eight<TB, false>(from + channel[k], p.channels - channel[k]);
+        e.expand(f);
+    };
+    const auto stream_values = [&](int k) {
+        const Eight<TS> e = VEC ? take<TS>(places + k * (2 * WB + WS) + 2 * WB) : load_eight<TS, false>(row.x + channel[k], p.channels - channel[k]);
+        e.expand(f);
+    };
+    const auto affine = [&](int k, const float *w, const float *b) {
+        Eight<float> weight, bias;
+        weight = load_eight<float, VEC>(w + channel[k], w ? p.channels - channel[k] : 0);
+        bias = load_eight<float, VEC>(b + channel[k], b ? p.channels - channel[k] : 0);
+        if (w) {
+            weight.expand(f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[k][i] *= A(f[i]);
+        }
+        if (b) {
+            bias.expand(f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[k][i] += A(f[i]);
+        }
+    };
     if (row.branch) {
 #pragma unroll
         for (int k = 0; k < N; ++k) {
-            load8<TB, VEC>(row.branch + channel[k], p.channels - channel[k], f);
+            block_values(k, row.branch, 0);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                v[k][i] = f[i];
-                if (CHECKED) size[k][i] = fabsf(f[i]);
-            }
+            for (int i = 0; i < 8; ++i) v[k][i] = A(f[i]);
         }
-        RowNorm<A> n{A(0), A(1)};
-        if (p.post_norm != LCE_NORM_NONE) n = row_norm(v, p.post_norm, p, channel, warps);
-        const float mean_size = fabsf((float)n.mean);
+        const A factor = p.post_norm != LCE_NORM_NONE ? row_norm(v, p.post_norm, p, channel, warps) : A(1);
 #pragma unroll
         for (int k = 0; k < N; ++k) {
-            const int count = p.channels - channel[k];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                v[k][i] *= n.factor;
-                if (CHECKED) size[k][i] = (size[k][i] + mean_size) * (float)n.factor;
-            }
-            if (p.post_weight) {
-                load8<float, VEC>(p.post_weight + channel[k], count, f);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    v[k][i] *= A(f[i]);
-                    if (CHECKED) size[k][i] *= fabsf(f[i]);
-                }
-            }
-            if (p.post_bias) {
-                load8<float, VEC>(p.post_bias + channel[k], count, f);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    v[k][i] += A(f[i]);
-                    if (CHECKED) size[k][i] += fabsf(f[i]);
-                }
-            }
-            float g[8];
+            for (int i = 0; i < 8; ++i) v[k][i] *= factor;
+            affine(k, p.post_weight, p.post_bias);
             if (row.gate) {
-                load8<TB, VEC>(row.gate + channel[k], count, g);
-                load8<TS, VEC>(row.x + channel[k], count, f);
+                block_values(k, row.gate, WB);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const A by = A(p.residual_scale) * (p.sigmoid ? sigmoid_of(A(g[i])) : A(g[i]));
-                    v[k][i] = i < count ? A(f[i]) + by * v[k][i] : A(0);
-                    if (CHECKED) size[k][i] = fabsf(f[i]) + fabsf((float)by) * size[k][i];
-                }
-            } else {
-                load8<TS, VEC>(row.x + channel[k], count, f);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    v[k][i] = i < count ? A(f[i]) + A(p.residual_scale) * v[k][i] : A(0);
-                    if (CHECKED) size[k][i] = fabsf(f[i]) + fabsf(p.residual_scale) * size[k][i];
-                }
+                for (int i = 0; i < 8; ++i) v[k][i] *= p.sigmoid ? sigmoid_of(A(f[i])) : A(f[i]);
             }
-            if (CHECKED) {
+            stream_values(k);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) size[k][i] = i < count ? size[k][i] : 0.0f;
-            }
+            for (int i = 0; i < 8; ++i) v[k][i] = channel[k] + i < p.channels ? A(f[i]) + A(p.residual_scale) * v[k][i] : A(0);
         }
     } else {
 #pragma unroll
         for (int k = 0; k < N; ++k) {
-            load8<TS, VEC>(row.x + channel[k], p.channels - channel[k], f);
+            stream_values(k);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                v[k][i] = f[i];
-                if (CHECKED) size[k][i] = fabsf(f[i]);
-            }
+            for (int i = 0; i < 8; ++i) v[k][i] = A(f[i]);
         }
     }
-    if (!CHECKED && row.y) {
+    if (row.y) {
 #pragma unroll
         for (int k = 0; k < N; ++k) {
 #pragma unroll
@@ -210,101 +219,72 @@ __device__ __forceinline__ bool norm_row(const NormParams &p, const NormRow<TS, 
             store8<TS, VEC>(row.y + channel[k], p.channels - channel[k], f);
         }
     }
-    if (!row.normed && !row.packed) return true;
-    float y[CHECKED ? N : 1][8];
-    float row_size = 0.0f;  // root mean square of the sizes
-    RowNorm<A> n{A(0), A(1)};
-    if (CHECKED) {
-#pragma unroll
-        for (int k = 0; k < N; ++k)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) y[CHECKED ? k : 0][i] = (float)v[k][i];
-        A more = (A)squares_of(size);
-        if (p.pre_norm != LCE_NORM_NONE) {
-            n = row_norm(v, p.pre_norm, p, channel, warps, &more);
-            row_size = sqrtf((float)more / (float)p.channels);
-        }
-    } else if (p.pre_norm != LCE_NORM_NONE) {
-        n = row_norm(v, p.pre_norm, p, channel, warps);
-    }
-    bool sure = true;
-    uint32_t bits[N];
-    const float spread = (1.0f + (float)n.factor * row_size) * (float)n.factor;
+    if (!row.normed && !row.packed) return;
+    const A factor = p.pre_norm != LCE_NORM_NONE ? row_norm(v, p.pre_norm, p, channel, warps + 2) : A(1);
 #pragma unroll
     for (int k = 0; k < N; ++k) {
         const int count = p.channels - channel[k];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            v[k][i] *= n.factor;
-            if (CHECKED) size[k][i] = (size[k][i] + row_size) * spread;
-        }
-        if (p.pre_weight) {
-            load8<float, VEC>(p.pre_weight + channel[k], count, f);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                v[k][i] *= A(f[i]);
-                if (CHECKED) size[k][i] *= fabsf(f[i]);
-            }
-        }
-        if (p.pre_bias) {
-            load8<float, VEC>(p.pre_bias + channel[k], count, f);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                v[k][i] += A(f[i]);
-                if (CHECKED) size[k][i] += fabsf(f[i]);
-            }
-        }
-        if (!CHECKED && row.normed) {
+        for (int i = 0; i < 8; ++i) v[k][i] *= factor;
+        affine(k, p.pre_weight, p.pre_bias);
+        if (row.normed) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) f[i] = (float)v[k][i];
             store8<TB, VEC>(row.normed + channel[k], count, f);
         }
-        bits[k] = 0;
+        // eight bits are a byte of their word: lowest channel lowest, the lowest byte first in memory
+        if (row.packed && channel[k] < 8 * p.vectors) {
+            uint32_t bits = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            bits[k] |= (i < count && v[k][i] < A(0) ? 1u : 0u) << i;
-            // a row with an infinity or a NaN is in doubt throughout; zeros of zeros are not
-            if (CHECKED) sure = sure && (i >= count || fabsf((float)v[k][i]) > kUnsure * size[k][i] || size[k][i] == 0.0f);
+            for (int i = 0; i < 8; ++i) bits |= (i < count && v[k][i] < A(0) ? 1u : 0u) << i;
+            row.packed[channel[k] / 8] = (uint8_t)bits;
         }
     }
-    if (CHECKED) {
-        sure = p.row_threads == 32 ? __all_sync(0xffffffffu, sure) : __syncthreads_and(sure);
-        if (!sure) return false;
-#pragma unroll
-        for (int k = 0; k < N; ++k) {
-            if (row.y) store8<TS, VEC>(row.y + channel[k], p.channels - channel[k], y[CHECKED ? k : 0]);
-            if (row.normed) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) f[i] = (float)v[k][i];
-                store8<TB, VEC>(row.normed + channel[k], p.channels - channel[k], f);
-            }
-        }
-    }
-    // eight bits are a byte of their word: lowest channel lowest, the lowest byte first in memory
-    if (row.packed) {
-#pragma unroll
-        for (int k = 0; k < N; ++k)
-            if (channel[k] < 8 * p.vectors) row.packed[channel[k] / 8] = (uint8_t)bits[k];
-    }
-    return true;
 }
 
-// TS, TB: elements of the stream and of the block; N vectors to a thread.
-template <typename TS, typename TB, int N, bool VEC, bool BITS>
-__global__ void __launch_bounds__(N == 1 ? 512 : 1024) residual_norm_kernel(const __grid_constant__ NormParams p, const TS *x, const TB *branch, const TB *gate,
-                                                                            TS *y, TB *normed)
+// TS, TB: elements of the stream and of the block; A: the arithmetic; N vectors to a thread.  A block (a warp, for short rows) takes row
+// after row.
+template <typename TS, typename TB, typename A, int N, bool VEC>
+__global__ void __launch_bounds__(512, N == 1 ? 2 : 1) residual_norm_kernel(const __grid_constant__ NormParams p, const TS *x, const TB *branch, const TB *gate, TS *y,
+                                                                            TB *normed)
 {
-    __shared__ float warps[2][32];
-    __shared__ double wide_warps[1][32];
+    extern __shared__ __align__(16) uint4 shared_places[];
+    // of each sum over the row, mean and squares of either norm; rows take the two sets in turn, so that one barrier to a sum does
+    __shared__ A warps[2][4][32];
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int64_t at = p.row_threads == 32 ? (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5) : blockIdx.x;
-    if (at >= p.rows) return;
-    const int thread = p.row_threads == 32 ? threadIdx.x & 31 : threadIdx.x;
-    const NormRow<TS, TB> row{x + at * p.x_stride, branch ? branch + at * p.branch_stride : nullptr, gate ? gate + at * p.gate_stride : nullptr,
-                              y ? y + at * p.y_stride : nullptr, normed ? normed + at * p.normed_stride : nullptr,
-                              BITS ? p.packed + at * p.vectors : nullptr};
-    if (!BITS) norm_row<TS, TB, float, N, VEC, false>(p, row, thread, warps);
-    else if (!norm_row<TS, TB, float, N, VEC, true>(p, row, thread, warps)) norm_row<TS, TB, double, N, VEC, false>(p, row, thread, wide_warps);
+    const bool warp_rows = p.row_threads == 32;
+    const int64_t first = warp_rows ? (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5) : blockIdx.x;
+    const int64_t step = warp_rows ? (int64_t)gridDim.x * (blockDim.x >> 5) : gridDim.x;
+    const int thread = warp_rows ? threadIdx.x & 31 : threadIdx.x;
+    uint4 *const places = shared_places + (threadIdx.x >> 5) * (32 * N * (2 * sizeof(TB) + sizeof(TS)) / 2);
+    const auto row_at = [&](int64_t at) {
+        return NormRow<TS, TB>{x + at * p.x_stride, branch ? branch + at * p.branch_stride : nullptr, gate ? gate + at * p.gate_stride : nullptr,
+                               y ? y + at * p.y_stride : nullptr, normed ? normed + at * p.normed_stride : nullptr,
+                               sizeof(A) == 8 ? p.packed + at * p.vectors : nullptr};
+    };
+    if (VEC && first < p.rows) fetch_share<TS, TB, N>(p, row_at(first), thread, places);
+    int set = 0;
+    for (int64_t at = first; at < p.rows; at += step, set ^= 1) {
+        const NormRow<TS, TB> row = row_at(at);
+        const uint4 *here = places;
+        if (VEC && p.stages == 2) {
+            // the other half of the places was read a row ago
+            here = places + set * p.stage_places;
+            __syncwarp();
+            if (at + step < p.rows) fetch_share<TS, TB, N>(p, row_at(at + step), thread, places + (set ^ 1) * p.stage_places);
+            else asm volatile("cp.async.commit_group;" ::: "memory");
+            asm volatile("cp.async.wait_group 1;" ::: "memory");
+            __syncwarp();
+        } else if (VEC) {
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+            __syncwarp();
+        }
+        norm_row<TS, TB, A, N, VEC>(p, row, here, thread, warps[set]);
+        if (VEC && p.stages == 1) {
+            __syncwarp();
+            if (at + step < p.rows) fetch_share<TS, TB, N>(p, row_at(at + step), thread, places);
+        }
+    }
 }
 
 struct NormBuffers {
@@ -312,39 +292,48 @@ struct NormBuffers {
     void *y, *normed;
 };
 
-template <typename TS, typename TB, int N, bool VEC, bool BITS>
+template <typename TS, typename TB, typename A, int N, bool VEC>
 lce_status launch(NormParams p, const NormBuffers &b, cudaStream_t s)
 {
+    p.row_threads = (p.vectors + 32 * N - 1) / (32 * N) * 32;
     int64_t blocks = p.rows;
     int threads = p.row_threads;
     if (threads == 32) {
         threads = 128;
         blocks = (p.rows + 3) / 4;
     }
-    if (blocks >= (1ll << 31)) return LCE_ERR_UNSUPPORTED;
-    return launch_dependent(residual_norm_kernel<TS, TB, N, VEC, BITS>, dim3((unsigned)blocks), threads, 0, s, p, static_cast<const TS *>(b.x),
-                            static_cast<const TB *>(b.branch), static_cast<const TB *>(b.gate), static_cast<TS *>(b.y), static_cast<TB *>(b.normed));
+    const size_t stage = VEC ? (size_t)threads * N * 8 * (2 * sizeof(TB) + sizeof(TS)) : 0;
+    p.stages = 2 * stage <= 200 * 1024 ? 2 : 1;
+    p.stage_places = (int32_t)(stage / 16);
+    const size_t smem = p.stages * stage;
+    static SmemOptIn opt_in;
+    const auto kernel = residual_norm_kernel<TS, TB, A, N, VEC>;
+    // (the kernel's own 2 KB count towards the 48 KB that need no opt-in)
+    if (!opt_in.ensure(kernel, smem > 40 * 1024 ? std::max<size_t>(smem, 48 * 1024 + 16) : smem)) return LCE_ERR_CUDA;
+    // as many blocks as the GPU holds: by registers (64 a thread, or 128 where it has more vectors), by shared memory
+    const int64_t by_threads = (N == 1 ? 1024 : 512) / threads, by_memory = smem ? (int64_t)(220 * 1024 / (smem + 4096)) : 16;
+    const int64_t most = 148 * std::max<int64_t>(1, std::min<int64_t>({by_threads, by_memory, 16}));
+    return launch_dependent(kernel, dim3((unsigned)std::min(blocks, most)), threads, smem, s, p, static_cast<const TS *>(b.x), static_cast<const TB *>(b.branch),
+                            static_cast<const TB *>(b.gate), static_cast<TS *>(b.y), static_cast<TB *>(b.normed));
 }
 
-template <typename TS, typename TB, bool VEC, bool BITS>
-lce_status launch_vectors(NormParams p, const NormBuffers &b, cudaStream_t s)
+template <typename TS, typename TB, typename A, bool VEC>
+lce_status launch_vectors(const NormParams &p, const NormBuffers &b, cudaStream_t s)
 {
-    // a warp to a row of up to 1024 channels, otherwise a block
-    const auto threads = [&](int n) { return (p.vectors + 32 * n - 1) / (32 * n) * 32; };
-    const int n = p.vectors <= 32 ? 1 : p.vectors <= 64 ? 2 : p.vectors <= 512 ? 1 : 2;
-    p.row_threads = threads(n);
-    return n == 1 ? launch<TS, TB, 1, VEC, BITS>(p, b, s) : launch<TS, TB, 2, VEC, BITS>(p, b, s);
+    // a warp to a row of up to 512 channels; otherwise a block with one vector to a thread as far as it goes
+    if (p.vectors <= 32 || (p.vectors > 64 && p.vectors <= 512)) return launch<TS, TB, A, 1, VEC>(p, b, s);
+    return p.vectors <= 1024 ? launch<TS, TB, A, 2, VEC>(p, b, s) : launch<TS, TB, A, 4, VEC>(p, b, s);
 }
 
 template <typename TS, typename TB>
 lce_status launch_types(const NormParams &p, const NormBuffers &b, cudaStream_t s)
 {
-    const auto rows16 = [&](const void *q, int64_t stride, size_t size) { return !q || (aligned(q, 16) && stride * size % 16 == 0); };
-    const bool vec = p.channels % 8 == 0 && rows16(b.x, p.x_stride, sizeof(TS)) && rows16(b.y, p.y_stride, sizeof(TS)) && rows16(b.branch, p.branch_stride, sizeof(TB)) &&
-                     rows16(b.gate, p.gate_stride, sizeof(TB)) && rows16(b.normed, p.normed_stride, sizeof(TB)) && aligned(p.post_weight, 16) &&
-                     aligned(p.post_bias, 16) && aligned(p.pre_weight, 16) && aligned(p.pre_bias, 16);
-    if (p.packed) return vec ? launch_vectors<TS, TB, true, true>(p, b, s) : launch_vectors<TS, TB, false, true>(p, b, s);
-    return vec ? launch_vectors<TS, TB, true, false>(p, b, s) : launch_vectors<TS, TB, false, false>(p, b, s);
+    const auto rows = [&](const void *q, int64_t stride, size_t size) { return !q || (aligned(q, 8 * size) && stride % 8 == 0); };
+    const bool vec = p.channels % 8 == 0 && rows(b.x, p.x_stride, sizeof(TS)) && rows(b.y, p.y_stride, sizeof(TS)) && rows(b.branch, p.branch_stride, sizeof(TB)) &&
+                     rows(b.gate, p.gate_stride, sizeof(TB)) && rows(b.normed, p.normed_stride, sizeof(TB)) && aligned(p.post_weight, 32) &&
+                     aligned(p.post_bias, 32) && aligned(p.pre_weight, 32) && aligned(p.pre_bias, 32);
+    if (p.packed) return vec ? launch_vectors<TS, TB, double, true>(p, b, s) : launch_vectors<TS, TB, double, false>(p, b, s);
+    return vec ? launch_vectors<TS, TB, float, true>(p, b, s) : launch_vectors<TS, TB, float, false>(p, b, s);
 }
 
 }  // namespace
