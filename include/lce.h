@@ -377,7 +377,7 @@ lce_status lce_residual_norm(const lce_residual_norm_desc *desc, const void *x, 
  * (operands ready, MMAs complete, accumulator read out); every such wait is limited to 0.2 s, after
  * which the kernel stops working, waits (bounded) for its copies and MMAs in flight, frees its tensor
  * memory and returns, leaving its output incomplete.  It records that in a device word and in a word
- * of mapped host memory; from then on lce_bconv2d, its host-buffer forms, lce_bconv2d_fused and lce_plan_run on that
+ * of mapped host memory; from then on lce_bconv2d, its host-buffer forms, lce_bconv2d_fused, lce_plan_run and lce_kv_attention of many rows on that
  * device return LCE_ERR_DEVICE_TIMEOUT without launching, until lce_device_status_reset.
  *   lce_device_status        *status (HOST pointer) = 0 if no wait has given up on the current device
  *                            since load or the last reset, 1 otherwise.  Synchronous (reads the device word).

@@ -1573,6 +1573,25 @@ __global__ void mx_wait_probe_kernel(uint64_t limit_ns, int *host_flag)
 }
 }  // namespace
 
+TimeoutReport tensor_timeout_report(cudaStream_t s)
+{
+    static std::atomic<int *> words[kFlagDevices];
+    TimeoutReport r{nullptr, mx_flag_for_launch(s)};
+    const int dev = current_device_index();
+    if (dev < 0) return r;
+    r.device_word = words[dev].load(std::memory_order_acquire);
+    if (!r.device_word) {
+        void *at = nullptr;
+        if (cudaGetSymbolAddress(&at, g_mx_status) != cudaSuccess) {
+            cudaGetLastError();
+            return r;
+        }
+        r.device_word = static_cast<int *>(at);
+        words[dev].store(r.device_word, std::memory_order_release);
+    }
+    return r;
+}
+
 lce_status tensor_wait_probe(uint64_t limit_ns, cudaStream_t s)
 {
     mx_wait_probe_kernel<<<1, 32, 0, s>>>(limit_ns, mx_flag_for_launch(s));

@@ -211,6 +211,12 @@ lce_status tensor_device_status(int *status);
 lce_status tensor_device_status_reset();
 bool tensor_timeout_flagged();
 lce_status tensor_wait_probe(uint64_t limit_ns, cudaStream_t s);
+// Where a kernel whose wait gave up says so: a word of the device (null: not to be had, the kernel must not be launched) and,
+// once it has been set up, one of mapped host memory (or null).
+struct TimeoutReport {
+    int *device_word, *host_word;
+};
+TimeoutReport tensor_timeout_report(cudaStream_t s);
 // Copies between pinned host memory and the device in one kernel; arrays on 4 bytes, sizes multiples of 4 below 2^31 in
 // all, empty ones allowed.  pinned_host_view: where a kernel may access a host array (`write`: store to it), null
 // where the array is the copy engine's (host_view.cuh).

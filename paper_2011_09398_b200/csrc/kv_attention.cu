@@ -16,7 +16,7 @@
 // what lies 2^-29 below the row's largest; p is rounded to f16 (relative error 2^-11 of each weight, which is what an fp16
 // result has, and averages out).  fp32 rows take Q and p as two f16 numbers each (22 bits), and codes as f16 c = n - 8: 1024 + n by
 // one AND-OR, less 1032 by one packed add.
-#include "kv_common.cuh"
+#include "kv_attention.cuh"
 
 #include <math.h>
 
@@ -27,158 +27,6 @@ constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kStages = 4;                // tiles in flight of a warp
 constexpr float kRise = 4.0f;             // a running maximum is raised when a score passes it by 2^4
 constexpr float kHeadroom = 10.0f;        // weights are held times 2^10: 2^(10 + 4 + 1) is the most that meets f16
-constexpr float kLowest = -1e30f;
-
-struct AttnParams {
-    KvGeom g;
-    int32_t batch, group, table_pages, table_tokens;
-    int32_t causal, window, type;
-    int32_t q_vectors;                 // eight channels of q are one load
-    int64_t tokens;
-    int64_t q_token, q_head, out_token, out_head;
-    float scale;                       // times log2(e)
-    const void *q;
-    const uint32_t *cache;
-    const int32_t *page_table, *lengths, *q_starts;
-    void *out;
-    float *parts;                      // [unit][kv head][column][32 blocks + 4]: sums, largest, weight
-    int32_t units, column_tiles, target, least_tiles;
-    int32_t cluster;                   // blocks that share a unit
-    int32_t join;                      // there may be units that are not a whole column tile
-    int32_t one_row;                   // each sequence has one row of q
-};
-
-// What a unit (a range of tiles for one tile of columns of a sequence) works on.
-struct Unit {
-    int32_t seq, column0, chunks;
-    int32_t length, rows;                             // tokens of the sequence, its rows of q
-    int64_t row0;                                     // its first row of q
-    int32_t tile0, tile1;                             // the unit's tiles
-};
-
-struct Sequence {
-    int32_t length, rows, column_tiles, first_tile, tiles;
-    int64_t row0;
-};
-
-template <int COLUMNS>
-__device__ __forceinline__ Sequence sequence(const AttnParams &p, int b)
-{
-    Sequence s{};
-    if (b >= p.batch) return s;
-    s.length = min(max(__ldg(p.lengths + b), 0), p.table_tokens);
-    s.row0 = b;
-    s.rows = 1;
-    if (p.q_starts) {
-        const int64_t from = min(max((int64_t)__ldg(p.q_starts + b), (int64_t)0), p.tokens), to = min(max((int64_t)__ldg(p.q_starts + b + 1), from), p.tokens);
-        s.row0 = from;
-        s.rows = (int32_t)(to - from);
-    }
-    s.column_tiles = (int32_t)(((int64_t)s.rows * p.group + COLUMNS - 1) / COLUMNS);
-    // tiles that some row sees
-    int32_t low = 0;
-    if (p.window > 0) low = (int32_t)max((int64_t)s.length - s.rows + 1 - p.window, (int64_t)0);
-    s.first_tile = low / kKvTile;
-    s.tiles = max((s.length + kKvTile - 1) / kKvTile - s.first_tile, 0);
-    return s;
-}
-
-// The work is cut evenly whatever the sequences' lengths: every column tile of a sequence into pieces of at most `most` tiles, where
-// `most` follows from the whole batch's tiles.  Every warp works this out for itself from the lengths (no launch in front, no host
-// copy of them).  Finds the `at`-th unit, or the first unit of the `at`-th column tile; false: there is no such one.
-template <int COLUMNS, bool BY_COLUMN_TILE>
-__device__ __forceinline__ bool find_unit(const AttnParams &p, int at, Unit *u, int *first_unit)
-{
-    const int lane = threadIdx.x & 31;
-    const Sequence first = sequence<COLUMNS>(p, lane);
-    int64_t total = 0;
-    for (int b0 = 0; b0 < p.batch; b0 += 32) {
-        const Sequence s = b0 ? sequence<COLUMNS>(p, b0 + lane) : first;
-        int64_t t = (int64_t)s.column_tiles * s.tiles;
-#pragma unroll
-        for (int d = 16; d; d >>= 1) t += __shfl_xor_sync(0xffffffffu, t, d);
-        total += t;
-    }
-    int32_t most = 1 << 30;
-    if (p.join) {
-        most = total < (1ll << 31) ? (int32_t)(((uint32_t)total + p.target - 1) / p.target) : (int32_t)min((total + p.target - 1) / p.target, (int64_t)most);
-        most = max(most, p.least_tiles);
-    }
-    int before = 0, units_before = 0;
-    for (int b0 = 0; b0 < p.batch; b0 += 32) {
-        const Sequence s = b0 ? sequence<COLUMNS>(p, b0 + lane) : first;
-        const int32_t chunks = max((s.tiles + most - 1) / most, 1), units = s.column_tiles * chunks, mine = BY_COLUMN_TILE ? s.column_tiles : units;
-        int32_t upto = mine, units_upto = units;  // of this and the lanes below
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int32_t o = __shfl_up_sync(0xffffffffu, upto, d), n = __shfl_up_sync(0xffffffffu, units_upto, d);
-            if (lane >= d) {
-                upto += o;
-                units_upto += n;
-            }
-        }
-        const uint32_t has = __ballot_sync(0xffffffffu, before + upto > at);
-        if (has) {
-            const int from = __ffs(has) - 1;
-            const int32_t local = at - (before + __shfl_sync(0xffffffffu, upto - mine, from));
-            u->seq = b0 + from;
-            u->chunks = __shfl_sync(0xffffffffu, chunks, from);
-            u->length = __shfl_sync(0xffffffffu, s.length, from);
-            u->rows = __shfl_sync(0xffffffffu, s.rows, from);
-            u->row0 = __shfl_sync(0xffffffffu, s.row0, from);
-            const int32_t tiles = __shfl_sync(0xffffffffu, s.tiles, from), first_tile = __shfl_sync(0xffffffffu, s.first_tile, from);
-            const int32_t column_tile = BY_COLUMN_TILE ? local : local / u->chunks, chunk = BY_COLUMN_TILE ? 0 : local - column_tile * u->chunks;
-            u->column0 = column_tile * COLUMNS;
-            *first_unit = units_before + __shfl_sync(0xffffffffu, units_upto - units, from) + column_tile * u->chunks;
-            // equal pieces
-            const int32_t each = tiles / u->chunks, more = tiles - each * u->chunks;
-            u->tile0 = first_tile + chunk * each + min(chunk, more);
-            u->tile1 = u->tile0 + each + (chunk < more ? 1 : 0);
-            return true;
-        }
-        before += __shfl_sync(0xffffffffu, upto, 31);
-        units_before += __shfl_sync(0xffffffffu, units_upto, 31);
-    }
-    return false;
-}
-
-// Tokens [lo, hi) that the row of a column sees; none for a column that does not exist.
-__device__ __forceinline__ void column_range(const AttnParams &p, const Unit &u, int column, int32_t *lo, int32_t *hi)
-{
-    const int32_t row = column / p.group;
-    *lo = *hi = 0;
-    if (row >= u.rows) return;
-    const int64_t position = (int64_t)u.length - u.rows + row;
-    *hi = p.causal ? (int32_t)min(max(position + 1, (int64_t)0), (int64_t)u.length) : u.length;
-    *lo = p.window > 0 ? (int32_t)min(max(position + 1 - p.window, (int64_t)0), (int64_t)u.length) : 0;
-}
-
-// Eight channels of a row of q; `count` of them exist.  SPLIT: fp32, otherwise f16 or bf16.
-template <bool SPLIT>
-__device__ __forceinline__ void load_row(const AttnParams &p, int64_t at, int count, float (&v)[8])
-{
-    if (SPLIT) {
-        const float *const q = static_cast<const float *>(p.q) + at;
-        if (p.q_vectors) load8<float, true>(q, count, v);
-        else load8<float, false>(q, count, v);
-    } else if (p.type == LCE_TYPE_FLOAT16) {
-        const __half *const q = static_cast<const __half *>(p.q) + at;
-        if (p.q_vectors) load8<__half, true>(q, count, v);
-        else load8<__half, false>(q, count, v);
-    } else {
-        const __nv_bfloat16 *const q = static_cast<const __nv_bfloat16 *>(p.q) + at;
-        if (p.q_vectors) load8<__nv_bfloat16, true>(q, count, v);
-        else load8<__nv_bfloat16, false>(q, count, v);
-    }
-}
-__device__ __forceinline__ void store_element(void *p, int32_t type, int64_t i, float v)
-{
-    switch (type) {
-        case LCE_TYPE_FLOAT32: static_cast<float *>(p)[i] = v; return;
-        case LCE_TYPE_FLOAT16: static_cast<__half *>(p)[i] = __float2half_rn(v); return;
-        default: static_cast<__nv_bfloat16 *>(p)[i] = __float2bfloat16_rn(v); return;
-    }
-}
 
 __device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t mask, uint32_t with)
 {
@@ -186,14 +34,6 @@ __device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t mask, uint32_t w
     asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(a), "r"(mask), "r"(with));
     return d;
 }
-__device__ __forceinline__ uint32_t pack_half2(float lo, float hi)
-{
-    uint32_t d;
-    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
-    return d;
-}
-__device__ __forceinline__ float half_low(uint32_t v) { return __half2float(__ushort_as_half((unsigned short)(v & 0xffffu))); }
-__device__ __forceinline__ float half_high(uint32_t v) { return __half2float(__ushort_as_half((unsigned short)(v >> 16))); }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t v)
 {
     uint32_t d;
@@ -219,15 +59,6 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
 {
     mma(d, a0, a1, a2, a3, b0, b1, d[0], d[1], d[2], d[3]);
 }
-__device__ __forceinline__ float exp2_fast(float x)
-{
-    float d;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(d) : "f"(x));
-    return d;
-}
-
-// Bytes exchanged in either half.
-__device__ __forceinline__ uint32_t swap_bytes(uint32_t w) { return __byte_perm(w, 0, 0x2301); }
 // A pair of codes on the mantissa of 1024, 1024 + 4 n or 1024 + 64 n, as f16 numbers c = n - 8.
 __device__ __forceinline__ uint32_t half_fma(uint32_t w, unsigned short by, unsigned short plus)
 {
@@ -885,6 +716,7 @@ lce_status launch_blocks(const AttnParams &p, cudaStream_t s)
     }
 }
 
+constexpr int kPromptLeast = 64;  // columns of a sequence, on average, from which the kernel for prompts is taken
 constexpr int kLeastTiles = 16;  // tiles of a warp that a piece is worth
 
 // one_row: without q_starts
@@ -907,6 +739,12 @@ lce_status make_params(const lce_kv_attention_desc *d, bool one_row, AttnParams 
     p->q_token = d->q_token_stride; p->q_head = d->q_head_stride; p->out_token = d->out_token_stride; p->out_head = d->out_head_stride;
     p->scale = d->scale * 1.44269504088896341f;
     *nt = p->g.blocks <= kWideBlocks && (d->tokens * p->group + d->batch - 1) / d->batch > 8 ? 2 : 1;
+    p->prompt = p->g.blocks <= 4 && d->type != LCE_TYPE_FLOAT32 && d->tokens * p->group >= (int64_t)kPromptLeast * d->batch;
+    if (p->prompt) {
+        p->units = p->column_tiles = (int32_t)(p->tokens * p->group / kPromptColumns + p->batch);
+        p->cluster = p->target = p->least_tiles = 1;
+        return LCE_OK;
+    }
     const int columns = 8 * *nt;
     const int64_t tiles = one_row ? (int64_t)p->batch * ((p->group + columns - 1) / columns) : p->tokens * p->group / columns + p->batch;
     // A cluster of up to eight blocks shares a unit, as many as the GPU has room for and as there are tiles for their warps.
@@ -965,9 +803,11 @@ extern "C" lce_status lce_kv_attention(const lce_kv_attention_desc *desc, const 
         return LCE_ERR_ALIGNMENT;
     if (workspace_size < workspace_bytes(p, nt)) return LCE_ERR_WORKSPACE;
     p.q_vectors = p.g.dim % 8 == 0 && aligned(q, 8 * element) && p.q_token % 8 == 0 && p.q_head % 8 == 0;
+    p.out_vectors = p.g.dim % 8 == 0 && aligned(out, 8 * element) && p.out_token % 8 == 0 && p.out_head % 8 == 0;
     p.q = q; p.cache = static_cast<const uint32_t *>(cache); p.page_table = page_table; p.lengths = lengths; p.q_starts = q_starts;
     p.out = out; p.parts = static_cast<float *>(workspace);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (p.prompt) return launch_kv_prompt(p, s);
     if (desc->type == LCE_TYPE_FLOAT32) return nt == 2 ? launch_blocks<2, true>(p, s) : launch_blocks<1, true>(p, s);
     return nt == 2 ? launch_blocks<2, false>(p, s) : launch_blocks<1, false>(p, s);
 }

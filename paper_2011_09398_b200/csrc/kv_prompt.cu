@@ -1,0 +1,572 @@
+// Attention of many rows of a sequence (a prompt, a chunk of one) over the 4-bit cache, on the 5th-generation tensor cores.
+//
+// A block works on 256 columns (rows of q that share a key/value head), two tiles of 128 that take turns, over tiles of 128 tokens:
+//   warps 0 - 3, 4 - 7  a tile of columns each, a thread to a column: scores from TMEM, running softmax, weights back to TMEM as f16
+//   warps 8 - 11        4-bit words from the cache to f16 keys and values in shared memory, two stages
+//   warp 12             one thread issues the products: S = Q K^T (128 x 128 x channels, both operands in shared memory) and
+//                       O += P V (P from TMEM), S of one tile of columns while the other one's weights are made
+// TMEM: S of both tiles (columns 0 - 255; the weights P take the place of the scores they come from), O of both (256 - 511).
+//
+// f16 holds a code times its scale exactly, 3 and 8 bits, so keys and values lose nothing as long as they fit its exponents.  They are
+// taken relative to a power of two: for the keys above the tile's largest scale, which goes back into the scores; for the values
+// above the largest so far, and when that grows O is scaled down, as it is when a row's running maximum grows by more than 2^8 (rare).
+// A code is decoded by one packed multiply-add from the subnormal number that its bits are: (n 2^-22) (s 2^22) - 8 s, five instructions
+// for two of four codes with the AND.
+//
+// Per 128 tokens and 256 columns of 128 channels: four products of 512 clocks, 32768 exponentials at 16 a clock, 2048 clocks each, and
+// 8000 instructions, 2000 clocks.
+#include "kv_attention.cuh"
+#include "mx_common.cuh"
+
+namespace lce {
+namespace {
+
+constexpr int kTokens = 128;                    // of a tile here: eight tiles of the cache
+constexpr int kSoftmaxWarps = 8, kProducerWarps = 4, kIssuerWarp = kSoftmaxWarps + kProducerWarps;
+constexpr int kThreads = 32 * (kIssuerWarp + 1);
+constexpr float kRise = 8.0f;                   // a running maximum is raised when a score passes it by 2^8
+constexpr float kHeadroom = 7.0f;               // weights are held times 2^7: 2^(7 + 8) is the most that meets f16
+constexpr int kInfos = 4;                       // the producers are less than three tiles ahead of the softmax
+
+enum { BAR_Q = 0, BAR_K_FULL, BAR_V_FULL = BAR_K_FULL + 2, BAR_K_EMPTY = BAR_V_FULL + 2, BAR_V_EMPTY = BAR_K_EMPTY + 2, BAR_S_FULL = BAR_V_EMPTY + 2,
+       BAR_P_FULL = BAR_S_FULL + 2, BAR_DONE = BAR_P_FULL + 2, BAR_COUNT };
+
+// What the softmax has to know of a tile.
+struct TileInfo {
+    float key_unit;      // 2^e: scores count in it
+    int32_t value_exponent;
+    uint32_t valid;      // bit per 16 tokens: their page is in the pool
+    uint32_t nan;        // some value's scale is NaN: see nans
+};
+
+struct Shared {
+    uint64_t bars[BAR_COUNT];
+    uint32_t tmem, largest[2][2][kProducerWarps];     // [turn][keys, values]
+    TileInfo info[kInfos];
+    alignas(16) __half key_scales[2][kTokens][4];     // relative to the tile's, times 2^15; [turn]
+    alignas(16) __half value_scales[2][kTokens / 2][4][2];
+    uint8_t nans[kInfos][kTokens];                    // blocks of a token's value that are NaN
+};
+
+constexpr int kMiscBytes = 8192;
+static_assert(sizeof(Shared) <= kMiscBytes, "");
+constexpr size_t prompt_smem(int blocks) { return kMiscBytes + 6 * (size_t)(kTokens * 64 * blocks); }
+
+__device__ __forceinline__ void mma_shared(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+        : "memory");
+}
+__device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+        : "memory");
+}
+// Operand in shared memory without swizzle: 8 rows x 16 bytes are 128 bytes in a row, those of the next eight k behind them, those of the next
+// eight rows `rows8` bytes on.
+__device__ __forceinline__ uint64_t operand(uint32_t at, uint32_t rows8)
+{
+    return (uint64_t)(at >> 4) | (uint64_t)(128 >> 4) << 16 | (uint64_t)(rows8 >> 4) << 32 | 1ull << 46;
+}
+
+// 32 columns of this warp's 32 lanes of TMEM
+__device__ __forceinline__ void tmem_load32(uint32_t at, uint32_t (&r)[32])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
+          "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]),
+          "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(at)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_store32(uint32_t at, const uint32_t (&r)[32])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::"r"(r[0]),
+        "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]),
+        "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]),
+        "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(at)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t (&r)[16])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]),
+        "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(at)
+        : "memory");
+}
+
+// The B words of a place (a lane's of ROWS = 64 places, a token's of 16), plane by plane.
+template <int B, int ROWS>
+__device__ __forceinline__ void load_planes(const uint32_t *base, int place, uint32_t (&w)[B])
+{
+    if (B == 4) {
+        const uint4 v = __ldg(reinterpret_cast<const uint4 *>(base) + place);
+        w[0] = v.x; w[B > 1 ? 1 : 0] = v.y; w[B > 2 ? 2 : 0] = v.z; w[B > 3 ? 3 : 0] = v.w;
+    } else {
+        if (B & 2) {
+            const uint2 v = __ldg(reinterpret_cast<const uint2 *>(base) + place);
+            w[0] = v.x; w[B > 1 ? 1 : 0] = v.y;
+        }
+        if (B & 1) w[B - 1] = __ldg(base + ROWS * (B - 1) + place);
+    }
+}
+
+__device__ __forceinline__ uint32_t half2_bits(__half2 v) { return *reinterpret_cast<const uint32_t *>(&v); }
+__device__ __forceinline__ uint32_t decode(uint32_t bits, __half2 by, __half2 plus)
+{
+    return half2_bits(__hfma2(*reinterpret_cast<const __half2 *>(&bits), by, plus));
+}
+
+__device__ __forceinline__ uint32_t r_low(uint32_t w) { return w << 16; }  // the key's scale, as fp32 bits
+__device__ __forceinline__ void producers_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+// The same, and whether all of them are well: where one's wait gave up, all leave together.
+__device__ __forceinline__ bool producers_sync_and(bool ok)
+{
+    uint32_t all;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 q, %1, 0;\n\t"
+        "bar.red.and.pred p, 1, 128, q;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(all)
+        : "r"((uint32_t)ok)
+        : "memory");
+    return all != 0;
+}
+
+// What a producer thread has of a tile before it decodes it.
+template <int B>
+struct Raw {
+    uint32_t scales[B];          // of its token
+    uint32_t keys[4][B], values[4][B];
+    uint32_t valid;
+};
+
+template <int B>
+__device__ __forceinline__ void load_raw(const AttnParams &p, const int32_t *table, int head, int length, int tile, int thread, Raw<B> &r)
+{
+    constexpr int TILE = kv_tile_words(B);
+    const int lane = thread & 31, warp = thread >> 5, tiles_per_page = p.g.page_size / kKvTile;
+    int32_t place = -1;
+    if (lane < 8) {
+        const int32_t t = tile * 8 + lane;
+        if (t * kKvTile < length) {
+            const int32_t in_table = t / tiles_per_page, page = __ldg(table + in_table);
+            if (page >= 0 && page < p.g.pages) place = (page * p.g.heads + head) * tiles_per_page + (t - in_table * tiles_per_page);
+        }
+    }
+    r.valid = __ballot_sync(0xffffffffu, place >= 0);
+    const auto tile_at = [&](int t) -> const uint32_t * {
+        const int32_t at = __shfl_sync(0xffffffffu, place, t);
+        return at >= 0 ? p.cache + (int64_t)at * TILE : nullptr;
+    };
+#pragma unroll
+    for (int b = 0; b < B; ++b) r.scales[b] = 0;
+    {
+        const uint32_t *const at = tile_at(thread >> 4);
+        if (at && tile * kTokens + thread < length) load_planes<B, 16>(at + 128 * B, thread & 15, r.scales);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int half = i * 4 + warp;
+        const uint32_t *const at = tile_at(half >> 1);
+#pragma unroll
+        for (int b = 0; b < B; ++b) r.keys[i][b] = 0;
+        if (at) load_planes<B, 64>(at, (half & 1) * 32 + (lane & 7) * 4 + (lane >> 3), r.keys[i]);
+    }
+    const uint32_t *const at = tile_at(thread >> 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+        for (int b = 0; b < B; ++b) r.values[i][b] = 0;
+        if (at) load_planes<B, 64>(at + 64 * B, (thread >> 3 & 1) * 32 + (thread & 7) * 4 + i, r.values[i]);
+    }
+}
+
+template <int B>
+__global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_constant__ AttnParams p, const TimeoutReport report)
+{
+    constexpr uint32_t ROWS8_QK = 512 * B, ROWS8_V = 2048;   // bytes from eight rows to the next
+    constexpr uint32_t TILE_BYTES = kTokens * 64 * B;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    Shared &sh = *reinterpret_cast<Shared *>(smem);
+    uint8_t *const q_smem = smem + kMiscBytes, *const k_smem = q_smem + 2 * TILE_BYTES, *const v_smem = k_smem + 2 * TILE_BYTES;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    Unit u;
+    int first_unit;
+    // the last column tiles see most tokens and come first
+    if (!find_unit<kPromptColumns, false>(p, p.units - 1 - (int)blockIdx.x, &u, &first_unit)) return;
+    const int head = blockIdx.y;
+    int32_t any_lo, any_hi, unused;
+    const int columns = u.rows * p.group;
+    column_range(p, u, u.column0, &any_lo, &unused);
+    column_range(p, u, min(u.column0 + kPromptColumns, columns) - 1, &unused, &any_hi);
+    const int32_t tile0 = any_lo / kTokens, tiles = any_hi > any_lo ? (any_hi + kTokens - 1) / kTokens - tile0 : 0;
+    const int tiles_of_columns = u.column0 + 128 < columns ? 2 : 1;
+
+    if (threadIdx.x == 0) {
+        mbar_init(&sh.bars[BAR_Q], 32 * kSoftmaxWarps);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&sh.bars[BAR_K_FULL + i], 32 * kProducerWarps);
+            mbar_init(&sh.bars[BAR_V_FULL + i], 32 * kProducerWarps);
+            mbar_init(&sh.bars[BAR_K_EMPTY + i], 1);
+            mbar_init(&sh.bars[BAR_V_EMPTY + i], 1);
+            mbar_init(&sh.bars[BAR_S_FULL + i], 1);
+            mbar_init(&sh.bars[BAR_P_FULL + i], 128);
+        }
+        mbar_init(&sh.bars[BAR_DONE], 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == kIssuerWarp) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&sh.tmem)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = sh.tmem;
+    bool ok = true;
+
+    if (warp < kSoftmaxWarps) {
+        // ---- softmax: a thread to a column ------------------------------------------------------------
+        const int half = warp >> 2, in_tile = threadIdx.x & 127, column = u.column0 + 128 * half + in_tile, row = column / p.group;
+        int32_t lo, hi;
+        column_range(p, u, column, &lo, &hi);
+        float factor;
+        {
+            const int64_t at = (u.row0 + row) * p.q_token + ((int64_t)head * p.group + (column - row * p.group)) * p.q_head;
+            uint32_t magnitude = 0;
+            float v[8];
+#pragma unroll
+            for (int c = 0; c < 4 * B; ++c) {
+                load_row<false>(p, at + 8 * c, row < u.rows ? p.g.dim - 8 * c : 0, v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) magnitude = max(magnitude, __float_as_uint(v[i]) & 0x7fffffffu);
+            }
+            const bool finite = magnitude < 0x7f800000u;
+            // times 2^k, so that the largest is in [2^14, 2^15); a scale below zero changes q's sign
+            const int e = finite && magnitude > 0 ? ilogbf(__uint_as_float(magnitude)) : 0, k = 14 - e, k1 = k / 2, k2 = k - k1;
+            const float s1 = __uint_as_float((uint32_t)(127 + k1) << 23) * (p.scale < 0.0f ? -1.0f : 1.0f), s2 = __uint_as_float((uint32_t)(127 + k2) << 23);
+            uint8_t *const to = q_smem + half * TILE_BYTES + (in_tile >> 3) * ROWS8_QK + (in_tile & 7) * 16;
+#pragma unroll
+            for (int c = 0; c < 4 * B; ++c) {
+                load_row<false>(p, at + 8 * c, row < u.rows ? p.g.dim - 8 * c : 0, v);  // again, from the L1
+                uint4 w;
+                // in the order in which a word's codes are decoded
+                w.x = pack_half2(v[0] * s1 * s2, v[4] * s1 * s2);
+                w.y = pack_half2(v[1] * s1 * s2, v[5] * s1 * s2);
+                w.z = pack_half2(v[2] * s1 * s2, v[6] * s1 * s2);
+                w.w = pack_half2(v[3] * s1 * s2, v[7] * s1 * s2);
+                *reinterpret_cast<uint4 *>(to + c * 128) = w;
+            }
+            const int kc = 8 - k, c1 = kc / 2, c2 = kc - c1;
+            factor = (finite ? fabsf(p.scale) : __uint_as_float(0x7fc00000u)) * __uint_as_float((uint32_t)(127 + c1) << 23) * __uint_as_float((uint32_t)(127 + c2) << 23);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            mbar_arrive(&sh.bars[BAR_Q]);
+        }
+        const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16, s_at = tmem + lanes + 128 * half, o_at = tmem + lanes + 256 + 128 * half;
+        float top = kLowest, weight[4] = {};
+        int32_t exponent = 0;
+        uint32_t nan_blocks = 0;
+        if (half < tiles_of_columns) {
+            for (int j = 0; ok && j < tiles; ++j) {
+                ok = __all_sync(0xffffffffu, mbar_wait_bounded(&sh.bars[BAR_S_FULL + half], j & 1));
+                if (!ok) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                const TileInfo info = sh.info[j % kInfos];
+                const int32_t token0 = (tile0 + j) * kTokens;
+                const float f = factor * info.key_unit;
+                // bits of tokens that count, where not all do
+                const bool all = __all_sync(0xffffffffu, info.valid == 0xffu && token0 >= lo && token0 + kTokens <= hi);
+                uint32_t seen[4] = {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};
+                if (!all) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const int32_t from = min(max(lo - (token0 + 32 * c), 0), 32), to = min(max(hi - (token0 + 32 * c), 0), 32);
+                        const uint32_t below = to >= 32 ? 0xffffffffu : (1u << to) - 1, above = from >= 32 ? 0u : 0xffffffffu << from;
+                        const uint32_t pages = (info.valid >> (2 * c) & 1 ? 0xffffu : 0u) | (info.valid >> (2 * c + 1) & 1 ? 0xffff0000u : 0u);
+                        seen[c] = below & above & pages;
+                    }
+                }
+                if (info.nan) {
+                    for (int t = 0; t < kTokens; ++t)
+                        if (seen[t >> 5] >> (t & 31) & 1) nan_blocks |= sh.nans[j % kInfos][t];
+                }
+                float m = -INFINITY;
+                uint32_t r[32];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    tmem_load32(s_at + 32 * c, r);
+                    if (all) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) m = fmaxf(m, __uint_as_float(r[i]));
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) m = fmaxf(m, seen[c] >> i & 1 ? __uint_as_float(r[i]) : -INFINITY);
+                    }
+                }
+                m = m == -INFINITY ? m : m * f;
+                // whole warps: the accumulators are read and written by warps
+                if (__any_sync(0xffffffffu, m > top + kRise || exponent != info.value_exponent)) {
+                    const float new_top = fmaxf(m, top), by = exp2f(top - new_top), by_o = by * exp2f((float)(exponent - info.value_exponent));
+                    if (j > 0) {
+#pragma unroll
+                        for (int c = 0; c < B; ++c) {
+                            tmem_load32(o_at + 32 * c, r);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * by_o);
+                            tmem_store32(o_at + 32 * c, r);
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) weight[i] *= by;
+                    top = new_top;
+                    exponent = info.value_exponent;
+                }
+                const float minus = kHeadroom - top;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    tmem_load32(s_at + 32 * c, r);
+                    uint32_t w[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        float x = fmaf(__uint_as_float(r[2 * i]), f, minus), y = fmaf(__uint_as_float(r[2 * i + 1]), f, minus);
+                        if (!all) {
+                            x = seen[c] >> (2 * i) & 1 ? x : -INFINITY;
+                            y = seen[c] >> (2 * i + 1) & 1 ? y : -INFINITY;
+                        }
+                        x = exp2_fast(x);
+                        y = exp2_fast(y);
+                        weight[2 * (i & 1)] += x;
+                        weight[2 * (i & 1) + 1] += y;
+                        w[i] = pack_half2(x, y);
+                    }
+                    tmem_store16(s_at + 16 * c, w);  // columns that have been read
+                }
+                asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                mbar_arrive(&sh.bars[BAR_P_FULL + half]);
+            }
+            if (ok && tiles > 0) ok = __all_sync(0xffffffffu, mbar_wait_bounded(&sh.bars[BAR_DONE], 0));
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            if (ok) {
+                const float total = (weight[0] + weight[1]) + (weight[2] + weight[3]);
+                const float by = (total == 0.0f ? 0.0f : 1.0f / total), unit = exp2f((float)(exponent + 8));
+                const int64_t at = (u.row0 + row) * p.out_token + ((int64_t)head * p.group + (column - row * p.group)) * p.out_head;
+#pragma unroll
+                for (int b = 0; b < B; ++b) {
+                    uint32_t r[32];
+                    if (tiles > 0) {
+                        tmem_load32(o_at + 32 * b, r);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) r[i] = 0;
+                    }
+                    // channel 4 g + i of the block is row 8 i + g of the product
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        float v[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float x = total == 0.0f ? 0.0f : __uint_as_float(r[(i & 3) * 8 + 2 * c + (i >> 2)]) * by * unit;
+                            v[i] = nan_blocks >> b & 1 ? __uint_as_float(0x7fc00000u) : x;
+                        }
+                        const int channel = 32 * b + 8 * c, count = row < u.rows ? p.g.dim - channel : 0;
+                        if (p.type == LCE_TYPE_FLOAT16) {
+                            __half *const out = static_cast<__half *>(p.out) + at + channel;
+                            if (p.out_vectors) store8<__half, true>(out, count, v);
+                            else store8<__half, false>(out, count, v);
+                        } else {
+                            __nv_bfloat16 *const out = static_cast<__nv_bfloat16 *>(p.out) + at + channel;
+                            if (p.out_vectors) store8<__nv_bfloat16, true>(out, count, v);
+                            else store8<__nv_bfloat16, false>(out, count, v);
+                        }
+                    }
+                }
+            }
+        }
+    } else if (warp < kIssuerWarp) {
+        // ---- keys and values: from 4 bits to f16 operands ------------------------------------------------
+        const int thread = threadIdx.x - 32 * kSoftmaxWarps, producer = warp - kSoftmaxWarps;
+        const int32_t *const table = p.page_table + (int64_t)u.seq * p.table_pages;
+        Raw<B> raw, next;
+        if (tiles > 0) load_raw<B>(p, table, head, u.length, tile0, thread, raw);
+        int32_t value_exponent = -1000;
+        const __half2 sixteenth = __float2half2_rn(0.0625f), eight = __float2half2_rn(-0x1p-19f);
+        for (int j = 0; j < tiles; ++j) {
+            if (j + 1 < tiles) load_raw<B>(p, table, head, u.length, tile0 + j + 1, thread, next);
+            const int stage = j & 1, turn = j & 1;
+            // the largest scales of the tile (bits of bf16 numbers compare like integers; a NaN does not count)
+            uint32_t nan = 0, top_k = 0, top_v = 0;
+#pragma unroll
+            for (int b = 0; b < B; ++b) {
+                const uint32_t ks = r_low(raw.scales[b]), vs = raw.scales[b] & 0xffff0000u;
+                if (ks < 0x7f800000u) top_k = max(top_k, ks);
+                if (vs < 0x7f800000u) top_v = max(top_v, vs);
+                else nan |= 1u << b;
+            }
+            top_k = __reduce_max_sync(0xffffffffu, top_k);
+            top_v = __reduce_max_sync(0xffffffffu, top_v);
+            const uint32_t some_nan = __ballot_sync(0xffffffffu, nan != 0);
+            if (lane == 0) {
+                sh.largest[turn][0][producer] = top_k;
+                sh.largest[turn][1][producer] = top_v | (some_nan ? 1u : 0u);
+            }
+            ok = producers_sync_and(ok);
+            if (!ok) break;
+            top_k = top_v = 0;
+            uint32_t any_nan = 0;
+#pragma unroll
+            for (int i = 0; i < kProducerWarps; ++i) {
+                top_k = max(top_k, sh.largest[turn][0][i]);
+                any_nan |= sh.largest[turn][1][i] & 1u;
+                top_v = max(top_v, sh.largest[turn][1][i] & 0xffff0000u);
+            }
+            const int key_exponent = max((int)(top_k >> 23) - 127, -100);
+            const int here = max((int)(top_v >> 23) - 127, -100);
+            if (top_v > 0 && here > value_exponent) value_exponent = here + 1;  // one more, so that it does not move often
+            const int ve = max(value_exponent, -100);
+            // relative scales times 2^15: below 2^15, exact in f16 down to 2^-10 of the largest
+            const float k_by = __uint_as_float((uint32_t)(127 + 14 - key_exponent) << 23), v_by = __uint_as_float((uint32_t)(127 + 14 - ve) << 23);
+#pragma unroll
+            for (int b = 0; b < B; ++b) {
+                const float vs = __uint_as_float(raw.scales[b] & 0xffff0000u);
+                sh.key_scales[turn][thread][b] = __float2half_rn(__uint_as_float(r_low(raw.scales[b])) * k_by);
+                sh.value_scales[turn][thread >> 1][b][thread & 1] = __float2half_rn(nan >> b & 1 ? 0.0f : vs * v_by);
+            }
+            if (any_nan) sh.nans[j % kInfos][thread] = (uint8_t)nan;
+            if (thread == 0) sh.info[j % kInfos] = TileInfo{__uint_as_float((uint32_t)(127 + key_exponent) << 23), ve, raw.valid, any_nan};
+            producers_sync();
+            if (j >= 2) ok = mbar_wait_bounded(&sh.bars[BAR_K_EMPTY + stage], (j >> 1 & 1) ^ 1);
+            constexpr uint32_t kEven = 0x003c003cu, kOdd = 0x03c003c0u;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int unit = i * 4 + producer, token = unit * 8 + (lane & 7), quarter = lane >> 3;
+                uint8_t *const to = k_smem + stage * TILE_BYTES + unit * ROWS8_QK + quarter * 128 + (lane & 7) * 16;
+#pragma unroll
+                for (int b = 0; b < B; ++b) {
+                    const __half2 even = __half2half2(sh.key_scales[turn][token][b]), odd = __hmul2(even, sixteenth), plus = __hmul2(even, eight);
+                    const uint32_t x = raw.keys[i][b], y = swap_bytes(x);
+                    *reinterpret_cast<uint4 *>(to + b * 512) =
+                        make_uint4(decode(x & kEven, even, plus), decode(x & kOdd, odd, plus), decode(y & kEven, even, plus), decode(y & kOdd, odd, plus));
+                }
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            mbar_arrive(&sh.bars[BAR_K_FULL + stage]);
+            if (j >= 2) ok = mbar_wait_bounded(&sh.bars[BAR_V_EMPTY + stage], (j >> 1 & 1) ^ 1) && ok;
+            {
+                const int eighth = thread & 7, group = thread >> 3;  // eight tokens
+                uint8_t *const to = v_smem + stage * TILE_BYTES + group * 128 + eighth * 16;
+#pragma unroll
+                for (int b = 0; b < B; ++b) {
+                    uint32_t w[4][4];  // [channel][pair of tokens]
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        const __half2 even = *reinterpret_cast<const __half2 *>(sh.value_scales[turn][group * 4 + t][b]), odd = __hmul2(even, sixteenth),
+                                      plus = __hmul2(even, eight);
+                        const uint32_t x = raw.values[t][b], y = swap_bytes(x);
+                        w[0][t] = decode(x & kEven, even, plus);
+                        w[1][t] = decode(x & kOdd, odd, plus);
+                        w[2][t] = decode(y & kEven, even, plus);
+                        w[3][t] = decode(y & kOdd, odd, plus);
+                    }
+                    // channel 4 eighth + i of the block is row 8 i + eighth of the operand
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4 *>(to + (4 * b + i) * ROWS8_V) = make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]);
+                }
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            mbar_arrive(&sh.bars[BAR_V_FULL + stage]);
+            raw = next;
+        }
+    } else if (lane == 0 && tiles > 0) {
+        // ---- the products ---------------------------------------------------------------------------------
+        constexpr uint32_t kCommon = 1u << 4 | (uint32_t)(128 >> 4) << 24;  // fp32 sums of f16 products, both operands along k, 128 rows
+        const uint32_t idesc_s = kCommon | (uint32_t)(kTokens >> 3) << 17, idesc_o = kCommon | (uint32_t)(32 * B >> 3) << 17;
+        const uint32_t q_at = smem_u32(q_smem), k_at = smem_u32(k_smem), v_at = smem_u32(v_smem);
+        const auto scores = [&](int half, int stage) {
+#pragma unroll
+            for (int k = 0; k < 2 * B; ++k)
+                mma_shared(tmem + 128 * half, operand(q_at + half * TILE_BYTES + k * 256, ROWS8_QK), operand(k_at + stage * TILE_BYTES + k * 256, ROWS8_QK), idesc_s, k > 0);
+        };
+        const auto sums = [&](int half, int stage, bool add) {
+#pragma unroll
+            for (int k = 0; k < kTokens / 16; ++k)
+                mma_tmem(tmem + 256 + 128 * half, tmem + 128 * half + 8 * k, operand(v_at + stage * TILE_BYTES + k * 256, ROWS8_V), idesc_o, add || k > 0);
+        };
+        ok = mbar_wait_bounded(&sh.bars[BAR_Q], 0) && mbar_wait_bounded(&sh.bars[BAR_K_FULL], 0);
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        if (ok) {
+            for (int half = 0; half < tiles_of_columns; ++half) {
+                scores(half, 0);
+                mma_commit(&sh.bars[BAR_S_FULL + half]);
+            }
+            mma_commit(&sh.bars[BAR_K_EMPTY]);
+        }
+        for (int j = 0; ok && j < tiles; ++j) {
+            const int stage = j & 1, next = stage ^ 1;
+            ok = mbar_wait_bounded(&sh.bars[BAR_V_FULL + stage], j >> 1 & 1);
+            if (ok && j + 1 < tiles) ok = mbar_wait_bounded(&sh.bars[BAR_K_FULL + next], (j + 1) >> 1 & 1);
+            for (int half = 0; ok && half < tiles_of_columns; ++half) {
+                ok = mbar_wait_bounded(&sh.bars[BAR_P_FULL + half], j & 1);
+                if (!ok) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                sums(half, stage, j > 0);
+                if (j + 1 < tiles) {  // in order behind the sums, which read the weights in its place
+                    scores(half, next);
+                    mma_commit(&sh.bars[BAR_S_FULL + half]);
+                }
+            }
+            if (!ok) break;
+            mma_commit(&sh.bars[BAR_V_EMPTY + stage]);
+            if (j + 1 < tiles) mma_commit(&sh.bars[BAR_K_EMPTY + next]);
+        }
+        // whatever happened: nothing is in flight when the tensor memory goes
+        mma_commit(&sh.bars[BAR_DONE]);
+        if (!mbar_wait_bounded(&sh.bars[BAR_DONE], 0)) ok = false;
+    }
+    if (!ok) {
+        *report.device_word = 1;
+        if (report.host_word) {
+            *reinterpret_cast<volatile int *>(report.host_word) = 1;
+            __threadfence_system();
+        }
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    if (warp == kIssuerWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+}
+
+template <int B>
+lce_status launch(const AttnParams &p, const TimeoutReport &report, cudaStream_t s)
+{
+    static SmemOptIn opt_in;
+    if (!opt_in.ensure(kv_prompt_kernel<B>, prompt_smem(B))) return LCE_ERR_CUDA;
+    return launch_dependent(kv_prompt_kernel<B>, dim3((unsigned)p.units, (unsigned)p.g.heads), kThreads, prompt_smem(B), s, p, report);
+}
+
+}  // namespace
+
+lce_status launch_kv_prompt(const AttnParams &p, cudaStream_t s)
+{
+    if (tensor_timeout_flagged()) return LCE_ERR_DEVICE_TIMEOUT;
+    const TimeoutReport report = tensor_timeout_report(s);
+    if (!report.device_word) return LCE_ERR_CUDA;
+    switch (p.g.blocks) {
+        case 1: return launch<1>(p, report, s);
+        case 2: return launch<2>(p, report, s);
+        case 3: return launch<3>(p, report, s);
+        default: return launch<4>(p, report, s);
+    }
+}
+
+}  // namespace lce

@@ -245,7 +245,7 @@ __device__ __forceinline__ void norm_row(const NormParams &p, const NormRow<TS, 
 // TS, TB: elements of the stream and of the block; A: the arithmetic; N vectors to a thread.  A block (a warp, for short rows) takes row
 // after row.
 template <typename TS, typename TB, typename A, int N, bool VEC>
-__global__ void __launch_bounds__(512, N == 1 ? 2 : 1) residual_norm_kernel(const __grid_constant__ NormParams p, const TS *x, const TB *branch, const TB *gate, TS *y,
+__global__ void __launch_bounds__(sizeof(A) == 8 && N == 2 ? 256 : 512, sizeof(A) == 8 && N == 2 ? 2 : N == 1 ? 2 : 1) residual_norm_kernel(const __grid_constant__ NormParams p, const TS *x, const TB *branch, const TB *gate, TS *y,
                                                                             TB *normed)
 {
     extern __shared__ __align__(16) uint4 shared_places[];
@@ -320,9 +320,15 @@ lce_status launch(NormParams p, const NormBuffers &b, cudaStream_t s)
 template <typename TS, typename TB, typename A, bool VEC>
 lce_status launch_vectors(const NormParams &p, const NormBuffers &b, cudaStream_t s)
 {
-    // a warp to a row of up to 512 channels; otherwise a block with one vector to a thread as far as it goes
-    if (p.vectors <= 32 || (p.vectors > 64 && p.vectors <= 512)) return launch<TS, TB, A, 1, VEC>(p, b, s);
-    return p.vectors <= 1024 ? launch<TS, TB, A, 2, VEC>(p, b, s) : launch<TS, TB, A, 4, VEC>(p, b, s);
+    // A warp to a row of up to 256 or 512 channels, otherwise a block.  One vector to a thread as far as it goes in fp32; fp64 does better with
+    // two (8000 rows of 4000 channels in fp32, layer norms and a gate: 119 us with one, 133 with two; with sign bits 175 and 161).
+    const int vectors = p.vectors;
+    if (sizeof(A) == 8) {
+        if (vectors <= 32) return launch<TS, TB, A, 1, VEC>(p, b, s);
+        return vectors <= 512 ? launch<TS, TB, A, 2, VEC>(p, b, s) : launch<TS, TB, A, 4, VEC>(p, b, s);
+    }
+    if (vectors <= 32 || (vectors > 64 && vectors <= 512)) return launch<TS, TB, A, 1, VEC>(p, b, s);
+    return vectors <= 1024 ? launch<TS, TB, A, 2, VEC>(p, b, s) : launch<TS, TB, A, 4, VEC>(p, b, s);
 }
 
 template <typename TS, typename TB>
