@@ -23,7 +23,10 @@ namespace {
 
 constexpr int kTokens = 128;                    // of a tile here: eight tiles of the cache
 constexpr int kSoftmaxWarps = 8, kProducerWarps = 4, kIssuerWarp = kSoftmaxWarps + kProducerWarps;
-constexpr int kThreads = 32 * (kIssuerWarp + 1);
+constexpr int kThreads = 32 * (kIssuerWarp + 4);  // whole warpgroups: registers are shared out between them
+// Registers a thread: 128 at the launch, 512 * 128 in all = 256 * 176 + 128 * 104 + 128 * 56.
+constexpr int kSoftmaxRegisters = 176, kProducerRegisters = 104, kIssuerRegisters = 56;
+static_assert(256 * kSoftmaxRegisters + 128 * kProducerRegisters + 128 * kIssuerRegisters <= kThreads * 128, "more registers than the block has");
 constexpr float kRise = 8.0f;                   // a running maximum is raised when a score passes it by 2^8
 constexpr float kHeadroom = 7.0f;               // weights are held times 2^7: 2^(7 + 8) is the most that meets f16
 constexpr int kInfos = 4;                       // the producers are less than three tiles ahead of the softmax
@@ -86,15 +89,44 @@ __device__ __forceinline__ void tmem_load32(uint32_t at, uint32_t (&r)[32])
         : "r"(at)
         : "memory");
 }
-__device__ __forceinline__ void tmem_store32(uint32_t at, const uint32_t (&r)[32])
+// 128 columns
+__device__ __forceinline__ void tmem_load128(uint32_t at, uint32_t (&r)[128])
 {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
-        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::"r"(r[0]),
-        "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]),
-        "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]),
-        "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(at)
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {"
+        "%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31"
+        "}, [%128];\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {"
+        "%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63"
+        "}, [%129];\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {"
+        "%64,%65,%66,%67,%68,%69,%70,%71,%72,%73,%74,%75,%76,%77,%78,%79,%80,%81,%82,%83,%84,%85,%86,%87,%88,%89,%90,%91,%92,%93,%94,%95"
+        "}, [%130];\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {"
+        "%96,%97,%98,%99,%100,%101,%102,%103,%104,%105,%106,%107,%108,%109,%110,%111,%112,%113,%114,%115,%116,%117,%118,%119,%120,%121,%122,%123,%124,%125,"
+        "%126,%127"
+        "}, [%131];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), 
+          "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), 
+          "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]), "=r"(r[32]), "=r"(r[33]), 
+          "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), 
+          "=r"(r[45]), "=r"(r[46]), "=r"(r[47]), "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]), 
+          "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63]), "=r"(r[64]), "=r"(r[65]), "=r"(r[66]), 
+          "=r"(r[67]), "=r"(r[68]), "=r"(r[69]), "=r"(r[70]), "=r"(r[71]), "=r"(r[72]), "=r"(r[73]), "=r"(r[74]), "=r"(r[75]), "=r"(r[76]), "=r"(r[77]), 
+          "=r"(r[78]), "=r"(r[79]), "=r"(r[80]), "=r"(r[81]), "=r"(r[82]), "=r"(r[83]), "=r"(r[84]), "=r"(r[85]), "=r"(r[86]), "=r"(r[87]), "=r"(r[88]), 
+          "=r"(r[89]), "=r"(r[90]), "=r"(r[91]), "=r"(r[92]), "=r"(r[93]), "=r"(r[94]), "=r"(r[95]), "=r"(r[96]), "=r"(r[97]), "=r"(r[98]), "=r"(r[99]), 
+          "=r"(r[100]), "=r"(r[101]), "=r"(r[102]), "=r"(r[103]), "=r"(r[104]), "=r"(r[105]), "=r"(r[106]), "=r"(r[107]), "=r"(r[108]), "=r"(r[109]), 
+          "=r"(r[110]), "=r"(r[111]), "=r"(r[112]), "=r"(r[113]), "=r"(r[114]), "=r"(r[115]), "=r"(r[116]), "=r"(r[117]), "=r"(r[118]), "=r"(r[119]), 
+          "=r"(r[120]), "=r"(r[121]), "=r"(r[122]), "=r"(r[123]), "=r"(r[124]), "=r"(r[125]), "=r"(r[126]), "=r"(r[127])
+        : "r"(at), "r"(at + 32), "r"(at + 64), "r"(at + 96)
         : "memory");
+}
+__device__ __forceinline__ void tmem_store8(uint32_t at, const uint32_t (&r)[8])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]),
+                 "r"(r[6]), "r"(r[7]), "r"(at)
+                 : "memory");
 }
 __device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t (&r)[16])
 {
@@ -139,6 +171,19 @@ __device__ __forceinline__ bool producers_sync_and(bool ok)
         : "r"((uint32_t)ok)
         : "memory");
     return all != 0;
+}
+
+// mbar_wait_bounded in place: a kernel that calls a function cannot share its registers out.
+__device__ __forceinline__ bool wait_bounded(uint64_t *bar, uint32_t parity)
+{
+    if (mbar_try_wait(bar, parity)) return true;
+    const uint64_t t0 = globaltimer_ns();
+    do {
+#pragma unroll 1
+        for (int i = 0; i < 32; ++i)
+            if (mbar_try_wait(bar, parity)) return true;
+    } while (globaltimer_ns() - t0 < kWaitLimitNs);
+    return false;
 }
 
 // What a producer thread has of a tile before it decodes it.
@@ -236,6 +281,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
     bool ok = true;
 
     if (warp < kSoftmaxWarps) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegisters));
         // ---- softmax: a thread to a column ------------------------------------------------------------
         const int half = warp >> 2, in_tile = threadIdx.x & 127, column = u.column0 + 128 * half + in_tile, row = column / p.group;
         int32_t lo, hi;
@@ -278,7 +324,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
         uint32_t nan_blocks = 0;
         if (half < tiles_of_columns) {
             for (int j = 0; ok && j < tiles; ++j) {
-                ok = __all_sync(0xffffffffu, mbar_wait_bounded(&sh.bars[BAR_S_FULL + half], j & 1));
+                ok = __all_sync(0xffffffffu, wait_bounded(&sh.bars[BAR_S_FULL + half], j & 1));
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 const TileInfo info = sh.info[j % kInfos];
@@ -300,30 +346,29 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
                     for (int t = 0; t < kTokens; ++t)
                         if (seen[t >> 5] >> (t & 31) & 1) nan_blocks |= sh.nans[j % kInfos][t];
                 }
-                float m = -INFINITY;
-                uint32_t r[32];
+                uint32_t r[kTokens];
+                tmem_load128(s_at, r);
+                if (!all) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    tmem_load32(s_at + 32 * c, r);
-                    if (all) {
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) m = fmaxf(m, __uint_as_float(r[i]));
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) m = fmaxf(m, seen[c] >> i & 1 ? __uint_as_float(r[i]) : -INFINITY);
-                    }
+                    for (int i = 0; i < kTokens; ++i) r[i] = seen[i >> 5] >> (i & 31) & 1 ? r[i] : 0xff800000u;
                 }
+                float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int i = 0; i < kTokens; ++i) tops[i & 3] = fmaxf(tops[i & 3], __uint_as_float(r[i]));
+                float m = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
                 m = m == -INFINITY ? m : m * f;
                 // whole warps: the accumulators are read and written by warps
                 if (__any_sync(0xffffffffu, m > top + kRise || exponent != info.value_exponent)) {
                     const float new_top = fmaxf(m, top), by = exp2f(top - new_top), by_o = by * exp2f((float)(exponent - info.value_exponent));
                     if (j > 0) {
 #pragma unroll
-                        for (int c = 0; c < B; ++c) {
-                            tmem_load32(o_at + 32 * c, r);
+                        for (int c = 0; c < 2 * B; ++c) {
+                            float o[16];
+                            tmem_ld16(o_at + 16 * c, o);
+                            uint32_t x[16];
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * by_o);
-                            tmem_store32(o_at + 32 * c, r);
+                            for (int i = 0; i < 16; ++i) x[i] = __float_as_uint(o[i] * by_o);
+                            tmem_store16(o_at + 16 * c, x);
                         }
                     }
 #pragma unroll
@@ -331,17 +376,18 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
                     top = new_top;
                     exponent = info.value_exponent;
                 }
-                const float minus = kHeadroom - top;
+                const float plus = kHeadroom - top;
+                const bool masked = !all && f == 0.0f;  // 0 times minus infinity
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    tmem_load32(s_at + 32 * c, r);
-                    uint32_t w[16];
+                for (int c = 0; c < 8; ++c) {
+                    uint32_t w[8];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        float x = fmaf(__uint_as_float(r[2 * i]), f, minus), y = fmaf(__uint_as_float(r[2 * i + 1]), f, minus);
-                        if (!all) {
-                            x = seen[c] >> (2 * i) & 1 ? x : -INFINITY;
-                            y = seen[c] >> (2 * i + 1) & 1 ? y : -INFINITY;
+                    for (int i = 0; i < 8; ++i) {
+                        const int t = 16 * c + 2 * i;
+                        float x = fmaf(__uint_as_float(r[t]), f, plus), y = fmaf(__uint_as_float(r[t + 1]), f, plus);
+                        if (masked) {
+                            x = r[t] == 0xff800000u ? -INFINITY : x;
+                            y = r[t + 1] == 0xff800000u ? -INFINITY : y;
                         }
                         x = exp2_fast(x);
                         y = exp2_fast(y);
@@ -349,13 +395,13 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
                         weight[2 * (i & 1) + 1] += y;
                         w[i] = pack_half2(x, y);
                     }
-                    tmem_store16(s_at + 16 * c, w);  // columns that have been read
+                    tmem_store8(s_at + 8 * c, w);
                 }
                 asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                 asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                 mbar_arrive(&sh.bars[BAR_P_FULL + half]);
             }
-            if (ok && tiles > 0) ok = __all_sync(0xffffffffu, mbar_wait_bounded(&sh.bars[BAR_DONE], 0));
+            if (ok && tiles > 0) ok = __all_sync(0xffffffffu, wait_bounded(&sh.bars[BAR_DONE], 0));
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             if (ok) {
                 const float total = (weight[0] + weight[1]) + (weight[2] + weight[3]);
@@ -394,6 +440,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
             }
         }
     } else if (warp < kIssuerWarp) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kProducerRegisters));
         // ---- keys and values: from 4 bits to f16 operands ------------------------------------------------
         const int thread = threadIdx.x - 32 * kSoftmaxWarps, producer = warp - kSoftmaxWarps;
         const int32_t *const table = p.page_table + (int64_t)u.seq * p.table_pages;
@@ -445,7 +492,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
             if (any_nan) sh.nans[j % kInfos][thread] = (uint8_t)nan;
             if (thread == 0) sh.info[j % kInfos] = TileInfo{__uint_as_float((uint32_t)(127 + key_exponent) << 23), ve, raw.valid, any_nan};
             producers_sync();
-            if (j >= 2) ok = mbar_wait_bounded(&sh.bars[BAR_K_EMPTY + stage], (j >> 1 & 1) ^ 1);
+            if (j >= 2) ok = wait_bounded(&sh.bars[BAR_K_EMPTY + stage], (j >> 1 & 1) ^ 1);
             constexpr uint32_t kEven = 0x003c003cu, kOdd = 0x03c003c0u;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -461,7 +508,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             mbar_arrive(&sh.bars[BAR_K_FULL + stage]);
-            if (j >= 2) ok = mbar_wait_bounded(&sh.bars[BAR_V_EMPTY + stage], (j >> 1 & 1) ^ 1) && ok;
+            if (j >= 2) ok = wait_bounded(&sh.bars[BAR_V_EMPTY + stage], (j >> 1 & 1) ^ 1) && ok;
             {
                 const int eighth = thread & 7, group = thread >> 3;  // eight tokens
                 uint8_t *const to = v_smem + stage * TILE_BYTES + group * 128 + eighth * 16;
@@ -487,7 +534,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
             mbar_arrive(&sh.bars[BAR_V_FULL + stage]);
             raw = next;
         }
-    } else if (lane == 0 && tiles > 0) {
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kIssuerRegisters));
+    }
+    if (warp == kIssuerWarp && lane == 0 && tiles > 0) {
         // ---- the products ---------------------------------------------------------------------------------
         constexpr uint32_t kCommon = 1u << 4 | (uint32_t)(128 >> 4) << 24;  // fp32 sums of f16 products, both operands along k, 128 rows
         const uint32_t idesc_s = kCommon | (uint32_t)(kTokens >> 3) << 17, idesc_o = kCommon | (uint32_t)(32 * B >> 3) << 17;
@@ -502,7 +552,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
             for (int k = 0; k < kTokens / 16; ++k)
                 mma_tmem(tmem + 256 + 128 * half, tmem + 128 * half + 8 * k, operand(v_at + stage * TILE_BYTES + k * 256, ROWS8_V), idesc_o, add || k > 0);
         };
-        ok = mbar_wait_bounded(&sh.bars[BAR_Q], 0) && mbar_wait_bounded(&sh.bars[BAR_K_FULL], 0);
+        ok = wait_bounded(&sh.bars[BAR_Q], 0) && wait_bounded(&sh.bars[BAR_K_FULL], 0);
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         if (ok) {
             for (int half = 0; half < tiles_of_columns; ++half) {
@@ -513,10 +563,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
         }
         for (int j = 0; ok && j < tiles; ++j) {
             const int stage = j & 1, next = stage ^ 1;
-            ok = mbar_wait_bounded(&sh.bars[BAR_V_FULL + stage], j >> 1 & 1);
-            if (ok && j + 1 < tiles) ok = mbar_wait_bounded(&sh.bars[BAR_K_FULL + next], (j + 1) >> 1 & 1);
+            ok = wait_bounded(&sh.bars[BAR_V_FULL + stage], j >> 1 & 1);
+            if (ok && j + 1 < tiles) ok = wait_bounded(&sh.bars[BAR_K_FULL + next], (j + 1) >> 1 & 1);
             for (int half = 0; ok && half < tiles_of_columns; ++half) {
-                ok = mbar_wait_bounded(&sh.bars[BAR_P_FULL + half], j & 1);
+                ok = wait_bounded(&sh.bars[BAR_P_FULL + half], j & 1);
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 sums(half, stage, j > 0);
@@ -531,7 +581,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
         }
         // whatever happened: nothing is in flight when the tensor memory goes
         mma_commit(&sh.bars[BAR_DONE]);
-        if (!mbar_wait_bounded(&sh.bars[BAR_DONE], 0)) ok = false;
+        if (!wait_bounded(&sh.bars[BAR_DONE], 0)) ok = false;
     }
     if (!ok) {
         *report.device_word = 1;
