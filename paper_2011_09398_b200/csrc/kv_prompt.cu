@@ -18,6 +18,8 @@
 #include "kv_attention.cuh"
 #include "mx_common.cuh"
 
+#include <type_traits>
+
 namespace lce {
 namespace {
 
@@ -153,6 +155,7 @@ __device__ __forceinline__ void load_planes(const uint32_t *base, int place, uin
 }
 
 __device__ __forceinline__ uint32_t half2_bits(__half2 v) { return *reinterpret_cast<const uint32_t *>(&v); }
+__device__ __forceinline__ __half2 as_half2(uint32_t v) { return *reinterpret_cast<const __half2 *>(&v); }
 __device__ __forceinline__ uint32_t decode(uint32_t bits, __half2 by, __half2 plus)
 {
     return half2_bits(__hfma2(*reinterpret_cast<const __half2 *>(&bits), by, plus));
@@ -194,19 +197,21 @@ struct Raw {
     uint32_t valid;
 };
 
+// The page that lane l's tile of the cache, the l-th of eight, lies on; negative behind the sequence.  Only loaded here: what is done with
+// it comes a tile later.
+__device__ __forceinline__ int32_t find_page(const AttnParams &p, const int32_t *table, int length, int tile, int lane)
+{
+    const int32_t t = tile * 8 + lane;
+    if (lane >= 8 || t >= (length + kKvTile - 1) / kKvTile) return -1;
+    return __ldg(table + t / (p.g.page_size / kKvTile));
+}
+
 template <int B>
-__device__ __forceinline__ void load_raw(const AttnParams &p, const int32_t *table, int head, int length, int tile, int thread, Raw<B> &r)
+__device__ __forceinline__ void load_raw(const AttnParams &p, int32_t page, int head, int length, int tile, int thread, Raw<B> &r)
 {
     constexpr int TILE = kv_tile_words(B);
     const int lane = thread & 31, warp = thread >> 5, tiles_per_page = p.g.page_size / kKvTile;
-    int32_t place = -1;
-    if (lane < 8) {
-        const int32_t t = tile * 8 + lane;
-        if (t * kKvTile < length) {
-            const int32_t in_table = t / tiles_per_page, page = __ldg(table + in_table);
-            if (page >= 0 && page < p.g.pages) place = (page * p.g.heads + head) * tiles_per_page + (t - in_table * tiles_per_page);
-        }
-    }
+    const int32_t place = page >= 0 && page < p.g.pages ? (page * p.g.heads + head) * tiles_per_page + (tile * 8 + lane) % tiles_per_page : -1;
     r.valid = __ballot_sync(0xffffffffu, place >= 0);
     const auto tile_at = [&](int t) -> const uint32_t * {
         const int32_t at = __shfl_sync(0xffffffffu, place, t);
@@ -289,29 +294,41 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
         float factor;
         {
             const int64_t at = (u.row0 + row) * p.q_token + ((int64_t)head * p.group + (column - row * p.group)) * p.q_head;
-            uint32_t magnitude = 0;
-            float v[8];
-#pragma unroll
-            for (int c = 0; c < 4 * B; ++c) {
-                load_row<false>(p, at + 8 * c, row < u.rows ? p.g.dim - 8 * c : 0, v);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) magnitude = max(magnitude, __float_as_uint(v[i]) & 0x7fffffffu);
-            }
-            const bool finite = magnitude < 0x7f800000u;
-            // times 2^k, so that the largest is in [2^14, 2^15); a scale below zero changes q's sign
-            const int e = finite && magnitude > 0 ? ilogbf(__uint_as_float(magnitude)) : 0, k = 14 - e, k1 = k / 2, k2 = k - k1;
-            const float s1 = __uint_as_float((uint32_t)(127 + k1) << 23) * (p.scale < 0.0f ? -1.0f : 1.0f), s2 = __uint_as_float((uint32_t)(127 + k2) << 23);
+            int k = 0;
+            bool finite = true;
             uint8_t *const to = q_smem + half * TILE_BYTES + (in_tile >> 3) * ROWS8_QK + (in_tile & 7) * 16;
+            const auto take_row = [&](auto element, auto vectors) {
+                using T = decltype(element);
+                Eight<T> e[4 * B];  // the whole row at once
 #pragma unroll
-            for (int c = 0; c < 4 * B; ++c) {
-                load_row<false>(p, at + 8 * c, row < u.rows ? p.g.dim - 8 * c : 0, v);  // again, from the L1
-                uint4 w;
-                // in the order in which a word's codes are decoded
-                w.x = pack_half2(v[0] * s1 * s2, v[4] * s1 * s2);
-                w.y = pack_half2(v[1] * s1 * s2, v[5] * s1 * s2);
-                w.z = pack_half2(v[2] * s1 * s2, v[6] * s1 * s2);
-                w.w = pack_half2(v[3] * s1 * s2, v[7] * s1 * s2);
-                *reinterpret_cast<uint4 *>(to + c * 128) = w;
+                for (int c = 0; c < 4 * B; ++c) e[c] = load_eight<T, decltype(vectors)::value>(static_cast<const T *>(p.q) + at + 8 * c, row < u.rows ? p.g.dim - 8 * c : 0);
+                uint32_t magnitude = 0;  // magnitudes compare like integers, infinity and NaN above all others
+                float v[8];
+#pragma unroll
+                for (int c = 0; c < 4 * B; ++c) {
+                    e[c].expand(v);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) magnitude = max(magnitude, __float_as_uint(v[i]) & 0x7fffffffu);
+                }
+                finite = magnitude < 0x7f800000u;
+                // times 2^k, so that the largest is in [2^14, 2^15); a scale below zero changes q's sign
+                k = 14 - (finite && magnitude > 0 ? ilogbf(__uint_as_float(magnitude)) : 0);
+                const int k1 = k / 2, k2 = k - k1;
+                const float s1 = __uint_as_float((uint32_t)(127 + k1) << 23) * (p.scale < 0.0f ? -1.0f : 1.0f), s2 = __uint_as_float((uint32_t)(127 + k2) << 23);
+#pragma unroll
+                for (int c = 0; c < 4 * B; ++c) {
+                    e[c].expand(v);
+                    // in the order in which a word's codes are decoded
+                    *reinterpret_cast<uint4 *>(to + c * 128) = make_uint4(pack_half2(v[0] * s1 * s2, v[4] * s1 * s2), pack_half2(v[1] * s1 * s2, v[5] * s1 * s2),
+                                                                          pack_half2(v[2] * s1 * s2, v[6] * s1 * s2), pack_half2(v[3] * s1 * s2, v[7] * s1 * s2));
+                }
+            };
+            if (p.type == LCE_TYPE_FLOAT16) {
+                if (p.q_vectors) take_row(__half(), std::true_type());
+                else take_row(__half(), std::false_type());
+            } else {
+                if (p.q_vectors) take_row(__nv_bfloat16(), std::true_type());
+                else take_row(__nv_bfloat16(), std::false_type());
             }
             const int kc = 8 - k, c1 = kc / 2, c2 = kc - c1;
             factor = (finite ? fabsf(p.scale) : __uint_as_float(0x7fc00000u)) * __uint_as_float((uint32_t)(127 + c1) << 23) * __uint_as_float((uint32_t)(127 + c2) << 23);
@@ -444,12 +461,18 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
         // ---- keys and values: from 4 bits to f16 operands ------------------------------------------------
         const int thread = threadIdx.x - 32 * kSoftmaxWarps, producer = warp - kSoftmaxWarps;
         const int32_t *const table = p.page_table + (int64_t)u.seq * p.table_pages;
-        Raw<B> raw, next;
-        if (tiles > 0) load_raw<B>(p, table, head, u.length, tile0, thread, raw);
+        Raw<B> even_raw, odd_raw;
+        int32_t page = -1;  // two tiles ahead; words one
+        if (tiles > 0) {
+            load_raw<B>(p, find_page(p, table, u.length, tile0, lane), head, u.length, tile0, thread, even_raw);
+            page = find_page(p, table, u.length, tile0 + 1, lane);
+        }
         int32_t value_exponent = -1000;
         const __half2 sixteenth = __float2half2_rn(0.0625f), eight = __float2half2_rn(-0x1p-19f);
-        for (int j = 0; j < tiles; ++j) {
-            if (j + 1 < tiles) load_raw<B>(p, table, head, u.length, tile0 + j + 1, thread, next);
+        // One tile; false where a wait gave up.
+        const auto produce = [&](int j, const Raw<B> &raw, Raw<B> &next) -> bool {
+            if (j + 1 < tiles) load_raw<B>(p, page, head, u.length, tile0 + j + 1, thread, next);
+            page = find_page(p, table, u.length, tile0 + j + 2, lane);
             const int stage = j & 1, turn = j & 1;
             // the largest scales of the tile (bits of bf16 numbers compare like integers; a NaN does not count)
             uint32_t nan = 0, top_k = 0, top_v = 0;
@@ -468,7 +491,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
                 sh.largest[turn][1][producer] = top_v | (some_nan ? 1u : 0u);
             }
             ok = producers_sync_and(ok);
-            if (!ok) break;
+            if (!ok) return false;
             top_k = top_v = 0;
             uint32_t any_nan = 0;
 #pragma unroll
@@ -498,9 +521,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
             for (int i = 0; i < 4; ++i) {
                 const int unit = i * 4 + producer, token = unit * 8 + (lane & 7), quarter = lane >> 3;
                 uint8_t *const to = k_smem + stage * TILE_BYTES + unit * ROWS8_QK + quarter * 128 + (lane & 7) * 16;
+                const uint2 scales = *reinterpret_cast<const uint2 *>(sh.key_scales[turn][token]);
 #pragma unroll
                 for (int b = 0; b < B; ++b) {
-                    const __half2 even = __half2half2(sh.key_scales[turn][token][b]), odd = __hmul2(even, sixteenth), plus = __hmul2(even, eight);
+                    const __half2 even = as_half2(__byte_perm(b & 2 ? scales.y : scales.x, 0, b & 1 ? 0x3232 : 0x1010)), odd = __hmul2(even, sixteenth), plus = __hmul2(even, eight);
                     const uint32_t x = raw.keys[i][b], y = swap_bytes(x);
                     *reinterpret_cast<uint4 *>(to + b * 512) =
                         make_uint4(decode(x & kEven, even, plus), decode(x & kOdd, odd, plus), decode(y & kEven, even, plus), decode(y & kOdd, odd, plus));
@@ -512,12 +536,15 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
             {
                 const int eighth = thread & 7, group = thread >> 3;  // eight tokens
                 uint8_t *const to = v_smem + stage * TILE_BYTES + group * 128 + eighth * 16;
+                uint4 scales[4];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) scales[t] = *reinterpret_cast<const uint4 *>(sh.value_scales[turn][group * 4 + t]);
 #pragma unroll
                 for (int b = 0; b < B; ++b) {
                     uint32_t w[4][4];  // [channel][pair of tokens]
 #pragma unroll
                     for (int t = 0; t < 4; ++t) {
-                        const __half2 even = *reinterpret_cast<const __half2 *>(sh.value_scales[turn][group * 4 + t][b]), odd = __hmul2(even, sixteenth),
+                        const __half2 even = as_half2(b == 0 ? scales[t].x : b == 1 ? scales[t].y : b == 2 ? scales[t].z : scales[t].w), odd = __hmul2(even, sixteenth),
                                       plus = __hmul2(even, eight);
                         const uint32_t x = raw.values[t][b], y = swap_bytes(x);
                         w[0][t] = decode(x & kEven, even, plus);
@@ -532,7 +559,11 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             mbar_arrive(&sh.bars[BAR_V_FULL + stage]);
-            raw = next;
+            return true;
+        };
+        for (int j = 0; j < tiles; j += 2) {
+            if (!produce(j, even_raw, odd_raw)) break;
+            if (j + 1 < tiles && !produce(j + 1, odd_raw, even_raw)) break;
         }
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kIssuerRegisters));
