@@ -34,7 +34,8 @@ constexpr float kHeadroom = 7.0f;               // weights are held times 2^7: 2
 constexpr int kInfos = 4;                       // the producers are less than three tiles ahead of the softmax
 
 enum { BAR_Q = 0, BAR_K_FULL, BAR_V_FULL = BAR_K_FULL + 2, BAR_K_EMPTY = BAR_V_FULL + 2, BAR_V_EMPTY = BAR_K_EMPTY + 2, BAR_S_FULL = BAR_V_EMPTY + 2,
-       BAR_P_FULL = BAR_S_FULL + 2, BAR_DONE = BAR_P_FULL + 2, BAR_COUNT };
+       BAR_P_FULL = BAR_S_FULL + 2,
+       BAR_P_REST = BAR_P_FULL + 2, BAR_DONE = BAR_P_REST + 2, BAR_COUNT };
 
 // What the softmax has to know of a tile.
 struct TileInfo {
@@ -136,6 +137,33 @@ __device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t (&r)[16
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]),
         "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(at)
         : "memory");
+}
+
+// Two fp32 numbers in one operation
+__device__ __forceinline__ uint64_t pair_of(float x, float y)
+{
+    uint64_t v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(x), "f"(y));
+    return v;
+}
+__device__ __forceinline__ void of_pair(uint64_t v, float &x, float &y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t v;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(a), "l"(b), "l"(c));
+    return v;
+}
+__device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b)
+{
+    uint64_t v;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+    return v;
+}
+__device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b)
+{
+    uint64_t v;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+    return v;
 }
 
 // The B words of a place (a lane's of ROWS = 64 places, a token's of 16), plane by plane.
@@ -271,6 +299,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
             mbar_init(&sh.bars[BAR_V_EMPTY + i], 1);
             mbar_init(&sh.bars[BAR_S_FULL + i], 1);
             mbar_init(&sh.bars[BAR_P_FULL + i], 128);
+            mbar_init(&sh.bars[BAR_P_REST + i], 128);
         }
         mbar_init(&sh.bars[BAR_DONE], 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -336,7 +365,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
             mbar_arrive(&sh.bars[BAR_Q]);
         }
         const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16, s_at = tmem + lanes + 128 * half, o_at = tmem + lanes + 256 + 128 * half;
-        float top = kLowest, weight[4] = {};
+        float top = kLowest;
+        uint64_t weight[2] = {};  // pairs of fp32 sums
         int32_t exponent = 0;
         uint32_t nan_blocks = 0;
         if (half < tiles_of_columns) {
@@ -388,40 +418,46 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
                             tmem_store16(o_at + 16 * c, x);
                         }
                     }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) weight[i] *= by;
+                    weight[0] = mul_pair(weight[0], pair_of(by, by));
+                    weight[1] = mul_pair(weight[1], pair_of(by, by));
                     top = new_top;
                     exponent = info.value_exponent;
                 }
-                const float plus = kHeadroom - top;
+                const uint64_t f2 = pair_of(f, f), plus = pair_of(kHeadroom - top, kHeadroom - top);
                 const bool masked = !all && f == 0.0f;  // 0 times minus infinity
+                // the first half of the weights is worked on while the second is made
 #pragma unroll
                 for (int c = 0; c < 8; ++c) {
                     uint32_t w[8];
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const int t = 16 * c + 2 * i;
-                        float x = fmaf(__uint_as_float(r[t]), f, plus), y = fmaf(__uint_as_float(r[t + 1]), f, plus);
+                        float x, y;
+                        of_pair(fma_pair(pair_of(__uint_as_float(r[t]), __uint_as_float(r[t + 1])), f2, plus), x, y);
                         if (masked) {
                             x = r[t] == 0xff800000u ? -INFINITY : x;
                             y = r[t + 1] == 0xff800000u ? -INFINITY : y;
                         }
                         x = exp2_fast(x);
                         y = exp2_fast(y);
-                        weight[2 * (i & 1)] += x;
-                        weight[2 * (i & 1) + 1] += y;
+                        weight[i & 1] = add_pair(weight[i & 1], pair_of(x, y));
                         w[i] = pack_half2(x, y);
                     }
                     tmem_store8(s_at + 8 * c, w);
+                    if (c == 3 || c == 7) {
+                        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                        mbar_arrive(&sh.bars[(c == 3 ? BAR_P_FULL : BAR_P_REST) + half]);
+                    }
                 }
-                asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-                asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                mbar_arrive(&sh.bars[BAR_P_FULL + half]);
             }
             if (ok && tiles > 0) ok = __all_sync(0xffffffffu, wait_bounded(&sh.bars[BAR_DONE], 0));
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             if (ok) {
-                const float total = (weight[0] + weight[1]) + (weight[2] + weight[3]);
+                float w0, w1, w2, w3;
+                of_pair(weight[0], w0, w1);
+                of_pair(weight[1], w2, w3);
+                const float total = (w0 + w1) + (w2 + w3);
                 const float by = (total == 0.0f ? 0.0f : 1.0f / total), unit = exp2f((float)(exponent + 8));
                 const int64_t at = (u.row0 + row) * p.out_token + ((int64_t)head * p.group + (column - row * p.group)) * p.out_head;
 #pragma unroll
@@ -578,9 +614,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
             for (int k = 0; k < 2 * B; ++k)
                 mma_shared(tmem + 128 * half, operand(q_at + half * TILE_BYTES + k * 256, ROWS8_QK), operand(k_at + stage * TILE_BYTES + k * 256, ROWS8_QK), idesc_s, k > 0);
         };
-        const auto sums = [&](int half, int stage, bool add) {
+        const auto sums = [&](int half, int stage, int part, bool add) {
 #pragma unroll
-            for (int k = 0; k < kTokens / 16; ++k)
+            for (int k = 4 * part; k < 4 * part + 4; ++k)
                 mma_tmem(tmem + 256 + 128 * half, tmem + 128 * half + 8 * k, operand(v_at + stage * TILE_BYTES + k * 256, ROWS8_V), idesc_o, add || k > 0);
         };
         ok = wait_bounded(&sh.bars[BAR_Q], 0) && wait_bounded(&sh.bars[BAR_K_FULL], 0);
@@ -600,7 +636,11 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
                 ok = wait_bounded(&sh.bars[BAR_P_FULL + half], j & 1);
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                sums(half, stage, j > 0);
+                sums(half, stage, 0, j > 0);
+                ok = wait_bounded(&sh.bars[BAR_P_REST + half], j & 1);
+                if (!ok) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                sums(half, stage, 1, true);
                 if (j + 1 < tiles) {  // in order behind the sums, which read the weights in its place
                     scores(half, next);
                     mma_commit(&sh.bars[BAR_S_FULL + half]);
