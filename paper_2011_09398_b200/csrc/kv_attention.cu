@@ -20,6 +20,8 @@
 
 #include <math.h>
 
+#include <algorithm>
+
 namespace lce {
 namespace {
 
@@ -28,12 +30,6 @@ constexpr int kStages = 4;                // tiles in flight of a warp
 constexpr float kRise = 4.0f;             // a running maximum is raised when a score passes it by 2^4
 constexpr float kHeadroom = 10.0f;        // weights are held times 2^10: 2^(10 + 4 + 1) is the most that meets f16
 
-__device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t mask, uint32_t with)
-{
-    uint32_t d;
-    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(a), "r"(mask), "r"(with));
-    return d;
-}
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t v)
 {
     uint32_t d;
@@ -119,10 +115,6 @@ __host__ __device__ constexpr int blocks_per_sm(int blocks, int nt, bool split)
 {
     return blocks * nt <= (split ? 3 : 4) ? 4 : blocks * nt <= (split ? 4 : 6) ? 3 : 2;
 }
-
-// Lets the join, which this call launches behind, take its place while this kernel runs.  It waits for all of it, and nothing
-// that a caller launches can start before the join is done.
-__device__ __forceinline__ void release_join() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // B blocks of 32 channels, NT tiles of 8 columns, SPLIT: fp32 rows.
 template <int B, int NT, bool SPLIT>
@@ -716,7 +708,7 @@ lce_status launch_blocks(const AttnParams &p, cudaStream_t s)
     }
 }
 
-constexpr int kPromptLeast = 64;  // columns of a sequence, on average, from which the kernel for prompts is taken
+constexpr int kPromptLeastTiles = 6;  // tiles of 128 tokens that a piece is worth there
 constexpr int kLeastTiles = 16;  // tiles of a warp that a piece is worth
 
 // one_row: without q_starts
@@ -739,10 +731,24 @@ lce_status make_params(const lce_kv_attention_desc *d, bool one_row, AttnParams 
     p->q_token = d->q_token_stride; p->q_head = d->q_head_stride; p->out_token = d->out_token_stride; p->out_head = d->out_head_stride;
     p->scale = d->scale * 1.44269504088896341f;
     *nt = p->g.blocks <= kWideBlocks && (d->tokens * p->group + d->batch - 1) / d->batch > 8 ? 2 : 1;
-    p->prompt = p->g.blocks <= 4 && d->type != LCE_TYPE_FLOAT32 && d->tokens * p->group >= (int64_t)kPromptLeast * d->batch;
+    // Many rows go to the kernel for prompts where it is estimated to be ahead (us for 128 channels, bf16; the two take what they were
+    // measured to take: 16 columns of a head of one kernel 8.6e-5 a token, 256 of the other 1.4e-4, and 12 more to begin and end).
+    // By the longest the sequences can be: their lengths are not known here.  One sequence of 512 / 4096 / 32768 tokens, 8 key heads of
+    // 4: 16 rows 12.5 / 26.9 / 105 us here, 22.8 / 34.0 / 80.8 there, 64 rows 15.2 / 60.2 / 312 and 26.9 / 39.9 / 83.8; 16 sequences
+    // of 512 / 4096, 8 rows each 17.3 / 107 and 25.5 / 99.0, 16 rows 31.8 / 189 and 25.9 / 102.
+    const int64_t each = (p->tokens * p->group + p->batch - 1) / p->batch;  // columns of a sequence, on average
+    const auto of_columns = [&](int64_t columns) { return (double)((each + columns - 1) / columns * p->batch * p->g.heads); };
+    p->prompt = p->g.blocks <= 4 && d->type != LCE_TYPE_FLOAT32 && (of_columns(16) * 8.6e-5 - of_columns(kPromptColumns) * 1.4e-4) * p->table_tokens > 12.0;
     if (p->prompt) {
-        p->units = p->column_tiles = (int32_t)(p->tokens * p->group / kPromptColumns + p->batch);
-        p->cluster = p->target = p->least_tiles = 1;
+        // a block to an SM; sequences are cut into pieces where that leaves SMs without one (joining costs a few us)
+        const int64_t tiles = p->tokens * p->group / kPromptColumns + p->batch, likely = p->batch * ((each + kPromptColumns - 1) / kPromptColumns);
+        p->cluster = 1;
+        p->least_tiles = 8 * kPromptLeastTiles;
+        p->join = likely * p->g.heads * 5 < 148 * 4 && p->table_tokens > 128 * kPromptLeastTiles;
+        const int64_t target = p->join ? std::max<int64_t>(148 / p->g.heads - likely, 1) : 0;
+        p->target = (int32_t)std::max<int64_t>(target, 1);
+        p->column_tiles = (int32_t)tiles;
+        p->units = (int32_t)(tiles + target);
         return LCE_OK;
     }
     const int columns = 8 * *nt;
@@ -765,7 +771,12 @@ lce_status make_params(const lce_kv_attention_desc *d, bool one_row, AttnParams 
     return LCE_OK;
 }
 
-size_t workspace_bytes(const AttnParams &p, int nt) { return !p.join ? 16 : (size_t)p.units * p.g.heads * 8 * nt * (32 * p.g.blocks + 4) * 4; }
+size_t workspace_bytes(const AttnParams &p, int nt)
+{
+    if (!p.join) return 16;
+    if (p.prompt) return (size_t)p.units * p.g.heads * kPromptColumns * (32 * p.g.blocks + 4) * 4;
+    return (size_t)p.units * p.g.heads * 8 * nt * (32 * p.g.blocks + 4) * 4;
+}
 
 }  // namespace
 }  // namespace lce

@@ -32,6 +32,7 @@ struct Unit {
     int32_t length, rows;                             // tokens of the sequence, its rows of q
     int64_t row0;                                     // its first row of q
     int32_t tile0, tile1;                             // the unit's tiles
+    bool first, last;                                 // piece of its column tile
 };
 
 struct Sequence {
@@ -112,6 +113,8 @@ __device__ __forceinline__ bool find_unit(const AttnParams &p, int at, Unit *u, 
             const int32_t each = tiles / u->chunks, more = tiles - each * u->chunks;
             u->tile0 = first_tile + chunk * each + min(chunk, more);
             u->tile1 = u->tile0 + each + (chunk < more ? 1 : 0);
+            u->first = chunk == 0;
+            u->last = chunk == u->chunks - 1;
             return true;
         }
         before += __shfl_sync(0xffffffffu, upto, 31);
@@ -173,8 +176,19 @@ __device__ __forceinline__ float exp2_fast(float x)
     return d;
 }
 
+// a & mask | with
+__device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t mask, uint32_t with)
+{
+    uint32_t d;
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(a), "r"(mask), "r"(with));
+    return d;
+}
 // Bytes exchanged in either half.
 __device__ __forceinline__ uint32_t swap_bytes(uint32_t w) { return __byte_perm(w, 0, 0x2301); }
+// Lets the join, which this call launches behind, take its place while this kernel runs.  It waits for all of it, and nothing
+// that a caller launches can start before the join is done.
+__device__ __forceinline__ void release_join() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // Prompts: kv_prompt.cu.  16-bit rows of up to 128 channels; `units` column tiles of kPromptColumns.
 constexpr int kPromptColumns = 256;
 lce_status launch_kv_prompt(const AttnParams &p, cudaStream_t s);

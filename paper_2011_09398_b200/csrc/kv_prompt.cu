@@ -10,8 +10,9 @@
 // f16 holds a code times its scale exactly, 3 and 8 bits, so keys and values lose nothing as long as they fit its exponents.  They are
 // taken relative to a power of two: for the keys above the tile's largest scale, which goes back into the scores; for the values
 // above the largest so far, and when that grows O is scaled down, as it is when a row's running maximum grows by more than 2^8 (rare).
-// A code is decoded by one packed multiply-add from the subnormal number that its bits are: (n 2^-22) (s 2^22) - 8 s, five instructions
-// for two of four codes with the AND.
+// Exact are then all whose scale is not below 2^-28 of that, whether a row sees the largest one or not.  Two codes take an AND-OR
+// (1024 + n), a packed multiply-add (n - 8) and a packed product with the scale.  (One multiply-add from the subnormal numbers that
+// their bits are would do, but its results reach down to 2^-10 of the largest only.)
 //
 // Per 128 tokens and 256 columns of 128 channels: four products of 512 clocks, 32768 exponentials at 16 a clock, 2048 clocks each, and
 // 8000 instructions, 2000 clocks.
@@ -49,7 +50,7 @@ struct Shared {
     uint64_t bars[BAR_COUNT];
     uint32_t tmem, largest[2][2][kProducerWarps];     // [turn][keys, values]
     TileInfo info[kInfos];
-    alignas(16) __half key_scales[2][kTokens][4];     // relative to the tile's, times 2^15; [turn]
+    alignas(16) __half key_scales[2][kTokens][4];     // relative to the tile's largest; [turn]
     alignas(16) __half value_scales[2][kTokens / 2][4][2];
     uint8_t nans[kInfos][kTokens];                    // blocks of a token's value that are NaN
 };
@@ -184,12 +185,19 @@ __device__ __forceinline__ void load_planes(const uint32_t *base, int place, uin
 
 __device__ __forceinline__ uint32_t half2_bits(__half2 v) { return *reinterpret_cast<const uint32_t *>(&v); }
 __device__ __forceinline__ __half2 as_half2(uint32_t v) { return *reinterpret_cast<const __half2 *>(&v); }
-__device__ __forceinline__ uint32_t decode(uint32_t bits, __half2 by, __half2 plus)
+// c s of the eight codes of a word, pair by pair: codes 0 and 4 (of the low and the high half), 1 and 5, 2 and 6, 3 and 7.
+__device__ __forceinline__ uint4 decode(uint32_t word, __half2 scale)
 {
-    return half2_bits(__hfma2(*reinterpret_cast<const __half2 *>(&bits), by, plus));
+    constexpr uint32_t kEven = 0x003c003cu, kOdd = 0x03c003c0u, kBase = 0x64006400u;
+    const __half2 quarter = as_half2(0x34003400u), less264 = as_half2(0xdc20dc20u), part64 = as_half2(0x24002400u), less24 = as_half2(0xce00ce00u);
+    const uint32_t other = swap_bytes(word);
+    return make_uint4(half2_bits(__hmul2(__hfma2(as_half2(and_or(word, kEven, kBase)), quarter, less264), scale)),
+                      half2_bits(__hmul2(__hfma2(as_half2(and_or(word, kOdd, kBase)), part64, less24), scale)),
+                      half2_bits(__hmul2(__hfma2(as_half2(and_or(other, kEven, kBase)), quarter, less264), scale)),
+                      half2_bits(__hmul2(__hfma2(as_half2(and_or(other, kOdd, kBase)), part64, less24), scale)));
 }
 
-__device__ __forceinline__ uint32_t r_low(uint32_t w) { return w << 16; }  // the key's scale, as fp32 bits
+__device__ __forceinline__ uint32_t key_scale(uint32_t word) { return word << 16; }  // as fp32 bits
 __device__ __forceinline__ void producers_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 // The same, and whether all of them are well: where one's wait gave up, all leave together.
 __device__ __forceinline__ bool producers_sync_and(bool ok)
@@ -280,14 +288,18 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
     asm volatile("griddepcontrol.wait;" ::: "memory");
     Unit u;
     int first_unit;
+    if (p.join) release_join();
     // the last column tiles see most tokens and come first
-    if (!find_unit<kPromptColumns, false>(p, p.units - 1 - (int)blockIdx.x, &u, &first_unit)) return;
+    const int unit = p.units - 1 - (int)blockIdx.x;
+    if (!find_unit<kPromptColumns, false>(p, unit, &u, &first_unit)) return;
     const int head = blockIdx.y;
     int32_t any_lo, any_hi, unused;
     const int columns = u.rows * p.group;
     column_range(p, u, u.column0, &any_lo, &unused);
     column_range(p, u, min(u.column0 + kPromptColumns, columns) - 1, &unused, &any_hi);
-    const int32_t tile0 = any_lo / kTokens, tiles = any_hi > any_lo ? (any_hi + kTokens - 1) / kTokens - tile0 : 0;
+    // pieces are cut in tiles of the cache: at whole tiles of this kernel, each piece's end where the next one begins
+    const int32_t tile0 = max(any_lo / kTokens, u.first ? 0 : u.tile0 * kKvTile / kTokens);
+    const int32_t tiles = any_hi > any_lo ? max(min((any_hi + kTokens - 1) / kTokens, u.last ? 0x7fffffff : u.tile1 * kKvTile / kTokens) - tile0, 0) : 0;
     const int tiles_of_columns = u.column0 + 128 < columns ? 2 : 1;
 
     if (threadIdx.x == 0) {
@@ -359,7 +371,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
                 if (p.q_vectors) take_row(__nv_bfloat16(), std::true_type());
                 else take_row(__nv_bfloat16(), std::false_type());
             }
-            const int kc = 8 - k, c1 = kc / 2, c2 = kc - c1;
+            const int kc = -11 - k, c1 = kc / 2, c2 = kc - c1;
             factor = (finite ? fabsf(p.scale) : __uint_as_float(0x7fc00000u)) * __uint_as_float((uint32_t)(127 + c1) << 23) * __uint_as_float((uint32_t)(127 + c2) << 23);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             mbar_arrive(&sh.bars[BAR_Q]);
@@ -458,7 +470,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
                 of_pair(weight[0], w0, w1);
                 of_pair(weight[1], w2, w3);
                 const float total = (w0 + w1) + (w2 + w3);
-                const float by = (total == 0.0f ? 0.0f : 1.0f / total), unit = exp2f((float)(exponent + 8));
+                const float by = (total == 0.0f ? 0.0f : 1.0f / total), scale_up = exp2f((float)(exponent - 11));
+                constexpr int D = 32 * B;
+                float *const part = p.parts + (((int64_t)unit * p.g.heads + head) * kPromptColumns + 128 * half + in_tile) * (D + 4);
+                if (u.chunks > 1) *reinterpret_cast<float2 *>(part + D) = make_float2(top, total);
                 const int64_t at = (u.row0 + row) * p.out_token + ((int64_t)head * p.group + (column - row * p.group)) * p.out_head;
 #pragma unroll
                 for (int b = 0; b < B; ++b) {
@@ -475,10 +490,15 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
                         float v[8];
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
-                            const float x = total == 0.0f ? 0.0f : __uint_as_float(r[(i & 3) * 8 + 2 * c + (i >> 2)]) * by * unit;
+                            const float x = total == 0.0f ? 0.0f : __uint_as_float(r[(i & 3) * 8 + 2 * c + (i >> 2)]) * scale_up * (u.chunks > 1 ? 1.0f : by);
                             v[i] = nan_blocks >> b & 1 ? __uint_as_float(0x7fc00000u) : x;
                         }
                         const int channel = 32 * b + 8 * c, count = row < u.rows ? p.g.dim - channel : 0;
+                        if (u.chunks > 1) {
+                            *reinterpret_cast<float4 *>(part + channel) = make_float4(v[0], v[1], v[2], v[3]);
+                            *reinterpret_cast<float4 *>(part + channel + 4) = make_float4(v[4], v[5], v[6], v[7]);
+                            continue;
+                        }
                         if (p.type == LCE_TYPE_FLOAT16) {
                             __half *const out = static_cast<__half *>(p.out) + at + channel;
                             if (p.out_vectors) store8<__half, true>(out, count, v);
@@ -504,7 +524,6 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
             page = find_page(p, table, u.length, tile0 + 1, lane);
         }
         int32_t value_exponent = -1000;
-        const __half2 sixteenth = __float2half2_rn(0.0625f), eight = __float2half2_rn(-0x1p-19f);
         // One tile; false where a wait gave up.
         const auto produce = [&](int j, const Raw<B> &raw, Raw<B> &next) -> bool {
             if (j + 1 < tiles) load_raw<B>(p, page, head, u.length, tile0 + j + 1, thread, next);
@@ -514,7 +533,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
             uint32_t nan = 0, top_k = 0, top_v = 0;
 #pragma unroll
             for (int b = 0; b < B; ++b) {
-                const uint32_t ks = r_low(raw.scales[b]), vs = raw.scales[b] & 0xffff0000u;
+                const uint32_t ks = key_scale(raw.scales[b]), vs = raw.scales[b] & 0xffff0000u;
                 if (ks < 0x7f800000u) top_k = max(top_k, ks);
                 if (vs < 0x7f800000u) top_v = max(top_v, vs);
                 else nan |= 1u << b;
@@ -540,19 +559,18 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
             const int here = max((int)(top_v >> 23) - 127, -100);
             if (top_v > 0 && here > value_exponent) value_exponent = here + 1;  // one more, so that it does not move often
             const int ve = max(value_exponent, -100);
-            // relative scales times 2^15: below 2^15, exact in f16 down to 2^-10 of the largest
-            const float k_by = __uint_as_float((uint32_t)(127 + 14 - key_exponent) << 23), v_by = __uint_as_float((uint32_t)(127 + 14 - ve) << 23);
+            // relative scales, below 2^12: 7 of them fit
+            const float k_by = __uint_as_float((uint32_t)(127 + 11 - key_exponent) << 23), v_by = __uint_as_float((uint32_t)(127 + 11 - ve) << 23);
 #pragma unroll
             for (int b = 0; b < B; ++b) {
                 const float vs = __uint_as_float(raw.scales[b] & 0xffff0000u);
-                sh.key_scales[turn][thread][b] = __float2half_rn(__uint_as_float(r_low(raw.scales[b])) * k_by);
+                sh.key_scales[turn][thread][b] = __float2half_rn(__uint_as_float(key_scale(raw.scales[b])) * k_by);
                 sh.value_scales[turn][thread >> 1][b][thread & 1] = __float2half_rn(nan >> b & 1 ? 0.0f : vs * v_by);
             }
             if (any_nan) sh.nans[j % kInfos][thread] = (uint8_t)nan;
             if (thread == 0) sh.info[j % kInfos] = TileInfo{__uint_as_float((uint32_t)(127 + key_exponent) << 23), ve, raw.valid, any_nan};
             producers_sync();
             if (j >= 2) ok = wait_bounded(&sh.bars[BAR_K_EMPTY + stage], (j >> 1 & 1) ^ 1);
-            constexpr uint32_t kEven = 0x003c003cu, kOdd = 0x03c003c0u;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int unit = i * 4 + producer, token = unit * 8 + (lane & 7), quarter = lane >> 3;
@@ -560,10 +578,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
                 const uint2 scales = *reinterpret_cast<const uint2 *>(sh.key_scales[turn][token]);
 #pragma unroll
                 for (int b = 0; b < B; ++b) {
-                    const __half2 even = as_half2(__byte_perm(b & 2 ? scales.y : scales.x, 0, b & 1 ? 0x3232 : 0x1010)), odd = __hmul2(even, sixteenth), plus = __hmul2(even, eight);
-                    const uint32_t x = raw.keys[i][b], y = swap_bytes(x);
-                    *reinterpret_cast<uint4 *>(to + b * 512) =
-                        make_uint4(decode(x & kEven, even, plus), decode(x & kOdd, odd, plus), decode(y & kEven, even, plus), decode(y & kOdd, odd, plus));
+                    const __half2 scale = as_half2(__byte_perm(b & 2 ? scales.y : scales.x, 0, b & 1 ? 0x3232 : 0x1010));
+                    *reinterpret_cast<uint4 *>(to + b * 512) = decode(raw.keys[i][b], scale);
                 }
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -577,20 +593,14 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
                 for (int t = 0; t < 4; ++t) scales[t] = *reinterpret_cast<const uint4 *>(sh.value_scales[turn][group * 4 + t]);
 #pragma unroll
                 for (int b = 0; b < B; ++b) {
-                    uint32_t w[4][4];  // [channel][pair of tokens]
+                    uint4 w[4];  // [pair of tokens]: its four channels
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) {
-                        const __half2 even = as_half2(b == 0 ? scales[t].x : b == 1 ? scales[t].y : b == 2 ? scales[t].z : scales[t].w), odd = __hmul2(even, sixteenth),
-                                      plus = __hmul2(even, eight);
-                        const uint32_t x = raw.values[t][b], y = swap_bytes(x);
-                        w[0][t] = decode(x & kEven, even, plus);
-                        w[1][t] = decode(x & kOdd, odd, plus);
-                        w[2][t] = decode(y & kEven, even, plus);
-                        w[3][t] = decode(y & kOdd, odd, plus);
-                    }
+                    for (int t = 0; t < 4; ++t) w[t] = decode(raw.values[t][b], as_half2(b == 0 ? scales[t].x : b == 1 ? scales[t].y : b == 2 ? scales[t].z : scales[t].w));
                     // channel 4 eighth + i of the block is row 8 i + eighth of the operand
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4 *>(to + (4 * b + i) * ROWS8_V) = make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]);
+                    *reinterpret_cast<uint4 *>(to + (4 * b + 0) * ROWS8_V) = make_uint4(w[0].x, w[1].x, w[2].x, w[3].x);
+                    *reinterpret_cast<uint4 *>(to + (4 * b + 1) * ROWS8_V) = make_uint4(w[0].y, w[1].y, w[2].y, w[3].y);
+                    *reinterpret_cast<uint4 *>(to + (4 * b + 2) * ROWS8_V) = make_uint4(w[0].z, w[1].z, w[2].z, w[3].z);
+                    *reinterpret_cast<uint4 *>(to + (4 * b + 3) * ROWS8_V) = make_uint4(w[0].w, w[1].w, w[2].w, w[3].w);
                 }
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -667,12 +677,48 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
     if (warp == kIssuerWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
 
+// Joins the pieces of the columns, always in the same order: a warp to a column, eight columns to a block.
+template <int B>
+__global__ void __launch_bounds__(256) kv_prompt_join_kernel(const __grid_constant__ AttnParams p)
+{
+    constexpr int D = 32 * B;
+    Unit u;
+    int first_unit;
+    const bool found = find_unit<kPromptColumns, true>(p, blockIdx.x, &u, &first_unit);
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // every block: what comes behind this kernel relies on the one in front, too
+    const int head = blockIdx.y, in_tile = blockIdx.z * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (!found || u.chunks == 1) return;
+    const int column = u.column0 + in_tile, row = column / p.group;
+    if (row >= u.rows) return;
+    const int64_t step = (int64_t)p.g.heads * kPromptColumns * (D + 4);
+    const float *const from = p.parts + (((int64_t)first_unit * p.g.heads + head) * kPromptColumns + in_tile) * (D + 4);
+    const int chunks = min(u.chunks, p.units - first_unit);
+    float top = -INFINITY;
+    for (int i = lane; i < chunks; i += 32) top = fmaxf(top, from[i * step + D]);
+#pragma unroll
+    for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+    float sum[B] = {}, weight = 0.0f;
+#pragma unroll 4
+    for (int i = 0; i < chunks; ++i) {
+        const float f = exp2f(from[i * step + D] - top);
+        weight = fmaf(f, from[i * step + D + 1], weight);
+#pragma unroll
+        for (int b = 0; b < B; ++b) sum[b] = fmaf(f, from[i * step + 32 * b + lane], sum[b]);
+    }
+    const int64_t at = (u.row0 + row) * p.out_token + ((int64_t)head * p.group + (column - row * p.group)) * p.out_head;
+#pragma unroll
+    for (int b = 0; b < B; ++b)
+        if (32 * b + lane < p.g.dim) store_element(p.out, p.type, at + 32 * b + lane, weight == 0.0f ? 0.0f : sum[b] / weight);
+}
+
 template <int B>
 lce_status launch(const AttnParams &p, const TimeoutReport &report, cudaStream_t s)
 {
     static SmemOptIn opt_in;
     if (!opt_in.ensure(kv_prompt_kernel<B>, prompt_smem(B))) return LCE_ERR_CUDA;
-    return launch_dependent(kv_prompt_kernel<B>, dim3((unsigned)p.units, (unsigned)p.g.heads), kThreads, prompt_smem(B), s, p, report);
+    const lce_status st = launch_dependent(kv_prompt_kernel<B>, dim3((unsigned)p.units, (unsigned)p.g.heads), kThreads, prompt_smem(B), s, p, report);
+    if (st != LCE_OK || !p.join) return st;
+    return launch_dependent(kv_prompt_join_kernel<B>, dim3((unsigned)p.column_tiles, (unsigned)p.g.heads, kPromptColumns / 8), 256, 0, s, p);
 }
 
 }  // namespace

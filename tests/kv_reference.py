@@ -35,7 +35,7 @@ def attention(q, k, v, k_scales, v_scales, shown, scale, rows_type):
     of at most 15 s |q| per channel, in 6 steps.  16-bit rows have codes as subnormal numbers n 2^-22 for operands: a product adds up
     17 terms cut at 2^-23 of what its largest exponents allow, 2^-14 |q| (not 2^-22 |q|): 17 * 2^-15 of a code's step and the largest
     |q| for each of a block's two products, and of the largest weight for each of a tile's two.  (Many rows have keys and values as f16
-    numbers c s for operands, exact down to 2^-10 of the largest scale; below, off by 2^-21 of the largest value.)"""
+    numbers c s for operands, exact down to 2^-28 of the largest scale of 128 tokens; below, off by 2^-39 of the largest value.)"""
     heads, group = q.shape[0], q.shape[0] // k.shape[1]
     out, bound = np.zeros(q.shape), np.zeros(q.shape)
     if not shown.any():
@@ -55,7 +55,7 @@ def attention(q, k, v, k_scales, v_scales, shown, scale, rows_type):
             if rows_type != "float32":
                 e += 34 * 2.0 ** -15 * abs(scale) * np.abs(q[h]).max() * k_scales[at, h // group].sum(-1).max()
                 cut = 34 * 2.0 ** -15 * np.repeat(w @ np.nan_to_num(v_scales[at, h // group]), 32)[:q.shape[1]]
-                cut = cut + 2.0 ** -21 * np.nan_to_num(np.abs(vv), nan=0.0).max()
+                cut = cut + 2.0 ** -39 * np.nan_to_num(np.abs(vv), nan=0.0).max()
             weight = (2.0 ** -11 if rows_type != "float32" else 2.0 ** -21) + 2 * e + (len(at) // 16 + 65) * 2.0 ** -23
             bound[h] = HALF_STEP[rows_type] * np.abs(out[h]) + cut + weight * (w @ np.abs(vv)) + 2.0 ** -31 * len(at) * np.nan_to_num(np.abs(vv), nan=0.0).max()
     return out, bound

@@ -130,6 +130,88 @@ def test_prompt_with_window_and_without_causality():
     check(lce.lce_kv_attention(*s.arguments(), causal=False), s.expected(causal=False))
 
 
+# shapes for which many rows are worth the tensor-core kernel: tables long enough, although not all of their sequences are
+@pytest.mark.parametrize("dtype,dim", [(F16, 8), (BF16, 32), (F16, 40), (F16, 64), (BF16, 96), (F16, 100), (BF16, 128)])
+def test_many_rows_of_every_head_size(dtype, dim):
+    s = Setup(dtype, [700, 201, 130, 40], [300, 201, 3, 90], 2, 4, dim, page=48, seed=30, table_extra=200)
+    check(lce.lce_kv_attention(*s.arguments()), s.expected())
+
+
+@pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 77), (False, 300), (True, 1)])
+def test_many_rows_masked(causal, window):
+    s = Setup(BF16, [700, 20, 515, 0], [500, 64, 515, 40], 1, 8, 128, page=16, seed=31, table_extra=400)
+    check(lce.lce_kv_attention(*s.arguments(), causal=causal, window=window), s.expected(causal=causal, window=window))
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("scale", [None, -0.2, 0.0])
+def test_many_rows_of_one_long_sequence_in_pieces(dtype, scale):
+    s = Setup(dtype, [6001], [260], 1, 2, 128, page=128, seed=32, table_extra=900)
+    args = s.arguments()
+    got = lce.lce_kv_attention(*args, scale=scale)
+    check(got, s.expected(scale=scale))
+    assert torch.equal(got, lce.lce_kv_attention(*args, scale=scale))
+
+
+@pytest.mark.parametrize("q_size", [1e-6, 40.0])
+def test_many_rows_with_scales_that_grow_and_shrink(q_size):
+    s = Setup(BF16, [900], [300], 2, 4, 64, page=32, seed=33, q_size=q_size, table_extra=300)
+    grow = torch.exp2(torch.linspace(-40, 40, 900, dtype=torch.float64)).view(-1, 1, 1).to(DEV)
+    for v in (s.v.double() * grow, s.v.double() * grow.flip(0)):
+        s.v = v.to(BF16)
+        s.store()
+        check(lce.lce_kv_attention(*s.arguments()), s.expected())
+
+
+def test_many_rows_and_what_is_not_a_number():
+    s = Setup(F16, [800], [400], 2, 4, 128, page=64, seed=34, table_extra=200)
+    s.k[650], s.v[700, 0, 40], s.v[701, 1, 100] = float("nan"), float("inf"), float("nan")  # seen by rows from 250, 300 and 301 on
+    s.store()
+    s.q[17, 3, 5], s.q[40, 0, 0] = float("inf"), float("nan")
+    out, bound = s.expected()
+    assert np.isfinite(out[:250][np.arange(250) != 17][:20]).all() and np.isnan(out[250:]).all()
+    check(lce.lce_kv_attention(*s.arguments()), (out, bound))
+    t = Setup(F16, [800], [400], 2, 4, 128, page=64, seed=34, table_extra=200)
+    t.v[700, 0, 40], t.v[701, 1, 100] = float("inf"), float("nan")
+    t.store()
+    out, bound = t.expected()
+    # a block of 32 channels of the value's own heads, from the first row that sees it on
+    assert np.isnan(out[300:, :4, 32:64]).all() and np.isfinite(out[300:, :4, 64:]).all() and np.isfinite(out[:300]).all() and np.isnan(out[301:, 4:, 96:]).all()
+    check(lce.lce_kv_attention(*t.arguments()), (out, bound))
+
+
+def test_many_rows_strides_bad_pages_and_rows_of_no_sequence():
+    s = Setup(BF16, [500, 333], [300, 200], 2, 4, 64, seed=35, table_extra=400)
+    s.table[0, 3], s.table[1, 0] = -1, s.desc.pages
+    want = s.expected(bad_tokens=[(0, slice(48, 64)), (1, slice(0, 16))])
+    wide = torch.full((510, 3 * 8 * 64 + 5), 5.0, dtype=BF16, device=DEV)
+    q = wide[:, 3:3 + 512].view(510, 8, 64)
+    q[:500] = s.q
+    args = s.arguments()
+    args[1] = q
+    back = torch.full((510, 8, 72), 9.0, dtype=BF16, device=DEV)
+    lce.lce_kv_attention(*args, out=back[:, :, 8:])
+    check(back[:500, :, 8:], want)
+    assert (back[500:] == 9).all() and (back[:, :, :8] == 9).all()
+
+
+def test_many_rows_captured_with_growing_sequences():
+    s = Setup(BF16, [600, 400], [256, 256], 2, 4, 128, page=64, seed=36, table_extra=100)
+    args = s.arguments()
+    out, graph = torch.empty_like(s.q), torch.cuda.CUDAGraph()
+    lce.lce_kv_attention(*args)
+    with torch.cuda.graph(graph):
+        lce.lce_kv_attention(*args, out=out)
+    for lengths in ([600, 400], [300, 256], [10, 0], [599, 399]):
+        args[4].copy_(torch.tensor(lengths, dtype=torch.int32))
+        graph.replay()
+        assert torch.equal(out, lce.lce_kv_attention(*args))
+    args[4].copy_(torch.tensor([600, 400], dtype=torch.int32))
+    graph.replay()
+    check(out, s.expected())
+    assert lce.lce_device_status() == 0
+
+
 @pytest.mark.parametrize("dtype", [F32, F16, BF16])
 def test_long_sequence_in_pieces(dtype):
     s = Setup(dtype, [20011, 3], [1, 1], 1, 2, 64, page=128, seed=9)
