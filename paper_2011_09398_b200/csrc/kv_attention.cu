@@ -21,6 +21,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 namespace lce {
 namespace {
@@ -130,21 +131,41 @@ struct Warp {
     int32_t lo[NT][2], hi[NT][2];
 };
 
-template <int B, int NT, bool SPLIT>
-__device__ __forceinline__ void load_queries(const AttnParams &p, const Unit &u, int head, Warp<B, NT, SPLIT> &w)
+// The lane's channels of its columns as they come from memory.
+template <int B, int NT, typename T>
+struct Queries {
+    Eight<T> e[NT][B];
+    template <bool VEC>
+    __device__ __forceinline__ void load(const AttnParams &p, const Unit &u, int head)
+    {
+        const int lane = threadIdx.x & 31, n = lane >> 2, quarter = lane & 3;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int column = u.column0 + 8 * nt + n, row = column / p.group;
+            const int64_t at = (u.row0 + row) * p.q_token + ((int64_t)head * p.group + (column - row * p.group)) * p.q_head + 8 * quarter;
+#pragma unroll
+            for (int b = 0; b < B; ++b) e[nt][b] = load_eight<T, VEC>(static_cast<const T *>(p.q) + at + 32 * b, row < u.rows ? p.g.dim - 32 * b - 8 * quarter : 0);
+        }
+    }
+};
+
+// T: float, or __half for the bits of any 16-bit row.
+template <int B, int NT, bool SPLIT, typename T>
+__device__ __forceinline__ void take_queries(const AttnParams &p, const Unit &u, const Queries<B, NT, T> &queries, Warp<B, NT, SPLIT> &w)
 {
-    const int lane = threadIdx.x & 31, n = lane >> 2, quarter = lane & 3;
+    const int lane = threadIdx.x & 31, quarter = lane & 3;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-        const int column = u.column0 + 8 * nt + n, row = column / p.group;
-        const bool there = row < u.rows;
-        const int64_t at = (u.row0 + row) * p.q_token + ((int64_t)head * p.group + (column - row * p.group)) * p.q_head;
         float v[B][8];
         uint32_t magnitude = 0;  // magnitudes compare like integers, infinity and NaN above all others
 #pragma unroll
         for (int b = 0; b < B; ++b) {
-            const int c = 32 * b + 8 * quarter;
-            load_row<SPLIT>(p, at + c, there ? p.g.dim - c : 0, v[b]);
+            if (!SPLIT && p.type == LCE_TYPE_BFLOAT16) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[b][i] = __uint_as_float((uint32_t)reinterpret_cast<const unsigned short *>(queries.e[nt][b].e)[i] << 16);
+            } else {
+                queries.e[nt][b].expand(v[b]);
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) magnitude = max(magnitude, __float_as_uint(v[b][i]) & 0x7fffffffu);
         }
@@ -427,18 +448,24 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(B, NT, SPLIT)) kv_atte
     int first_unit;
     const int unit = blockIdx.x / p.cluster, rank = blockIdx.x - unit * p.cluster;
     if (!find_unit<COLUMNS, false>(p, unit, &u, &first_unit)) return;
-    const int head = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, head = p.solo ? blockIdx.y * kWarps + warp : blockIdx.y;
+    if (head >= p.g.heads) return;  // whole warps, which then meet nobody
     // tokens that every column sees, and those that one sees at least: the ranges' ends grow with the rows
     int32_t any_lo, all_hi, all_lo, any_hi;
     column_range(p, u, u.column0, &any_lo, &all_hi);
     column_range(p, u, min(u.column0 + COLUMNS, u.rows * p.group) - 1, &all_lo, &any_hi);
     const int32_t tile0 = any_hi > 0 ? max(u.tile0, any_lo / kKvTile) : u.tile1, tile1 = min(u.tile1, (any_hi + kKvTile - 1) / kKvTile);
 
+    // on their way while the pages are looked up
+    Queries<B, NT, typename std::conditional<SPLIT, float, __half>::type> queries;
+    if (p.q_vectors) queries.template load<true>(p, u, head);
+    else queries.template load<false>(p, u, head);
+
     uint32_t *const ring = smem + warp * kStages * TILE;
     const int32_t *const table = p.page_table + (int64_t)u.seq * p.table_pages;
     const int tiles_per_page = p.g.page_size / kKvTile;
     // a cluster's warps take its tiles in turn
-    const int first_warp = rank * kWarps + warp, step = kWarps * p.cluster;
+    const int first_warp = p.solo ? 0 : rank * kWarps + warp, step = p.solo ? 1 : kWarps * p.cluster;
     // the warp's next 32 tiles in the cache, one to a lane; negative: not in the pool
     int32_t places = -1;
     const int32_t mine = max((tile1 - tile0 - first_warp + step - 1) / step, 0);
@@ -464,7 +491,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(B, NT, SPLIT)) kv_atte
 #pragma unroll
     for (int i = 0; i < kStages - 1; ++i) good |= fetch(i, ring_at + i * (TILE * 4)) ? 1u << i : 0u;
     Warp<B, NT, SPLIT> w;
-    load_queries(p, u, head, w);  // while the first tiles are on their way
+    take_queries(p, u, queries, w);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -496,6 +523,31 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(B, NT, SPLIT)) kv_atte
         else tile_step<B, NT, SPLIT, true>(tile, token0, w);
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
+    if (p.solo) {
+        // nobody to join: 4 channels of a block to a lane and column
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                float l = w.weight[nt][j];
+                l += __shfl_xor_sync(0xffffffffu, l, 4);
+                l += __shfl_xor_sync(0xffffffffu, l, 8);
+                l += __shfl_xor_sync(0xffffffffu, l, 16);
+                const int q = u.column0 + 8 * nt + 2 * (lane & 3) + j, row = q / p.group;
+                if (row >= u.rows) continue;
+                const int64_t to = (u.row0 + row) * p.out_token + ((int64_t)head * p.group + (q - row * p.group)) * p.out_head + 4 * (lane >> 2);
+#pragma unroll
+                for (int b = 0; b < B; ++b) {
+                    const float v[4] = {w.o[b][0][nt][j], w.o[b][0][nt][2 + j], w.o[b][1][nt][j], w.o[b][1][nt][2 + j]};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        constexpr float kEven = SPLIT ? 1.0f : 0x1p22f, kOdd = SPLIT ? 1.0f : 0x1p18f;  // what the codes stood for
+                        if (32 * b + 4 * (lane >> 2) + i < p.g.dim) store_element(p.out, p.type, to + 32 * b + i, l == 0.0f ? 0.0f : v[i] * (i & 1 ? kOdd : kEven) / l);
+                    }
+                }
+            }
+        return;
+    }
     __syncthreads();
 
     // The warps' sums meet in shared memory: [warp][column][32 B], largest and weight of each behind them.
@@ -594,9 +646,9 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(B, NT, SPLIT)) kv_atte
     cluster_sync();  // nobody leaves while its sums are read
 }
 
-// Joins the pieces of a column, always in the same order: a block to a column, its warps' share of the pieces first, then the
-// warps.  It is there before the pieces are (release_join) and has found its own by then.
-constexpr int kJoinWarps = 8;
+// Joins the pieces of a column, always in the same order: a warp to a column, or where there are many pieces a block, its warps' share of
+// them first, then the warps.  It is there before the pieces are (release_join) and has found its own by then.
+constexpr int kJoinWarps = 8, kFewPieces = 16;
 
 template <int NT>
 __global__ void __launch_bounds__(32 * kJoinWarps) kv_attention_join_kernel(const __grid_constant__ AttnParams p)
@@ -610,51 +662,85 @@ __global__ void __launch_bounds__(32 * kJoinWarps) kv_attention_join_kernel(cons
     // the lengths are what the kernel in front read: nothing has written them since
     const bool found = find_unit<COLUMNS, true>(p, blockIdx.x, &u, &first_unit);
     asm volatile("griddepcontrol.wait;" ::: "memory");  // every block: what comes behind this kernel relies on the one in front, too
-    const int head = blockIdx.y, column = blockIdx.z, D = 32 * p.g.blocks;
-    if (!found || u.chunks == 1) return;
-    const int q = u.column0 + column, row = q / p.group;
-    if (row >= u.rows) return;
+    const int head = blockIdx.y, D = 32 * p.g.blocks;
+    if (!found) return;
     const int64_t step = (int64_t)p.g.heads * COLUMNS * (D + 4);
-    const float *const from = p.parts + (((int64_t)first_unit * p.g.heads + head) * COLUMNS + column) * (D + 4);
     const int chunks = min(u.chunks, p.units - first_unit);
-    float top = -INFINITY;
-    for (int i = warp * 32 + lane; i < chunks; i += 32 * kJoinWarps) top = fmaxf(top, from[i * step + D]);
+    const auto column_parts = [&](int column) { return p.parts + (((int64_t)first_unit * p.g.heads + head) * COLUMNS + column) * (D + 4); };
+    const auto add = [](float4 &sum, float f, const float4 &v) {
+        sum.x = fmaf(f, v.x, sum.x);
+        sum.y = fmaf(f, v.y, sum.y);
+        sum.z = fmaf(f, v.z, sum.z);
+        sum.w = fmaf(f, v.w, sum.w);
+    };
+    if (chunks <= kFewPieces) {
+        // a warp to a column
+        for (int column = blockIdx.z * kJoinWarps + warp; column < COLUMNS; column += gridDim.z * kJoinWarps) {
+            const int q = u.column0 + column, row = q / p.group;
+            if (row >= u.rows) return;
+            const float *const from = column_parts(column);
+            float top = lane < chunks ? from[lane * step + D] : -INFINITY;
 #pragma unroll
-    for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-    if (lane == 0) tops[warp] = top;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kJoinWarps; ++i) top = fmaxf(top, tops[i]);
-    float weight = 0.0f;
-    float4 sum[2] = {};
+            for (int d = kFewPieces / 2; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+            top = __shfl_sync(0xffffffffu, top, 0);
+            float weight = 0.0f;
+            float4 sum[2] = {};
 #pragma unroll 4
-    for (int i = warp; i < chunks; i += kJoinWarps) {
-        const float f = exp2f(from[i * step + D] - top);
-        weight = fmaf(f, from[i * step + D + 1], weight);
+            for (int i = 0; i < chunks; ++i) {
+                const float f = exp2f(from[i * step + D] - top);
+                weight = fmaf(f, from[i * step + D + 1], weight);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int c = 4 * (lane + 32 * h);
-            if (c >= D) break;
-            const float4 v = *reinterpret_cast<const float4 *>(from + i * step + c);
-            sum[h].x = fmaf(f, v.x, sum[h].x);
-            sum[h].y = fmaf(f, v.y, sum[h].y);
-            sum[h].z = fmaf(f, v.z, sum[h].z);
-            sum[h].w = fmaf(f, v.w, sum[h].w);
+                for (int h = 0; h < 2; ++h)
+                    if (4 * (lane + 32 * h) < D) add(sum[h], f, *reinterpret_cast<const float4 *>(from + i * step + 4 * (lane + 32 * h)));
+            }
+            const int64_t at = (u.row0 + row) * p.out_token + ((int64_t)head * p.group + (q - row * p.group)) * p.out_head;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float v[4] = {sum[h].x, sum[h].y, sum[h].z, sum[h].w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (4 * (lane + 32 * h) + i < p.g.dim) store_element(p.out, p.type, at + 4 * (lane + 32 * h) + i, weight == 0.0f ? 0.0f : v[i] / weight);
+            }
         }
+        return;
     }
-    sums[warp][0][lane] = sum[0];
-    sums[warp][1][lane] = sum[1];
-    if (lane == 0) weights[warp] = weight;
-    __syncthreads();
-    for (int c = threadIdx.x; c < p.g.dim; c += 32 * kJoinWarps) {
-        float s = 0.0f, l = 0.0f;
+    for (int column = blockIdx.z; column < COLUMNS; column += gridDim.z) {
+        const int q = u.column0 + column, row = q / p.group;
+        if (row >= u.rows) return;
+        const float *const from = column_parts(column);
+        float top = -INFINITY;
+        for (int i = warp * 32 + lane; i < chunks; i += 32 * kJoinWarps) top = fmaxf(top, from[i * step + D]);
 #pragma unroll
-        for (int i = 0; i < kJoinWarps; ++i) {
-            s += reinterpret_cast<const float *>(sums[i])[c];
-            l += weights[i];
+        for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+        if (lane == 0) tops[warp] = top;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kJoinWarps; ++i) top = fmaxf(top, tops[i]);
+        float weight = 0.0f;
+        float4 sum[2] = {};
+#pragma unroll 4
+        for (int i = warp; i < chunks; i += kJoinWarps) {
+            const float f = exp2f(from[i * step + D] - top);
+            weight = fmaf(f, from[i * step + D + 1], weight);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (4 * (lane + 32 * h) < D) add(sum[h], f, *reinterpret_cast<const float4 *>(from + i * step + 4 * (lane + 32 * h)));
         }
-        store_element(p.out, p.type, (u.row0 + row) * p.out_token + ((int64_t)head * p.group + (q - row * p.group)) * p.out_head + c,
-                      l == 0.0f ? 0.0f : s / l);
+        sums[warp][0][lane] = sum[0];
+        sums[warp][1][lane] = sum[1];
+        if (lane == 0) weights[warp] = weight;
+        __syncthreads();
+        for (int c = threadIdx.x; c < p.g.dim; c += 32 * kJoinWarps) {
+            float s = 0.0f, l = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kJoinWarps; ++i) {
+                s += reinterpret_cast<const float *>(sums[i])[c];
+                l += weights[i];
+            }
+            store_element(p.out, p.type, (u.row0 + row) * p.out_token + ((int64_t)head * p.group + (q - row * p.group)) * p.out_head + c,
+                          l == 0.0f ? 0.0f : s / l);
+        }
+        __syncthreads();
     }
 }
 
@@ -667,7 +753,7 @@ lce_status launch(const AttnParams &p, cudaStream_t s)
     static SmemOptIn opt_in;
     if (!opt_in.ensure(kv_attention_kernel<B, NT, SPLIT>, smem)) return LCE_ERR_CUDA;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(p.units * p.cluster), (unsigned)p.g.heads, 1);
+    cfg.gridDim = dim3((unsigned)(p.units * p.cluster), (unsigned)(p.solo ? (p.g.heads + kWarps - 1) / kWarps : p.g.heads), 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
@@ -684,9 +770,10 @@ lce_status launch(const AttnParams &p, cudaStream_t s)
         return LCE_ERR_CUDA;
     }
     if (!p.join) return LCE_OK;
-    // columns that there can be in a tile
-    const int64_t columns = p.tokens * p.group < 8 * NT ? p.tokens * p.group : p.one_row && p.group < 8 * NT ? p.group : 8 * NT;
-    return launch_dependent(kv_attention_join_kernel<NT>, dim3((unsigned)p.column_tiles, (unsigned)p.g.heads, (unsigned)columns), 32 * kJoinWarps, 0, s, p);
+    // At most `target` column tiles are in pieces; columns that there can be in one; about a block for each place that the GPU has.
+    const int64_t split = std::min<int64_t>(p.column_tiles, p.target), columns = std::min<int64_t>(p.tokens * p.group, p.one_row && p.group < 8 * NT ? p.group : 8 * NT);
+    const int64_t side = std::max<int64_t>(1, std::min<int64_t>(columns, 148 * 8 / (split * p.g.heads)));
+    return launch_dependent(kv_attention_join_kernel<NT>, dim3((unsigned)split, (unsigned)p.g.heads, (unsigned)side), 32 * kJoinWarps, 0, s, p);
 }
 
 // 16 columns where their sums and operands fit a thread's registers
@@ -709,6 +796,8 @@ lce_status launch_blocks(const AttnParams &p, cudaStream_t s)
 }
 
 constexpr int kPromptLeastTiles = 6;  // tiles of 128 tokens that a piece is worth there
+constexpr int kWaves = 6;       // quarters of what the GPU holds: pieces that several sequences are cut into
+constexpr int kSoloTiles = 64;
 constexpr int kLeastTiles = 16;  // tiles of a warp that a piece is worth
 
 // one_row: without q_starts
@@ -758,12 +847,15 @@ lce_status make_params(const lce_kv_attention_desc *d, bool one_row, AttnParams 
     int64_t most = (p->table_tokens + kKvTile - 1) / kKvTile;  // tiles that a sequence can have in view
     if (p->window > 0 && one_row && p->window / kKvTile + 2 < most) most = p->window / kKvTile + 2;
     p->cluster = 1;
-    while (p->cluster < 8 && most <= kWarps * 8 * kLeastTiles && tiles * p->g.heads * p->cluster * 2 <= blocks && p->cluster * kWarps < most) p->cluster *= 2;
+    const int64_t likely = p->batch * ((each + columns - 1) / columns);  // column tiles, were all sequences alike
+    while (p->cluster < 8 && most <= kWarps * 8 * kLeastTiles && likely * p->g.heads * p->cluster * 2 <= blocks && p->cluster * kWarps < most) p->cluster *= 2;
     // Sequences longer than that pays for are cut further.
     p->least_tiles = kWarps * p->cluster * kLeastTiles;
     p->join = most > p->least_tiles;
-    const int waves = p->batch > 1 ? 2 : 1;  // pieces of one sequence are all alike
-    const int64_t target = p->join ? (blocks * waves / p->cluster + p->g.heads - 1) / p->g.heads : 0;
+    // Many short sequences: a warp to each, without the joining (256 of 512 tokens, 8 key heads: 71.7 us by blocks).
+    p->solo = !p->join && p->cluster == 1 && most <= kSoloTiles && likely * p->g.heads >= 3 * blocks;
+    const int waves = p->batch > 1 ? kWaves : 4;  // pieces of one sequence are all alike
+    const int64_t target = p->join ? (blocks * waves / 4 / p->cluster + p->g.heads - 1) / p->g.heads : 0;
     p->target = (int32_t)(target > 0 ? target : 1);
     if ((tiles + target) * p->cluster >= (1ll << 31) || (int64_t)p->g.slots / kKvTile * p->g.heads >= (1ll << 31)) return LCE_ERR_UNSUPPORTED;
     p->units = (int32_t)(tiles + target);

@@ -21,6 +21,7 @@ struct AttnParams {
     float *parts;                      // [unit][kv head][column][32 blocks + 4]: sums, largest, weight
     int32_t units, column_tiles, target, least_tiles;
     int32_t cluster;                   // blocks that share a unit
+    int32_t solo;                      // a warp to a unit and head: many short sequences
     int32_t join;                      // there may be units that are not a whole column tile
     int32_t prompt;                    // the kernel for prompts
     int32_t one_row;                   // each sequence has one row of q
@@ -64,19 +65,39 @@ __device__ __forceinline__ Sequence sequence(const AttnParams &p, int b)
 
 // The work is cut evenly whatever the sequences' lengths: every column tile of a sequence into pieces of at most `most` tiles, where
 // `most` follows from the whole batch's tiles.  Every warp works this out for itself from the lengths (no launch in front, no host
-// copy of them).  Finds the `at`-th unit, or the first unit of the `at`-th column tile; false: there is no such one.
-template <int COLUMNS, bool BY_COLUMN_TILE>
+// copy of them).  Finds the `at`-th unit, or the first unit of the `at`-th column tile that is in pieces; false: there is no such one.
+template <int COLUMNS, bool IN_PIECES>
 __device__ __forceinline__ bool find_unit(const AttnParams &p, int at, Unit *u, int *first_unit)
 {
     const int lane = threadIdx.x & 31;
+    if (!p.join && !p.q_starts) {
+        // a row for each sequence, and whole column tiles: no search
+        const int32_t column_tiles = (p.group + COLUMNS - 1) / COLUMNS, seq = at / column_tiles;
+        if (seq >= p.batch) return false;
+        const Sequence s = sequence<COLUMNS>(p, seq);
+        u->seq = seq;
+        u->chunks = 1;
+        u->length = s.length;
+        u->rows = 1;
+        u->row0 = seq;
+        u->column0 = (at - seq * column_tiles) * COLUMNS;
+        u->tile0 = s.first_tile;
+        u->tile1 = s.first_tile + s.tiles;
+        u->first = u->last = true;
+        *first_unit = at;
+        return true;
+    }
     const Sequence first = sequence<COLUMNS>(p, lane);
     int64_t total = 0;
-    for (int b0 = 0; b0 < p.batch; b0 += 32) {
-        const Sequence s = b0 ? sequence<COLUMNS>(p, b0 + lane) : first;
-        int64_t t = (int64_t)s.column_tiles * s.tiles;
+    if (p.join) {
+        total = (int64_t)first.column_tiles * first.tiles;
+#pragma unroll 4
+        for (int b0 = 32; b0 < p.batch; b0 += 32) {
+            const Sequence s = sequence<COLUMNS>(p, b0 + lane);
+            total += (int64_t)s.column_tiles * s.tiles;
+        }
 #pragma unroll
-        for (int d = 16; d; d >>= 1) t += __shfl_xor_sync(0xffffffffu, t, d);
-        total += t;
+        for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
     }
     int32_t most = 1 << 30;
     if (p.join) {
@@ -86,7 +107,7 @@ __device__ __forceinline__ bool find_unit(const AttnParams &p, int at, Unit *u, 
     int before = 0, units_before = 0;
     for (int b0 = 0; b0 < p.batch; b0 += 32) {
         const Sequence s = b0 ? sequence<COLUMNS>(p, b0 + lane) : first;
-        const int32_t chunks = max((s.tiles + most - 1) / most, 1), units = s.column_tiles * chunks, mine = BY_COLUMN_TILE ? s.column_tiles : units;
+        const int32_t chunks = max((s.tiles + most - 1) / most, 1), units = s.column_tiles * chunks, mine = !IN_PIECES ? units : chunks > 1 ? s.column_tiles : 0;
         int32_t upto = mine, units_upto = units;  // of this and the lanes below
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -106,7 +127,7 @@ __device__ __forceinline__ bool find_unit(const AttnParams &p, int at, Unit *u, 
             u->rows = __shfl_sync(0xffffffffu, s.rows, from);
             u->row0 = __shfl_sync(0xffffffffu, s.row0, from);
             const int32_t tiles = __shfl_sync(0xffffffffu, s.tiles, from), first_tile = __shfl_sync(0xffffffffu, s.first_tile, from);
-            const int32_t column_tile = BY_COLUMN_TILE ? local : local / u->chunks, chunk = BY_COLUMN_TILE ? 0 : local - column_tile * u->chunks;
+            const int32_t column_tile = IN_PIECES ? local : local / u->chunks, chunk = IN_PIECES ? 0 : local - column_tile * u->chunks;
             u->column0 = column_tile * COLUMNS;
             *first_unit = units_before + __shfl_sync(0xffffffffu, units_upto - units, from) + column_tile * u->chunks;
             // equal pieces
@@ -134,24 +155,6 @@ __device__ __forceinline__ void column_range(const AttnParams &p, const Unit &u,
     *lo = p.window > 0 ? (int32_t)min(max(position + 1 - p.window, (int64_t)0), (int64_t)u.length) : 0;
 }
 
-// Eight channels of a row of q; `count` of them exist.  SPLIT: fp32, otherwise f16 or bf16.
-template <bool SPLIT>
-__device__ __forceinline__ void load_row(const AttnParams &p, int64_t at, int count, float (&v)[8])
-{
-    if (SPLIT) {
-        const float *const q = static_cast<const float *>(p.q) + at;
-        if (p.q_vectors) load8<float, true>(q, count, v);
-        else load8<float, false>(q, count, v);
-    } else if (p.type == LCE_TYPE_FLOAT16) {
-        const __half *const q = static_cast<const __half *>(p.q) + at;
-        if (p.q_vectors) load8<__half, true>(q, count, v);
-        else load8<__half, false>(q, count, v);
-    } else {
-        const __nv_bfloat16 *const q = static_cast<const __nv_bfloat16 *>(p.q) + at;
-        if (p.q_vectors) load8<__nv_bfloat16, true>(q, count, v);
-        else load8<__nv_bfloat16, false>(q, count, v);
-    }
-}
 __device__ __forceinline__ void store_element(void *p, int32_t type, int64_t i, float v)
 {
     switch (type) {

@@ -19,6 +19,7 @@
 #include "kv_attention.cuh"
 #include "mx_common.cuh"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace lce {
@@ -687,7 +688,7 @@ __global__ void __launch_bounds__(256) kv_prompt_join_kernel(const __grid_consta
     const bool found = find_unit<kPromptColumns, true>(p, blockIdx.x, &u, &first_unit);
     asm volatile("griddepcontrol.wait;" ::: "memory");  // every block: what comes behind this kernel relies on the one in front, too
     const int head = blockIdx.y, in_tile = blockIdx.z * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-    if (!found || u.chunks == 1) return;
+    if (!found) return;
     const int column = u.column0 + in_tile, row = column / p.group;
     if (row >= u.rows) return;
     const int64_t step = (int64_t)p.g.heads * kPromptColumns * (D + 4);
@@ -718,7 +719,7 @@ lce_status launch(const AttnParams &p, const TimeoutReport &report, cudaStream_t
     if (!opt_in.ensure(kv_prompt_kernel<B>, prompt_smem(B))) return LCE_ERR_CUDA;
     const lce_status st = launch_dependent(kv_prompt_kernel<B>, dim3((unsigned)p.units, (unsigned)p.g.heads), kThreads, prompt_smem(B), s, p, report);
     if (st != LCE_OK || !p.join) return st;
-    return launch_dependent(kv_prompt_join_kernel<B>, dim3((unsigned)p.column_tiles, (unsigned)p.g.heads, kPromptColumns / 8), 256, 0, s, p);
+    return launch_dependent(kv_prompt_join_kernel<B>, dim3((unsigned)std::min(p.column_tiles, p.target), (unsigned)p.g.heads, kPromptColumns / 8), 256, 0, s, p);
 }
 
 }  // namespace

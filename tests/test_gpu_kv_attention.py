@@ -130,6 +130,17 @@ def test_prompt_with_window_and_without_causality():
     check(lce.lce_kv_attention(*s.arguments(), causal=False), s.expected(causal=False))
 
 
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("kv_heads,group,dim", [(6, 2, 40), (7, 8, 64), (5, 12, 128)])
+def test_many_short_sequences(dtype, kv_heads, group, dim):
+    """A warp to a sequence and head."""
+    lengths = [(i * 37) % 70 for i in range(380)]
+    s = Setup(dtype, lengths, [1] * len(lengths), kv_heads, group, dim, seed=40, table_extra=2)
+    check(lce.lce_kv_attention(*s.arguments()[:5]), s.expected())
+    s.table[5, 0], s.table[8, 1] = -1, s.desc.pages
+    check(lce.lce_kv_attention(*s.arguments()[:5], window=30), s.expected(window=30, bad_tokens=[(5, slice(0, 16)), (8, slice(16, 32))]))
+
+
 # shapes for which many rows are worth the tensor-core kernel: tables long enough, although not all of their sequences are
 @pytest.mark.parametrize("dtype,dim", [(F16, 8), (BF16, 32), (F16, 40), (F16, 64), (BF16, 96), (F16, 100), (BF16, 128)])
 def test_many_rows_of_every_head_size(dtype, dim):
