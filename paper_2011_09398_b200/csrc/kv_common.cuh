@@ -162,12 +162,13 @@ __device__ __forceinline__ void store8(T *p, int count, const float (&v)[8])
 
 // --- the quantiser ------------------------------------------------------------------------------
 
-// The smallest bf16 s with 7 s >= a, a finite and not negative.  7 s is exact (3 + 8 bits).  The quotient rounded to fp32 lies
-// within half a step of a / 7, so cut to bf16 it is that s or the number before it.
+// The smallest bf16 s with 7 s >= a, a finite and not negative.  7 s is exact (3 + 8 bits).  The product with a seventh lies within two
+// units of a / 7, so cut to bf16 it is that s or one of its neighbours.
 __device__ __forceinline__ float kv_scale(float a)
 {
-    const uint32_t cut = __float_as_uint(__fdiv_rn(a, 7.0f)) & 0xffff0000u;
-    return __uint_as_float(7.0f * __uint_as_float(cut) < a ? cut + 0x10000u : cut);
+    const uint32_t cut = __float_as_uint(__fmul_rn(a, 1.0f / 7.0f)) & 0xffff0000u;
+    if (7.0f * __uint_as_float(cut) < a) return __uint_as_float(cut + 0x10000u);
+    return cut != 0 && 7.0f * __uint_as_float(cut - 0x10000u) >= a ? __uint_as_float(cut - 0x10000u) : __uint_as_float(cut);
 }
 
 // round-half-even(x / s) for 0 <= x <= 7 s.  The product with the reciprocal is off by a few units of its last place, so the
@@ -191,7 +192,7 @@ __device__ __noinline__ static uint32_t kv_codes_any(float v0, float v1, float v
 {
     const float v[8] = {v0, v1, v2, v3, v4, v5, v6, v7};
     const float up = s < 0x1p-100f ? 0x1p80f : 1.0f;  // away from subnormal numbers, exactly
-    const float t = s * up, r = __fdiv_rn(1.0f, t);
+    const float t = s * up, r = __frcp_rn(t);
     uint32_t word = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -207,7 +208,7 @@ __device__ __noinline__ static uint32_t kv_codes_any(float v0, float v1, float v
 // constant.  Five operations a value where the general form takes twelve.
 __device__ __forceinline__ uint32_t kv_codes_short(const float (&v)[8], float s)
 {
-    const float r = __fdiv_rn(1.0f, s);
+    const float r = __frcp_rn(s);
     uint32_t word = 0;
 #pragma unroll
     for (int i = 7; i >= 0; --i) {
