@@ -38,19 +38,64 @@ __device__ __forceinline__ float max_or_nan(float a, float b)
     return d;
 }
 
-// Scale of the block that four neighbouring lanes hold, NaN where a value is not finite.
-__device__ __forceinline__ float block_scale(const float (&v)[8])
-{
-    float a = fabsf(v[0]);
+__device__ __forceinline__ float scale_or_nan(float a) { return a < __uint_as_float(0x7f800000u) ? kv_scale(a) : __uint_as_float(0x7fc00000u); }
+
+// Scales of the blocks of keys and of values that four neighbouring lanes hold, NaN where a value is not finite.
+template <typename T>
+struct BlockScales {  // fp32
+    static __device__ __forceinline__ void find(const Eight<T> &k, const Eight<T> &v, float &ks, float &vs)
+    {
+        float a = fabsf(k.e[0]), b = fabsf(v.e[0]);
 #pragma unroll
-    for (int i = 1; i < 8; ++i) a = max_or_nan(a, fabsf(v[i]));
-    a = max_or_nan(a, __shfl_xor_sync(0xffffffffu, a, 1));
-    a = max_or_nan(a, __shfl_xor_sync(0xffffffffu, a, 2));
-    return a < __uint_as_float(0x7f800000u) ? kv_scale(a) : __uint_as_float(0x7fc00000u);
-}
+        for (int i = 1; i < 8; ++i) {
+            a = max_or_nan(a, fabsf(k.e[i]));
+            b = max_or_nan(b, fabsf(v.e[i]));
+        }
+#pragma unroll
+        for (int d = 1; d <= 2; ++d) {
+            a = max_or_nan(a, __shfl_xor_sync(0xffffffffu, a, d));
+            b = max_or_nan(b, __shfl_xor_sync(0xffffffffu, b, d));
+        }
+        ks = scale_or_nan(a);
+        vs = scale_or_nan(b);
+    }
+};
+// 16 bits: two values at a time, then the key's and the value's largest in one word
+template <typename T, typename T2>
+struct PairScales {
+    static __device__ __forceinline__ T2 largest(const Eight<T> &x)
+    {
+        const uint32_t *const w = reinterpret_cast<const uint32_t *>(x.e);
+        T2 m[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t a = w[i] & 0x7fff7fffu;
+            m[i] = *reinterpret_cast<const T2 *>(&a);
+        }
+        return __hmax2_nan(__hmax2_nan(m[0], m[1]), __hmax2_nan(m[2], m[3]));
+    }
+    static __device__ __forceinline__ void find(const Eight<T> &k, const Eight<T> &v, float &ks, float &vs)
+    {
+        const T2 a = largest(k), b = largest(v);
+        const uint32_t x = *reinterpret_cast<const uint32_t *>(&a), y = *reinterpret_cast<const uint32_t *>(&b);
+        const uint32_t low = __byte_perm(x, y, 0x5410), high = __byte_perm(x, y, 0x7632);  // (key, value)
+        T2 m = __hmax2_nan(*reinterpret_cast<const T2 *>(&low), *reinterpret_cast<const T2 *>(&high));
+#pragma unroll
+        for (int d = 1; d <= 2; ++d) {
+            const uint32_t o = __shfl_xor_sync(0xffffffffu, *reinterpret_cast<const uint32_t *>(&m), d);
+            m = __hmax2_nan(m, *reinterpret_cast<const T2 *>(&o));
+        }
+        ks = scale_or_nan(to_float(m.x));
+        vs = scale_or_nan(to_float(m.y));
+    }
+};
+template <>
+struct BlockScales<__half> : PairScales<__half, __half2> {};
+template <>
+struct BlockScales<__nv_bfloat16> : PairScales<__nv_bfloat16, __nv_bfloat162> {};
 
 template <typename T>
-constexpr bool kShort = sizeof(T) == 2;
+constexpr int kValues = sizeof(T) == 4 ? KV_ANY : std::is_same<T, __half>::value ? KV_HALF : KV_SHORT;
 
 // BLOCKS of 32 channels; 0: p.g.blocks.
 template <typename T, bool VEC, int BLOCKS>
@@ -87,12 +132,13 @@ __global__ void __launch_bounds__(kThreads, 5) kv_quantize_kernel(const __grid_c
         float kx[8], vx[8];
         ke.expand(kx);
         ve.expand(vx);
-        const float ks = block_scale(kx), vs = block_scale(vx);
+        float ks, vs;
+        BlockScales<T>::find(ke, ve, ks, vs);
         if (!there || slot < 0 || slot >= p.g.slots) continue;
         uint32_t *const tile = whole ? staged : kv_tile_of(p, slot, head);
         const int in_tile = slot % kKvTile;
-        tile[kv_key_word(blocks, in_tile, block, quarter)] = kv_codes<kShort<T>>(kx, ks);
-        const uint32_t codes = kv_codes<kShort<T>>(vx, vs);
+        tile[kv_key_word(blocks, in_tile, block, quarter)] = kv_codes<kValues<T>>(kx, ks);
+        const uint32_t codes = kv_codes<kValues<T>>(vx, vs);
         uint16_t *const halves = reinterpret_cast<uint16_t *>(tile) + (in_tile & 1);
         halves[2 * kv_value_word(blocks, in_tile >> 1, block, 2 * quarter)] = (uint16_t)codes;
         halves[2 * kv_value_word(blocks, in_tile >> 1, block, 2 * quarter + 1)] = (uint16_t)(codes >> 16);

@@ -218,12 +218,12 @@ __device__ __forceinline__ uint32_t kv_codes_short(const float (&v)[8], float s)
     return word - 0x4b400000u * 0x11111111u;
 }
 
-// SHORT: the values are f16 or bf16 numbers
-template <bool SHORT>
+enum { KV_ANY, KV_SHORT, KV_HALF };  // any fp32 numbers; f16 or bf16 ones; f16 ones, whose scales are above 2^-28
+template <int VALUES>
 __device__ __forceinline__ uint32_t kv_codes(const float (&v)[8], float s)
 {
     if (!(s > 0.0f)) return kv_rotate(0x88888888u);  // all zeros, or NaN
-    if (SHORT && s >= 0x1p-100f) return kv_rotate(kv_codes_short(v, s));
+    if (VALUES == KV_HALF || (VALUES == KV_SHORT && s >= 0x1p-100f)) return kv_rotate(kv_codes_short(v, s));
     return kv_rotate(kv_codes_any(v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7], s));
 }
 
