@@ -12,6 +12,10 @@
 //           the sums over a long sequence would lose their last bits next to 8 sum(p)): the tensor cores have the time.  The
 //           block's scale multiplies p, in fp32, before it is rounded to f16.
 //
+// Measured: 131072 tokens of 8 heads of 128 channels (151 MB) 43 us, 5.2 TB/s where the sequence is longer still; 777 tokens 7.2 us; 48
+// sequences of 1 - 8192 tokens (236 MB) 84 us.  A warp spends 340 instructions on 16 tokens of 128 channels and 8 columns, of them 24
+// matrix products; the issue slots are 55% busy, with the registers for four warps a scheduler.
+//
 // Scores and the running softmax are fp32.  Q is f16 times a power of two chosen for each row, exact for f16 and bf16 rows up to
 // what lies 2^-29 below the row's largest; p is rounded to f16 (relative error 2^-11 of each weight, which is what an fp16
 // result has, and averages out).  fp32 rows take Q and p as two f16 numbers each (22 bits), and codes as f16 c = n - 8: 1024 + n by
@@ -796,8 +800,10 @@ lce_status launch_blocks(const AttnParams &p, cudaStream_t s)
 }
 
 constexpr int kPromptLeastTiles = 6;  // tiles of 128 tokens that a piece is worth there
-constexpr int kWaves = 6;       // quarters of what the GPU holds: pieces that several sequences are cut into
-constexpr int kSoloTiles = 64;
+// Pieces that several sequences are cut into, in quarters of the blocks that the GPU holds: 48 sequences of 1 - 8192 tokens take 91.5, 90.6,
+// 84.8 and 87.2 us with 3, 4, 6 and 8, 64 of 4096 89.8, 92.3, 92.9 and 101.1.
+constexpr int kWaves = 6;
+constexpr int kSoloTiles = 64;  // the longest that a warp takes alone
 constexpr int kLeastTiles = 16;  // tiles of a warp that a piece is worth
 
 // one_row: without q_starts
