@@ -104,7 +104,6 @@ template <typename T, bool VEC, int BLOCKS>
 __global__ void __launch_bounds__(kThreads, 5) kv_quantize_kernel(const __grid_constant__ KvRows p, const T *k, const T *v)
 {
     __shared__ __align__(16) uint32_t staged[kv_tile_words(kKvMaxDim / 32)];
-    __shared__ int32_t slots[kKvTile];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int blocks = BLOCKS ? BLOCKS : p.g.blocks;
     const int group = p.by_heads((int)blockIdx.x), head = blockIdx.x - group * p.g.heads;
@@ -118,12 +117,12 @@ __global__ void __launch_bounds__(kThreads, 5) kv_quantize_kernel(const __grid_c
         ve = load_eight<T, VEC>(v + (token0 + token) * p.v_token + head * p.v_head + channel, p.g.dim - channel);
     };
     load(min((int)threadIdx.x, items - 1));  // on their way while the slots are
-    bool whole = false;  // a whole tile, in order
+    // A whole tile, in order?  Every warp reads the sixteen slots for itself, which takes no barrier.
+    const int first = __ldg(p.slots + token0);
+    bool whole = false;
     if (tokens == kKvTile) {
-        if (threadIdx.x < kKvTile) slots[threadIdx.x] = __ldg(p.slots + token0 + threadIdx.x);
-        __syncthreads();
-        const int first = slots[0];
-        whole = __syncthreads_and(threadIdx.x >= kKvTile || (first >= 0 && (first & 15) == 0 && first < p.g.slots && slots[threadIdx.x] == first + (int)threadIdx.x));
+        const int sixteenth = threadIdx.x % kKvTile;
+        whole = __all_sync(0xffffffffu, first >= 0 && (first & 15) == 0 && first < p.g.slots && __ldg(p.slots + token0 + sixteenth) == first + sixteenth);
     }
     // whole warps go round together: the shuffles need every lane
     for (int at = threadIdx.x; at - (int)(threadIdx.x & 31) < items; at += kThreads) {
@@ -148,7 +147,7 @@ __global__ void __launch_bounds__(kThreads, 5) kv_quantize_kernel(const __grid_c
     }
     if (!whole) return;
     __syncthreads();
-    uint4 *const to = reinterpret_cast<uint4 *>(kv_tile_of(p, slots[0], head));
+    uint4 *const to = reinterpret_cast<uint4 *>(kv_tile_of(p, first, head));
     for (int i = threadIdx.x; i < kv_tile_words(blocks) / 4; i += kThreads) to[i] = reinterpret_cast<const uint4 *>(staged)[i];
 }
 
