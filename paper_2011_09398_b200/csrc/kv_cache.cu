@@ -110,11 +110,13 @@ __global__ void __launch_bounds__(kThreads, 5) kv_quantize_kernel(const __grid_c
     const int64_t token0 = (int64_t)group * kKvTile;
     const int tokens = (int)min(p.tokens - token0, (int64_t)kKvTile);
     const int threads_per_token = 4 * blocks, items = tokens * threads_per_token;
+    // the block's part of an address once, in 64 bits
+    const T *const key_rows = k + (token0 * p.k_token + head * p.k_head), *const value_rows = v + (token0 * p.v_token + head * p.v_head);
     Eight<T> ke, ve;
     const auto load = [&](int at) {
         const int token = at / threads_per_token, channel = 8 * (at - token * threads_per_token);
-        ke = load_eight<T, VEC>(k + (token0 + token) * p.k_token + head * p.k_head + channel, p.g.dim - channel);
-        ve = load_eight<T, VEC>(v + (token0 + token) * p.v_token + head * p.v_head + channel, p.g.dim - channel);
+        ke = load_eight<T, VEC>(key_rows + (token * p.k_token + channel), p.g.dim - channel);
+        ve = load_eight<T, VEC>(value_rows + (token * p.v_token + channel), p.g.dim - channel);
     };
     load(min((int)threadIdx.x, items - 1));  // on their way while the slots are
     // A whole tile, in order?  Every warp reads the sixteen slots for itself, which takes no barrier.
@@ -125,27 +127,40 @@ __global__ void __launch_bounds__(kThreads, 5) kv_quantize_kernel(const __grid_c
         whole = __all_sync(0xffffffffu, first >= 0 && (first & 15) == 0 && first < p.g.slots && __ldg(p.slots + token0 + sixteenth) == first + sixteenth);
     }
     // whole warps go round together: the shuffles need every lane
-    for (int at = threadIdx.x; at - (int)(threadIdx.x & 31) < items; at += kThreads) {
-        const bool there = at < items;
-        const int token = min(at, items - 1) / threads_per_token, in_row = min(at, items - 1) - token * threads_per_token;
-        const int block = in_row >> 2, quarter = in_row & 3, slot = __ldg(p.slots + token0 + token);
-        if (at >= kThreads) load(min(at, items - 1));
-        float kx[8], vx[8];
-        ke.expand(kx);
-        ve.expand(vx);
-        float ks, vs;
-        BlockScales<T>::find(ke, ve, ks, vs);
-        if (!there || slot < 0 || slot >= p.g.slots) continue;
-        uint32_t *const tile = whole ? staged : kv_tile_of(p, slot, head);
-        const int in_tile = slot % kKvTile;
-        tile[kv_key_word(blocks, in_tile, block, quarter)] = kv_codes<kValues<T>>(kx, ks);
-        const uint32_t codes = kv_codes<kValues<T>>(vx, vs);
-        uint16_t *const halves = reinterpret_cast<uint16_t *>(tile) + (in_tile & 1);
-        halves[2 * kv_value_word(blocks, in_tile >> 1, block, 2 * quarter)] = (uint16_t)codes;
-        halves[2 * kv_value_word(blocks, in_tile >> 1, block, 2 * quarter + 1)] = (uint16_t)(codes >> 16);
-        if (quarter == 0) tile[kv_scale_word(blocks, in_tile, block)] = (__float_as_uint(ks) >> 16) | (__float_as_uint(vs) & 0xffff0000u);
+    const auto items_to = [&](auto tile_of) {
+        for (int at = threadIdx.x; at - (int)(threadIdx.x & 31) < items; at += kThreads) {
+            const bool there = at < items;
+            const int token = min(at, items - 1) / threads_per_token, in_row = min(at, items - 1) - token * threads_per_token;
+            const int block = in_row >> 2, quarter = in_row & 3;
+            if (at >= kThreads) load(min(at, items - 1));
+            float kx[8], vx[8];
+            ke.expand(kx);
+            ve.expand(vx);
+            float ks, vs;
+            BlockScales<T>::find(ke, ve, ks, vs);
+            int in_tile;
+            uint32_t *const tile = tile_of(token, in_tile);
+            if (!there || !tile) continue;
+            tile[kv_key_word(blocks, in_tile, block, quarter)] = kv_codes<kValues<T>>(kx, ks);
+            const uint32_t codes = kv_codes<kValues<T>>(vx, vs);
+            uint16_t *const halves = reinterpret_cast<uint16_t *>(tile) + (in_tile & 1);
+            halves[2 * kv_value_word(blocks, in_tile >> 1, block, 2 * quarter)] = (uint16_t)codes;
+            halves[2 * kv_value_word(blocks, in_tile >> 1, block, 2 * quarter + 1)] = (uint16_t)(codes >> 16);
+            if (quarter == 0) tile[kv_scale_word(blocks, in_tile, block)] = (__float_as_uint(ks) >> 16) | (__float_as_uint(vs) & 0xffff0000u);
+        }
+    };
+    if (!whole) {
+        items_to([&](int token, int &in_tile) -> uint32_t * {
+            const int slot = __ldg(p.slots + token0 + token);
+            in_tile = slot % kKvTile;
+            return slot >= 0 && slot < p.g.slots ? kv_tile_of(p, slot, head) : nullptr;
+        });
+        return;
     }
-    if (!whole) return;
+    items_to([&](int token, int &in_tile) {
+        in_tile = token;
+        return staged;
+    });
     __syncthreads();
     uint4 *const to = reinterpret_cast<uint4 *>(kv_tile_of(p, first, head));
     for (int i = threadIdx.x; i < kv_tile_words(blocks) / 4; i += kThreads) to[i] = reinterpret_cast<const uint4 *>(staged)[i];
