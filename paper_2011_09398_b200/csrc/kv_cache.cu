@@ -127,11 +127,12 @@ __global__ void __launch_bounds__(kThreads, 5) kv_quantize_kernel(const __grid_c
         whole = __all_sync(0xffffffffu, first >= 0 && (first & 15) == 0 && first < p.g.slots && __ldg(p.slots + token0 + sixteenth) == first + sixteenth);
     }
     // whole warps go round together: the shuffles need every lane
-    const auto items_to = [&](auto tile_of) {
+    const auto items_to = [&](int items, auto tile_of) {
         for (int at = threadIdx.x; at - (int)(threadIdx.x & 31) < items; at += kThreads) {
             const bool there = at < items;
-            const int token = min(at, items - 1) / threads_per_token, in_row = min(at, items - 1) - token * threads_per_token;
+            const int token = (uint32_t)min(at, items - 1) / (uint32_t)threads_per_token, in_row = min(at, items - 1) - token * threads_per_token;
             const int block = in_row >> 2, quarter = in_row & 3;
+            __builtin_assume(block >= 0 && block < blocks);
             if (at >= kThreads) load(min(at, items - 1));
             float kx[8], vx[8];
             ke.expand(kx);
@@ -150,14 +151,14 @@ __global__ void __launch_bounds__(kThreads, 5) kv_quantize_kernel(const __grid_c
         }
     };
     if (!whole) {
-        items_to([&](int token, int &in_tile) -> uint32_t * {
+        items_to(items, [&](int token, int &in_tile) -> uint32_t * {
             const int slot = __ldg(p.slots + token0 + token);
             in_tile = slot % kKvTile;
             return slot >= 0 && slot < p.g.slots ? kv_tile_of(p, slot, head) : nullptr;
         });
         return;
     }
-    items_to([&](int token, int &in_tile) {
+    items_to(kKvTile * threads_per_token, [&](int token, int &in_tile) {
         in_tile = token;
         return staged;
     });
