@@ -202,18 +202,48 @@ __device__ __noinline__ static uint32_t kv_codes_any(float v0, float v1, float v
     return word;
 }
 
-// The same of f16 or bf16 values: x and s have 11 and 8 significant bits, so a quotient that is no tie is 2^-13 away from one at least
-// and rounding it to fp32 first (a product with the reciprocal and one correction by the remainder is that rounding) changes
-// nothing.  The sum with 1.5 * 2^23 + 8 rounds half to even and leaves n in its lowest bits; what stands above them adds up to a
-// constant.  Five operations a value where the general form takes twelve.
+// Two fp32 numbers in one operation
+__device__ __forceinline__ uint64_t pair_of(float x, float y)
+{
+    uint64_t v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(x), "f"(y));
+    return v;
+}
+__device__ __forceinline__ void of_pair(uint64_t v, float &x, float &y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t v;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(a), "l"(b), "l"(c));
+    return v;
+}
+__device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b)
+{
+    uint64_t v;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+    return v;
+}
+__device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b)
+{
+    uint64_t v;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+    return v;
+}
+
+// The same of f16 or bf16 values: x and s have 11 and 8 significant bits, so a quotient that is no tie is 2^-13 away from one at least.
+// The product with a reciprocal that is off by a unit or two is off by less than 2^-18; its remainder x - q s is exact to 2^-24 of
+// itself, and what the correction by it leaves is below 2^-40, so that a tie is hit and nothing else comes near one.  The sum with
+// 1.5 * 2^23 + 8 rounds half to even and leaves n in its lowest bits; what stands above them adds up to a constant.  Three operations
+// a value where the general form takes twelve.
 __device__ __forceinline__ uint32_t kv_codes_short(const float (&v)[8], float s)
 {
-    const float r = __frcp_rn(s);
+    float reciprocal;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(reciprocal) : "f"(s));
+    const uint64_t r = pair_of(reciprocal, reciprocal), less = pair_of(-s, -s), add = pair_of(12582920.0f, 12582920.0f);
     uint32_t word = 0;
 #pragma unroll
-    for (int i = 7; i >= 0; --i) {
-        const float q = v[i] * r, exact = fmaf(fmaf(-q, s, v[i]), r, q);
-        word = word * 16 + __float_as_uint(exact + 12582920.0f);
+    for (int i = 6; i >= 0; i -= 2) {
+        const uint64_t x = pair_of(v[i], v[i + 1]), q = mul_pair(x, r), n = add_pair(fma_pair(fma_pair(q, less, x), r, q), add);
+        word = (word * 16 + (uint32_t)(n >> 32)) * 16 + (uint32_t)n;
     }
     return word - 0x4b400000u * 0x11111111u;
 }

@@ -143,33 +143,6 @@ __device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t (&r)[16
         : "memory");
 }
 
-// Two fp32 numbers in one operation
-__device__ __forceinline__ uint64_t pair_of(float x, float y)
-{
-    uint64_t v;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(x), "f"(y));
-    return v;
-}
-__device__ __forceinline__ void of_pair(uint64_t v, float &x, float &y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
-__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c)
-{
-    uint64_t v;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(a), "l"(b), "l"(c));
-    return v;
-}
-__device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b)
-{
-    uint64_t v;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
-    return v;
-}
-__device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b)
-{
-    uint64_t v;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
-    return v;
-}
-
 // The B words of a place (a lane's of ROWS = 64 places, a token's of 16), plane by plane.
 template <int B, int ROWS>
 __device__ __forceinline__ void load_planes(const uint32_t *base, int place, uint32_t (&w)[B])
