@@ -4,7 +4,7 @@
 // 32 channels, whose largest value they find with two shuffles; no value is read twice.  A block of threads works on sixteen
 // consecutive tokens of a head, because that is what shares the cache's sectors: a token's values lie in two bytes each all over
 // its tile.  Where the sixteen are a whole tile (a prompt) they are put together in shared memory and leave in 16-byte stores.
-// 16384 tokens of 8 heads of 128 channels in bf16 (67 MB) are stored in 30 us and read back in 15; what bounds storing is the
+// 16384 tokens of 8 heads of 128 channels in bf16 (67 MB) are stored in 28 us and read back in 15; what bounds storing is the
 // quantiser's instructions (70 % of the issue slots), reading the stores (32768 tokens: 36 us, 4.7 TB/s).
 #include "kv_common.cuh"
 
@@ -99,9 +99,10 @@ struct BlockScales<__nv_bfloat16> : PairScales<__nv_bfloat16, __nv_bfloat162> {}
 template <typename T>
 constexpr int kValues = sizeof(T) == 4 ? KV_ANY : std::is_same<T, __half>::value ? KV_HALF : KV_SHORT;
 
-// BLOCKS of 32 channels; 0: p.g.blocks.
+// BLOCKS of 32 channels; 0: p.g.blocks.  16-bit values fit 40 registers and six blocks to an SM (16384 tokens in bf16 stored and read
+// back: five 44.6 us, six 43.1); fp32 would spill.
 template <typename T, bool VEC, int BLOCKS>
-__global__ void __launch_bounds__(kThreads, 5) kv_quantize_kernel(const __grid_constant__ KvRows p, const T *k, const T *v)
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 2 ? 6 : 5) kv_quantize_kernel(const __grid_constant__ KvRows p, const T *k, const T *v)
 {
     __shared__ __align__(16) uint32_t staged[kv_tile_words(kKvMaxDim / 32)];
     asm volatile("griddepcontrol.wait;" ::: "memory");

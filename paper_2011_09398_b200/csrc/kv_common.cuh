@@ -234,8 +234,13 @@ __device__ __forceinline__ uint64_t mul_pair(uint64_t a, uint64_t b)
 // itself, and what the correction by it leaves is below 2^-40, so that a tie is hit and nothing else comes near one.  The sum with
 // 1.5 * 2^23 + 8 rounds half to even and leaves n in its lowest bits; what stands above them adds up to a constant.  Three operations
 // a value where the general form takes twelve.
-__device__ __forceinline__ uint32_t kv_codes_short(const float (&v)[8], float s)
+__device__ __forceinline__ uint32_t kv_codes_short(float (&v)[8], float s, bool small)
 {
+    if (small && s < 0x1p-100f) {  // away from subnormal numbers, exactly
+        s *= 0x1p80f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= 0x1p80f;
+    }
     float reciprocal;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(reciprocal) : "f"(s));
     const uint64_t r = pair_of(reciprocal, reciprocal), less = pair_of(-s, -s), add = pair_of(12582920.0f, 12582920.0f);
@@ -250,10 +255,10 @@ __device__ __forceinline__ uint32_t kv_codes_short(const float (&v)[8], float s)
 
 enum { KV_ANY, KV_SHORT, KV_HALF };  // any fp32 numbers; f16 or bf16 ones; f16 ones, whose scales are above 2^-28
 template <int VALUES>
-__device__ __forceinline__ uint32_t kv_codes(const float (&v)[8], float s)
+__device__ __forceinline__ uint32_t kv_codes(float (&v)[8], float s)
 {
     if (!(s > 0.0f)) return kv_rotate(0x88888888u);  // all zeros, or NaN
-    if (VALUES == KV_HALF || (VALUES == KV_SHORT && s >= 0x1p-100f)) return kv_rotate(kv_codes_short(v, s));
+    if (VALUES != KV_ANY) return kv_rotate(kv_codes_short(v, s, VALUES == KV_SHORT));
     return kv_rotate(kv_codes_any(v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7], s));
 }
 
