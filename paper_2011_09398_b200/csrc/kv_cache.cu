@@ -5,7 +5,7 @@
 // consecutive tokens of a head, because that is what shares the cache's sectors: a token's values lie in two bytes each all over
 // its tile.  Where the sixteen are a whole tile (a prompt) they are put together in shared memory and leave in 16-byte stores.
 // 16384 tokens of 8 heads of 128 channels in bf16 (67 MB) are stored in 28 us and read back in 15; what bounds storing is the
-// quantiser's instructions (70 % of the issue slots), reading the stores (32768 tokens: 36 us, 4.7 TB/s).
+// quantiser's instructions (73 % of the issue slots), reading the stores (32768 tokens: 36 us, 4.7 TB/s).
 #include "kv_common.cuh"
 
 #include <type_traits>
