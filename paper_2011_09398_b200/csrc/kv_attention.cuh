@@ -30,7 +30,7 @@ struct AttnParams {
 // What a unit (a range of tiles for one tile of columns of a sequence) works on.
 struct Unit {
     int32_t seq, column0, chunks;
-    int32_t length, rows;                             // tokens of the sequence, its rows of q
+    int32_t length, rows;                             // tokens of the sequence, which its rows' positions follow from; its rows of q
     int64_t row0;                                     // its first row of q
     int32_t tile0, tile1;                             // the unit's tiles
     bool first, last;                                 // piece of its column tile
@@ -41,12 +41,15 @@ struct Sequence {
     int64_t row0;
 };
 
+// Tokens of a sequence that its row of the page table can hold; those behind are masked.
+__device__ __forceinline__ int32_t tokens_held(const AttnParams &p, int32_t length) { return min(length, p.table_tokens); }
+
 template <int COLUMNS>
 __device__ __forceinline__ Sequence sequence(const AttnParams &p, int b)
 {
     Sequence s{};
     if (b >= p.batch) return s;
-    s.length = min(max(__ldg(p.lengths + b), 0), p.table_tokens);
+    s.length = max(__ldg(p.lengths + b), 0);
     s.row0 = b;
     s.rows = 1;
     if (p.q_starts) {
@@ -56,10 +59,11 @@ __device__ __forceinline__ Sequence sequence(const AttnParams &p, int b)
     }
     s.column_tiles = (int32_t)(((int64_t)s.rows * p.group + COLUMNS - 1) / COLUMNS);
     // tiles that some row sees
+    const int32_t held = tokens_held(p, s.length);
     int32_t low = 0;
-    if (p.window > 0) low = (int32_t)max((int64_t)s.length - s.rows + 1 - p.window, (int64_t)0);
+    if (p.window > 0) low = (int32_t)min(max((int64_t)s.length - s.rows + 1 - p.window, (int64_t)0), (int64_t)held);
     s.first_tile = low / kKvTile;
-    s.tiles = max((s.length + kKvTile - 1) / kKvTile - s.first_tile, 0);
+    s.tiles = (held + kKvTile - 1) / kKvTile - s.first_tile;
     return s;
 }
 
@@ -151,8 +155,9 @@ __device__ __forceinline__ void column_range(const AttnParams &p, const Unit &u,
     *lo = *hi = 0;
     if (row >= u.rows) return;
     const int64_t position = (int64_t)u.length - u.rows + row;
-    *hi = p.causal ? (int32_t)min(max(position + 1, (int64_t)0), (int64_t)u.length) : u.length;
-    *lo = p.window > 0 ? (int32_t)min(max(position + 1 - p.window, (int64_t)0), (int64_t)u.length) : 0;
+    const int32_t held = tokens_held(p, u.length);
+    *hi = p.causal ? (int32_t)min(max(position + 1, (int64_t)0), (int64_t)held) : held;
+    *lo = p.window > 0 ? (int32_t)min(max(position + 1 - p.window, (int64_t)0), (int64_t)held) : 0;
 }
 
 __device__ __forceinline__ void store_element(void *p, int32_t type, int64_t i, float v)

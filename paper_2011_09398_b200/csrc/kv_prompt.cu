@@ -493,17 +493,18 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
         // ---- keys and values: from 4 bits to f16 operands ------------------------------------------------
         const int thread = threadIdx.x - 32 * kSoftmaxWarps, producer = warp - kSoftmaxWarps;
         const int32_t *const table = p.page_table + (int64_t)u.seq * p.table_pages;
+        const int32_t held = tokens_held(p, u.length);
         Raw<B> even_raw, odd_raw;
         int32_t page = -1;  // two tiles ahead; words one
         if (tiles > 0) {
-            load_raw<B>(p, find_page(p, table, u.length, tile0, lane), head, u.length, tile0, thread, even_raw);
-            page = find_page(p, table, u.length, tile0 + 1, lane);
+            load_raw<B>(p, find_page(p, table, held, tile0, lane), head, held, tile0, thread, even_raw);
+            page = find_page(p, table, held, tile0 + 1, lane);
         }
         int32_t value_exponent = -1000;
         // One tile; false where a wait gave up.
         const auto produce = [&](int j, const Raw<B> &raw, Raw<B> &next) -> bool {
-            if (j + 1 < tiles) load_raw<B>(p, page, head, u.length, tile0 + j + 1, thread, next);
-            page = find_page(p, table, u.length, tile0 + j + 2, lane);
+            if (j + 1 < tiles) load_raw<B>(p, page, head, held, tile0 + j + 1, thread, next);
+            page = find_page(p, table, held, tile0 + j + 2, lane);
             const int stage = j & 1, turn = j & 1;
             // the largest scales of the tile (bits of bf16 numbers compare like integers; a NaN does not count)
             uint32_t nan = 0, top_k = 0, top_v = 0;
