@@ -367,13 +367,13 @@ __device__ __forceinline__ void tile_step(const uint32_t *tile, int32_t token0, 
     if (Q > 4) plane_scores<B, NT, SPLIT, (Q > 4 ? 4 : 0), 4>(tile, w, sc, s);
     if (T) plane_scores<B, NT, SPLIT, (T ? Q : 0), 2>(tile, w, sc, s);
     if (S) plane_scores<B, NT, SPLIT, B - 1, 1>(tile, w, sc, s);
-    bool shown[2][NT][2];
+    bool shown[2][NT][2], some[2];
     uint32_t largest = 0;  // scale of a value of the lane's tokens, in the high half
     float highest = -INFINITY;
     float e[2][NT][2];     // log2 of the weights first
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
-        bool some = !MASKED;
+        some[r] = !MASKED;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -384,18 +384,23 @@ __device__ __forceinline__ void tile_step(const uint32_t *tile, int32_t token0, 
                     const int32_t token = token0 + 8 * r + (lane >> 2);
                     shown[r][nt][j] = token >= w.lo[nt][j] && token < w.hi[nt][j];
                     if (!shown[r][nt][j]) e[r][nt][j] = -INFINITY;
-                    some = some || shown[r][nt][j];
+                    some[r] = some[r] || shown[r][nt][j];
                 }
                 highest = fmaxf(highest, e[r][nt][j]);
             }
 #pragma unroll
-        for (int b = 0; b < B; ++b) largest = max(largest, some ? sc[r][b] : 0u);
+        for (int b = 0; b < B; ++b) largest = max(largest, some[r] ? sc[r][b] : 0u);
     }
     if (__any_sync(0xffffffffu, largest > w.high || highest > w.limit)) {
         // rare behind the first tiles: the references move up and the sums with them
         const float old_shift = w.shift;
+        largest = 0;  // again, without those that are NaN: their blocks' results are, the others keep their reference
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int b = 0; b < B; ++b) largest = max(largest, some[r] && sc[r][b] < 0x7f800000u ? sc[r][b] : 0u);
         largest = __reduce_max_sync(0xffffffffu, largest);
-        if (largest > w.high && largest < 0x7f800000u) {  // a NaN moves nothing
+        if (largest > w.high) {
             const int x = max((int)(largest >> 23) - 126, -100);  // scales < 2^x; the weights themselves stay in range
             w.shift = kHeadroom - (float)x;
             w.high = (uint32_t)(127 + x) << 23 | 0xffffu;

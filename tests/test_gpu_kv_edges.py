@@ -44,3 +44,19 @@ def test_positions_where_the_table_is_shorter_than_the_sequence(dtype, causal, w
         args = s.arguments()
         args[4] = torch.tensor(lengths, dtype=torch.int32, device=DEV)
         check(lce.lce_kv_attention(*args, causal=causal, window=window), expected_of_lengths(s, lengths, causal, window))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("size", [1e6, 1.0, 1e-9])
+@pytest.mark.parametrize("new", [1, 12])
+@pytest.mark.parametrize("at", [5, 35])
+def test_values_next_to_a_block_that_is_not_finite(dtype, size, new, at):
+    """A block of NaN leaves the others of its tile as they are, whatever their size."""
+    s = Setup(dtype, [40], [new], 1, 2, 64, seed=51)
+    s.v *= size
+    s.v[at, 0, 40] = float("inf")
+    s.store()
+    out, bound = s.expected()
+    rows = torch.arange(new) >= at - (40 - new)  # those that see it
+    assert np.isfinite(out[:, :, :32]).all() and np.isnan(out[rows.numpy()][:, :, 32:]).all() and np.isfinite(out[~rows.numpy()]).all()
+    check(lce.lce_kv_attention(*s.arguments()), (out, bound))
