@@ -412,7 +412,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_prompt_kernel(const __grid_con
                     exponent = info.value_exponent;
                 }
                 const uint64_t f2 = pair_of(f, f), plus = pair_of(kHeadroom - top, kHeadroom - top);
-                const bool masked = !all && f == 0.0f;  // 0 times minus infinity
+                const bool masked = !all && !(f > 0.0f);  // 0, or what a row that is not finite has, times minus infinity
                 // the first half of the weights is worked on while the second is made
 #pragma unroll
                 for (int c = 0; c < 8; ++c) {

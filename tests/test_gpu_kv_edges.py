@@ -60,3 +60,13 @@ def test_values_next_to_a_block_that_is_not_finite(dtype, size, new, at):
     rows = torch.arange(new) >= at - (40 - new)  # those that see it
     assert np.isfinite(out[:, :, :32]).all() and np.isnan(out[rows.numpy()][:, :, 32:]).all() and np.isfinite(out[~rows.numpy()]).all()
     check(lce.lce_kv_attention(*s.arguments()), (out, bound))
+
+
+def test_many_rows_that_are_not_finite_and_see_nothing():
+    """A row that sees no token is 0 whatever it holds."""
+    s = Setup(F16, [700, 20], [500, 64], 2, 4, 64, page=16, seed=52, table_extra=400)
+    want = s.expected()
+    s.q[503, 1, 5], s.q[520] = float("inf"), float("nan")  # at positions -41 and -24
+    got = lce.lce_kv_attention(*s.arguments())
+    assert not got[500:544].any()
+    check(got, want)
