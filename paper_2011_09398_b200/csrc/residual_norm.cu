@@ -98,6 +98,34 @@ __device__ __forceinline__ A row_norm(A (&v)[N][8], int kind, const NormParams &
     return inverse_root(row_sum(squares_of(v), p.row_threads, warps[1]) * each + A(p.eps));
 }
 
+// Results of the arithmetic rounded to an output's type, once: fp64 to 16 bits by way of fp32 would round twice.
+template <typename T>
+__device__ __forceinline__ T rounded(float v) { return from_float<T>(v); }
+template <typename T>
+__device__ __forceinline__ T rounded(double v);
+template <>
+__device__ __forceinline__ float rounded<float>(double v) { return (float)v; }
+template <>
+__device__ __forceinline__ __half rounded<__half>(double v) { return __double2half(v); }
+template <>
+__device__ __forceinline__ __nv_bfloat16 rounded<__nv_bfloat16>(double v) { return __double2bfloat16(v); }
+
+template <typename T, bool VEC, typename A>
+__device__ __forceinline__ void store_rounded(T *p, int count, const A (&v)[8])
+{
+    if (VEC) {
+        if (count <= 0) return;
+        Eight<T> r;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r.e[i] = rounded<T>(v[i]);
+        store_eight(p, r);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < count) p[i] = rounded<T>(v[i]);
+    }
+}
+
 template <typename TS, typename TB>
 struct NormRow {  // one row's tensors
     const TS *x;
@@ -213,11 +241,7 @@ __device__ __forceinline__ void norm_row(const NormParams &p, const NormRow<TS, 
     }
     if (row.y) {
 #pragma unroll
-        for (int k = 0; k < N; ++k) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = (float)v[k][i];
-            store8<TS, VEC>(row.y + channel[k], p.channels - channel[k], f);
-        }
+        for (int k = 0; k < N; ++k) store_rounded<TS, VEC>(row.y + channel[k], p.channels - channel[k], v[k]);
     }
     if (!row.normed && !row.packed) return;
     const A factor = p.pre_norm != LCE_NORM_NONE ? row_norm(v, p.pre_norm, p, channel, warps + 2) : A(1);
@@ -227,11 +251,7 @@ __device__ __forceinline__ void norm_row(const NormParams &p, const NormRow<TS, 
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[k][i] *= factor;
         affine(k, p.pre_weight, p.pre_bias);
-        if (row.normed) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = (float)v[k][i];
-            store8<TB, VEC>(row.normed + channel[k], count, f);
-        }
+        if (row.normed) store_rounded<TB, VEC>(row.normed + channel[k], count, v[k]);
         // eight bits are a byte of their word: lowest channel lowest, the lowest byte first in memory
         if (row.packed && channel[k] < 8 * p.vectors) {
             uint32_t bits = 0;
