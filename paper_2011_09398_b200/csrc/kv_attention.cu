@@ -824,7 +824,7 @@ lce_status make_params(const lce_kv_attention_desc *d, bool one_row, AttnParams 
         if (s < 0 || s >= (1ll << 40)) return LCE_ERR_INVALID_ARG;
     p->batch = d->batch; p->group = d->heads / d->cache.kv_heads; p->table_pages = d->table_pages;
     p->one_row = one_row;
-    if (d->tokens * d->heads >= (1ll << 31) || (int64_t)d->table_pages * d->cache.page_size >= (1ll << 31) || d->batch >= (1 << 20)) return LCE_ERR_UNSUPPORTED;
+    if (d->tokens >= (1ll << 31) || d->tokens * d->heads >= (1ll << 31) || (int64_t)d->table_pages * d->cache.page_size >= (1ll << 31) || d->batch >= (1 << 20)) return LCE_ERR_UNSUPPORTED;
     p->table_tokens = d->table_pages * d->cache.page_size;
     p->causal = d->causal; p->window = d->window; p->type = d->type;
     p->tokens = d->tokens;
