@@ -323,7 +323,7 @@ __device__ __forceinline__ void plane_values(const uint32_t *tile, Warp<B, NT, S
 }
 
 template <int B, int NT, bool SPLIT, bool MASKED>
-__device__ __forceinline__ void tile_step(const uint32_t *tile, int32_t token0, Warp<B, NT, SPLIT> &w)
+__device__ __forceinline__ void tile_step(const uint32_t *tile, int32_t token0, int32_t least_exponent, Warp<B, NT, SPLIT> &w)
 {
     constexpr int Q = B / 4 * 4;
     constexpr bool T = (B & 2) != 0, S = (B & 1) != 0;
@@ -401,7 +401,7 @@ __device__ __forceinline__ void tile_step(const uint32_t *tile, int32_t token0, 
             for (int b = 0; b < B; ++b) largest = max(largest, some[r] && sc[r][b] < 0x7f800000u ? sc[r][b] : 0u);
         largest = __reduce_max_sync(0xffffffffu, largest);
         if (largest > w.high) {
-            const int x = max((int)(largest >> 23) - 126, -100);  // scales < 2^x; the weights themselves stay in range
+            const int x = max((int)(largest >> 23) - 126, least_exponent);  // scales < 2^x; the weights' sum stays in range
             w.shift = kHeadroom - (float)x;
             w.high = (uint32_t)(127 + x) << 23 | 0xffffu;
             w.limit = w.shift + kRise;
@@ -528,8 +528,8 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(B, NT, SPLIT)) kv_atte
         __syncwarp();
         if (!(good & 1)) continue;
         const uint32_t *const tile = ring + stage * TILE;
-        if (token0 >= all_lo && token0 + kKvTile <= all_hi) tile_step<B, NT, SPLIT, false>(tile, token0, w);
-        else tile_step<B, NT, SPLIT, true>(tile, token0, w);
+        if (token0 >= all_lo && token0 + kKvTile <= all_hi) tile_step<B, NT, SPLIT, false>(tile, token0, p.least_exponent, w);
+        else tile_step<B, NT, SPLIT, true>(tile, token0, p.least_exponent, w);
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
     if (p.solo) {
@@ -826,6 +826,10 @@ lce_status make_params(const lce_kv_attention_desc *d, bool one_row, AttnParams 
     p->one_row = one_row;
     if (d->tokens >= (1ll << 31) || d->tokens * d->heads >= (1ll << 31) || (int64_t)d->table_pages * d->cache.page_size >= (1ll << 31) || d->batch >= (1 << 20)) return LCE_ERR_UNSUPPORTED;
     p->table_tokens = d->table_pages * d->cache.page_size;
+    // A weight is at most 2^(kHeadroom + kRise - x): with x no less than this, the sum of a whole table's stays below 2^127.
+    int bits = 0;
+    while ((1ll << bits) < p->table_tokens) ++bits;
+    p->least_exponent = std::max(-100, bits + (int)(kHeadroom + kRise) - 127);
     p->causal = d->causal; p->window = d->window; p->type = d->type;
     p->tokens = d->tokens;
     p->q_token = d->q_token_stride; p->q_head = d->q_head_stride; p->out_token = d->out_token_stride; p->out_head = d->out_head_stride;

@@ -14,6 +14,7 @@ struct AttnParams {
     int64_t tokens;
     int64_t q_token, q_head, out_token, out_head;
     float scale;                       // times log2(e)
+    int32_t least_exponent;            // of the scales' reference, in the kernel for few rows
     const void *q;
     const uint32_t *cache;
     const int32_t *page_table, *lengths, *q_starts;

@@ -70,3 +70,16 @@ def test_many_rows_that_are_not_finite_and_see_nothing():
     got = lce.lce_kv_attention(*s.arguments())
     assert not got[500:544].any()
     check(got, want)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("size", [-102, -98, -90, -60, 0, 60])
+def test_values_of_any_size_over_a_long_sequence(dtype, size):
+    """Equal weights: the sum of 300000 of them stays within fp32 next to the smallest values."""
+    tokens = 300000
+    s = Setup(dtype, [tokens], [1], 1, 1, 32, page=128, seed=53, q_size=0.0)
+    s.v = torch.ldexp(torch.ones(tokens, 1, 32, device=DEV), torch.tensor(size, device=DEV)).to(dtype) * 7
+    s.store()
+    got = lce.lce_kv_attention(*s.arguments()).double().cpu().numpy()
+    # all the values are the same: weights and their sum are exact powers of two times counts, the rest is the output's rounding
+    np.testing.assert_allclose(got, 7 * 2.0 ** size, rtol=2.0 ** -8 if dtype == BF16 else (tokens // 16 + 65) * 2.0 ** -23, atol=0)
