@@ -56,3 +56,30 @@ def test_wait_probe_rejects_limits_outside_its_range():
         with pytest.raises(lce.LceError) as e:
             lce.lce_device_wait_probe(bad)
         assert e.value.status == 1
+
+
+def test_attention_of_many_rows_refuses_after_an_expired_wait_until_the_reset():
+    """The kernel for many rows waits in the same bounded way and reports to the same place; the one for few rows waits for nothing."""
+    rng = np.random.default_rng(4)
+    heads, dim, tokens, page = 4, 64, 1024, 64
+    kv = lce.make_kv_desc(tokens // page, page, 1, dim)
+    cache = torch.empty(lce.lce_kv_cache_bytes(kv), dtype=torch.uint8, device=DEV)
+    k, v, q = (torch.from_numpy(rng.standard_normal((tokens, n, dim))).half().to(DEV) for n in (1, 1, heads))
+    lce.lce_kv_quantize(kv, k, v, torch.arange(tokens, dtype=torch.int32, device=DEV), cache)
+    table = torch.arange(tokens // page, dtype=torch.int32, device=DEV).view(1, -1)
+    lengths, starts = torch.tensor([tokens], dtype=torch.int32, device=DEV), torch.tensor([0, tokens], dtype=torch.int32, device=DEV)
+    many = lambda: lce.lce_kv_attention(kv, q, cache, table, lengths, starts)
+    one = lambda: lce.lce_kv_attention(kv, q[-1:], cache, table, lengths)
+    before, last = many(), one()
+    assert lce.lce_device_status() == 0
+    try:
+        lce.lce_device_wait_probe(20_000)
+        torch.cuda.synchronize()
+        assert lce.lce_device_status() == 1
+        with pytest.raises(lce.LceError) as e:
+            many()
+        assert e.value.status == 5
+        assert torch.equal(one(), last)
+    finally:
+        lce.lce_device_status_reset()
+    assert torch.equal(many(), before) and lce.lce_device_status() == 0
