@@ -394,12 +394,15 @@ __device__ __forceinline__ void tile_step(const uint32_t *tile, int32_t token0, 
     if (__any_sync(0xffffffffu, largest > w.high || highest > w.limit)) {
         // rare behind the first tiles: the references move up and the sums with them
         const float old_shift = w.shift;
-        largest = 0;  // again, without those that are NaN: their blocks' results are, the others keep their reference
-#pragma unroll
-        for (int r = 0; r < 2; ++r)
-#pragma unroll
-            for (int b = 0; b < B; ++b) largest = max(largest, some[r] && sc[r][b] < 0x7f800000u ? sc[r][b] : 0u);
         largest = __reduce_max_sync(0xffffffffu, largest);
+        if (largest >= 0x7f800000u) {  // again without those that are NaN: their blocks' results are, the others keep their reference
+            largest = 0;
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+#pragma unroll
+                for (int b = 0; b < B; ++b) largest = max(largest, some[r] && sc[r][b] < 0x7f800000u ? sc[r][b] : 0u);
+            largest = __reduce_max_sync(0xffffffffu, largest);
+        }
         if (largest > w.high) {
             const int x = max((int)(largest >> 23) - 126, least_exponent);  // scales < 2^x; the weights' sum stays in range
             w.shift = kHeadroom - (float)x;
