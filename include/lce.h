@@ -324,15 +324,21 @@ lce_status lce_kv_dequantize(const lce_kv_desc *desc, const void *cache, const i
  * at slot page_table[b][t / page_size] * page_size + t % page_size, and n = q_starts[b + 1] - q_starts[b] rows of q
  * (q_starts NULL: one row each, tokens == batch).  Its row i stands at position p = lengths[b] - n + i, and for query head h
  *   out = sum_t softmax_t(scale q . k_t) v_t   over tokens t < lengths[b],  t <= p if causal,  t > p - window if window > 0
- * with keys and values of head h / (heads / kv_heads).  A row that sees no token (an empty sequence, p < 0) is 0.
- *   q, out      [tokens][heads][head_dim] of `type`, strides in elements as above; out rows that belong to no sequence stay
+ * with keys and values of head h / (heads / kv_heads).  A row that sees no token (of an empty sequence, say, or at p < 0 where causal)
+ * is 0 whatever it holds.
+ *   q, out      [tokens][heads][head_dim] of `type`, strides in elements as above, rows of out apart from one another; out rows that
+ *               belong to no sequence stay
  *   page_table  int32[batch][table_pages]; tokens on a page outside the pool are masked, and so are those behind
- *               table_pages * page_size
+ *               table_pages * page_size (positions follow from lengths[b] all the same)
  *   lengths     int32[batch], q_starts int32[batch + 1] from 0 to tokens, none decreasing; all on the device, so a captured
  *               call serves growing sequences
  *   workspace   lce_kv_attention_workspace_bytes(desc) bytes, 16-byte aligned; it needs no clearing and belongs to the call
  *               until its kernels are done (calls that may overlap need one each)
- * Long sequences are cut into pieces that are worked on side by side and joined in a fixed order: results repeat bit for bit. */
+ * Long sequences are cut into pieces that are worked on side by side and joined in a fixed order: results repeat bit for bit.
+ * Scores, the softmax's statistics and the sums are fp32.  The weights that meet the values are rounded to f16 (each off by 2^-11 at most),
+ * for fp32 rows to 22 bits, and in 16-bit rows products are cut at 2^-14 of a block's scale times |q|: about a half step of fp16 in all.
+ * Values whose scale is below 2^-24 (fp32 rows: 2^-12) of the largest that the rows worked on together see are off by up to 2^-31 of
+ * that largest.  All this for value scales between 2^-94 and 2^90. */
 typedef struct {
     lce_kv_desc cache;
     int32_t batch, heads, table_pages;

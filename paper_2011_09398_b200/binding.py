@@ -359,8 +359,8 @@ def lce_kv_attention(desc: KvDesc, q: torch.Tensor, cache: torch.Tensor, page_ta
                      out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention of q [tokens, heads, head_dim] over the 4-bit cache.  page_table int32 [sequences, pages]; lengths int32
     [sequences], the new tokens included; q_starts int32 [sequences + 1] where a sequence's rows of q begin (None: one row for
-    each sequence).  scale: 1 / sqrt(head_dim) when None.  Rows of no sequence stay as they are in `out`.  out and workspace (uint8, lce_kv_attention_workspace_bytes) are allocated with
-    torch when not given."""
+    each sequence).  scale: 1 / sqrt(head_dim) when None.  Rows of no sequence stay as they are in `out` (arbitrary where it is not
+    given).  out and workspace (uint8, lce_kv_attention_workspace_bytes for the same dtype) are allocated with torch when not given."""
     return _native.kv_attention(desc, q, cache, page_table, lengths, q_starts, desc.head_dim ** -0.5 if scale is None else scale,
                                 causal, window, out, workspace)
 

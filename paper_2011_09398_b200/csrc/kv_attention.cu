@@ -16,10 +16,11 @@
 // sequences of 1 - 8192 tokens (236 MB) 84 us.  A warp spends 340 instructions on 16 tokens of 128 channels and 8 columns, of them 24
 // matrix products; the issue slots are 55% busy, with the registers for four warps a scheduler.
 //
-// Scores and the running softmax are fp32.  Q is f16 times a power of two chosen for each row, exact for f16 and bf16 rows up to
-// what lies 2^-29 below the row's largest; p is rounded to f16 (relative error 2^-11 of each weight, which is what an fp16
-// result has, and averages out).  fp32 rows take Q and p as two f16 numbers each (22 bits), and codes as f16 c = n - 8: 1024 + n by
-// one AND-OR, less 1032 by one packed add.
+// Scores and the running softmax are fp32.  Q is f16 times a power of two chosen for each row.  Odd channels, whose codes count 16 times as
+// they stand, are held as a sixteenth: f16 rows are exact where a number is not below 2^-24 of its row's largest, bf16 rows where it is
+// not below 2^-27, and what is lost of smaller ones is below 2^-35 of the largest.  p is rounded to f16 (relative error 2^-11 of each
+// weight, which is what an fp16 result has, and averages out): matrix products of more bits would take twice as many.  fp32 rows take Q
+// and p as two f16 numbers each (22 bits), and codes as f16 c = n - 8: 1024 + n by one AND-OR, less 1032 by one packed add.
 #include "kv_attention.cuh"
 
 #include <math.h>

@@ -131,8 +131,6 @@ __device__ __forceinline__ Eight<T> load_eight(const T *p, int count)
     }
     return r;
 }
-template <typename T, bool VEC>
-__device__ __forceinline__ void load8(const T *p, int count, float (&v)[8]) { load_eight<T, VEC>(p, count).expand(v); }
 template <typename T>
 __device__ __forceinline__ void store_eight(T *p, const Eight<T> &r)
 {

@@ -16,8 +16,10 @@
 //
 // Per 128 tokens and 256 columns of 128 channels: four products of 512 clocks at the tensor cores' rate (those for the scores take longer:
 // both operands come from shared memory), 32768 exponentials at 16 a clock, 2048 clocks, and 8000 instructions, 2000 clocks.  Measured
-// 2.5 us, 1.84 with the products alone, and 13 us to begin and end a block: 16384 tokens and 4096 columns of 8 heads 347 us (792
+// 2.5 us, 1.84 with the products alone, and 13 us to begin and end a block: 16384 tokens and 4096 columns of 8 heads 394 us (697
 // TFLOP/s), two sequences of 1024 rows of 4 columns on 5120 tokens 262 us (1140 on the kernel for few rows).
+//
+// Scores, softmax and sums are fp32.  Weights are rounded to f16 (2^-11 of each, as in the kernel for few rows): what the products take.
 #include "kv_attention.cuh"
 #include "mx_common.cuh"
 
