@@ -105,3 +105,22 @@ def test_one_token_that_takes_all_the_weight(dtype, dim, group):
           (0.0 if dtype == F32 else 34 * 2.0 ** -15 * step) + 2.0 ** -31 * 1099 * most
     assert (np.abs(got - out) <= off).all(), (np.abs(got - out) - off).max()
     assert (off < 0.5 * step).all()  # another token, or a code more or less, would be seen
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_thousands_of_sequences_of_all_lengths(dtype):
+    """The search for a block's work goes through them 32 at a time: empty ones, some without rows, a long one among them in pieces."""
+    rng = np.random.default_rng(63)
+    lengths, news = rng.integers(0, 40, 4101).tolist(), rng.integers(0, 4, 4101).tolist()
+    lengths[2600], news[2600], lengths[4100], news[4100] = 3000, 2, 17, 5
+    s = Setup(dtype, lengths, news, 1, 2, 32, seed=63)
+    assert room(s, False) > 16
+    args = s.arguments()
+    want = s.expected()
+    check(lce.lce_kv_attention(*args), want)
+    one = np.concatenate([[0], np.cumsum(news)])[:-1][np.array(news) > 0]  # the first row of each that has one, by itself
+    keep = torch.from_numpy(one).to(DEV)
+    has = torch.from_numpy(np.flatnonzero(np.array(news) > 0)).to(DEV)
+    shorter = torch.tensor(np.array(lengths) - np.array(news) + 1, dtype=torch.int32, device=DEV)  # where that row stands last
+    got = lce.lce_kv_attention(s.desc, s.q[keep], s.cache, args[3][has], shorter[has])
+    check(got, (want[0][one], want[1][one]))
