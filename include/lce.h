@@ -379,6 +379,90 @@ lce_status lce_residual_norm(const lce_residual_norm_desc *desc, const void *x, 
                              const float *post_weight, const float *post_bias, const float *pre_weight, const float *pre_bias,
                              void *y, void *normed, uint32_t *packed, void *stream);
 
+/* Rotary positions: the pairs (x, y) of a head's first rotary_dim channels turn by the angle position * f_i,
+ *   (x, y) -> amplitude (x cos - y sin, x sin + y cos),   i = 0 .. rotary_dim / 2 - 1
+ * with channels i and i + rotary_dim / 2 for a pair (HALVES) or 2 i and 2 i + 1 (PAIRS); the channels behind are copied as they are.
+ * The frequencies are an input, as steps: the part of a turn by which one position turns a pair, in units of 2^-64 turns, so that
+ * position * step modulo 2^64 is the angle at any position, exactly.  lce_rotary_steps makes the usual ones (HOST function, and
+ * `steps` is a HOST array of rotary_dim / 2, to be brought to the device once):
+ *   PLAIN    f_i = base^(-2 i / rotary_dim)
+ *   LINEAR   f_i / factor
+ *   BASE     f_i with the base times factor^(rotary_dim / (rotary_dim - 2))
+ *   PARTS    f_i (g + (1 - g) / factor), g = clamp((r - low_turns) / (high_turns - low_turns), 0, 1) where r = original_length f_i / 2 pi
+ *            is the number of turns over the length that a model was made for: fast pairs stay, slow ones are stretched
+ * Steps of one's own are 2^64 f / 2 pi modulo 2^64; negated steps turn back, which with the same amplitude is also the gradient. */
+typedef enum { LCE_ROTARY_HALVES = 0, LCE_ROTARY_PAIRS = 1 } lce_rotary_layout;
+typedef enum { LCE_ROTARY_PLAIN = 0, LCE_ROTARY_LINEAR = 1, LCE_ROTARY_BASE = 2, LCE_ROTARY_PARTS = 3 } lce_rotary_scaling;
+lce_status lce_rotary_steps(int32_t rotary_dim, int32_t scaling, double base, double factor, double original_length, double low_turns,
+                            double high_turns, uint64_t *steps);
+
+/*   q, k        [tokens][q_heads or k_heads][head_dim] of `type`, channels next to one another; strides in elements between tokens and
+ *               between heads, not negative.  head_dim 1 .. 256, rotary_dim even, 0 .. head_dim.  k_heads 0: no k
+ *   positions   int32[tokens], any sign
+ *   q_out, k_out  likewise; q_out may be q with q's strides, k_out k with k's.  Rows of an output must be apart from one another
+ * Angles are exact to 2^-32 of a turn, sines and cosines to 2^-23, products and sums fp32, rounded to `type` once.  tokens == 0 is a no-op. */
+typedef struct {
+    int32_t head_dim, rotary_dim;
+    int32_t layout;                /* lce_rotary_layout */
+    int32_t type;                  /* lce_type */
+    int32_t q_heads, k_heads;
+    float amplitude;
+    int64_t tokens;
+    int64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride;
+    int64_t q_out_token_stride, q_out_head_stride, k_out_token_stride, k_out_head_stride;
+} lce_rotary_desc;
+lce_status lce_rotary(const lce_rotary_desc *desc, const void *q, const void *k, const int32_t *positions, const uint64_t *steps, void *q_out,
+                      void *k_out, void *stream);
+
+/* How much attention each token of the cache gets from its sequence's newest rows: for sequence b, key/value head h and token t < lengths[b]
+ *   out[b][h][t] = decay * previous[b][h][t] + sum over the rows i of b and the query heads of h of softmax_t(scale q . k_t)
+ * with the rows, positions and masks of lce_kv_attention (which these are the weights of).  The tokens that the rows themselves stand at, the
+ * last n of the sequence, are new: what `previous` holds for them does not count.  So a buffer that carries the sums from call to call
+ * needs no clearing as sequences grow.  A row that sees no token adds nothing; one that is not finite, or sees a key that is not, makes
+ * the weights of all tokens that it sees NaN.  A sequence without rows is only decayed.
+ *   previous    fp32, or NULL (zeros); may be `out` with its strides.  With decay 0 it is not read
+ *   out         fp32 [batch][kv_heads][table_pages * page_size], strides in elements between sequences and between heads; nothing
+ *               behind a sequence's last token changes
+ *   workspace   lce_kv_attention_weights_workspace_bytes(desc) bytes, 16-byte aligned, no clearing, the call's until its kernels are done
+ * The other arguments as for lce_kv_attention.  Everything is fp32: 16-bit rows of q meet the cache's keys without a rounding (of
+ * channels below 2^-24 of their row's largest a part is lost), fp32 rows are taken in 22 bits.  No sum depends on the order in which blocks run:
+ * results repeat bit for bit. */
+typedef struct {
+    lce_kv_desc cache;
+    int32_t batch, heads, table_pages;
+    int32_t type;                  /* lce_type of q */
+    int32_t causal, window;        /* 0 or 1; 0: none */
+    float scale, decay;
+    int64_t tokens;                /* rows of q */
+    int64_t q_token_stride, q_head_stride;
+    int64_t previous_seq_stride, previous_head_stride, out_seq_stride, out_head_stride;
+} lce_kv_attention_weights_desc;
+size_t lce_kv_attention_weights_workspace_bytes(const lce_kv_attention_weights_desc *desc);
+lce_status lce_kv_attention_weights(const lce_kv_attention_weights_desc *desc, const void *q, const void *cache, const int32_t *page_table,
+                                    const int32_t *lengths, const int32_t *q_starts, const float *previous, float *out, void *workspace,
+                                    size_t workspace_bytes, void *stream);
+
+/* Eviction: of each sequence's tokens every key/value head keeps `budget`, those with the highest scores, and their rows move to pages of
+ * their own.  Of n = lengths[b] tokens (those on a page outside the pool and those behind the table do not count and are dropped) a head keeps
+ * all where they are no more than the budget; otherwise the first `first` and the last `recent` of the n places, and of the others those
+ * with the highest scores: ties go to the earlier token, a NaN is below every number.  What a head keeps stays in its order; the j-th goes to
+ *   slot kept_table[b][j / page_size] * page_size + j % page_size
+ * and the heads of a slot may then hold different tokens.  Pages of kept_table must not be among those that the call reads, nor come twice (the rows
+ * of a page outside the pool are not written; what else such a page holds stays).
+ *   scores        fp32 [batch][kv_heads][..], strides in elements; a head stride of 0 makes all heads keep the same tokens
+ *   kept          int32 [batch][kv_heads][budget]: the places that each kept token came from, ascending, -1 behind the last
+ *   kept_lengths  int32 [batch]: how many there are
+ *   kept_scores   fp32 [batch][kv_heads][..] with strides of its own, or NULL: their scores in `budget` places, 0 behind the last
+ * Nothing else of the cache changes: its old pages are the caller's again.  first + recent <= budget <= kept_pages * page_size. */
+typedef struct {
+    lce_kv_desc cache;
+    int32_t batch, table_pages, kept_pages;
+    int32_t budget, first, recent;
+    int64_t scores_seq_stride, scores_head_stride, kept_scores_seq_stride, kept_scores_head_stride;
+} lce_kv_evict_desc;
+lce_status lce_kv_evict(const lce_kv_evict_desc *desc, void *cache, const int32_t *page_table, const int32_t *lengths, const float *scores,
+                        const int32_t *kept_table, int32_t *kept, int32_t *kept_lengths, float *kept_scores, void *stream);
+
 /* Status of the bounded device-side waits.  The tensor-core kernel's warps meet through mbarriers
  * (operands ready, MMAs complete, accumulator read out); every such wait is limited to 0.2 s, after
  * which the kernel stops working, waits (bounded) for its copies and MMAs in flight, frees its tensor

@@ -12,5 +12,7 @@ from .binding import (  # noqa: F401
     lce_bitpack, lce_bmaxpool, lce_device_status, lce_device_status_reset, lce_device_wait_probe, lce_status_string, lce_unpack, lce_version, library,
     make_desc, pack_weights,
     KvDesc, KvAttentionDesc, ResidualNormDesc, make_kv_desc, lce_kv_cache_bytes, lce_kv_quantize, lce_kv_dequantize, lce_kv_attention,
+    ROTARY_BASE, ROTARY_HALVES, ROTARY_LINEAR, ROTARY_PAIRS, ROTARY_PARTS, ROTARY_PLAIN, RotaryDesc, KvAttentionWeightsDesc, KvEvictDesc, make_rotary_desc,
+    lce_rotary_steps, lce_rotary, lce_kv_attention_weights, lce_kv_attention_weights_workspace_bytes, lce_kv_evict,
     lce_kv_attention_workspace_bytes, make_norm_desc, lce_residual_norm,
 )

@@ -16,6 +16,8 @@ ACT_NONE, ACT_RELU, ACT_SIGMOID = 0, 1, 2
 KERNEL_AUTO, KERNEL_DIRECT, KERNEL_TILED, KERNEL_TENSOR = 0, 1, 2, 3
 TYPE_FLOAT32, TYPE_FLOAT16, TYPE_BFLOAT16 = 0, 1, 2
 NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
+ROTARY_HALVES, ROTARY_PAIRS = 0, 1
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_PARTS = 0, 1, 2, 3
 _TYPES = {torch.float32: TYPE_FLOAT32, torch.float16: TYPE_FLOAT16, torch.bfloat16: TYPE_BFLOAT16}
 
 
@@ -49,6 +51,27 @@ class ResidualNormDesc(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in ("channels", "post_norm", "pre_norm", "gate_activation")] + \
                [("eps", ctypes.c_float), ("residual_scale", ctypes.c_float), ("stream_type", ctypes.c_int32), ("type", ctypes.c_int32)] + \
                [(n, ctypes.c_int64) for n in ("x_stride", "branch_stride", "gate_stride", "y_stride", "normed_stride")]
+
+
+class RotaryDesc(ctypes.Structure):
+    """Mirror of lce_rotary_desc; type, heads, tokens and strides are filled in from the tensors of a call."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("head_dim", "rotary_dim", "layout", "type", "q_heads", "k_heads")] + [("amplitude", ctypes.c_float)] + \
+               [(n, ctypes.c_int64) for n in ("tokens", "q_token_stride", "q_head_stride", "k_token_stride", "k_head_stride",
+                                              "q_out_token_stride", "q_out_head_stride", "k_out_token_stride", "k_out_head_stride")]
+
+
+class KvAttentionWeightsDesc(ctypes.Structure):
+    """Mirror of lce_kv_attention_weights_desc."""
+    _fields_ = [("cache", KvDesc)] + [(n, ctypes.c_int32) for n in ("batch", "heads", "table_pages", "type", "causal", "window")] + \
+               [("scale", ctypes.c_float), ("decay", ctypes.c_float)] + \
+               [(n, ctypes.c_int64) for n in ("tokens", "q_token_stride", "q_head_stride", "previous_seq_stride", "previous_head_stride",
+                                              "out_seq_stride", "out_head_stride")]
+
+
+class KvEvictDesc(ctypes.Structure):
+    """Mirror of lce_kv_evict_desc."""
+    _fields_ = [("cache", KvDesc)] + [(n, ctypes.c_int32) for n in ("batch", "table_pages", "kept_pages", "budget", "first", "recent")] + \
+               [(n, ctypes.c_int64) for n in ("scores_seq_stride", "scores_head_stride", "kept_scores_seq_stride", "kept_scores_head_stride")]
 
 
 _lib = None
@@ -121,8 +144,14 @@ def library() -> ctypes.CDLL:
         lib.lce_kv_attention_workspace_bytes.argtypes = [ctypes.POINTER(KvAttentionDesc)]
         lib.lce_kv_attention_workspace_bytes.restype = st
         lib.lce_kv_attention.argtypes = [ctypes.POINTER(KvAttentionDesc), vp, vp, vp, vp, vp, vp, vp, st, vp]
+        lib.lce_rotary_steps.argtypes = [i32, i32] + [ctypes.c_double] * 5 + [vp]
+        lib.lce_rotary.argtypes = [ctypes.POINTER(RotaryDesc), vp, vp, vp, vp, vp, vp, vp]
+        lib.lce_kv_attention_weights_workspace_bytes.argtypes = [ctypes.POINTER(KvAttentionWeightsDesc)]
+        lib.lce_kv_attention_weights_workspace_bytes.restype = st
+        lib.lce_kv_attention_weights.argtypes = [ctypes.POINTER(KvAttentionWeightsDesc), vp, vp, vp, vp, vp, vp, vp, vp, st, vp]
+        lib.lce_kv_evict.argtypes = [ctypes.POINTER(KvEvictDesc)] + [vp] * 9
         lib.lce_residual_norm.argtypes = [ctypes.POINTER(ResidualNormDesc)] + [vp] * 11
-        for name in ("lce_kv_quantize", "lce_kv_dequantize", "lce_kv_attention", "lce_residual_norm", "lce_bitpack", "lce_unpack", "lce_bconv2d_out_shape", "lce_bconv2d", "lce_bconv2d_host",
+        for name in ("lce_rotary_steps", "lce_rotary", "lce_kv_attention_weights", "lce_kv_evict", "lce_kv_quantize", "lce_kv_dequantize", "lce_kv_attention", "lce_residual_norm", "lce_bitpack", "lce_unpack", "lce_bconv2d_out_shape", "lce_bconv2d", "lce_bconv2d_host",
                      "lce_bconv2d_pack_weights",
                      "lce_bmaxpool", "lce_add_f32"):
             getattr(lib, name).restype = ctypes.c_int
@@ -363,6 +392,57 @@ def lce_kv_attention(desc: KvDesc, q: torch.Tensor, cache: torch.Tensor, page_ta
     given).  out and workspace (uint8, lce_kv_attention_workspace_bytes for the same dtype) are allocated with torch when not given."""
     return _native.kv_attention(desc, q, cache, page_table, lengths, q_starts, desc.head_dim ** -0.5 if scale is None else scale,
                                 causal, window, out, workspace)
+
+
+def make_rotary_desc(head_dim, rotary_dim=None, layout=ROTARY_HALVES, amplitude=1.0) -> RotaryDesc:
+    """Rotary positions of the first rotary_dim channels of a head (None: all of them)."""
+    return RotaryDesc(head_dim, head_dim if rotary_dim is None else rotary_dim, layout, 0, 0, 0, amplitude)
+
+
+def lce_rotary_steps(rotary_dim: int, base: float = 10000.0, scaling: int = ROTARY_PLAIN, factor: float = 1.0, original_length: float = 0.0,
+                     low_turns: float = 1.0, high_turns: float = 32.0) -> torch.Tensor:
+    """What a position turns each pair by, in units of 2^-64 turns: int64 [rotary_dim / 2] (the bits of uint64) on the host, to be
+    brought to the device once.  scaling: ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE or ROTARY_PARTS (lce.h has the formulas).
+    Negated steps turn back."""
+    steps = torch.empty(max(rotary_dim // 2, 0), dtype=torch.int64)
+    _check(library().lce_rotary_steps(rotary_dim, scaling, base, factor, original_length, low_turns, high_turns, steps.data_ptr() or 8), "lce_rotary_steps")
+    return steps
+
+
+def lce_rotary(desc: RotaryDesc, q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, steps: torch.Tensor,
+               q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """Turns q [tokens, heads, head_dim] and k [tokens, kv heads, head_dim] (fp32, fp16 or bf16; views with strides are fine; k may be
+    None) by their positions (int32 [tokens]) and steps (lce_rotary_steps on the device).  q_out may be q, k_out k."""
+    return _native.rotary(desc, q, k, positions, steps, q_out, k_out)
+
+
+def lce_kv_attention_weights_workspace_bytes(desc: KvDesc, batch: int, tokens: int, heads: int, table_pages: int,
+                                             dtype: torch.dtype = torch.float32) -> int:
+    """Bytes of lce_kv_attention_weights' workspace for q [tokens, heads, head_dim] and a page table [batch, table_pages]."""
+    full = KvAttentionWeightsDesc(desc, batch, heads, table_pages, _TYPES.get(dtype, -2), 0, 0, 1.0, 1.0, tokens, 0, 0, 0, 0, 0, 0)
+    return int(library().lce_kv_attention_weights_workspace_bytes(ctypes.byref(full)))
+
+
+def lce_kv_attention_weights(desc: KvDesc, q: torch.Tensor, cache: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor,
+                             q_starts: Optional[torch.Tensor] = None, previous: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                             scale: Optional[float] = None, causal: bool = True, window: int = 0, decay: float = 1.0,
+                             workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """out[sequence, kv head, token] = decay * previous + the attention weights that lce_kv_attention's rows of q give the token, added
+    up over the rows and the head's query heads.  previous and out: fp32 [sequences, kv_heads, page_table.shape[1] * page_size or more], out may
+    be previous; the tokens that the rows stand at have no previous weight.  Nothing behind a sequence's last token is written
+    (arbitrary where out is not given).  The other arguments as for lce_kv_attention."""
+    return _native.kv_attention_weights(desc, q, cache, page_table, lengths, q_starts, previous, out, desc.head_dim ** -0.5 if scale is None else scale,
+                                        causal, window, decay, workspace)
+
+
+def lce_kv_evict(desc: KvDesc, cache: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, scores: torch.Tensor, kept_table: torch.Tensor,
+                 budget: int, first: int = 0, recent: int = 0, kept: Optional[torch.Tensor] = None, kept_lengths: Optional[torch.Tensor] = None,
+                 kept_scores: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """Every head of a sequence keeps `budget` tokens: the `first` first, the `recent` last, and those with the highest scores (fp32
+    [sequences, kv_heads, page_table.shape[1] * page_size or more]; expanded over the heads all of them keep the same).  Their rows move, in order, to
+    the pages of kept_table (int32 [sequences, pages]), none of which may be one that is read.  Returns kept (int32 [sequences,
+    kv_heads, budget]: where each came from, -1 behind the last), kept_lengths and kept_scores [sequences, kv_heads, budget or more]."""
+    return _native.kv_evict(desc, cache, page_table, lengths, scores, kept_table, budget, first, recent, kept, kept_lengths, kept_scores)
 
 
 def make_norm_desc(rows, channels, post_norm=NORM_RMS, pre_norm=NORM_RMS, eps=1e-5, residual_scale=1.0,

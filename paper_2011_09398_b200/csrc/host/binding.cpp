@@ -365,7 +365,7 @@ struct Rows {  // [tokens][heads][channels], channels next to one another
 Rows rows(const at::Tensor &t, int64_t heads, int64_t channels, const char *name)
 {
     on_current_device(t, name);
-    if (t.dim() != 3 || t.size(1) != heads || t.size(2) != channels || (channels > 1 && t.stride(2) != 1))
+    if (t.dim() != 3 || t.size(1) != heads || t.size(2) != channels || (channels > 1 && t.size(0) > 0 && t.stride(2) != 1))
         value_error(std::string(name) + " must be [tokens, " + std::to_string(heads) + ", " + std::to_string(channels) + "] with its channels next to one another");
     return {static_cast<char *>(t.data_ptr()), t.size(0), t.stride(0), t.stride(1)};
 }
@@ -474,6 +474,203 @@ PyObject *kv_attention(PyObject *const *a)
     return returned(a[9], made);
 }
 
+// Rows [sequences][heads][tokens] of fp32 numbers, a row's tokens next to one another; None -> null.
+float *token_rows(PyObject *o, int64_t sequences, int64_t heads, int64_t tokens, int64_t *seq_stride, int64_t *head_stride, const char *name)
+{
+    if (o == Py_None) return nullptr;
+    const at::Tensor &t = tensor(o, name);
+    on_current_device(t, name);
+    if (t.scalar_type() != at::kFloat) value_error(std::string(name) + " must be torch.float32");
+    if (t.dim() != 3 || t.size(0) != sequences || t.size(1) != heads || t.size(2) < tokens || (t.size(2) > 1 && t.stride(2) != 1))
+        value_error(std::string(name) + " must be [" + std::to_string(sequences) + ", " + std::to_string(heads) + ", " + std::to_string(tokens) +
+                    " or more] with a row's tokens next to one another");
+    *seq_stride = t.stride(0);
+    *head_stride = t.stride(1);
+    return static_cast<float *>(t.data_ptr());
+}
+
+// A page table [sequences][pages] and an entry for each sequence.
+const int32_t *page_table(PyObject *o, const char *name, int32_t *sequences, int32_t *pages)
+{
+    auto *p = static_cast<const int32_t *>(current_device_pointer(o, at::kInt, name));
+    const at::Tensor &t = tensor(o, name);
+    if (t.dim() != 2) value_error(std::string(name) + " must be [sequences, pages]");
+    if (t.size(0) >= (1ll << 31) || t.size(1) >= (1ll << 31)) value_error(std::string(name) + " is too large");
+    *sequences = (int32_t)t.size(0);
+    *pages = (int32_t)t.size(1);
+    return p;
+}
+
+int32_t int_argument(PyObject *o, const char *name)
+{
+    const long v = PyLong_AsLong(o);
+    if (v == -1 && PyErr_Occurred()) throw Raised{};
+    if (v < -(1ll << 31) || v >= (1ll << 31)) value_error(std::string(name) + " does not fit 32 bits");
+    return (int32_t)v;
+}
+
+// desc, q, k, positions, steps, q_out, k_out
+PyObject *rotary(PyObject *const *a)
+{
+    const Buffer<lce_rotary_desc> desc(a[0], "RotaryDesc");
+    lce_rotary_desc d = desc.d;
+    const at::Tensor &tq = tensor(a[1], "q");
+    if (tq.dim() != 3) value_error("q must be [tokens, heads, head_dim]");
+    if (tq.size(1) >= (1ll << 31)) value_error("q is too large");
+    d.q_heads = (int32_t)tq.size(1);
+    d.type = element_type(tq, "q");
+    const Rows q = rows(tq, d.q_heads, d.head_dim, "q");
+    d.tokens = q.tokens;
+    auto *pp = static_cast<const int32_t *>(current_device_pointer(a[3], at::kInt, "positions"));
+    if (a[3] == Py_None || tensor(a[3], "positions").numel() != d.tokens) value_error("positions must have one entry for each token");
+    auto *ps = static_cast<const uint64_t *>(current_device_pointer(a[4], at::kLong, "steps"));
+    if (a[4] == Py_None || tensor(a[4], "steps").numel() != d.rotary_dim / 2) value_error("steps must have one entry for each pair of channels");
+    at::Tensor made[2];
+    Rows in[2] = {q, {nullptr, 0, 0, 0}}, out[2] = {};
+    const char *names[2] = {"q_out", "k_out"};
+    if (a[2] != Py_None) {
+        const at::Tensor &tk = tensor(a[2], "k");
+        if (tk.dim() != 3) value_error("k must be [tokens, heads, head_dim]");
+        if (tk.size(1) >= (1ll << 31)) value_error("k is too large");
+        d.k_heads = (int32_t)tk.size(1);
+        in[1] = rows(tk, d.k_heads, d.head_dim, "k");
+        if (element_type(tk, "k") != d.type || in[1].tokens != d.tokens) value_error("k must be of q's type and have its tokens");
+    } else if (a[6] != Py_None) {
+        value_error("k_out without k");
+    }
+    for (int i = 0; i < 2; ++i) {
+        const int64_t heads = i ? d.k_heads : d.q_heads;
+        if (i && a[2] == Py_None) continue;
+        if (a[5 + i] == Py_None) made[i] = empty_like_device({d.tokens, heads, d.head_dim}, tq.scalar_type(), tq);
+        const at::Tensor &t = a[5 + i] == Py_None ? made[i] : tensor(a[5 + i], names[i]);
+        out[i] = rows(t, heads, d.head_dim, names[i]);
+        if (out[i].tokens != d.tokens || t.scalar_type() != tq.scalar_type()) value_error(std::string(names[i]) + " must be like what it is made from");
+        if (out[i].data == in[i].data && d.tokens > 1 && (out[i].token_stride != in[i].token_stride || (heads > 1 && out[i].head_stride != in[i].head_stride)))
+            value_error(std::string(names[i]) + " in place must have the strides of what it is made from");
+    }
+    d.q_token_stride = in[0].token_stride; d.q_head_stride = in[0].head_stride;
+    d.k_token_stride = in[1].token_stride; d.k_head_stride = in[1].head_stride;
+    d.q_out_token_stride = out[0].token_stride; d.q_out_head_stride = out[0].head_stride;
+    d.k_out_token_stride = out[1].token_stride; d.k_out_head_stride = out[1].head_stride;
+    void *s = current_stream();
+    check(without_gil([&] { return lce_rotary(&d, in[0].data, in[1].data, pp, ps, out[0].data, out[1].data, s); }), "lce_rotary");
+    PyObject *qo = returned(a[5], made[0]), *ko;
+    if (a[2] == Py_None) {
+        Py_INCREF(Py_None);
+        ko = Py_None;
+    } else {
+        ko = returned(a[6], made[1]);
+    }
+    PyObject *both = PyTuple_Pack(2, qo, ko);
+    Py_XDECREF(qo);
+    Py_XDECREF(ko);
+    return both;
+}
+
+// desc (KvDesc), q, cache, page_table, lengths, q_starts, previous, out, scale, causal, window, decay, workspace
+PyObject *kv_attention_weights(PyObject *const *a)
+{
+    const Buffer<lce_kv_desc> desc(a[0], "KvDesc");
+    lce_kv_attention_weights_desc d{};
+    d.cache = desc.d;
+    const at::Tensor &tq = tensor(a[1], "q"), &cache = tensor(a[2], "cache"), &lengths = tensor(a[4], "lengths");
+    if (tq.dim() != 3) value_error("q must be [tokens, heads, head_dim]");
+    if (tq.size(1) >= (1ll << 31)) value_error("q is too large");
+    d.heads = (int32_t)tq.size(1);
+    const Rows q = rows(tq, d.heads, d.cache.head_dim, "q");
+    d.type = element_type(tq, "q");
+    d.tokens = q.tokens;
+    d.q_token_stride = q.token_stride; d.q_head_stride = q.head_stride;
+    cache_fits(cache, d.cache);
+    auto *pt = page_table(a[3], "page_table", &d.batch, &d.table_pages);
+    auto *pl = static_cast<const int32_t *>(current_device_pointer(a[4], at::kInt, "lengths"));
+    auto *pq = static_cast<const int32_t *>(current_device_pointer(a[5], at::kInt, "q_starts"));
+    if (lengths.numel() != d.batch) value_error("lengths must have an entry for each sequence");
+    if (pq && tensor(a[5], "q_starts").numel() != (int64_t)d.batch + 1) value_error("q_starts must have one entry more than there are sequences");
+    if (!pq && q.tokens != d.batch) value_error("without q_starts q must have one row for each sequence");
+    const int64_t room_for = (int64_t)d.table_pages * d.cache.page_size;
+    at::Tensor made, room;
+    const float *previous = token_rows(a[6], d.batch, d.cache.kv_heads, room_for, &d.previous_seq_stride, &d.previous_head_stride, "previous");
+    float *out;
+    if (a[7] == Py_None) {
+        made = empty_like_device({d.batch, d.cache.kv_heads, room_for}, at::kFloat, tq);
+        out = static_cast<float *>(made.data_ptr());
+        d.out_seq_stride = made.stride(0);
+        d.out_head_stride = made.stride(1);
+    } else {
+        out = token_rows(a[7], d.batch, d.cache.kv_heads, room_for, &d.out_seq_stride, &d.out_head_stride, "out");
+    }
+    if (previous == out && previous && (d.previous_seq_stride != d.out_seq_stride || d.previous_head_stride != d.out_head_stride))
+        value_error("out in place must have the strides of previous");
+    const double scale = PyFloat_AsDouble(a[8]), decay = PyFloat_AsDouble(a[11]);
+    const int causal = PyObject_IsTrue(a[9]);
+    if (PyErr_Occurred()) throw Raised{};
+    const int32_t window = int_argument(a[10], "window");
+    if (window < 0) value_error("window must not be negative");
+    d.scale = (float)scale;
+    d.decay = (float)decay;
+    d.causal = causal;
+    d.window = window;
+    if (d.batch == 0 || room_for == 0) return returned(a[7], made);
+    if (a[12] == Py_None) room = empty_like_device({(int64_t)lce_kv_attention_weights_workspace_bytes(&d)}, at::kByte, tq);
+    const at::Tensor &ws = a[12] == Py_None ? room : tensor(a[12], "workspace");
+    on_current_device(ws, "workspace");
+    void *pw = device_pointer(ws, at::kByte, "workspace"), *pc = device_pointer(cache, at::kByte, "cache"), *s = current_stream();
+    const size_t bytes = (size_t)ws.numel();
+    check(without_gil([&] { return lce_kv_attention_weights(&d, q.data, pc, pt, pl, pq, previous, out, pw, bytes, s); }), "lce_kv_attention_weights");
+    return returned(a[7], made);
+}
+
+// desc (KvDesc), cache, page_table, lengths, scores, kept_table, budget, first, recent, kept, kept_lengths, kept_scores
+PyObject *kv_evict(PyObject *const *a)
+{
+    const Buffer<lce_kv_desc> desc(a[0], "KvDesc");
+    lce_kv_evict_desc d{};
+    d.cache = desc.d;
+    const at::Tensor &cache = tensor(a[1], "cache"), &lengths = tensor(a[3], "lengths");
+    cache_fits(cache, d.cache);
+    auto *pt = page_table(a[2], "page_table", &d.batch, &d.table_pages);
+    int32_t sequences;
+    auto *pk = page_table(a[5], "kept_table", &sequences, &d.kept_pages);
+    if (sequences != d.batch) value_error("kept_table must have a row for each sequence");
+    auto *pl = static_cast<const int32_t *>(current_device_pointer(a[3], at::kInt, "lengths"));
+    if (lengths.numel() != d.batch) value_error("lengths must have an entry for each sequence");
+    d.budget = int_argument(a[6], "budget");
+    d.first = int_argument(a[7], "first");
+    d.recent = int_argument(a[8], "recent");
+    if (d.budget <= 0) value_error("budget must be positive");
+    const int64_t heads = d.cache.kv_heads, shape[3] = {d.batch, heads, d.budget};
+    const float *ps = token_rows(a[4], d.batch, heads, (int64_t)d.table_pages * d.cache.page_size, &d.scores_seq_stride, &d.scores_head_stride, "scores");
+    if (!ps && d.batch > 0) value_error("scores must be given");
+    at::Tensor made[3];
+    int32_t *whole[2];
+    for (int i = 0; i < 2; ++i) {
+        const at::IntArrayRef wanted(shape, i ? 1 : 3);
+        const char *name = i ? "kept_lengths" : "kept";
+        if (a[9 + i] == Py_None) made[i] = empty_like_device(wanted, at::kInt, cache);
+        const at::Tensor &t = a[9 + i] == Py_None ? made[i] : tensor(a[9 + i], name);
+        on_current_device(t, name);
+        whole[i] = static_cast<int32_t *>(device_pointer(t, at::kInt, name));
+        if (t.sizes() != wanted) value_error(std::string(name) + (i ? " must have an entry for each sequence" : " must be [sequences, kv_heads, budget]"));
+    }
+    float *pks;
+    if (a[11] == Py_None) {
+        made[2] = empty_like_device(at::IntArrayRef(shape, 3), at::kFloat, cache);
+        pks = static_cast<float *>(made[2].data_ptr());
+        d.kept_scores_seq_stride = made[2].stride(0);
+        d.kept_scores_head_stride = made[2].stride(1);
+    } else {
+        pks = token_rows(a[11], d.batch, heads, d.budget, &d.kept_scores_seq_stride, &d.kept_scores_head_stride, "kept_scores");
+    }
+    void *pc = device_pointer(cache, at::kByte, "cache"), *s = current_stream();
+    if (d.batch > 0) check(without_gil([&] { return lce_kv_evict(&d, pc, pt, pl, ps, pk, whole[0], whole[1], pks, s); }), "lce_kv_evict");
+    PyObject *out[3];
+    for (int i = 0; i < 3; ++i) out[i] = returned(a[9 + i], made[i]);
+    PyObject *all = PyTuple_Pack(3, out[0], out[1], out[2]);
+    for (PyObject *o : out) Py_XDECREF(o);
+    return all;
+}
+
 // Rows of `channels` elements next to one another: any tensor whose leading axes are one run of rows.
 char *norm_rows(PyObject *o, const lce_residual_norm_desc &d, at::ScalarType dtype, bool one_row_for_all, int64_t *stride, const char *name)
 {
@@ -540,6 +737,9 @@ PyMethodDef g_methods[] = {
     LCE_METHOD("kv_quantize", kv_quantize, 5),
     LCE_METHOD("kv_dequantize", kv_dequantize, 6),
     LCE_METHOD("kv_attention", kv_attention, 11),
+    LCE_METHOD("rotary", rotary, 7),
+    LCE_METHOD("kv_attention_weights", kv_attention_weights, 13),
+    LCE_METHOD("kv_evict", kv_evict, 12),
     LCE_METHOD("residual_norm", residual_norm, 11),
     {nullptr, nullptr, 0, nullptr}};
 

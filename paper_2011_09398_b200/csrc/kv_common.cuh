@@ -1,4 +1,4 @@
-// The 4-bit key/value cache: its layout, the element types of its callers and the quantiser's arithmetic.
+// The 4-bit key/value cache: its layout, the element types of its callers, clusters of blocks and the quantiser's arithmetic.
 //
 // A tile is 16 tokens of one head: with B = ceil(head_dim / 32) blocks, uint32 K[64 B], V[64 B], scales[16 B].  Its blocks come
 // in planes of 4, then 2, then 1 (6 = 4 + 2), W blocks each, so that a lane's words of a plane are one vector load:
@@ -71,6 +71,20 @@ __host__ __device__ __forceinline__ int kv_scale_word(int blocks, int token, int
     int first, width;
     kv_plane(blocks, b, &first, &width);
     return 128 * blocks + 16 * first + token * width + (b - first);
+}
+
+// --- clusters of blocks ---------------------------------------------------------------------------
+
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+}
+// The same place in the shared memory of block `rank` of the cluster.
+__device__ __forceinline__ uint32_t remote_place(const void *p, int rank)
+{
+    uint32_t at;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+    return at;
 }
 
 // --- elements of the callers' tensors ---------------------------------------------------------------

@@ -1,0 +1,591 @@
+// How much attention every token of the 4-bit cache gets: sums of softmax weights over a sequence's newest rows.
+//
+// For the rows of one sequence that share a key/value head (its new tokens x the group's query heads: the "columns" here) the softmax needs
+// the largest score and the sum of a whole column before the first weight is known.  So there are two kernels over pieces of the
+// sequences: the first makes the scores, S = K Q^T with the 4-bit keys on the 16-row side of m16n8k16 products and 8 or 16 columns on the other,
+// and each piece's largest and sum of every column; the second joins the pieces' (always in the same order) and adds a token's weights up
+// over the columns.  Where a sequence's columns fit one tile of them, as in a decode step, the second kernel reads the scores that the first
+// one left, 4 bytes each, next to which the keys were 80 bytes for 128 channels; otherwise it makes them again.
+//
+// Keys are codes times a block's scale.  The codes c = n - 8 are exact f16 operands (1024 + n by one AND-OR, less 1032 by a packed
+// multiply-add), the scale multiplies a block's finished sums in fp32; 16-bit rows of q are one f16 number times a power of two of the row,
+// fp32 rows two of them.
+#include "kv_mma.cuh"
+
+#include <math.h>
+
+#include <algorithm>
+
+namespace lce {
+namespace {
+
+constexpr int kWarps = 4, kThreads = 32 * kWarps;
+constexpr int kStages = 4;                  // tiles in flight of a warp
+constexpr int kMostTiles = 256;             // of a piece: its tokens' sums are in shared memory
+constexpr int kLeastTiles = kWarps;         // that a piece is worth
+constexpr int kBlocksPerSm = 4;
+constexpr int64_t kMostScores = 256 << 20;  // bytes of workspace that scores may take
+constexpr int64_t kMostStats = 64 << 20;
+
+struct WeightsParams : AttnParams {
+    float decay;
+    int64_t previous_seq, previous_head, out_seq, out_head;
+    const float *previous;
+    float *sums;                            // where the weights go
+    float2 *stats;                          // [kv head][row * group + query head][piece]: largest, sum
+    float *scores;                          // [kv head][token of the batch][columns], or null
+    int64_t scores_head;
+    int32_t columns;                        // of a tile of them
+    int32_t pieces;                         // that a sequence can have
+};
+
+__host__ __device__ constexpr int key_words(int blocks) { return 80 * blocks; }  // of a tile: its keys and scales
+
+// A range of tiles of a sequence.
+struct Piece {
+    Unit u;                // columns [column0, ..): set by the loops over them
+    int32_t index, pieces; // which one of the sequence's
+    int32_t columns;
+    int64_t tiles_before;  // tiles of the sequences in front
+};
+
+// Finds the `at`-th piece; false: there is no such one.  Every warp works this out from the lengths: pieces of at most `most` tiles, where
+// `most` follows from the whole batch's.
+__device__ __forceinline__ bool find_piece(const WeightsParams &p, int at, Piece *piece)
+{
+    const int lane = threadIdx.x & 31;
+    const auto tiles_of = [&](int b) { return b < p.batch ? (tokens_held(p, max(__ldg(p.lengths + b), 0)) + kKvTile - 1) / kKvTile : 0; };
+    const int32_t first = tiles_of(lane);
+    int64_t total = first;
+    for (int b0 = 32; b0 < p.batch; b0 += 32) total += tiles_of(b0 + lane);
+#pragma unroll
+    for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
+    const int32_t most = (int32_t)min(max((total + p.target - 1) / p.target, (int64_t)kLeastTiles), (int64_t)kMostTiles);
+    int32_t before = 0;
+    int64_t tiles_before = 0;
+    for (int b0 = 0; b0 < p.batch; b0 += 32) {
+        const int32_t tiles = b0 ? tiles_of(b0 + lane) : first, pieces = (tiles + most - 1) / most;
+        int32_t upto = pieces;
+        int64_t tiles_upto = tiles;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int32_t o = __shfl_up_sync(0xffffffffu, upto, d);
+            const int64_t n = __shfl_up_sync(0xffffffffu, tiles_upto, d);
+            if (lane >= d) {
+                upto += o;
+                tiles_upto += n;
+            }
+        }
+        const uint32_t has = __ballot_sync(0xffffffffu, before + upto > at);
+        if (has) {
+            const int from = __ffs(has) - 1;
+            const int32_t n = __shfl_sync(0xffffffffu, tiles, from);
+            piece->pieces = __shfl_sync(0xffffffffu, pieces, from);
+            piece->index = at - (before + __shfl_sync(0xffffffffu, upto - pieces, from));
+            piece->tiles_before = tiles_before + __shfl_sync(0xffffffffu, tiles_upto - tiles, from);
+            const Sequence s = sequence<8>(p, b0 + from);
+            piece->u.seq = b0 + from;
+            piece->u.length = s.length;
+            piece->u.rows = s.rows;
+            piece->u.row0 = s.row0;
+            piece->u.column0 = 0;
+            piece->columns = s.rows * p.group;
+            const int32_t each = n / piece->pieces, more = n - each * piece->pieces;  // equal pieces
+            piece->u.tile0 = piece->index * each + min(piece->index, more);
+            piece->u.tile1 = piece->u.tile0 + each + (piece->index < more ? 1 : 0);
+            return true;
+        }
+        before += __shfl_sync(0xffffffffu, upto, 31);
+        tiles_before += __shfl_sync(0xffffffffu, tiles_upto, 31);
+    }
+    return false;
+}
+
+// Tiles of the piece that some column of [column0, column0 + count) sees: columns' ranges move up with the rows.  all_lo, all_hi: tokens that
+// each of them sees.
+struct View {
+    int32_t tile0, tile1, all_lo, all_hi;
+};
+__device__ __forceinline__ View view(const WeightsParams &p, const Piece &piece, int count)
+{
+    View v;
+    int32_t any_lo, any_hi;
+    column_range(p, piece.u, piece.u.column0, &any_lo, &v.all_hi);
+    column_range(p, piece.u, min(piece.u.column0 + count, piece.columns) - 1, &v.all_lo, &any_hi);
+    v.tile0 = max(piece.u.tile0, any_lo / kKvTile);
+    v.tile1 = min(piece.u.tile1, (any_hi + kKvTile - 1) / kKvTile);
+    if (any_hi <= any_lo) v.tile1 = v.tile0;
+    return v;
+}
+
+// B blocks of 32 channels, NT tiles of 8 columns, SPLIT: fp32 rows.
+template <int B, int NT, bool SPLIT>
+struct Columns {
+    uint32_t qf[B][2][NT][2], ql[SPLIT ? B : 1][2][NT][2];  // B operands of the products
+    float factor[NT][2];                                    // scores, as powers of two, are this times the sums over blocks
+    int32_t lo[NT][2], hi[NT][2];                           // tokens that the lane's columns 8 nt + 2 (lane % 4) + {0, 1} see
+
+    template <typename T>
+    __device__ __forceinline__ void take(const WeightsParams &p, const Unit &u, const Queries<B, NT, T> &queries)
+    {
+        const int lane = threadIdx.x & 31, quarter = lane & 3;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            float v[B][8];
+            uint32_t magnitude = 0;  // magnitudes compare like integers, infinity and NaN above all others
+#pragma unroll
+            for (int b = 0; b < B; ++b) {
+                if (!SPLIT && p.type == LCE_TYPE_BFLOAT16) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[b][i] = __uint_as_float((uint32_t)reinterpret_cast<const unsigned short *>(queries.e[nt][b].e)[i] << 16);
+                } else {
+                    queries.e[nt][b].expand(v[b]);
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) magnitude = max(magnitude, __float_as_uint(v[b][i]) & 0x7fffffffu);
+            }
+            magnitude = max(magnitude, __shfl_xor_sync(0xffffffffu, magnitude, 1));
+            magnitude = max(magnitude, __shfl_xor_sync(0xffffffffu, magnitude, 2));
+            const bool finite = magnitude < 0x7f800000u;
+            // times 2^k, so that the largest is in [2^14, 2^15)
+            const int k = 14 - (finite && magnitude > 0 ? ilogbf(__uint_as_float(magnitude)) : 0), k1 = k / 2, k2 = k - k1;
+            const float s1 = __uint_as_float((uint32_t)(127 + k1) << 23), s2 = __uint_as_float((uint32_t)(127 + k2) << 23);
+#pragma unroll
+            for (int b = 0; b < B; ++b)
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int odd = 0; odd < 2; ++odd) {
+                        // channels 2 m and 2 m + 4, then 2 m + 1 and 2 m + 5, in the order in which a word's codes come apart
+                        const float x = v[b][2 * m + odd] * s1 * s2, y = v[b][2 * m + odd + 4] * s1 * s2;
+                        const uint32_t a = pack_half2(x, y);
+                        qf[b][m][nt][odd] = a;
+                        if (SPLIT) ql[SPLIT ? b : 0][m][nt][odd] = pack_half2(x - half_low(a), y - half_high(a));
+                    }
+            const float f = finite ? p.scale : __uint_as_float(0x7fc00000u);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int from = (2 * quarter + j) * 4, kc = -__shfl_sync(0xffffffffu, k, from), c1 = kc / 2, c2 = kc - c1;
+                factor[nt][j] = __shfl_sync(0xffffffffu, f, from) * __uint_as_float((uint32_t)(127 + c1) << 23) * __uint_as_float((uint32_t)(127 + c2) << 23);
+                column_range(p, u, u.column0 + 8 * nt + 2 * quarter + j, &lo[nt][j], &hi[nt][j]);
+            }
+        }
+    }
+    __device__ __forceinline__ void load(const WeightsParams &p, const Unit &u, int head)
+    {
+        Queries<B, NT, typename std::conditional<SPLIT, float, __half>::type> queries;  // __half: the bits of any 16-bit row
+        if (p.q_vectors) queries.template load<true>(p, u, head);
+        else queries.template load<false>(p, u, head);
+        take(p, u, queries);
+    }
+
+    // Sums over one plane's blocks for tokens 8 r + lane / 4 of the tile and the lane's columns: s[nt][2 r + j].
+    template <int FIRST, int W>
+    __device__ __forceinline__ void plane(const uint32_t *tile, float (&s)[NT][4]) const
+    {
+        constexpr uint32_t kEven = 0x003c003cu, kOdd = 0x03c003c0u, kBase = 0x64006400u;
+        const int lane = threadIdx.x & 31;
+        uint32_t k[2][W], sc[2][W];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            load_words<W>(tile + 64 * FIRST + (32 * h + lane) * W, k[h]);
+            load_words<W>(tile + 64 * B + 16 * FIRST + (8 * h + (lane >> 2)) * W, sc[h]);
+        }
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            const int b = FIRST + i;
+            const uint32_t u0 = k[0][i], u1 = k[1][i], v0 = swap_bytes(u0), v1 = swap_bytes(u1);
+            const uint32_t a[8] = {signed_even(and_or(u0, kEven, kBase)), signed_even(and_or(u1, kEven, kBase)), signed_odd(and_or(u0, kOdd, kBase)),
+                                   signed_odd(and_or(u1, kOdd, kBase)),   signed_even(and_or(v0, kEven, kBase)), signed_even(and_or(v1, kEven, kBase)),
+                                   signed_odd(and_or(v0, kOdd, kBase)),   signed_odd(and_or(v1, kOdd, kBase))};
+            const float s0 = __uint_as_float(sc[0][i] << 16), s1 = __uint_as_float(sc[1][i] << 16);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                float d[4];
+                if (SPLIT) {
+                    mma(d, a[0], a[1], a[2], a[3], ql[SPLIT ? b : 0][0][nt][0], ql[SPLIT ? b : 0][0][nt][1], 0.0f, 0.0f, 0.0f, 0.0f);
+                    mma(d, a[4], a[5], a[6], a[7], ql[SPLIT ? b : 0][1][nt][0], ql[SPLIT ? b : 0][1][nt][1]);
+                    mma(d, a[0], a[1], a[2], a[3], qf[b][0][nt][0], qf[b][0][nt][1]);
+                } else {
+                    mma(d, a[0], a[1], a[2], a[3], qf[b][0][nt][0], qf[b][0][nt][1], 0.0f, 0.0f, 0.0f, 0.0f);
+                }
+                mma(d, a[4], a[5], a[6], a[7], qf[b][1][nt][0], qf[b][1][nt][1]);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    s[nt][j] = fmaf(s0, d[j], s[nt][j]);
+                    s[nt][2 + j] = fmaf(s1, d[2 + j], s[nt][2 + j]);
+                }
+            }
+        }
+    }
+    // Scores of a tile; minus infinity where a column does not see the token (only looked at where `masked`).
+    __device__ __forceinline__ void scores(const uint32_t *tile, int32_t token0, bool masked, float (&s)[NT][4]) const
+    {
+        constexpr int Q = B / 4 * 4;
+        constexpr bool T = (B & 2) != 0, S = (B & 1) != 0;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[nt][i] = 0.0f;
+        if (Q > 0) plane<0, 4>(tile, s);
+        if (Q > 4) plane<(Q > 4 ? 4 : 0), 4>(tile, s);
+        if (T) plane<(T ? Q : 0), 2>(tile, s);
+        if (S) plane<B - 1, 1>(tile, s);
+        const int lane = threadIdx.x & 31;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[nt][i] *= factor[nt][i & 1];
+                if (masked) {
+                    const int32_t token = token0 + 8 * (i >> 1) + (lane >> 2);
+                    if (token < lo[nt][i & 1] || token >= hi[nt][i & 1]) s[nt][i] = -INFINITY;
+                }
+            }
+    }
+};
+
+// The warp's tiles of a view, brought to shared memory one after the other: body(tile, its words or null where its page is outside the pool).
+template <int B, typename Body>
+__device__ __forceinline__ void each_tile(const WeightsParams &p, const Piece &piece, const View &v, int head, uint32_t *ring, Body body)
+{
+    constexpr int WORDS = key_words(B), PIECES = WORDS / 4;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int32_t *const table = p.page_table + (int64_t)piece.u.seq * p.table_pages;
+    const int tiles_per_page = p.g.page_size / kKvTile;
+    const int32_t mine = max((v.tile1 - v.tile0 - warp + kWarps - 1) / kWarps, 0);
+    const char *const cache = reinterpret_cast<const char *>(p.cache);
+    const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
+    int32_t places = -1;  // the warp's next 32 tiles in the cache, one to a lane; negative: not in the pool
+    const auto fetch = [&](int i, int stage) {
+        if ((i & 31) == 0) {
+            const int32_t t = v.tile0 + warp + (i + lane) * kWarps, in_table = t / tiles_per_page;
+            const int32_t page = t < v.tile1 ? __ldg(table + in_table) : -1;
+            places = page >= 0 && page < p.g.pages ? (page * p.g.heads + head) * tiles_per_page + (t - in_table * tiles_per_page) : -1;
+        }
+        const int32_t place = __shfl_sync(0xffffffffu, places, i & 31);
+        if (place >= 0) {
+            const char *const from = cache + (int64_t)place * (kv_tile_words(B) * 4);
+#pragma unroll
+            for (int c = 0; c < (PIECES + 31) / 32; ++c) {
+                const int at = c * 32 + lane;
+                if (c * 32 + 32 <= PIECES || at < PIECES) cp_async16(ring_at + (stage * WORDS + 4 * at) * 4, from + 16 * (at < 16 * B ? at : at + 16 * B));
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        return place >= 0;
+    };
+    uint32_t good = 0;  // whether the warp's next tiles are there, the next one in bit 0
+#pragma unroll
+    for (int i = 0; i < kStages - 1; ++i) good |= fetch(i, i) ? 1u << i : 0u;
+    for (int i = 0, stage = 0; i < mine; ++i, good >>= 1, stage = stage + 1 == kStages ? 0 : stage + 1) {
+        __syncwarp();  // everyone is done with the stage that comes next
+        good |= fetch(i + kStages - 1, stage ? stage - 1 : kStages - 1) ? 1u << (kStages - 1) : 0u;
+        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+        __syncwarp();
+        body(v.tile0 + warp + i * kWarps, good & 1 ? ring + stage * WORDS : nullptr);
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncwarp();
+}
+
+__device__ __forceinline__ bool keeps_scores(const WeightsParams &p, const Piece &piece) { return p.scores && piece.columns <= p.columns; }
+// Scores of a token: the sequence's columns, rounded up to an even number; a sequence begins where room for a whole tile of columns puts it.
+__device__ __forceinline__ float *scores_at(const WeightsParams &p, const Piece &piece, int head, int32_t tile)
+{
+    return p.scores + head * p.scores_head + (piece.tiles_before * p.columns + (int64_t)tile * ((piece.columns + 1) & ~1)) * kKvTile;
+}
+
+// The sum of a column's powers of two, joined: s e^.. is held as (largest, sum relative to it).
+__device__ __forceinline__ void join_sums(float &top, float &sum, float other_top, float other_sum)
+{
+    const float high = fmaxf(top, other_top), base = high == -INFINITY ? 0.0f : high;
+    sum = sum * exp2f(top - base) + other_sum * exp2f(other_top - base);
+    top = high;
+}
+
+template <int B, int NT, bool SPLIT>
+__global__ void __launch_bounds__(kThreads, kBlocksPerSm) kv_weights_scores_kernel(const __grid_constant__ WeightsParams p)
+{
+    constexpr int COLUMNS = 8 * NT;
+    extern __shared__ __align__(16) uint32_t smem[];
+    __shared__ float tops[kWarps][COLUMNS], sums[kWarps][COLUMNS];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the second kernel takes its place; it waits for all of this one
+    Piece piece;
+    if (!find_piece(p, blockIdx.x, &piece)) return;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, head = blockIdx.y;
+    const bool keeps = keeps_scores(p, piece);
+    const int stride = (piece.columns + 1) & ~1;
+    for (piece.u.column0 = 0; piece.u.column0 < piece.columns; piece.u.column0 += COLUMNS) {
+        const View v = view(p, piece, COLUMNS);
+        Columns<B, NT, SPLIT> c;
+        c.load(p, piece.u, head);
+        float top[NT][2], sum[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                top[nt][j] = -INFINITY;
+                sum[nt][j] = 0.0f;
+            }
+        each_tile<B>(p, piece, v, head, smem + warp * kStages * key_words(B), [&](int32_t tile, const uint32_t *words) {
+            float s[NT][4];
+            const int32_t token0 = tile * kKvTile;
+            if (words) {
+                c.scores(words, token0, token0 < v.all_lo || token0 + kKvTile > v.all_hi, s);
+            } else {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[nt][i] = -INFINITY;
+            }
+            if (keeps) {
+                float *const to = scores_at(p, piece, head, tile) + (lane >> 2) * stride + 2 * (lane & 3);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+                    if (8 * nt + 2 * (lane & 3) < stride) {
+                        *reinterpret_cast<float2 *>(to + 8 * nt) = make_float2(s[nt][0], s[nt][1]);
+                        *reinterpret_cast<float2 *>(to + 8 * nt + 8 * stride) = make_float2(s[nt][2], s[nt][3]);
+                    }
+            }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const float high = fmaxf(top[nt][j], fmaxf(s[nt][j], s[nt][2 + j])), base = high == -INFINITY ? 0.0f : high;
+                    sum[nt][j] = fmaf(sum[nt][j], exp2_fast(top[nt][j] - base), exp2_fast(s[nt][j] - base) + exp2_fast(s[nt][2 + j] - base));
+                    top[nt][j] = high;
+                }
+        });
+        // eight lanes have a column's tokens, then the warps
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) {
+                    const float t = __shfl_xor_sync(0xffffffffu, top[nt][j], d), s = __shfl_xor_sync(0xffffffffu, sum[nt][j], d);
+                    join_sums(top[nt][j], sum[nt][j], t, s);
+                }
+                if (lane < 4) {
+                    tops[warp][8 * nt + 2 * lane + j] = top[nt][j];
+                    sums[warp][8 * nt + 2 * lane + j] = sum[nt][j];
+                }
+            }
+        __syncthreads();
+        if (threadIdx.x < COLUMNS && piece.u.column0 + (int)threadIdx.x < piece.columns) {
+            float t = tops[0][threadIdx.x], s = sums[0][threadIdx.x];
+#pragma unroll
+            for (int w = 1; w < kWarps; ++w) join_sums(t, s, tops[w][threadIdx.x], sums[w][threadIdx.x]);
+            const int64_t column = (head * p.tokens + piece.u.row0) * p.group + piece.u.column0 + threadIdx.x;
+            p.stats[column * p.pieces + piece.index] = make_float2(t, s);
+        }
+        __syncthreads();
+    }
+}
+
+template <int B, int NT, bool SPLIT>
+__global__ void __launch_bounds__(kThreads, kBlocksPerSm) kv_weights_sum_kernel(const __grid_constant__ WeightsParams p)
+{
+    constexpr int COLUMNS = 8 * NT;
+    extern __shared__ __align__(16) uint32_t smem[];
+    __shared__ float tops[COLUMNS], parts[COLUMNS];
+    float *const weights = reinterpret_cast<float *>(smem) + kWarps * kStages * key_words(B);  // of the piece's tokens
+    Piece piece;
+    // the lengths are what the kernel in front read: nothing has written them since
+    const bool found = find_piece(p, blockIdx.x, &piece);
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // every block: what comes behind this kernel relies on the one in front, too
+    if (!found) return;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, head = blockIdx.y;
+    const int tokens = (piece.u.tile1 - piece.u.tile0) * kKvTile;
+    for (int i = threadIdx.x; i < tokens; i += kThreads) weights[i] = 0.0f;
+    for (piece.u.column0 = 0; piece.u.column0 < piece.columns; piece.u.column0 += COLUMNS) {
+        {   // a column's largest and what its powers are multiplied with; 0 where it sees nothing
+            constexpr int EACH = kThreads / COLUMNS;
+            const int in_tile = threadIdx.x / EACH, column = piece.u.column0 + in_tile;
+            float top = -INFINITY, sum = 0.0f;
+            if (column < piece.columns) {
+                const float2 *const from = p.stats + ((head * p.tokens + piece.u.row0) * p.group + column) * p.pieces;
+                for (int i = threadIdx.x % EACH; i < piece.pieces; i += EACH) join_sums(top, sum, from[i].x, from[i].y);
+            }
+#pragma unroll
+            for (int d = 1; d < EACH; d <<= 1) {
+                const float t = __shfl_xor_sync(0xffffffffu, top, d), s = __shfl_xor_sync(0xffffffffu, sum, d);
+                join_sums(top, sum, t, s);
+            }
+            if (threadIdx.x % EACH == 0) {
+                tops[in_tile] = top == -INFINITY ? 0.0f : top;
+                parts[in_tile] = sum == 0.0f ? 0.0f : 1.0f / sum;
+            }
+        }
+        __syncthreads();
+        const View v = view(p, piece, COLUMNS);
+        if (keeps_scores(p, piece)) {
+            const int stride = (piece.columns + 1) & ~1;
+            const float *const from = scores_at(p, piece, head, v.tile0);
+            for (int i = threadIdx.x; i < (v.tile1 - v.tile0) * kKvTile; i += kThreads) {
+                float w = 0.0f;
+                for (int c = 0; c < piece.columns; c += 2) {
+                    const float2 s = *reinterpret_cast<const float2 *>(from + (int64_t)i * stride + c);
+                    w += s.x == -INFINITY ? 0.0f : exp2_fast(s.x - tops[c]) * parts[c];
+                    if (c + 1 < piece.columns) w += s.y == -INFINITY ? 0.0f : exp2_fast(s.y - tops[c + 1]) * parts[c + 1];
+                }
+                weights[(v.tile0 - piece.u.tile0) * kKvTile + i] = w;
+            }
+        } else {
+            Columns<B, NT, SPLIT> c;
+            c.load(p, piece.u, head);
+            float top[NT][2], part[NT][2];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    top[nt][j] = tops[8 * nt + 2 * (lane & 3) + j];
+                    part[nt][j] = parts[8 * nt + 2 * (lane & 3) + j];
+                }
+            each_tile<B>(p, piece, v, head, smem + warp * kStages * key_words(B), [&](int32_t tile, const uint32_t *words) {
+                if (!words) return;
+                float s[NT][4], w[2] = {0.0f, 0.0f};
+                const int32_t token0 = tile * kKvTile;
+                c.scores(words, token0, token0 < v.all_lo || token0 + kKvTile > v.all_hi, s);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) w[i >> 1] += s[nt][i] == -INFINITY ? 0.0f : exp2_fast(s[nt][i] - top[nt][i & 1]) * part[nt][i & 1];
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    w[r] += __shfl_xor_sync(0xffffffffu, w[r], 1);
+                    w[r] += __shfl_xor_sync(0xffffffffu, w[r], 2);
+                    if ((lane & 3) == 0) weights[(tile - piece.u.tile0) * kKvTile + 8 * r + (lane >> 2)] += w[r];
+                }
+            });
+        }
+        __syncthreads();
+    }
+    __syncthreads();
+    const int32_t held = tokens_held(p, piece.u.length), first_new = piece.u.length - piece.u.rows;
+    for (int i = threadIdx.x; i < tokens; i += kThreads) {
+        const int32_t t = piece.u.tile0 * kKvTile + i;
+        if (t >= held) break;
+        float w = weights[i];
+        if (p.previous && t < first_new) w = fmaf(p.decay, p.previous[piece.u.seq * p.previous_seq + head * p.previous_head + t], w);
+        p.sums[piece.u.seq * p.out_seq + head * p.out_head + t] = w;
+    }
+}
+
+template <int B, int NT, bool SPLIT>
+lce_status launch(const WeightsParams &p, cudaStream_t s)
+{
+    constexpr size_t ring = (size_t)kWarps * kStages * key_words(B) * 4, all = ring + (size_t)kMostTiles * kKvTile * 4;
+    static SmemOptIn first_opt_in, second_opt_in;
+    if (!first_opt_in.ensure(kv_weights_scores_kernel<B, NT, SPLIT>, ring) || !second_opt_in.ensure(kv_weights_sum_kernel<B, NT, SPLIT>, all)) return LCE_ERR_CUDA;
+    const dim3 grid((unsigned)p.units, (unsigned)p.g.heads);
+    if (p.tokens > 0) {
+        const lce_status st = launch_dependent(kv_weights_scores_kernel<B, NT, SPLIT>, grid, kThreads, ring, s, p);
+        if (st != LCE_OK) return st;
+    }
+    return launch_dependent(kv_weights_sum_kernel<B, NT, SPLIT>, grid, kThreads, all, s, p);
+}
+
+// 16 columns where their operands fit a thread's registers
+constexpr int kWideBlocks = 4;
+
+template <int NT, bool SPLIT>
+lce_status launch_blocks(const WeightsParams &p, cudaStream_t s)
+{
+    switch (p.g.blocks) {
+        case 1: return launch<1, NT, SPLIT>(p, s);
+        case 2: return launch<2, NT, SPLIT>(p, s);
+        case 3: return launch<3, NT, SPLIT>(p, s);
+        case 4: return launch<4, NT, SPLIT>(p, s);
+        case 5: return launch<5, 1, SPLIT>(p, s);
+        case 6: return launch<6, 1, SPLIT>(p, s);
+        case 7: return launch<7, 1, SPLIT>(p, s);
+        default: return launch<8, 1, SPLIT>(p, s);
+    }
+}
+
+bool stride_ok(int64_t s) { return s >= 0 && s < (1ll << 40); }
+
+lce_status make_params(const lce_kv_attention_weights_desc *d, WeightsParams *p, int *nt)
+{
+    if (!d) return LCE_ERR_INVALID_ARG;
+    const lce_status st = make_kv_geom(&d->cache, &p->g);
+    if (st != LCE_OK) return st;
+    if (d->batch <= 0 || d->heads <= 0 || d->table_pages <= 0 || d->tokens < 0 || d->window < 0 || !type_known(d->type)) return LCE_ERR_INVALID_ARG;
+    if (d->causal != 0 && d->causal != 1) return LCE_ERR_INVALID_ARG;
+    if (d->heads % d->cache.kv_heads != 0 || !isfinite(d->scale) || !isfinite(d->decay)) return LCE_ERR_INVALID_ARG;
+    for (const int64_t s : {d->q_token_stride, d->q_head_stride, d->previous_seq_stride, d->previous_head_stride, d->out_seq_stride, d->out_head_stride})
+        if (!stride_ok(s)) return LCE_ERR_INVALID_ARG;
+    if (d->tokens >= (1ll << 31) || d->tokens * d->heads >= (1ll << 31) || (int64_t)d->table_pages * d->cache.page_size >= (1ll << 31) || d->batch >= (1 << 20) ||
+        (int64_t)p->g.slots / kKvTile * p->g.heads >= (1ll << 31))
+        return LCE_ERR_UNSUPPORTED;
+    p->batch = d->batch; p->group = d->heads / d->cache.kv_heads; p->table_pages = d->table_pages;
+    p->table_tokens = d->table_pages * d->cache.page_size;
+    p->causal = d->causal; p->window = d->window; p->type = d->type;
+    p->tokens = d->tokens;
+    p->q_token = d->q_token_stride; p->q_head = d->q_head_stride;
+    p->scale = d->scale * 1.44269504088896341f;
+    p->decay = d->decay;
+    p->previous_seq = d->previous_seq_stride; p->previous_head = d->previous_head_stride;
+    p->out_seq = d->out_seq_stride; p->out_head = d->out_head_stride;
+    *nt = p->g.blocks <= kWideBlocks && (d->tokens * p->group + d->batch - 1) / d->batch > 8 ? 2 : 1;
+    // As many pieces as the GPU has places for; fewer where there are so many columns that their sums would take much room.
+    const int64_t columns = std::max<int64_t>(p->tokens * d->heads, 1);
+    p->target = (int32_t)std::max<int64_t>(1, std::min<int64_t>((148 * kBlocksPerSm + p->g.heads - 1) / p->g.heads, kMostStats / 8 / columns));
+    const int64_t tiles = (p->table_tokens + kKvTile - 1) / kKvTile, units = p->batch + std::max<int64_t>(p->target, (p->batch * tiles + kMostTiles - 1) / kMostTiles);
+    if (units >= (1ll << 31)) return LCE_ERR_UNSUPPORTED;
+    p->units = (int32_t)units;
+    p->pieces = (int32_t)std::min<int64_t>(tiles, std::max<int64_t>(p->target, (tiles + kMostTiles - 1) / kMostTiles) + 1);
+    p->columns = 8 * *nt;
+    p->scores_head = p->batch * tiles * kKvTile * p->columns;
+    return LCE_OK;
+}
+
+size_t stats_bytes(const WeightsParams &p) { return ((size_t)p.tokens * p.group * p.g.heads * p.pieces * 8 + 15) / 16 * 16; }
+// Scores are kept where there is room for them and, on average, sequences have no more columns than a tile of them.
+size_t scores_bytes(const WeightsParams &p)
+{
+    const int64_t bytes = p.scores_head * p.g.heads * 4;
+    return p.tokens * p.group <= (int64_t)p.batch * p.columns && bytes <= kMostScores ? (size_t)bytes : 0;
+}
+
+}  // namespace
+}  // namespace lce
+
+extern "C" size_t lce_kv_attention_weights_workspace_bytes(const lce_kv_attention_weights_desc *desc)
+{
+    using namespace lce;
+    WeightsParams p{};
+    int nt;
+    if (make_params(desc, &p, &nt) != LCE_OK) return 0;
+    return std::max<size_t>(stats_bytes(p) + scores_bytes(p), 16);
+}
+
+extern "C" lce_status lce_kv_attention_weights(const lce_kv_attention_weights_desc *desc, const void *q, const void *cache, const int32_t *page_table,
+                                               const int32_t *lengths, const int32_t *q_starts, const float *previous, float *out, void *workspace,
+                                               size_t workspace_size, void *stream)
+{
+    using namespace lce;
+    WeightsParams p{};
+    int nt;
+    const lce_status st = make_params(desc, &p, &nt);
+    if (st != LCE_OK) return st;
+    if (!q_starts && desc->tokens != desc->batch) return LCE_ERR_INVALID_ARG;
+    if ((!q && desc->tokens > 0) || !cache || !page_table || !lengths || !out || !workspace) return LCE_ERR_INVALID_ARG;
+    const size_t element = type_size(desc->type);
+    if (!aligned(q, element) || !aligned(cache, 16) || !aligned(page_table, 4) || !aligned(lengths, 4) || !aligned(q_starts, 4) || !aligned(previous, 4) ||
+        !aligned(out, 4) || !aligned(workspace, 16))
+        return LCE_ERR_ALIGNMENT;
+    if (workspace_size < std::max<size_t>(stats_bytes(p) + scores_bytes(p), 16)) return LCE_ERR_WORKSPACE;
+    p.q_vectors = p.g.dim % 8 == 0 && aligned(q, 8 * element) && p.q_token % 8 == 0 && p.q_head % 8 == 0;
+    p.q = q; p.cache = static_cast<const uint32_t *>(cache); p.page_table = page_table; p.lengths = lengths; p.q_starts = q_starts;
+    p.previous = desc->decay != 0.0f ? previous : nullptr;
+    p.sums = out;
+    p.stats = static_cast<float2 *>(workspace);
+    p.scores = scores_bytes(p) ? reinterpret_cast<float *>(static_cast<char *>(workspace) + stats_bytes(p)) : nullptr;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (desc->type == LCE_TYPE_FLOAT32) return nt == 2 ? launch_blocks<2, true>(p, s) : launch_blocks<1, true>(p, s);
+    return nt == 2 ? launch_blocks<2, false>(p, s) : launch_blocks<1, false>(p, s);
+}
