@@ -424,7 +424,7 @@ lce_status lce_rotary(const lce_rotary_desc *desc, const void *q, const void *k,
  *   out         fp32 [batch][kv_heads][table_pages * page_size], strides in elements between sequences and between heads; nothing
  *               behind a sequence's last token changes
  *   workspace   lce_kv_attention_weights_workspace_bytes(desc) bytes, 16-byte aligned, no clearing, the call's until its kernels are done
- * The other arguments as for lce_kv_attention.  Everything is fp32: 16-bit rows of q meet the cache's keys without a rounding (of
+ * The other arguments as for lce_kv_attention; tables are below 2^30 tokens.  Everything is fp32: 16-bit rows of q meet the cache's keys without a rounding (of
  * channels below 2^-24 of their row's largest a part is lost), fp32 rows are taken in 22 bits.  No sum depends on the order in which blocks run:
  * results repeat bit for bit. */
 typedef struct {
@@ -453,7 +453,7 @@ lce_status lce_kv_attention_weights(const lce_kv_attention_weights_desc *desc, c
  *   kept          int32 [batch][kv_heads][budget]: the places that each kept token came from, ascending, -1 behind the last
  *   kept_lengths  int32 [batch]: how many there are
  *   kept_scores   fp32 [batch][kv_heads][..] with strides of its own, or NULL: their scores in `budget` places, 0 behind the last
- * Nothing else of the cache changes: its old pages are the caller's again.  first + recent <= budget <= kept_pages * page_size. */
+ * Nothing else of the cache changes: its old pages are the caller's again.  Tables are below 2^30 tokens; first + recent <= budget <= kept_pages * page_size. */
 typedef struct {
     lce_kv_desc cache;
     int32_t batch, table_pages, kept_pages;

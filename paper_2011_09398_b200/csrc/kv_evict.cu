@@ -17,7 +17,6 @@ namespace {
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kBins = 2048, kDigits = 3;
-constexpr int kHeldKeys = 40960;     // of a block, in shared memory; behind that they are made again from the scores
 constexpr int kClusterTokens = 2048; // tokens that a block more is worth
 
 struct EvictParams {
@@ -72,23 +71,23 @@ __device__ __forceinline__ uint32_t key_of(const EvictParams &p, const int32_t *
     return page >= 0 && page < p.g.pages ? key : 0;
 }
 
-struct SelectShared {
+struct alignas(16) SelectShared {
     uint32_t bins[kDigits][kBins];
     uint32_t warp_sums[kWarps];
     uint2 warp_counts[kWarps];
     uint2 counts;                 // of the block: tokens above the threshold, on it
-    uint32_t digit, left, total;
+    uint32_t digit, left, whole;
 };
 
-template <bool HELD>
+// KEYS of a thread, the warp's run of tokens 32 at a time, in registers; 0: any number, made again from the scores wherever they are
+// looked at.
+template <int KEYS>
 __global__ void __launch_bounds__(kThreads) kv_evict_select_kernel(const __grid_constant__ EvictParams p)
 {
-    extern __shared__ __align__(16) uint8_t smem[];
-    SelectShared &sh = *reinterpret_cast<SelectShared *>(smem);
-    uint32_t *const keys = reinterpret_cast<uint32_t *>(smem + sizeof(SelectShared));
+    __shared__ SelectShared sh;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int row = blockIdx.x / p.cluster, rank = blockIdx.x - row * p.cluster, seq = row / p.g.heads, head = row - seq * p.g.heads;
-    for (int i = threadIdx.x; i < kDigits * kBins; i += kThreads) (&sh.bins[0][0])[i] = 0;
+    for (int i = threadIdx.x; i < kDigits * kBins / 4; i += kThreads) reinterpret_cast<uint4 *>(&sh.bins[0][0])[i] = make_uint4(0, 0, 0, 0);
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the moving takes its place; it waits for all of this kernel
     const int32_t length = max(__ldg(p.lengths + seq), 0), held = min(length, p.table_tokens);
@@ -98,35 +97,54 @@ __global__ void __launch_bounds__(kThreads) kv_evict_select_kernel(const __grid_
     const int32_t share = (held + p.cluster - 1) / p.cluster, begin = min(rank * (int64_t)share, (int64_t)held), end = min(begin + (int64_t)share, (int64_t)held);
     const int32_t run = ((end - begin + kWarps - 1) / kWarps + 31) / 32 * 32;
     const int32_t run_begin = min(begin + (int64_t)warp * run, (int64_t)end), run_end = min(run_begin + (int64_t)run, (int64_t)end);
-    const auto key_at = [&](int32_t token) { return HELD ? keys[token - begin] : key_of(p, table, scores, token, length); };
-    if (HELD)
-        for (int32_t t = run_begin + lane; t < run_end; t += 32) keys[t - begin] = key_of(p, table, scores, t, length);
+    uint32_t keys[KEYS > 0 ? KEYS : 1];
+    if (KEYS > 0) {
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i) {
+            const int32_t t = run_begin + 32 * i + lane;
+            keys[i] = t < run_end ? key_of(p, table, scores, t, length) : 0;
+        }
+    }
+    // body(first of 32 tokens, the lane's key; 0 behind the run), by whole warps
+    const auto each_key = [&](auto body) {
+        if (KEYS > 0) {
+#pragma unroll
+            for (int i = 0; i < KEYS; ++i)
+                if (run_begin + 32 * i < run_end) body(run_begin + 32 * i, keys[i]);
+        } else {
+#pragma unroll 4
+            for (int32_t t0 = run_begin; t0 < run_end; t0 += 32) body(t0, t0 + lane < run_end ? key_of(p, table, scores, t0 + lane, length) : 0);
+        }
+    };
     __syncthreads();
 
-    uint32_t prefix = 0, left = (uint32_t)p.budget;  // the threshold's digits so far; how many are still to be taken among the keys with them
-    bool everything = false;
+    // the threshold's digits so far; how many are still to be taken among the keys that have them
+    uint32_t prefix = 0, left = (uint32_t)p.budget, threshold = 0, ties = 0;
 #pragma unroll 1
     for (int digit = 0; digit < kDigits; ++digit) {
         const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, bits = digit == 2 ? 10 : 11;
-        for (int32_t t0 = run_begin; t0 < run_end; t0 += 32) {
-            const int32_t t = t0 + lane;
-            const uint32_t key = t < run_end ? key_at(t) : 0;
+        uint32_t *const bins = sh.bins[digit];
+        each_key([&](int32_t, uint32_t key) {
             const bool counts = key != 0 && (digit == 0 || key >> (shift + bits) == prefix);
             const uint32_t bin = key >> shift & ((1u << bits) - 1);
-            // equal ones in one go: scores that are all alike would queue up
+            // all alike in one go: they would queue up
             const uint32_t those = __ballot_sync(0xffffffffu, counts);
-            if (!those) continue;
+            if (!those) return;
             const int leader = __ffs(those) - 1;
-            const uint32_t common = __shfl_sync(0xffffffffu, bin, leader), alike = __ballot_sync(0xffffffffu, counts && bin == common);
-            if (lane == leader) atomicAdd(&sh.bins[digit][bin], (uint32_t)__popc(alike));
-            else if (counts && bin != common) atomicAdd(&sh.bins[digit][bin], 1u);
-        }
+            const uint32_t common = __shfl_sync(0xffffffffu, bin, leader);
+            if (__all_sync(0xffffffffu, !counts || bin == common)) {
+                if (lane == leader) atomicAdd(&bins[common], (uint32_t)__popc(those));
+            } else if (counts) {
+                atomicAdd(&bins[bin], 1u);
+            }
+        });
         cluster_sync();
         // four bins a thread, the highest first, over all blocks
         const int bin0 = kBins - 4 - 4 * (int)threadIdx.x;
         uint32_t n[4] = {};
+#pragma unroll 8
         for (int r = 0; r < p.cluster; ++r) {
-            const uint4 v = remote4(&sh.bins[digit][bin0], r);
+            const uint4 v = remote4(&bins[bin0], r);
             n[0] += v.w;
             n[1] += v.z;
             n[2] += v.y;
@@ -147,29 +165,30 @@ __global__ void __launch_bounds__(kThreads) kv_evict_select_kernel(const __grid_
             if (w < warp) before += sh.warp_sums[w];
             total += sh.warp_sums[w];
         }
-        if (digit == 0 && total <= left) everything = true;  // all that there are
-        if (!everything && before < left && before + mine >= left) {
+        if (digit == 0 && total <= left) break;  // all that there are stay
+        if (before < left && before + mine >= left) {
             int i = 0;
             while (before + n[i] < left) before += n[i++];
             sh.digit = bin0 + 3 - i;
             sh.left = left - before;
+            sh.whole = before + n[i] == left;
         }
         __syncthreads();
-        if (everything) {
-            left = total;
-            break;
-        }
         prefix = prefix << bits | sh.digit;
         left = sh.left;
+        if (sh.whole) {  // all keys that begin like this stay: their other digits do not matter
+            threshold = max(prefix << shift, 1u) - 1;
+            break;
+        }
+        threshold = prefix;
+        ties = digit == kDigits - 1 ? left : 0;
     }
-    const uint32_t threshold = everything ? 0 : prefix, ties = everything ? 0 : left;
 
     uint2 mine = make_uint2(0, 0);
-    for (int32_t t0 = run_begin; t0 < run_end; t0 += 32) {
-        const uint32_t key = t0 + lane < run_end ? key_at(t0 + lane) : 0;
+    each_key([&](int32_t, uint32_t key) {
         mine.x += __popc(__ballot_sync(0xffffffffu, key > threshold));
         mine.y += __popc(__ballot_sync(0xffffffffu, key == threshold && key != 0));
-    }
+    });
     if (lane == 0) sh.warp_counts[warp] = mine;
     __syncthreads();
     uint2 before = make_uint2(0, 0), all = make_uint2(0, 0);
@@ -197,19 +216,19 @@ __global__ void __launch_bounds__(kThreads) kv_evict_select_kernel(const __grid_
     const uint32_t count = above + ties;
     int32_t *const kept = p.kept + (int64_t)row * p.budget;
     float *const kept_scores = p.kept_scores ? p.kept_scores + seq * p.kept_seq + head * p.kept_head : nullptr;
-    for (int32_t t0 = run_begin; t0 < run_end; t0 += 32) {
-        const int32_t t = t0 + lane;
-        const uint32_t key = t < run_end ? key_at(t) : 0, below = (1u << lane) - 1;
-        const uint32_t higher = __ballot_sync(0xffffffffu, key > threshold), equal = __ballot_sync(0xffffffffu, key == threshold && key != 0);
+    each_key([&](int32_t t0, uint32_t key) {
+        const uint32_t below = (1u << lane) - 1;
+        const bool is_equal = key == threshold && key != 0;
+        const uint32_t higher = __ballot_sync(0xffffffffu, key > threshold), equal = __ballot_sync(0xffffffffu, is_equal);
         const uint32_t ties_before = before.y + __popc(equal & below);
         const uint32_t at = before.x + __popc(higher & below) + min(ties_before, ties);
-        if (key > threshold || (key == threshold && key != 0 && ties_before < ties)) {
-            kept[at] = t;
-            if (kept_scores) kept_scores[at] = __ldg(scores + t);
+        if (key > threshold || (is_equal && ties_before < ties)) {
+            kept[at] = t0 + lane;
+            if (kept_scores) kept_scores[at] = __ldg(scores + t0 + lane);
         }
         before.x += __popc(higher);
         before.y += __popc(equal);
-    }
+    });
     for (int64_t i = count + (int64_t)rank * kThreads + threadIdx.x; i < p.budget; i += (int64_t)p.cluster * kThreads) {
         kept[i] = -1;
         if (kept_scores) kept_scores[i] = 0.0f;
@@ -245,50 +264,72 @@ __device__ __forceinline__ void store_words(uint32_t *p, const Words<W> &r)
     else *p = r.w[0];
 }
 
-// 64 places of keys, 64 of values, 16 of scales for a plane of a tile; two tiles to a block.
+// 64 places of keys, 64 of values, 16 of scales for a plane of a tile; two tiles side by side in a block, TILES pairs of them one behind the
+// other.  A word is four loads away (where it goes, what is kept there, that token's page, the word), so a thread has its tiles'
+// loads of each kind on their way together.
 constexpr int kPlaces = 144, kMoveThreads = 2 * kPlaces;
 
+template <int TILES>
 __global__ void __launch_bounds__(kMoveThreads) kv_evict_move_kernel(const __grid_constant__ EvictParams p)
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int in_block = threadIdx.x / kPlaces, place = threadIdx.x - in_block * kPlaces;
-    const int tile = 2 * blockIdx.x + in_block, head = blockIdx.y, seq = blockIdx.z, j0 = tile * kKvTile;
-    if (j0 >= p.budget) return;
-    const int32_t in_table = p.by_page(j0), page = __ldg(p.kept_table + (int64_t)seq * p.kept_pages + in_table);
-    if (page < 0 || page >= p.g.pages) return;
+    const int head = blockIdx.y, seq = blockIdx.z, blocks = p.g.blocks;
     const bool values = place >= 64 && place < 128;
     const int in_part = values ? place - 64 : place < 64 ? place : place - 128;
     // the token, or the first of the two, that the place is for
     const int token = values ? 8 * (in_part >> 5) + 2 * (in_part & 3) : place < 64 ? 8 * (in_part >> 5) + ((in_part & 31) >> 2) : in_part;
     const int32_t *const kept = p.kept + ((int64_t)seq * p.g.heads + head) * p.budget, *const table = p.page_table + (int64_t)seq * p.table_pages;
-    const int32_t from0 = j0 + token < p.budget ? kept[j0 + token] : -1, from1 = values && j0 + token + 1 < p.budget ? kept[j0 + token + 1] : -1;
-    if (from0 < 0) return;  // those behind are not there either
-    const int32_t slot0 = slot_of(p, table, from0), slot1 = from1 >= 0 ? slot_of(p, table, from1) : -1;
-    const uint32_t *const tile0 = tile_of(p, slot0, head), *const tile1 = slot1 >= 0 ? tile_of(p, slot1, head) : tile0;
-    const int t0 = slot0 % kKvTile, t1 = slot1 >= 0 ? slot1 % kKvTile : t0;
-    uint32_t *const to = tile_of(p, page * p.g.page_size + (j0 - in_table * p.g.page_size), head);
-    const int blocks = p.g.blocks;
+    uint32_t *to[TILES];
+    int32_t from0[TILES], from1[TILES];
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) {
+        const int j0 = (2 * (blockIdx.x * TILES + i) + in_block) * kKvTile, in_table = p.by_page(j0);
+        const int32_t page = j0 < p.budget ? __ldg(p.kept_table + (int64_t)seq * p.kept_pages + in_table) : -1;
+        to[i] = page >= 0 && page < p.g.pages ? tile_of(p, page * p.g.page_size + (j0 - in_table * p.g.page_size), head) : nullptr;
+        from0[i] = j0 + token < p.budget ? kept[j0 + token] : -1;  // where it is none, those behind are none either
+        from1[i] = values && j0 + token + 1 < p.budget ? kept[j0 + token + 1] : -1;
+    }
+    const uint32_t *tile0[TILES], *tile1[TILES];
+    int t0[TILES], t1[TILES];
+#pragma unroll
+    for (int i = 0; i < TILES; ++i) {
+        if (from0[i] < 0) to[i] = nullptr;
+        const int32_t slot0 = to[i] ? slot_of(p, table, from0[i]) : 0, slot1 = to[i] && from1[i] >= 0 ? slot_of(p, table, from1[i]) : slot0;
+        tile0[i] = tile_of(p, slot0, head);
+        tile1[i] = tile_of(p, slot1, head);
+        t0[i] = slot0 % kKvTile;
+        t1[i] = slot1 % kKvTile;
+    }
     const auto plane = [&](int first, auto width) {
         constexpr int W = decltype(width)::value;
-        if (values) {
-            const int base = 64 * blocks + 64 * first, eighth = (in_part & 31) >> 2;
-            const Words<W> a = load_words<W>(tile0 + base + ((t0 >> 3) * 32 + eighth * 4 + (t0 >> 1 & 3)) * W);
-            const Words<W> b = load_words<W>(tile1 + base + ((t1 >> 3) * 32 + eighth * 4 + (t1 >> 1 & 3)) * W);
-            uint32_t *const at = to + base + in_part * W;
-            if (from1 >= 0) {
+        Words<W> a[TILES], b[TILES];
+        const int base = values ? 64 * blocks + 64 * first : place < 64 ? 64 * first : 128 * blocks + 16 * first;
+#pragma unroll
+        for (int i = 0; i < TILES; ++i) {
+            if (!to[i]) continue;
+            const auto word = [&](int t) {
+                if (values) return (t >> 3) * 32 + (in_part & 28) + (t >> 1 & 3);
+                return place < 64 ? (t >> 3) * 32 + (t & 7) * 4 + (in_part & 3) : t;
+            };
+            a[i] = load_words<W>(tile0[i] + base + word(t0[i]) * W);
+            if (values) b[i] = load_words<W>(tile1[i] + base + word(t1[i]) * W);
+        }
+#pragma unroll
+        for (int i = 0; i < TILES; ++i) {
+            if (!to[i]) continue;
+            uint32_t *const at = to[i] + base + in_part * W;
+            if (!values) {
+                store_words<W>(at, a[i]);
+            } else if (from1[i] >= 0) {
                 Words<W> r;
 #pragma unroll
-                for (int i = 0; i < W; ++i) r.w[i] = __byte_perm(a.w[i], b.w[i], (t0 & 1 ? 0x32 : 0x10) | (t1 & 1 ? 0x7600 : 0x5400));
+                for (int w = 0; w < W; ++w) r.w[w] = __byte_perm(a[i].w[w], b[i].w[w], (t0[i] & 1 ? 0x32 : 0x10) | (t1[i] & 1 ? 0x7600 : 0x5400));
                 store_words<W>(at, r);
-            } else {
+            } else {  // the last token: its half of the words
 #pragma unroll
-                for (int i = 0; i < W; ++i) *reinterpret_cast<uint16_t *>(at + i) = (uint16_t)(a.w[i] >> (t0 & 1 ? 16 : 0));
+                for (int w = 0; w < W; ++w) *reinterpret_cast<uint16_t *>(at + w) = (uint16_t)(a[i].w[w] >> (t0[i] & 1 ? 16 : 0));
             }
-        } else if (place < 64) {
-            store_words<W>(to + 64 * first + in_part * W, load_words<W>(tile0 + 64 * first + ((t0 >> 3) * 32 + (t0 & 7) * 4 + (in_part & 3)) * W));
-        } else {
-            const int base = 128 * blocks + 16 * first;
-            store_words<W>(to + base + in_part * W, load_words<W>(tile0 + base + t0 * W));
         }
     };
     for (int first = 0; first + 4 <= blocks; first += 4) plane(first, std::integral_constant<int, 4>());
@@ -296,15 +337,24 @@ __global__ void __launch_bounds__(kMoveThreads) kv_evict_move_kernel(const __gri
     if (blocks & 1) plane(blocks - 1, std::integral_constant<int, 1>());
 }
 
-template <bool HELD>
-lce_status launch_select(const EvictParams &p, size_t smem, cudaStream_t s)
+lce_status launch_move(const EvictParams &p, cudaStream_t s)
 {
-    static SmemOptIn opt_in;
-    if (!opt_in.ensure(kv_evict_select_kernel<HELD>, smem)) return LCE_ERR_CUDA;
+    constexpr int kTogether = 4;
+    const int64_t pairs = ((p.budget + kKvTile - 1) / kKvTile + 1) / 2;
+    // several tiles to a thread once every SM has its blocks without
+    if (pairs * p.g.heads * p.batch > 148 * 6)
+        return launch_dependent(kv_evict_move_kernel<kTogether>, dim3((unsigned)((pairs + kTogether - 1) / kTogether), (unsigned)p.g.heads, (unsigned)p.batch), kMoveThreads, 0, s, p);
+    return launch_dependent(kv_evict_move_kernel<1>, dim3((unsigned)pairs, (unsigned)p.g.heads, (unsigned)p.batch), kMoveThreads, 0, s, p);
+}
+
+lce_status launch_select(const EvictParams &p, cudaStream_t s)
+{
+    const int64_t share = ((int64_t)p.table_tokens + p.cluster - 1) / p.cluster;
+    const auto kernel = share <= 2 * kThreads ? kv_evict_select_kernel<2> : share <= 8 * kThreads ? kv_evict_select_kernel<8>
+                      : share <= 32 * kThreads ? kv_evict_select_kernel<32> : kv_evict_select_kernel<0>;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(p.batch * p.g.heads * p.cluster), 1, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
-    cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -314,7 +364,7 @@ lce_status launch_select(const EvictParams &p, size_t smem, cudaStream_t s)
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    if (cudaLaunchKernelEx(&cfg, kv_evict_select_kernel<HELD>, p) != cudaSuccess) {
+    if (cudaLaunchKernelEx(&cfg, kernel, p) != cudaSuccess) {
         cudaGetLastError();
         return LCE_ERR_CUDA;
     }
@@ -339,7 +389,7 @@ extern "C" lce_status lce_kv_evict(const lce_kv_evict_desc *desc, void *cache, c
     if ((int64_t)d.first + d.recent > d.budget || d.budget > (int64_t)d.kept_pages * d.cache.page_size) return LCE_ERR_INVALID_ARG;
     for (const int64_t s : {d.scores_seq_stride, d.scores_head_stride, d.kept_scores_seq_stride, d.kept_scores_head_stride})
         if (!stride_ok(s)) return LCE_ERR_INVALID_ARG;
-    if ((int64_t)d.table_pages * d.cache.page_size >= (1ll << 31) || (int64_t)d.kept_pages * d.cache.page_size >= (1ll << 31) || d.batch > 65535 ||
+    if ((int64_t)d.table_pages * d.cache.page_size >= (1ll << 30) || (int64_t)d.kept_pages * d.cache.page_size >= (1ll << 30) || d.batch > 65535 ||
         (int64_t)d.batch * d.cache.kv_heads * 8 >= (1ll << 31))
         return LCE_ERR_UNSUPPORTED;
     if (!cache || !page_table || !lengths || !scores || !kept_table || !kept || !kept_lengths) return LCE_ERR_INVALID_ARG;
@@ -358,11 +408,7 @@ extern "C" lce_status lce_kv_evict(const lce_kv_evict_desc *desc, void *cache, c
     // blocks to a row, as long as the GPU has places for them
     p.cluster = 1;
     while (p.cluster < 8 && p.table_tokens > kClusterTokens * p.cluster && (int64_t)p.batch * p.g.heads * p.cluster * 2 <= 148 * 2) p.cluster *= 2;
-    const int64_t share = ((int64_t)p.table_tokens + p.cluster - 1) / p.cluster;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const bool held = share <= kHeldKeys;
-    const lce_status chosen = held ? launch_select<true>(p, sizeof(SelectShared) + 4 * (size_t)share, s) : launch_select<false>(p, sizeof(SelectShared), s);
-    if (chosen != LCE_OK) return chosen;
-    const int64_t tiles = (p.budget + kKvTile - 1) / kKvTile;
-    return launch_dependent(kv_evict_move_kernel, dim3((unsigned)((tiles + 1) / 2), (unsigned)p.g.heads, (unsigned)p.batch), kMoveThreads, 0, s, p);
+    const lce_status chosen = launch_select(p, s);
+    return chosen != LCE_OK ? chosen : launch_move(p, s);
 }

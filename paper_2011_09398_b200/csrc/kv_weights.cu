@@ -11,6 +11,7 @@
 // multiply-add), the scale multiplies a block's finished sums in fp32; 16-bit rows of q are one f16 number times a power of two of the row,
 // fp32 rows two of them.
 #include "kv_mma.cuh"
+#include "kv_weights.cuh"
 
 #include <math.h>
 
@@ -19,104 +20,13 @@
 namespace lce {
 namespace {
 
+__host__ __device__ constexpr int key_words(int blocks) { return 80 * blocks; }  // of a tile: its keys and scales
+
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kStages = 4;                  // tiles in flight of a warp
-constexpr int kMostTiles = 256;             // of a piece: its tokens' sums are in shared memory
-constexpr int kLeastTiles = kWarps;         // that a piece is worth
 constexpr int kBlocksPerSm = 4;
 constexpr int64_t kMostScores = 256 << 20;  // bytes of workspace that scores may take
 constexpr int64_t kMostStats = 64 << 20;
-
-struct WeightsParams : AttnParams {
-    float decay;
-    int64_t previous_seq, previous_head, out_seq, out_head;
-    const float *previous;
-    float *sums;                            // where the weights go
-    float2 *stats;                          // [kv head][row * group + query head][piece]: largest, sum
-    float *scores;                          // [kv head][token of the batch][columns], or null
-    int64_t scores_head;
-    int32_t columns;                        // of a tile of them
-    int32_t pieces;                         // that a sequence can have
-};
-
-__host__ __device__ constexpr int key_words(int blocks) { return 80 * blocks; }  // of a tile: its keys and scales
-
-// A range of tiles of a sequence.
-struct Piece {
-    Unit u;                // columns [column0, ..): set by the loops over them
-    int32_t index, pieces; // which one of the sequence's
-    int32_t columns;
-    int64_t tiles_before;  // tiles of the sequences in front
-};
-
-// Finds the `at`-th piece; false: there is no such one.  Every warp works this out from the lengths: pieces of at most `most` tiles, where
-// `most` follows from the whole batch's.
-__device__ __forceinline__ bool find_piece(const WeightsParams &p, int at, Piece *piece)
-{
-    const int lane = threadIdx.x & 31;
-    const auto tiles_of = [&](int b) { return b < p.batch ? (tokens_held(p, max(__ldg(p.lengths + b), 0)) + kKvTile - 1) / kKvTile : 0; };
-    const int32_t first = tiles_of(lane);
-    int64_t total = first;
-    for (int b0 = 32; b0 < p.batch; b0 += 32) total += tiles_of(b0 + lane);
-#pragma unroll
-    for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
-    const int32_t most = (int32_t)min(max((total + p.target - 1) / p.target, (int64_t)kLeastTiles), (int64_t)kMostTiles);
-    int32_t before = 0;
-    int64_t tiles_before = 0;
-    for (int b0 = 0; b0 < p.batch; b0 += 32) {
-        const int32_t tiles = b0 ? tiles_of(b0 + lane) : first, pieces = (tiles + most - 1) / most;
-        int32_t upto = pieces;
-        int64_t tiles_upto = tiles;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int32_t o = __shfl_up_sync(0xffffffffu, upto, d);
-            const int64_t n = __shfl_up_sync(0xffffffffu, tiles_upto, d);
-            if (lane >= d) {
-                upto += o;
-                tiles_upto += n;
-            }
-        }
-        const uint32_t has = __ballot_sync(0xffffffffu, before + upto > at);
-        if (has) {
-            const int from = __ffs(has) - 1;
-            const int32_t n = __shfl_sync(0xffffffffu, tiles, from);
-            piece->pieces = __shfl_sync(0xffffffffu, pieces, from);
-            piece->index = at - (before + __shfl_sync(0xffffffffu, upto - pieces, from));
-            piece->tiles_before = tiles_before + __shfl_sync(0xffffffffu, tiles_upto - tiles, from);
-            const Sequence s = sequence<8>(p, b0 + from);
-            piece->u.seq = b0 + from;
-            piece->u.length = s.length;
-            piece->u.rows = s.rows;
-            piece->u.row0 = s.row0;
-            piece->u.column0 = 0;
-            piece->columns = s.rows * p.group;
-            const int32_t each = n / piece->pieces, more = n - each * piece->pieces;  // equal pieces
-            piece->u.tile0 = piece->index * each + min(piece->index, more);
-            piece->u.tile1 = piece->u.tile0 + each + (piece->index < more ? 1 : 0);
-            return true;
-        }
-        before += __shfl_sync(0xffffffffu, upto, 31);
-        tiles_before += __shfl_sync(0xffffffffu, tiles_upto, 31);
-    }
-    return false;
-}
-
-// Tiles of the piece that some column of [column0, column0 + count) sees: columns' ranges move up with the rows.  all_lo, all_hi: tokens that
-// each of them sees.
-struct View {
-    int32_t tile0, tile1, all_lo, all_hi;
-};
-__device__ __forceinline__ View view(const WeightsParams &p, const Piece &piece, int count)
-{
-    View v;
-    int32_t any_lo, any_hi;
-    column_range(p, piece.u, piece.u.column0, &any_lo, &v.all_hi);
-    column_range(p, piece.u, min(piece.u.column0 + count, piece.columns) - 1, &v.all_lo, &any_hi);
-    v.tile0 = max(piece.u.tile0, any_lo / kKvTile);
-    v.tile1 = min(piece.u.tile1, (any_hi + kKvTile - 1) / kKvTile);
-    if (any_hi <= any_lo) v.tile1 = v.tile0;
-    return v;
-}
 
 // B blocks of 32 channels, NT tiles of 8 columns, SPLIT: fp32 rows.
 template <int B, int NT, bool SPLIT>
@@ -289,11 +199,10 @@ __device__ __forceinline__ void each_tile(const WeightsParams &p, const Piece &p
     __syncwarp();
 }
 
-__device__ __forceinline__ bool keeps_scores(const WeightsParams &p, const Piece &piece) { return p.scores && piece.columns <= p.columns; }
-// Scores of a token: the sequence's columns, rounded up to an even number; a sequence begins where room for a whole tile of columns puts it.
+// Scores of a tile's first token.
 __device__ __forceinline__ float *scores_at(const WeightsParams &p, const Piece &piece, int head, int32_t tile)
 {
-    return p.scores + head * p.scores_head + (piece.tiles_before * p.columns + (int64_t)tile * ((piece.columns + 1) & ~1)) * kKvTile;
+    return p.scores + head * p.scores_head + piece.scores_before + (int64_t)tile * kKvTile * scores_stride(piece.columns);
 }
 
 // The sum of a column's powers of two, joined: s e^.. is held as (largest, sum relative to it).
@@ -315,8 +224,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) kv_weights_scores_kern
     Piece piece;
     if (!find_piece(p, blockIdx.x, &piece)) return;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, head = blockIdx.y;
-    const bool keeps = keeps_scores(p, piece);
-    const int stride = (piece.columns + 1) & ~1;
+    const int stride = scores_stride(piece.columns);
     for (piece.u.column0 = 0; piece.u.column0 < piece.columns; piece.u.column0 += COLUMNS) {
         const View v = view(p, piece, COLUMNS);
         Columns<B, NT, SPLIT> c;
@@ -340,13 +248,13 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) kv_weights_scores_kern
 #pragma unroll
                     for (int i = 0; i < 4; ++i) s[nt][i] = -INFINITY;
             }
-            if (keeps) {
-                float *const to = scores_at(p, piece, head, tile) + (lane >> 2) * stride + 2 * (lane & 3);
+            if (p.scores) {
+                float *const to = scores_at(p, piece, head, tile) + (int64_t)(lane >> 2) * stride + piece.u.column0 + 2 * (lane & 3);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
-                    if (8 * nt + 2 * (lane & 3) < stride) {
+                    if (piece.u.column0 + 8 * nt + 2 * (lane & 3) < stride) {
                         *reinterpret_cast<float2 *>(to + 8 * nt) = make_float2(s[nt][0], s[nt][1]);
-                        *reinterpret_cast<float2 *>(to + 8 * nt + 8 * stride) = make_float2(s[nt][2], s[nt][3]);
+                        *reinterpret_cast<float2 *>(to + 8 * nt + 8 * (int64_t)stride) = make_float2(s[nt][2], s[nt][3]);
                     }
             }
 #pragma unroll
@@ -385,6 +293,106 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) kv_weights_scores_kern
     }
 }
 
+// The pieces' parts of `count` columns joined: a column's largest score and what its powers of two are multiplied with, 0 where it sees nothing or
+// is none.  Eight threads to a column.
+__device__ __forceinline__ void column_totals(const WeightsParams &p, const Piece &piece, int head, int count, float *tops, float *parts)
+{
+    constexpr int EACH = 8;
+    for (int in_tile = threadIdx.x / EACH; in_tile - (int)(threadIdx.x & 31) / EACH < count; in_tile += blockDim.x / EACH) {
+        float top = -INFINITY, sum = 0.0f;
+        if (in_tile < count && piece.u.column0 + in_tile < piece.columns) {
+            const float2 *const from = p.stats + ((head * p.tokens + piece.u.row0) * p.group + piece.u.column0 + in_tile) * p.pieces;
+#pragma unroll 4
+            for (int i = threadIdx.x % EACH; i < piece.pieces; i += EACH) {
+                const float2 part = from[i];
+                join_sums(top, sum, part.x, part.y);
+            }
+        }
+#pragma unroll
+        for (int d = 1; d < EACH; d <<= 1) {
+            const float t = __shfl_xor_sync(0xffffffffu, top, d), s = __shfl_xor_sync(0xffffffffu, sum, d);
+            join_sums(top, sum, t, s);
+        }
+        if (in_tile < count && threadIdx.x % EACH == 0) {
+            tops[in_tile] = top == -INFINITY ? 0.0f : top;
+            parts[in_tile] = sum == 0.0f ? 0.0f : 1.0f / sum;
+        }
+    }
+}
+
+// What stood there before, as far as it counts, and the weight w of token t.
+__device__ __forceinline__ void put_weight(const WeightsParams &p, const Piece &piece, int head, int32_t t, float w)
+{
+    if (p.previous && t < piece.u.length - piece.u.rows) w = fmaf(p.decay, p.previous[piece.u.seq * p.previous_seq + head * p.previous_head + t], w);
+    p.sums[piece.u.seq * p.out_seq + head * p.out_head + t] = w;
+}
+
+// Scores that were kept: a thread to a token, kTogether at a time.
+constexpr int kKeptThreads = 256, kTogether = 4, kKeptColumns = 128;
+
+__global__ void __launch_bounds__(kKeptThreads) kv_weights_kept_kernel(const __grid_constant__ WeightsParams p)
+{
+    __shared__ float tops[kKeptColumns], parts[kKeptColumns];
+    __shared__ int2 ranges[kKeptColumns];  // tokens that a column sees: the others' places may never have been written
+    Piece piece;
+    // the lengths are what the kernel in front read: nothing has written them since
+    const bool found = find_piece(p, blockIdx.x, &piece);
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // every block: what comes behind this kernel relies on the one in front, too
+    if (!found) return;
+    const int head = blockIdx.y, stride = scores_stride(piece.columns);
+    const View v = view(p, piece, piece.columns);
+    const int32_t first = piece.u.tile0 * kKvTile, last = min(piece.u.tile1 * kKvTile, tokens_held(p, piece.u.length));
+    const int32_t step = kKeptThreads * kTogether;
+    const float *const scores = scores_at(p, piece, head, 0);
+    // whole blocks go round together: the columns' totals are theirs
+    for (int32_t t0 = first + blockIdx.z * step; t0 < last; t0 += gridDim.z * step) {
+        float w[kTogether] = {};
+        for (piece.u.column0 = 0; piece.u.column0 < piece.columns; piece.u.column0 += kKeptColumns) {
+            const int count = min(kKeptColumns, piece.columns - piece.u.column0);
+            if (piece.columns > kKeptColumns || t0 == first + (int32_t)blockIdx.z * step) {
+                __syncthreads();
+                column_totals(p, piece, head, count, tops, parts);
+                if ((int)threadIdx.x < count) column_range(p, piece.u, piece.u.column0 + threadIdx.x, &ranges[threadIdx.x].x, &ranges[threadIdx.x].y);
+                __syncthreads();
+            }
+            const auto go = [&](auto vector) {
+                constexpr int N = sizeof(vector) / 4;
+                for (int c = 0; c < count; c += N) {
+                    decltype(vector) s[kTogether];
+#pragma unroll
+                    for (int k = 0; k < kTogether; ++k) {
+                        const int32_t t = t0 + k * kKeptThreads + threadIdx.x;
+                        const bool seen = t < last && t >= v.tile0 * kKvTile && t < v.tile1 * kKvTile;
+                        float *const e = reinterpret_cast<float *>(s + k);
+                        if (seen) {
+                            s[k] = *reinterpret_cast<const decltype(vector) *>(scores + (int64_t)t * stride + piece.u.column0 + c);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < N; ++i) e[i] = -INFINITY;
+                        }
+                    }
+#pragma unroll
+                    for (int k = 0; k < kTogether; ++k)
+#pragma unroll
+                        for (int i = 0; i < N; ++i)
+                            if (c + i < count) {
+                                const float x = reinterpret_cast<const float *>(s + k)[i];
+                                const int32_t t = t0 + k * kKeptThreads + threadIdx.x;
+                                if (x != -INFINITY && t >= ranges[c + i].x && t < ranges[c + i].y) w[k] += exp2_fast(x - tops[c + i]) * parts[c + i];
+                            }
+                }
+            };
+            if (stride % 4 == 0) go(float4());
+            else go(float2());
+        }
+#pragma unroll
+        for (int k = 0; k < kTogether; ++k) {
+            const int32_t t = t0 + k * kKeptThreads + threadIdx.x;
+            if (t < last) put_weight(p, piece, head, t, w[k]);
+        }
+    }
+}
+
 template <int B, int NT, bool SPLIT>
 __global__ void __launch_bounds__(kThreads, kBlocksPerSm) kv_weights_sum_kernel(const __grid_constant__ WeightsParams p)
 {
@@ -401,39 +409,10 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) kv_weights_sum_kernel(
     const int tokens = (piece.u.tile1 - piece.u.tile0) * kKvTile;
     for (int i = threadIdx.x; i < tokens; i += kThreads) weights[i] = 0.0f;
     for (piece.u.column0 = 0; piece.u.column0 < piece.columns; piece.u.column0 += COLUMNS) {
-        {   // a column's largest and what its powers are multiplied with; 0 where it sees nothing
-            constexpr int EACH = kThreads / COLUMNS;
-            const int in_tile = threadIdx.x / EACH, column = piece.u.column0 + in_tile;
-            float top = -INFINITY, sum = 0.0f;
-            if (column < piece.columns) {
-                const float2 *const from = p.stats + ((head * p.tokens + piece.u.row0) * p.group + column) * p.pieces;
-                for (int i = threadIdx.x % EACH; i < piece.pieces; i += EACH) join_sums(top, sum, from[i].x, from[i].y);
-            }
-#pragma unroll
-            for (int d = 1; d < EACH; d <<= 1) {
-                const float t = __shfl_xor_sync(0xffffffffu, top, d), s = __shfl_xor_sync(0xffffffffu, sum, d);
-                join_sums(top, sum, t, s);
-            }
-            if (threadIdx.x % EACH == 0) {
-                tops[in_tile] = top == -INFINITY ? 0.0f : top;
-                parts[in_tile] = sum == 0.0f ? 0.0f : 1.0f / sum;
-            }
-        }
+        column_totals(p, piece, head, COLUMNS, tops, parts);
         __syncthreads();
         const View v = view(p, piece, COLUMNS);
-        if (keeps_scores(p, piece)) {
-            const int stride = (piece.columns + 1) & ~1;
-            const float *const from = scores_at(p, piece, head, v.tile0);
-            for (int i = threadIdx.x; i < (v.tile1 - v.tile0) * kKvTile; i += kThreads) {
-                float w = 0.0f;
-                for (int c = 0; c < piece.columns; c += 2) {
-                    const float2 s = *reinterpret_cast<const float2 *>(from + (int64_t)i * stride + c);
-                    w += s.x == -INFINITY ? 0.0f : exp2_fast(s.x - tops[c]) * parts[c];
-                    if (c + 1 < piece.columns) w += s.y == -INFINITY ? 0.0f : exp2_fast(s.y - tops[c + 1]) * parts[c + 1];
-                }
-                weights[(v.tile0 - piece.u.tile0) * kKvTile + i] = w;
-            }
-        } else {
+        {
             Columns<B, NT, SPLIT> c;
             c.load(p, piece.u, head);
             float top[NT][2], part[NT][2];
@@ -464,14 +443,8 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) kv_weights_sum_kernel(
         __syncthreads();
     }
     __syncthreads();
-    const int32_t held = tokens_held(p, piece.u.length), first_new = piece.u.length - piece.u.rows;
-    for (int i = threadIdx.x; i < tokens; i += kThreads) {
-        const int32_t t = piece.u.tile0 * kKvTile + i;
-        if (t >= held) break;
-        float w = weights[i];
-        if (p.previous && t < first_new) w = fmaf(p.decay, p.previous[piece.u.seq * p.previous_seq + head * p.previous_head + t], w);
-        p.sums[piece.u.seq * p.out_seq + head * p.out_head + t] = w;
-    }
+    const int32_t held = tokens_held(p, piece.u.length);
+    for (int i = threadIdx.x; i < tokens && piece.u.tile0 * kKvTile + i < held; i += kThreads) put_weight(p, piece, head, piece.u.tile0 * kKvTile + i, weights[i]);
 }
 
 template <int B, int NT, bool SPLIT>
@@ -485,6 +458,8 @@ lce_status launch(const WeightsParams &p, cudaStream_t s)
         const lce_status st = launch_dependent(kv_weights_scores_kernel<B, NT, SPLIT>, grid, kThreads, ring, s, p);
         if (st != LCE_OK) return st;
     }
+    // a block's tokens in one go where the GPU has room for that many blocks
+    if (p.scores) return launch_dependent(kv_weights_kept_kernel, dim3(grid.x, grid.y, 2), kKeptThreads, 0, s, p);
     return launch_dependent(kv_weights_sum_kernel<B, NT, SPLIT>, grid, kThreads, all, s, p);
 }
 
@@ -518,7 +493,7 @@ lce_status make_params(const lce_kv_attention_weights_desc *d, WeightsParams *p,
     if (d->heads % d->cache.kv_heads != 0 || !isfinite(d->scale) || !isfinite(d->decay)) return LCE_ERR_INVALID_ARG;
     for (const int64_t s : {d->q_token_stride, d->q_head_stride, d->previous_seq_stride, d->previous_head_stride, d->out_seq_stride, d->out_head_stride})
         if (!stride_ok(s)) return LCE_ERR_INVALID_ARG;
-    if (d->tokens >= (1ll << 31) || d->tokens * d->heads >= (1ll << 31) || (int64_t)d->table_pages * d->cache.page_size >= (1ll << 31) || d->batch >= (1 << 20) ||
+    if (d->tokens >= (1ll << 31) || d->tokens * d->heads >= (1ll << 31) || (int64_t)d->table_pages * d->cache.page_size >= (1ll << 30) || d->batch >= (1 << 20) ||
         (int64_t)p->g.slots / kKvTile * p->g.heads >= (1ll << 31))
         return LCE_ERR_UNSUPPORTED;
     p->batch = d->batch; p->group = d->heads / d->cache.kv_heads; p->table_pages = d->table_pages;
@@ -538,17 +513,17 @@ lce_status make_params(const lce_kv_attention_weights_desc *d, WeightsParams *p,
     if (units >= (1ll << 31)) return LCE_ERR_UNSUPPORTED;
     p->units = (int32_t)units;
     p->pieces = (int32_t)std::min<int64_t>(tiles, std::max<int64_t>(p->target, (tiles + kMostTiles - 1) / kMostTiles) + 1);
-    p->columns = 8 * *nt;
-    p->scores_head = p->batch * tiles * kKvTile * p->columns;
+    // what sequences as long as the table would leave
+    p->scores_head = (p->tokens * p->group + p->batch) * tiles * kKvTile;
     return LCE_OK;
 }
 
 size_t stats_bytes(const WeightsParams &p) { return ((size_t)p.tokens * p.group * p.g.heads * p.pieces * 8 + 15) / 16 * 16; }
-// Scores are kept where there is room for them and, on average, sequences have no more columns than a tile of them.
+// Scores are kept where there is room for them.
 size_t scores_bytes(const WeightsParams &p)
 {
-    const int64_t bytes = p.scores_head * p.g.heads * 4;
-    return p.tokens * p.group <= (int64_t)p.batch * p.columns && bytes <= kMostScores ? (size_t)bytes : 0;
+    const double bytes = 4.0 * p.scores_head * p.g.heads;
+    return p.tokens > 0 && bytes <= kMostScores ? (size_t)p.scores_head * p.g.heads * 4 : 0;
 }
 
 }  // namespace

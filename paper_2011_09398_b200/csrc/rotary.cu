@@ -9,12 +9,12 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 namespace lce {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kTogether = 4;    // heads whose loads are on their way at once
 constexpr int kMostHeads = 8;   // of a thread
 
 struct RotaryRows {
@@ -50,8 +50,9 @@ __device__ __forceinline__ void turn_of(uint32_t part, float amplitude, float &c
     if (quarter & 2) s = -s;
 }
 
-template <typename T, bool VEC, bool PAIRS>
-__global__ void __launch_bounds__(kThreads) rotary_kernel(const __grid_constant__ RotaryParams p)
+// kTogether heads' loads are on their way at once.
+template <typename T, bool VEC, bool PAIRS, int kTogether>
+__global__ void __launch_bounds__(kThreads, kTogether * sizeof(T) <= 4 ? 3 : 2) rotary_kernel(const __grid_constant__ RotaryParams p)
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int64_t item = (int64_t)blockIdx.x * kThreads + threadIdx.x;
@@ -148,9 +149,13 @@ lce_status launch(const RotaryParams &p, bool pairs, cudaStream_t s)
         for (const int64_t stride : {r.in_token, r.in_head, r.out_token, r.out_head}) vec = vec && stride % 8 == 0;
     }
     const dim3 grid((unsigned)((p.items + kThreads - 1) / kThreads), (unsigned)((p.heads + p.per_thread - 1) / p.per_thread));
-    const auto kernel = pairs ? (vec ? rotary_kernel<T, true, true> : rotary_kernel<T, false, true>)
-                              : (vec ? rotary_kernel<T, true, false> : rotary_kernel<T, false, false>);
-    return launch_dependent(kernel, grid, kThreads, 0, s, p);
+    const auto go = [&](auto together) {
+        constexpr int N = decltype(together)::value;
+        const auto kernel = pairs ? (vec ? rotary_kernel<T, true, true, N> : rotary_kernel<T, false, true, N>)
+                                  : (vec ? rotary_kernel<T, true, false, N> : rotary_kernel<T, false, false, N>);
+        return launch_dependent(kernel, grid, kThreads, 0, s, p);
+    };
+    return p.per_thread == 1 ? go(std::integral_constant<int, 1>()) : go(std::integral_constant<int, sizeof(T) == 2 ? 4 : 2>());
 }
 
 bool stride_ok(int64_t s) { return s >= 0 && s < (1ll << 40); }

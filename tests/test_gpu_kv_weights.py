@@ -227,3 +227,23 @@ def test_graph_of_growing_sequences_and_workspaces():
         got = lce.lce_kv_attention_weights(*arguments, out=torch.full_like(out, MARK))
     torch.cuda.synchronize()
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("dim, group, news", [(64, 3, [1, 1]), (128, 4, [6, 2]), (192, 9, [1, 3])])
+def test_tables_too_wide_for_scores_to_be_kept(dtype, dim, group, news):
+    s = Setup(dtype, [300, 70], news, 1, group, dim, seed=15, table_extra=1000000)
+    room = lce.lce_kv_attention_weights_workspace_bytes(s.desc, 2, sum(news), group, s.table.shape[1], dtype)
+    assert room < 128 << 20  # the scores of such a table would be above 256 MB
+    out = run(s, window=150)
+    narrow = Setup(dtype, [300, 70], news, 1, group, dim, seed=15)
+    want, bound = expected(narrow, window=150)
+    n = want.shape[2]
+    check(out[:, :, :n], (want, bound))
+    assert bool((out[:, :, n:] == MARK).all())
+
+
+@pytest.mark.parametrize("group", [129, 260])
+def test_more_columns_than_are_joined_at_once(group):
+    s = Setup(F32, [70, 33], [1, 2], 1, group, 32, seed=16)
+    check(run(s), expected(s))
