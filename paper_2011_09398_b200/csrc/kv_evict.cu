@@ -15,7 +15,7 @@
 namespace lce {
 namespace {
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kThreads = 1024, kWarps = kThreads / 32;
 constexpr int kBins = 2048, kDigits = 3;
 constexpr int kClusterTokens = 2048; // tokens that a block more is worth
 
@@ -33,12 +33,6 @@ struct EvictParams {
     float *kept_scores;
 };
 
-__device__ __forceinline__ uint4 remote4(const void *p, int rank)
-{
-    uint4 v;
-    asm volatile("ld.shared::cluster.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(remote_place(p, rank)) : "memory");
-    return v;
-}
 __device__ __forceinline__ uint2 remote2(const void *p, int rank)
 {
     uint2 v;
@@ -46,29 +40,14 @@ __device__ __forceinline__ uint2 remote2(const void *p, int rank)
     return v;
 }
 
-// Where a token of a sequence lies: its slot, or negative on a page outside the pool.
-__device__ __forceinline__ int32_t slot_of(const EvictParams &p, const int32_t *table, int32_t token)
-{
-    const int32_t in_table = p.by_page(token), page = __ldg(table + in_table);
-    return page >= 0 && page < p.g.pages ? page * p.g.page_size + (token - in_table * p.g.page_size) : -1;
-}
-__device__ __forceinline__ uint32_t *tile_of(const EvictParams &p, int32_t slot, int head)
-{
-    const int32_t page = p.by_page(slot);
-    const int64_t tile = ((int64_t)page * p.g.heads + head) * (p.g.page_size / kKvTile) + (slot - page * p.g.page_size) / kKvTile;
-    return p.cache + tile * kv_tile_words(p.g.blocks);
-}
-
 // 0 never stays and the highest always does; in between NaN and then numbers in their order, both zeros alike.
-__device__ __forceinline__ uint32_t key_of(const EvictParams &p, const int32_t *table, const float *scores, int32_t token, int32_t length)
+__device__ __forceinline__ uint32_t key_of(const EvictParams &p, int32_t page, float score, int32_t token, int32_t length)
 {
-    const int32_t in_table = p.by_page(token), page = __ldg(table + in_table);
-    const float score = __ldg(scores + token);
     const uint32_t bits = __float_as_uint(score + 0.0f);
-    uint32_t key = bits & 0x80000000u ? ~bits : bits | 0x80000000u;
+    uint32_t key = bits ^ ((uint32_t)((int32_t)bits >> 31) | 0x80000000u);
     if (score != score) key = 1;
     if (length > p.budget && (token < p.first || token >= length - p.recent)) key = 0xffffffffu;
-    return page >= 0 && page < p.g.pages ? key : 0;
+    return (uint32_t)page < (uint32_t)p.g.pages ? key : 0;
 }
 
 struct alignas(16) SelectShared {
@@ -98,11 +77,17 @@ __global__ void __launch_bounds__(kThreads) kv_evict_select_kernel(const __grid_
     const int32_t run = ((end - begin + kWarps - 1) / kWarps + 31) / 32 * 32;
     const int32_t run_begin = min(begin + (int64_t)warp * run, (int64_t)end), run_end = min(run_begin + (int64_t)run, (int64_t)end);
     uint32_t keys[KEYS > 0 ? KEYS : 1];
-    if (KEYS > 0) {
+    if (KEYS > 0 && run_begin < run_end) {
+        // all loads at once; behind the run its last token again
+        float score[KEYS > 0 ? KEYS : 1];
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i) score[i] = __ldg(scores + min(run_begin + 32 * i + lane, run_end - 1));
+#pragma unroll
+        for (int i = 0; i < KEYS; ++i) keys[i] = (uint32_t)__ldg(table + p.by_page(min(run_begin + 32 * i + lane, run_end - 1)));
 #pragma unroll
         for (int i = 0; i < KEYS; ++i) {
             const int32_t t = run_begin + 32 * i + lane;
-            keys[i] = t < run_end ? key_of(p, table, scores, t, length) : 0;
+            keys[i] = t < run_end ? key_of(p, (int32_t)keys[i], score[i], t, length) : 0;
         }
     }
     // body(first of 32 tokens, the lane's key; 0 behind the run), by whole warps
@@ -113,7 +98,11 @@ __global__ void __launch_bounds__(kThreads) kv_evict_select_kernel(const __grid_
                 if (run_begin + 32 * i < run_end) body(run_begin + 32 * i, keys[i]);
         } else {
 #pragma unroll 4
-            for (int32_t t0 = run_begin; t0 < run_end; t0 += 32) body(t0, t0 + lane < run_end ? key_of(p, table, scores, t0 + lane, length) : 0);
+            for (int32_t t0 = run_begin; t0 < run_end; t0 += 32) {
+                const int32_t t = min(t0 + lane, run_end - 1);
+                const uint32_t key = key_of(p, __ldg(table + p.by_page(t)), __ldg(scores + t), t, length);
+                body(t0, t0 + lane < run_end ? key : 0);
+            }
         }
     };
     __syncthreads();
@@ -128,29 +117,25 @@ __global__ void __launch_bounds__(kThreads) kv_evict_select_kernel(const __grid_
             const bool counts = key != 0 && (digit == 0 || key >> (shift + bits) == prefix);
             const uint32_t bin = key >> shift & ((1u << bits) - 1);
             // all alike in one go: they would queue up
-            const uint32_t those = __ballot_sync(0xffffffffu, counts);
-            if (!those) return;
-            const int leader = __ffs(those) - 1;
-            const uint32_t common = __shfl_sync(0xffffffffu, bin, leader);
-            if (__all_sync(0xffffffffu, !counts || bin == common)) {
-                if (lane == leader) atomicAdd(&bins[common], (uint32_t)__popc(those));
+            const uint32_t common = __shfl_sync(0xffffffffu, bin, 0);
+            const bool alike = counts && bin == common;
+            if (__all_sync(0xffffffffu, alike)) {
+                if (lane == 0) atomicAdd(&bins[bin], 32u);
             } else if (counts) {
                 atomicAdd(&bins[bin], 1u);
             }
         });
         cluster_sync();
-        // four bins a thread, the highest first, over all blocks
-        const int bin0 = kBins - 4 - 4 * (int)threadIdx.x;
-        uint32_t n[4] = {};
+        // two bins a thread, the highest first, over all blocks
+        const int bin0 = kBins - 2 - 2 * (int)threadIdx.x;
+        uint32_t n[2] = {};
 #pragma unroll 8
         for (int r = 0; r < p.cluster; ++r) {
-            const uint4 v = remote4(&bins[bin0], r);
-            n[0] += v.w;
-            n[1] += v.z;
-            n[2] += v.y;
-            n[3] += v.x;
+            const uint2 v = remote2(&bins[bin0], r);
+            n[0] += v.y;
+            n[1] += v.x;
         }
-        const uint32_t mine = n[0] + n[1] + n[2] + n[3];
+        const uint32_t mine = n[0] + n[1];
         uint32_t upto = mine;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -159,17 +144,13 @@ __global__ void __launch_bounds__(kThreads) kv_evict_select_kernel(const __grid_
         }
         if (lane == 31) sh.warp_sums[warp] = upto;
         __syncthreads();
-        uint32_t before = upto - mine, total = 0;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-            if (w < warp) before += sh.warp_sums[w];
-            total += sh.warp_sums[w];
-        }
+        const uint32_t of_lane = sh.warp_sums[lane], total = __reduce_add_sync(0xffffffffu, of_lane);
+        uint32_t before = upto - mine + __reduce_add_sync(0xffffffffu, lane < warp ? of_lane : 0);
         if (digit == 0 && total <= left) break;  // all that there are stay
         if (before < left && before + mine >= left) {
-            int i = 0;
-            while (before + n[i] < left) before += n[i++];
-            sh.digit = bin0 + 3 - i;
+            const int i = before + n[0] < left;
+            if (i) before += n[0];
+            sh.digit = bin0 + 1 - i;
             sh.left = left - before;
             sh.whole = before + n[i] == left;
         }
@@ -186,22 +167,16 @@ __global__ void __launch_bounds__(kThreads) kv_evict_select_kernel(const __grid_
 
     uint2 mine = make_uint2(0, 0);
     each_key([&](int32_t, uint32_t key) {
-        mine.x += __popc(__ballot_sync(0xffffffffu, key > threshold));
-        mine.y += __popc(__ballot_sync(0xffffffffu, key == threshold && key != 0));
+        mine.x += key > threshold;
+        mine.y += key == threshold && ties > 0;  // ties: of a threshold above 0
     });
+    mine.x = __reduce_add_sync(0xffffffffu, mine.x);
+    mine.y = __reduce_add_sync(0xffffffffu, mine.y);
     if (lane == 0) sh.warp_counts[warp] = mine;
     __syncthreads();
-    uint2 before = make_uint2(0, 0), all = make_uint2(0, 0);
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-        const uint2 c = sh.warp_counts[w];
-        if (w < warp) {
-            before.x += c.x;
-            before.y += c.y;
-        }
-        all.x += c.x;
-        all.y += c.y;
-    }
+    const uint2 of_lane = sh.warp_counts[lane];
+    uint2 before = make_uint2(__reduce_add_sync(0xffffffffu, lane < warp ? of_lane.x : 0), __reduce_add_sync(0xffffffffu, lane < warp ? of_lane.y : 0));
+    const uint2 all = make_uint2(__reduce_add_sync(0xffffffffu, of_lane.x), __reduce_add_sync(0xffffffffu, of_lane.y));
     if (threadIdx.x == 0) sh.counts = all;
     cluster_sync();
     uint32_t above = 0;
@@ -217,17 +192,20 @@ __global__ void __launch_bounds__(kThreads) kv_evict_select_kernel(const __grid_
     int32_t *const kept = p.kept + (int64_t)row * p.budget;
     float *const kept_scores = p.kept_scores ? p.kept_scores + seq * p.kept_seq + head * p.kept_head : nullptr;
     each_key([&](int32_t t0, uint32_t key) {
-        const uint32_t below = (1u << lane) - 1;
-        const bool is_equal = key == threshold && key != 0;
-        const uint32_t higher = __ballot_sync(0xffffffffu, key > threshold), equal = __ballot_sync(0xffffffffu, is_equal);
-        const uint32_t ties_before = before.y + __popc(equal & below);
-        const uint32_t at = before.x + __popc(higher & below) + min(ties_before, ties);
-        if (key > threshold || (is_equal && ties_before < ties)) {
+        const uint32_t below = (1u << lane) - 1, higher = __ballot_sync(0xffffffffu, key > threshold);
+        uint32_t at = before.x + __popc(higher & below);
+        bool stays = key > threshold;
+        if (ties > 0) {
+            const uint32_t equal = __ballot_sync(0xffffffffu, key == threshold), ties_before = before.y + __popc(equal & below);
+            at += min(ties_before, ties);
+            stays = stays || (key == threshold && ties_before < ties);
+            before.y += __popc(equal);
+        }
+        if (stays) {
             kept[at] = t0 + lane;
             if (kept_scores) kept_scores[at] = __ldg(scores + t0 + lane);
         }
         before.x += __popc(higher);
-        before.y += __popc(equal);
     });
     for (int64_t i = count + (int64_t)rank * kThreads + threadIdx.x; i < p.budget; i += (int64_t)p.cluster * kThreads) {
         kept[i] = -1;
@@ -264,94 +242,120 @@ __device__ __forceinline__ void store_words(uint32_t *p, const Words<W> &r)
     else *p = r.w[0];
 }
 
-// 64 places of keys, 64 of values, 16 of scales for a plane of a tile; two tiles side by side in a block, TILES pairs of them one behind the
-// other.  A word is four loads away (where it goes, what is kept there, that token's page, the word), so a thread has its tiles'
-// loads of each kind on their way together.
-constexpr int kPlaces = 144, kMoveThreads = 2 * kPlaces;
+// TILES tiles to a block: where their tokens are (what is kept there, its page) is found out once, a thread to a token.  Then every thread
+// has one of the 64 places of keys, 64 of values and 16 of scales that a plane of a tile has, of several tiles whose loads are on
+// their way together.
+constexpr int kMoveThreads = 256;
+
+// The token's tile of the cache and its place there; negative: there is none.
+struct Source {
+    int32_t tile, token;
+};
 
 template <int TILES>
-__global__ void __launch_bounds__(kMoveThreads) kv_evict_move_kernel(const __grid_constant__ EvictParams p)
+__global__ void __launch_bounds__(kMoveThreads, 4) kv_evict_move_kernel(const __grid_constant__ EvictParams p)
 {
+    static_assert(TILES * kKvTile <= kMoveThreads && TILES % 4 == 0, "");
+    __shared__ alignas(16) Source sources[TILES * kKvTile];
+    __shared__ int32_t targets[TILES];
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int in_block = threadIdx.x / kPlaces, place = threadIdx.x - in_block * kPlaces;
-    const int head = blockIdx.y, seq = blockIdx.z, blocks = p.g.blocks;
-    const bool values = place >= 64 && place < 128;
-    const int in_part = values ? place - 64 : place < 64 ? place : place - 128;
-    // the token, or the first of the two, that the place is for
-    const int token = values ? 8 * (in_part >> 5) + 2 * (in_part & 3) : place < 64 ? 8 * (in_part >> 5) + ((in_part & 31) >> 2) : in_part;
-    const int32_t *const kept = p.kept + ((int64_t)seq * p.g.heads + head) * p.budget, *const table = p.page_table + (int64_t)seq * p.table_pages;
-    uint32_t *to[TILES];
-    int32_t from0[TILES], from1[TILES];
-#pragma unroll
-    for (int i = 0; i < TILES; ++i) {
-        const int j0 = (2 * (blockIdx.x * TILES + i) + in_block) * kKvTile, in_table = p.by_page(j0);
-        const int32_t page = j0 < p.budget ? __ldg(p.kept_table + (int64_t)seq * p.kept_pages + in_table) : -1;
-        to[i] = page >= 0 && page < p.g.pages ? tile_of(p, page * p.g.page_size + (j0 - in_table * p.g.page_size), head) : nullptr;
-        from0[i] = j0 + token < p.budget ? kept[j0 + token] : -1;  // where it is none, those behind are none either
-        from1[i] = values && j0 + token + 1 < p.budget ? kept[j0 + token + 1] : -1;
-    }
-    const uint32_t *tile0[TILES], *tile1[TILES];
-    int t0[TILES], t1[TILES];
-#pragma unroll
-    for (int i = 0; i < TILES; ++i) {
-        if (from0[i] < 0) to[i] = nullptr;
-        const int32_t slot0 = to[i] ? slot_of(p, table, from0[i]) : 0, slot1 = to[i] && from1[i] >= 0 ? slot_of(p, table, from1[i]) : slot0;
-        tile0[i] = tile_of(p, slot0, head);
-        tile1[i] = tile_of(p, slot1, head);
-        t0[i] = slot0 % kKvTile;
-        t1[i] = slot1 % kKvTile;
-    }
-    const auto plane = [&](int first, auto width) {
-        constexpr int W = decltype(width)::value;
-        Words<W> a[TILES], b[TILES];
-        const int base = values ? 64 * blocks + 64 * first : place < 64 ? 64 * first : 128 * blocks + 16 * first;
-#pragma unroll
-        for (int i = 0; i < TILES; ++i) {
-            if (!to[i]) continue;
-            const auto word = [&](int t) {
-                if (values) return (t >> 3) * 32 + (in_part & 28) + (t >> 1 & 3);
-                return place < 64 ? (t >> 3) * 32 + (t & 7) * 4 + (in_part & 3) : t;
-            };
-            a[i] = load_words<W>(tile0[i] + base + word(t0[i]) * W);
-            if (values) b[i] = load_words<W>(tile1[i] + base + word(t1[i]) * W);
+    const int head = blockIdx.y, seq = blockIdx.z, blocks = p.g.blocks, tiles_per_page = p.g.page_size / kKvTile;
+    const int32_t first = blockIdx.x * TILES * kKvTile;
+    const auto tile_on = [&](int32_t page, int32_t in_page) { return (page * p.g.heads + head) * tiles_per_page + in_page / kKvTile; };
+    if (threadIdx.x < TILES * kKvTile) {
+        const int32_t j = first + threadIdx.x;
+        const int32_t from = j < p.budget ? p.kept[((int64_t)seq * p.g.heads + head) * p.budget + j] : -1;
+        const int32_t in_kept = p.by_page(j), target = j < p.budget ? __ldg(p.kept_table + (int64_t)seq * p.kept_pages + in_kept) : -1;
+        Source s{-1, 0};
+        if (from >= 0) {
+            const int32_t in_table = p.by_page(from), page = __ldg(p.page_table + (int64_t)seq * p.table_pages + in_table), in_page = from - in_table * p.g.page_size;
+            s.tile = tile_on(page, in_page);  // of the pool: what is kept is
+            s.token = in_page % kKvTile;
         }
+        sources[threadIdx.x] = s;
+        if (threadIdx.x % kKvTile == 0) targets[threadIdx.x / kKvTile] = (uint32_t)target < (uint32_t)p.g.pages ? tile_on(target, j - in_kept * p.g.page_size) : -1;
+    }
+    __syncthreads();
+    const int words = kv_tile_words(blocks);
+    const auto plane = [&](int plane0, auto width) {
+        constexpr int W = decltype(width)::value, EACH = TILES / 4;
+        // keys: thread's place of every fourth tile
+        {
+            const int place = threadIdx.x & 63, token = 8 * (place >> 5) + ((place & 31) >> 2), at = 64 * plane0;
+            Words<W> w[EACH];
 #pragma unroll
-        for (int i = 0; i < TILES; ++i) {
-            if (!to[i]) continue;
-            uint32_t *const at = to[i] + base + in_part * W;
-            if (!values) {
-                store_words<W>(at, a[i]);
-            } else if (from1[i] >= 0) {
-                Words<W> r;
+            for (int i = 0; i < EACH; ++i) {
+                const Source s = sources[(4 * i + (threadIdx.x >> 6)) * kKvTile + token];
+                if (s.tile >= 0) w[i] = load_words<W>(p.cache + (int64_t)s.tile * words + at + ((s.token >> 3) * 32 + (s.token & 7) * 4 + (place & 3)) * W);
+            }
 #pragma unroll
-                for (int w = 0; w < W; ++w) r.w[w] = __byte_perm(a[i].w[w], b[i].w[w], (t0[i] & 1 ? 0x32 : 0x10) | (t1[i] & 1 ? 0x7600 : 0x5400));
-                store_words<W>(at, r);
-            } else {  // the last token: its half of the words
-#pragma unroll
-                for (int w = 0; w < W; ++w) *reinterpret_cast<uint16_t *>(at + w) = (uint16_t)(a[i].w[w] >> (t0[i] & 1 ? 16 : 0));
+            for (int i = 0; i < EACH; ++i) {
+                const int tile = 4 * i + (threadIdx.x >> 6);
+                if (sources[tile * kKvTile + token].tile >= 0 && targets[tile] >= 0) store_words<W>(p.cache + (int64_t)targets[tile] * words + at + place * W, w[i]);
             }
         }
+        // values: a word is of two tokens
+        {
+            const int place = threadIdx.x & 63, token = 8 * (place >> 5) + 2 * (place & 3), at = 64 * blocks + 64 * plane0;
+            constexpr int SOME = EACH > 2 ? 2 : EACH;
+#pragma unroll
+            for (int i0 = 0; i0 < EACH; i0 += SOME) {
+                Words<W> w[SOME][2];
+                int4 both[SOME];
+#pragma unroll
+                for (int i = 0; i < SOME; ++i) {
+                    both[i] = *reinterpret_cast<const int4 *>(&sources[(4 * (i0 + i) + (threadIdx.x >> 6)) * kKvTile + token]);
+                    const auto load = [&](int32_t tile, int32_t t) { return load_words<W>(p.cache + (int64_t)tile * words + at + ((t >> 3) * 32 + (place & 28) + (t >> 1 & 3)) * W); };
+                    if (both[i].x >= 0) w[i][0] = load(both[i].x, both[i].y);
+                    if (both[i].z >= 0) w[i][1] = load(both[i].z, both[i].w);
+                }
+#pragma unroll
+                for (int i = 0; i < SOME; ++i) {
+                    const int32_t target = targets[4 * (i0 + i) + (threadIdx.x >> 6)];
+                    if (target < 0 || both[i].x < 0) continue;
+                    uint32_t *const to = p.cache + (int64_t)target * words + at + place * W;
+                    if (both[i].z >= 0) {
+                        Words<W> r;
+                        const uint32_t select = (both[i].y & 1 ? 0x32 : 0x10) | (both[i].w & 1 ? 0x7600 : 0x5400);
+#pragma unroll
+                        for (int x = 0; x < W; ++x) r.w[x] = __byte_perm(w[i][0].w[x], w[i][1].w[x], select);
+                        store_words<W>(to, r);
+                    } else {  // the last token: its half of the words
+#pragma unroll
+                        for (int x = 0; x < W; ++x) *reinterpret_cast<uint16_t *>(to + x) = (uint16_t)(w[i][0].w[x] >> (both[i].y & 1 ? 16 : 0));
+                    }
+                }
+            }
+        }
+        // scales: a thread to a token
+        if (threadIdx.x < TILES * kKvTile) {
+            const Source s = sources[threadIdx.x];
+            const int32_t target = targets[threadIdx.x / kKvTile];
+            const int at = 128 * blocks + 16 * plane0;
+            if (s.tile >= 0 && target >= 0)
+                store_words<W>(p.cache + (int64_t)target * words + at + (threadIdx.x % kKvTile) * W, load_words<W>(p.cache + (int64_t)s.tile * words + at + s.token * W));
+        }
     };
-    for (int first = 0; first + 4 <= blocks; first += 4) plane(first, std::integral_constant<int, 4>());
+    for (int plane0 = 0; plane0 + 4 <= blocks; plane0 += 4) plane(plane0, std::integral_constant<int, 4>());
     if (blocks & 2) plane(blocks & ~3, std::integral_constant<int, 2>());
     if (blocks & 1) plane(blocks - 1, std::integral_constant<int, 1>());
 }
 
 lce_status launch_move(const EvictParams &p, cudaStream_t s)
 {
-    constexpr int kTogether = 4;
-    const int64_t pairs = ((p.budget + kKvTile - 1) / kKvTile + 1) / 2;
-    // several tiles to a thread once every SM has its blocks without
-    if (pairs * p.g.heads * p.batch > 148 * 6)
-        return launch_dependent(kv_evict_move_kernel<kTogether>, dim3((unsigned)((pairs + kTogether - 1) / kTogether), (unsigned)p.g.heads, (unsigned)p.batch), kMoveThreads, 0, s, p);
-    return launch_dependent(kv_evict_move_kernel<1>, dim3((unsigned)pairs, (unsigned)p.g.heads, (unsigned)p.batch), kMoveThreads, 0, s, p);
+    const int64_t tiles = (p.budget + kKvTile - 1) / kKvTile;
+    const auto go = [&](auto kernel, int each) {
+        return launch_dependent(kernel, dim3((unsigned)((tiles + each - 1) / each), (unsigned)p.g.heads, (unsigned)p.batch), kMoveThreads, 0, s, p);
+    };
+    // as many tiles to a block as leave every SM its blocks
+    return tiles * p.g.heads * p.batch > 148 * 16 ? go(kv_evict_move_kernel<16>, 16) : go(kv_evict_move_kernel<4>, 4);
 }
 
 lce_status launch_select(const EvictParams &p, cudaStream_t s)
 {
     const int64_t share = ((int64_t)p.table_tokens + p.cluster - 1) / p.cluster;
-    const auto kernel = share <= 2 * kThreads ? kv_evict_select_kernel<2> : share <= 8 * kThreads ? kv_evict_select_kernel<8>
-                      : share <= 32 * kThreads ? kv_evict_select_kernel<32> : kv_evict_select_kernel<0>;
+    const auto kernel = share <= kThreads ? kv_evict_select_kernel<1> : share <= 4 * kThreads ? kv_evict_select_kernel<4>
+                      : share <= 16 * kThreads ? kv_evict_select_kernel<16> : kv_evict_select_kernel<0>;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(p.batch * p.g.heads * p.cluster), 1, 1);
     cfg.blockDim = dim3(kThreads, 1, 1);
@@ -390,7 +394,7 @@ extern "C" lce_status lce_kv_evict(const lce_kv_evict_desc *desc, void *cache, c
     for (const int64_t s : {d.scores_seq_stride, d.scores_head_stride, d.kept_scores_seq_stride, d.kept_scores_head_stride})
         if (!stride_ok(s)) return LCE_ERR_INVALID_ARG;
     if ((int64_t)d.table_pages * d.cache.page_size >= (1ll << 30) || (int64_t)d.kept_pages * d.cache.page_size >= (1ll << 30) || d.batch > 65535 ||
-        (int64_t)d.batch * d.cache.kv_heads * 8 >= (1ll << 31))
+        (int64_t)d.batch * d.cache.kv_heads * 8 >= (1ll << 31) || (int64_t)p.g.slots / kKvTile * p.g.heads >= (1ll << 31))
         return LCE_ERR_UNSUPPORTED;
     if (!cache || !page_table || !lengths || !scores || !kept_table || !kept || !kept_lengths) return LCE_ERR_INVALID_ARG;
     if (!aligned(cache, 16) || !aligned(page_table, 4) || !aligned(lengths, 4) || !aligned(scores, 4) || !aligned(kept_table, 4) || !aligned(kept, 4) ||
