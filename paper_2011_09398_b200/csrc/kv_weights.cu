@@ -16,6 +16,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 namespace lce {
 namespace {
@@ -25,6 +26,10 @@ __host__ __device__ constexpr int key_words(int blocks) { return 80 * blocks; } 
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kStages = 4;                  // tiles in flight of a warp
 constexpr int kBlocksPerSm = 4;
+// that a variant's registers let it hold
+__host__ __device__ constexpr int blocks_per_sm(int blocks, int nt, bool split) { return blocks * nt * (split ? 2 : 1) < 8 ? kBlocksPerSm : 3; }
+constexpr float kNothing = -3e38f;          // stands for the largest score where there is none
+constexpr float kRise = 16.0f;              // the score that powers of two are relative to is raised when one passes it by this much
 constexpr int64_t kMostScores = 256 << 20;  // bytes of workspace that scores may take
 constexpr int64_t kMostStats = 64 << 20;
 
@@ -128,8 +133,9 @@ struct Columns {
             }
         }
     }
-    // Scores of a tile; minus infinity where a column does not see the token (only looked at where `masked`).
-    __device__ __forceinline__ void scores(const uint32_t *tile, int32_t token0, bool masked, float (&s)[NT][4]) const
+    // Scores of a tile; minus infinity where a column does not see the token (only looked at where MASKED).
+    template <bool MASKED>
+    __device__ __forceinline__ void scores(const uint32_t *tile, int32_t token0, float (&s)[NT][4]) const
     {
         constexpr int Q = B / 4 * 4;
         constexpr bool T = (B & 2) != 0, S = (B & 1) != 0;
@@ -147,7 +153,7 @@ struct Columns {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 s[nt][i] *= factor[nt][i & 1];
-                if (masked) {
+                if (MASKED) {
                     const int32_t token = token0 + 8 * (i >> 1) + (lane >> 2);
                     if (token < lo[nt][i & 1] || token >= hi[nt][i & 1]) s[nt][i] = -INFINITY;
                 }
@@ -205,16 +211,16 @@ __device__ __forceinline__ float *scores_at(const WeightsParams &p, const Piece 
     return p.scores + head * p.scores_head + piece.scores_before + (int64_t)tile * kKvTile * scores_stride(piece.columns);
 }
 
-// The sum of a column's powers of two, joined: s e^.. is held as (largest, sum relative to it).
+// Sums of powers of two relative to `top` and to `other_top`, joined.
 __device__ __forceinline__ void join_sums(float &top, float &sum, float other_top, float other_sum)
 {
-    const float high = fmaxf(top, other_top), base = high == -INFINITY ? 0.0f : high;
-    sum = sum * exp2f(top - base) + other_sum * exp2f(other_top - base);
+    const float high = fmaxf(top, other_top);
+    sum = sum * exp2f(top - high) + other_sum * exp2f(other_top - high);
     top = high;
 }
 
 template <int B, int NT, bool SPLIT>
-__global__ void __launch_bounds__(kThreads, kBlocksPerSm) kv_weights_scores_kernel(const __grid_constant__ WeightsParams p)
+__global__ void __launch_bounds__(kThreads, blocks_per_sm(B, NT, SPLIT)) kv_weights_scores_kernel(const __grid_constant__ WeightsParams p)
 {
     constexpr int COLUMNS = 8 * NT;
     extern __shared__ __align__(16) uint32_t smem[];
@@ -224,7 +230,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) kv_weights_scores_kern
     Piece piece;
     if (!find_piece(p, blockIdx.x, &piece)) return;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, head = blockIdx.y;
-    const int stride = scores_stride(piece.columns);
+    const int64_t stride = scores_stride(piece.columns);
     for (piece.u.column0 = 0; piece.u.column0 < piece.columns; piece.u.column0 += COLUMNS) {
         const View v = view(p, piece, COLUMNS);
         Columns<B, NT, SPLIT> c;
@@ -234,37 +240,59 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) kv_weights_scores_kern
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                top[nt][j] = -INFINITY;
+                top[nt][j] = kNothing;
                 sum[nt][j] = 0.0f;
             }
-        each_tile<B>(p, piece, v, head, smem + warp * kStages * key_words(B), [&](int32_t tile, const uint32_t *words) {
+        float *to = p.scores ? scores_at(p, piece, head, v.tile0 + warp) + (lane >> 2) * stride + piece.u.column0 + 2 * (lane & 3) : nullptr;
+        const auto tile_step = [&](int32_t tile, const uint32_t *words, auto masked) {
             float s[NT][4];
-            const int32_t token0 = tile * kKvTile;
-            if (words) {
-                c.scores(words, token0, token0 < v.all_lo || token0 + kKvTile > v.all_hi, s);
-            } else {
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) s[nt][i] = -INFINITY;
-            }
+            c.template scores<decltype(masked)::value>(words, tile * kKvTile, s);
             if (p.scores) {
-                float *const to = scores_at(p, piece, head, tile) + (int64_t)(lane >> 2) * stride + piece.u.column0 + 2 * (lane & 3);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
                     if (piece.u.column0 + 8 * nt + 2 * (lane & 3) < stride) {
                         *reinterpret_cast<float2 *>(to + 8 * nt) = make_float2(s[nt][0], s[nt][1]);
-                        *reinterpret_cast<float2 *>(to + 8 * nt + 8 * (int64_t)stride) = make_float2(s[nt][2], s[nt][3]);
+                        *reinterpret_cast<float2 *>(to + 8 * nt + 8 * stride) = make_float2(s[nt][2], s[nt][3]);
+                    }
+            }
+            float e[NT][4], highest = -INFINITY;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    e[nt][i] = s[nt][i] - top[nt][i & 1];
+                    highest = fmaxf(highest, e[nt][i]);
+                }
+            if (__any_sync(0xffffffffu, highest > kRise)) {  // rare behind the first tiles: the lane's references move up
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const float high = fmaxf(top[nt][j], fmaxf(s[nt][j], s[nt][2 + j]));
+                        sum[nt][j] *= exp2f(top[nt][j] - high);
+                        top[nt][j] = high;
+                        e[nt][j] = s[nt][j] - high;
+                        e[nt][2 + j] = s[nt][2 + j] - high;
                     }
             }
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const float high = fmaxf(top[nt][j], fmaxf(s[nt][j], s[nt][2 + j])), base = high == -INFINITY ? 0.0f : high;
-                    sum[nt][j] = fmaf(sum[nt][j], exp2_fast(top[nt][j] - base), exp2_fast(s[nt][j] - base) + exp2_fast(s[nt][2 + j] - base));
-                    top[nt][j] = high;
-                }
+                for (int j = 0; j < 2; ++j) sum[nt][j] += exp2_fast(e[nt][j]) + exp2_fast(e[nt][2 + j]);
+        };
+        each_tile<B>(p, piece, v, head, smem + warp * kStages * key_words(B), [&](int32_t tile, const uint32_t *words) {
+            if (!words) {
+                if (p.scores)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+                        if (piece.u.column0 + 8 * nt + 2 * (lane & 3) < stride)
+                            *reinterpret_cast<float2 *>(to + 8 * nt) = *reinterpret_cast<float2 *>(to + 8 * nt + 8 * stride) = make_float2(-INFINITY, -INFINITY);
+            } else if (tile * kKvTile >= v.all_lo && tile * kKvTile + kKvTile <= v.all_hi) {
+                tile_step(tile, words, std::false_type());
+            } else {
+                tile_step(tile, words, std::true_type());
+            }
+            to += (int64_t)kWarps * kKvTile * stride;
         });
         // eight lanes have a column's tokens, then the warps
 #pragma unroll
@@ -294,29 +322,27 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) kv_weights_scores_kern
 }
 
 // The pieces' parts of `count` columns joined: a column's largest score and what its powers of two are multiplied with, 0 where it sees nothing or
-// is none.  Eight threads to a column.
-__device__ __forceinline__ void column_totals(const WeightsParams &p, const Piece &piece, int head, int count, float *tops, float *parts)
+// is none.  A warp to a column.
+__device__ __forceinline__ void column_totals(const WeightsParams &p, const Piece &piece, int head, int count, float2 *totals)
 {
-    constexpr int EACH = 8;
-    for (int in_tile = threadIdx.x / EACH; in_tile - (int)(threadIdx.x & 31) / EACH < count; in_tile += blockDim.x / EACH) {
-        float top = -INFINITY, sum = 0.0f;
-        if (in_tile < count && piece.u.column0 + in_tile < piece.columns) {
+    const int lane = threadIdx.x & 31;
+    for (int in_tile = threadIdx.x >> 5; in_tile < count; in_tile += blockDim.x >> 5) {
+        float top = kNothing, sum = 0.0f;
+        if (piece.u.column0 + in_tile < piece.columns) {
             const float2 *const from = p.stats + ((head * p.tokens + piece.u.row0) * p.group + piece.u.column0 + in_tile) * p.pieces;
 #pragma unroll 4
-            for (int i = threadIdx.x % EACH; i < piece.pieces; i += EACH) {
+            for (int i = lane; i < piece.pieces; i += 32) {
                 const float2 part = from[i];
                 join_sums(top, sum, part.x, part.y);
             }
         }
+        float high = top;
 #pragma unroll
-        for (int d = 1; d < EACH; d <<= 1) {
-            const float t = __shfl_xor_sync(0xffffffffu, top, d), s = __shfl_xor_sync(0xffffffffu, sum, d);
-            join_sums(top, sum, t, s);
-        }
-        if (in_tile < count && threadIdx.x % EACH == 0) {
-            tops[in_tile] = top == -INFINITY ? 0.0f : top;
-            parts[in_tile] = sum == 0.0f ? 0.0f : 1.0f / sum;
-        }
+        for (int d = 1; d < 32; d <<= 1) high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, d));
+        sum *= exp2f(top - high);
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        if (lane == 0) totals[in_tile] = sum == 0.0f ? make_float2(0.0f, 0.0f) : make_float2(high, 1.0f / sum);
     }
 }
 
@@ -330,60 +356,68 @@ __device__ __forceinline__ void put_weight(const WeightsParams &p, const Piece &
 // Scores that were kept: a thread to a token, kTogether at a time.
 constexpr int kKeptThreads = 256, kTogether = 4, kKeptColumns = 128;
 
-__global__ void __launch_bounds__(kKeptThreads) kv_weights_kept_kernel(const __grid_constant__ WeightsParams p)
+__global__ void __launch_bounds__(kKeptThreads, 4) kv_weights_kept_kernel(const __grid_constant__ WeightsParams p)
 {
-    __shared__ float tops[kKeptColumns], parts[kKeptColumns];
-    __shared__ int2 ranges[kKeptColumns];  // tokens that a column sees: the others' places may never have been written
+    __shared__ alignas(16) float2 totals[kKeptColumns];
     Piece piece;
     // the lengths are what the kernel in front read: nothing has written them since
     const bool found = find_piece(p, blockIdx.x, &piece);
     asm volatile("griddepcontrol.wait;" ::: "memory");  // every block: what comes behind this kernel relies on the one in front, too
     if (!found) return;
-    const int head = blockIdx.y, stride = scores_stride(piece.columns);
-    const View v = view(p, piece, piece.columns);
+    const int head = blockIdx.y;
+    const int64_t stride = scores_stride(piece.columns);
     const int32_t first = piece.u.tile0 * kKvTile, last = min(piece.u.tile1 * kKvTile, tokens_held(p, piece.u.length));
-    const int32_t step = kKeptThreads * kTogether;
+    constexpr int32_t kStep = kKeptThreads * kTogether;
     const float *const scores = scores_at(p, piece, head, 0);
     // whole blocks go round together: the columns' totals are theirs
-    for (int32_t t0 = first + blockIdx.z * step; t0 < last; t0 += gridDim.z * step) {
+    for (int32_t t0 = first; t0 < last; t0 += kStep) {
         float w[kTogether] = {};
         for (piece.u.column0 = 0; piece.u.column0 < piece.columns; piece.u.column0 += kKeptColumns) {
             const int count = min(kKeptColumns, piece.columns - piece.u.column0);
-            if (piece.columns > kKeptColumns || t0 == first + (int32_t)blockIdx.z * step) {
+            if (piece.columns > kKeptColumns || t0 == first) {
                 __syncthreads();
-                column_totals(p, piece, head, count, tops, parts);
-                if ((int)threadIdx.x < count) column_range(p, piece.u, piece.u.column0 + threadIdx.x, &ranges[threadIdx.x].x, &ranges[threadIdx.x].y);
+                column_totals(p, piece, head, count, totals);
                 __syncthreads();
             }
-            const auto go = [&](auto vector) {
-                constexpr int N = sizeof(vector) / 4;
+            // tokens whose scores are there: those that some column sees; all of these columns see the step's
+            const View v = view(p, piece, kKeptColumns);
+            const bool all = t0 >= v.all_lo && min(t0 + kStep, last) <= v.all_hi;
+            const auto go = [&](auto vector, auto masked) {
+                using V = decltype(vector);
+                constexpr int N = sizeof(V) / 4;
                 for (int c = 0; c < count; c += N) {
-                    decltype(vector) s[kTogether];
+                    union Scores {
+                        V v;
+                        float e[N];
+                    } s[kTogether];
 #pragma unroll
                     for (int k = 0; k < kTogether; ++k) {
                         const int32_t t = t0 + k * kKeptThreads + threadIdx.x;
-                        const bool seen = t < last && t >= v.tile0 * kKvTile && t < v.tile1 * kKvTile;
-                        float *const e = reinterpret_cast<float *>(s + k);
-                        if (seen) {
-                            s[k] = *reinterpret_cast<const decltype(vector) *>(scores + (int64_t)t * stride + piece.u.column0 + c);
-                        } else {
 #pragma unroll
-                            for (int i = 0; i < N; ++i) e[i] = -INFINITY;
-                        }
+                        for (int i = 0; i < N; ++i) s[k].e[i] = -INFINITY;
+                        if (t < last && t >= v.tile0 * kKvTile && t < v.tile1 * kKvTile) s[k].v = *reinterpret_cast<const V *>(scores + t * stride + piece.u.column0 + c);
                     }
 #pragma unroll
-                    for (int k = 0; k < kTogether; ++k)
+                    for (int i = 0; i < N; ++i) {
+                        if (N > 1 && c + i >= count) break;
+                        const float2 total = totals[c + i];
+                        int32_t lo = 0, hi = 0x7fffffff;
+                        if (decltype(masked)::value) column_range(p, piece.u, piece.u.column0 + c + i, &lo, &hi);  // other tokens' may never have been written
 #pragma unroll
-                        for (int i = 0; i < N; ++i)
-                            if (c + i < count) {
-                                const float x = reinterpret_cast<const float *>(s + k)[i];
-                                const int32_t t = t0 + k * kKeptThreads + threadIdx.x;
-                                if (x != -INFINITY && t >= ranges[c + i].x && t < ranges[c + i].y) w[k] += exp2_fast(x - tops[c + i]) * parts[c + i];
-                            }
+                        for (int k = 0; k < kTogether; ++k) {
+                            const int32_t t = t0 + k * kKeptThreads + threadIdx.x;
+                            if (!decltype(masked)::value || (s[k].e[i] != -INFINITY && t >= lo && t < hi)) w[k] = fmaf(exp2_fast(s[k].e[i] - total.x), total.y, w[k]);
+                        }
+                    }
                 }
             };
-            if (stride % 4 == 0) go(float4());
-            else go(float2());
+            // 0 times what a column that is not finite has would not be 0
+            bool finite = true;
+            if (all)
+                for (int c = threadIdx.x & 31; c < count; c += 32) finite = finite && totals[c].y == totals[c].y;
+            const bool plain = __all_sync(0xffffffffu, all && finite);
+            if (stride % 4 == 0) plain ? go(float4(), std::false_type()) : go(float4(), std::true_type());
+            else plain ? go(float2(), std::false_type()) : go(float2(), std::true_type());
         }
 #pragma unroll
         for (int k = 0; k < kTogether; ++k) {
@@ -394,11 +428,11 @@ __global__ void __launch_bounds__(kKeptThreads) kv_weights_kept_kernel(const __g
 }
 
 template <int B, int NT, bool SPLIT>
-__global__ void __launch_bounds__(kThreads, kBlocksPerSm) kv_weights_sum_kernel(const __grid_constant__ WeightsParams p)
+__global__ void __launch_bounds__(kThreads, blocks_per_sm(B, NT, SPLIT)) kv_weights_sum_kernel(const __grid_constant__ WeightsParams p)
 {
     constexpr int COLUMNS = 8 * NT;
     extern __shared__ __align__(16) uint32_t smem[];
-    __shared__ float tops[COLUMNS], parts[COLUMNS];
+    __shared__ float2 totals[COLUMNS];
     float *const weights = reinterpret_cast<float *>(smem) + kWarps * kStages * key_words(B);  // of the piece's tokens
     Piece piece;
     // the lengths are what the kernel in front read: nothing has written them since
@@ -409,7 +443,7 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) kv_weights_sum_kernel(
     const int tokens = (piece.u.tile1 - piece.u.tile0) * kKvTile;
     for (int i = threadIdx.x; i < tokens; i += kThreads) weights[i] = 0.0f;
     for (piece.u.column0 = 0; piece.u.column0 < piece.columns; piece.u.column0 += COLUMNS) {
-        column_totals(p, piece, head, COLUMNS, tops, parts);
+        column_totals(p, piece, head, COLUMNS, totals);
         __syncthreads();
         const View v = view(p, piece, COLUMNS);
         {
@@ -420,14 +454,15 @@ __global__ void __launch_bounds__(kThreads, kBlocksPerSm) kv_weights_sum_kernel(
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    top[nt][j] = tops[8 * nt + 2 * (lane & 3) + j];
-                    part[nt][j] = parts[8 * nt + 2 * (lane & 3) + j];
+                    top[nt][j] = totals[8 * nt + 2 * (lane & 3) + j].x;
+                    part[nt][j] = totals[8 * nt + 2 * (lane & 3) + j].y;
                 }
             each_tile<B>(p, piece, v, head, smem + warp * kStages * key_words(B), [&](int32_t tile, const uint32_t *words) {
                 if (!words) return;
                 float s[NT][4], w[2] = {0.0f, 0.0f};
                 const int32_t token0 = tile * kKvTile;
-                c.scores(words, token0, token0 < v.all_lo || token0 + kKvTile > v.all_hi, s);
+                if (token0 >= v.all_lo && token0 + kKvTile <= v.all_hi) c.template scores<false>(words, token0, s);
+                else c.template scores<true>(words, token0, s);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -458,8 +493,7 @@ lce_status launch(const WeightsParams &p, cudaStream_t s)
         const lce_status st = launch_dependent(kv_weights_scores_kernel<B, NT, SPLIT>, grid, kThreads, ring, s, p);
         if (st != LCE_OK) return st;
     }
-    // a block's tokens in one go where the GPU has room for that many blocks
-    if (p.scores) return launch_dependent(kv_weights_kept_kernel, dim3(grid.x, grid.y, 2), kKeptThreads, 0, s, p);
+    if (p.scores) return launch_dependent(kv_weights_kept_kernel, grid, kKeptThreads, 0, s, p);
     return launch_dependent(kv_weights_sum_kernel<B, NT, SPLIT>, grid, kThreads, all, s, p);
 }
 
