@@ -31,6 +31,7 @@ __host__ __device__ constexpr int blocks_per_sm(int blocks, int nt, bool split) 
 constexpr float kNothing = -3e38f;          // stands for the largest score where there is none
 constexpr float kRise = 16.0f;              // the score that powers of two are relative to is raised when one passes it by this much
 constexpr int64_t kMostScores = 256 << 20;  // bytes of workspace that scores may take
+constexpr int kFewColumns = 32;             // of a sequence, on average
 constexpr int64_t kMostStats = 64 << 20;
 
 // B blocks of 32 channels, NT tiles of 8 columns, SPLIT: fp32 rows.
@@ -346,13 +347,6 @@ __device__ __forceinline__ void column_totals(const WeightsParams &p, const Piec
     }
 }
 
-// What stood there before, as far as it counts, and the weight w of token t.
-__device__ __forceinline__ void put_weight(const WeightsParams &p, const Piece &piece, int head, int32_t t, float w)
-{
-    if (p.previous && t < piece.u.length - piece.u.rows) w = fmaf(p.decay, p.previous[piece.u.seq * p.previous_seq + head * p.previous_head + t], w);
-    p.sums[piece.u.seq * p.out_seq + head * p.out_head + t] = w;
-}
-
 // Scores that were kept: a thread to a token, kTogether at a time.
 constexpr int kKeptThreads = 256, kTogether = 4, kKeptColumns = 128;
 
@@ -422,7 +416,7 @@ __global__ void __launch_bounds__(kKeptThreads, 4) kv_weights_kept_kernel(const 
 #pragma unroll
         for (int k = 0; k < kTogether; ++k) {
             const int32_t t = t0 + k * kKeptThreads + threadIdx.x;
-            if (t < last) put_weight(p, piece, head, t, w[k]);
+            if (t < last) put_weight(p, piece.u, head, t, w[k]);
         }
     }
 }
@@ -479,7 +473,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(B, NT, SPLIT)) kv_weig
     }
     __syncthreads();
     const int32_t held = tokens_held(p, piece.u.length);
-    for (int i = threadIdx.x; i < tokens && piece.u.tile0 * kKvTile + i < held; i += kThreads) put_weight(p, piece, head, piece.u.tile0 * kKvTile + i, weights[i]);
+    for (int i = threadIdx.x; i < tokens && piece.u.tile0 * kKvTile + i < held; i += kThreads) put_weight(p, piece.u, head, piece.u.tile0 * kKvTile + i, weights[i]);
 }
 
 template <int B, int NT, bool SPLIT>
@@ -540,6 +534,9 @@ lce_status make_params(const lce_kv_attention_weights_desc *d, WeightsParams *p,
     p->previous_seq = d->previous_seq_stride; p->previous_head = d->previous_head_stride;
     p->out_seq = d->out_seq_stride; p->out_head = d->out_head_stride;
     *nt = p->g.blocks <= kWideBlocks && (d->tokens * p->group + d->batch - 1) / d->batch > 8 ? 2 : 1;
+    // Many rows go to the tensor cores' kernels.
+    p->prompt = p->g.blocks <= 4 && d->type != LCE_TYPE_FLOAT32 && p->tokens * p->group > p->batch * (int64_t)kFewColumns &&
+                (double)p->g.heads * p->batch * (p->table_tokens / 256 + 1) < (1u << 31);
     // As many pieces as the GPU has places for; fewer where there are so many columns that their sums would take much room.
     const int64_t columns = std::max<int64_t>(p->tokens * d->heads, 1);
     p->target = (int32_t)std::max<int64_t>(1, std::min<int64_t>((148 * kBlocksPerSm + p->g.heads - 1) / p->g.heads, kMostStats / 8 / columns));
@@ -560,6 +557,11 @@ size_t scores_bytes(const WeightsParams &p)
     return p.tokens > 0 && bytes <= kMostScores ? (size_t)p.scores_head * p.g.heads * 4 : 0;
 }
 
+size_t workspace_bytes(const WeightsParams &p)
+{
+    return std::max<size_t>(p.prompt ? kv_weights_prompt_bytes(p) : stats_bytes(p) + scores_bytes(p), 16);
+}
+
 }  // namespace
 }  // namespace lce
 
@@ -569,7 +571,7 @@ extern "C" size_t lce_kv_attention_weights_workspace_bytes(const lce_kv_attentio
     WeightsParams p{};
     int nt;
     if (make_params(desc, &p, &nt) != LCE_OK) return 0;
-    return std::max<size_t>(stats_bytes(p) + scores_bytes(p), 16);
+    return workspace_bytes(p);
 }
 
 extern "C" lce_status lce_kv_attention_weights(const lce_kv_attention_weights_desc *desc, const void *q, const void *cache, const int32_t *page_table,
@@ -587,11 +589,12 @@ extern "C" lce_status lce_kv_attention_weights(const lce_kv_attention_weights_de
     if (!aligned(q, element) || !aligned(cache, 16) || !aligned(page_table, 4) || !aligned(lengths, 4) || !aligned(q_starts, 4) || !aligned(previous, 4) ||
         !aligned(out, 4) || !aligned(workspace, 16))
         return LCE_ERR_ALIGNMENT;
-    if (workspace_size < std::max<size_t>(stats_bytes(p) + scores_bytes(p), 16)) return LCE_ERR_WORKSPACE;
+    if (workspace_size < workspace_bytes(p)) return LCE_ERR_WORKSPACE;
     p.q_vectors = p.g.dim % 8 == 0 && aligned(q, 8 * element) && p.q_token % 8 == 0 && p.q_head % 8 == 0;
     p.q = q; p.cache = static_cast<const uint32_t *>(cache); p.page_table = page_table; p.lengths = lengths; p.q_starts = q_starts;
     p.previous = desc->decay != 0.0f ? previous : nullptr;
     p.sums = out;
+    if (p.prompt) return launch_kv_weights_prompt(p, workspace, static_cast<cudaStream_t>(stream));
     p.stats = static_cast<float2 *>(workspace);
     p.scores = scores_bytes(p) ? reinterpret_cast<float *>(static_cast<char *>(workspace) + stats_bytes(p)) : nullptr;
     cudaStream_t s = static_cast<cudaStream_t>(stream);

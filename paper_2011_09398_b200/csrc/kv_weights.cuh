@@ -99,4 +99,15 @@ __device__ __forceinline__ View view(const WeightsParams &p, const Piece &piece,
     return v;
 }
 
+// What stood there before, as far as it counts, and the weight w of token t.
+__device__ __forceinline__ void put_weight(const WeightsParams &p, const Unit &u, int head, int32_t t, float w)
+{
+    if (p.previous && t < u.length - u.rows) w = fmaf(p.decay, p.previous[u.seq * p.previous_seq + head * p.previous_head + t], w);
+    p.sums[u.seq * p.out_seq + head * p.out_head + t] = w;
+}
+
+// Many rows: kv_weights_prompt.cu.  16-bit rows of up to 128 channels; a workspace of so many bytes, 16-byte aligned.
+size_t kv_weights_prompt_bytes(const WeightsParams &p);
+lce_status launch_kv_weights_prompt(const WeightsParams &p, void *workspace, cudaStream_t s);
+
 }  // namespace lce
