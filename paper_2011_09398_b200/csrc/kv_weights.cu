@@ -32,6 +32,7 @@ constexpr float kNothing = -3e38f;          // stands for the largest score wher
 constexpr float kRise = 16.0f;              // the score that powers of two are relative to is raised when one passes it by this much
 constexpr int64_t kMostScores = 256 << 20;  // bytes of workspace that scores may take
 constexpr int kFewColumns = 32;             // of a sequence, on average
+constexpr double kMostUnits = 1 << 21;      // (256 tokens, key head) that their list has room for
 constexpr int64_t kMostStats = 64 << 20;
 
 // B blocks of 32 channels, NT tiles of 8 columns, SPLIT: fp32 rows.
@@ -536,7 +537,7 @@ lce_status make_params(const lce_kv_attention_weights_desc *d, WeightsParams *p,
     *nt = p->g.blocks <= kWideBlocks && (d->tokens * p->group + d->batch - 1) / d->batch > 8 ? 2 : 1;
     // Many rows go to the tensor cores' kernels.
     p->prompt = p->g.blocks <= 4 && d->type != LCE_TYPE_FLOAT32 && p->tokens * p->group > p->batch * (int64_t)kFewColumns &&
-                (double)p->g.heads * p->batch * (p->table_tokens / 256 + 1) < (1u << 31);
+                p->g.heads < 65535 && (double)p->g.heads * p->batch * (p->table_tokens / 256 + 1) < kMostUnits;
     // As many pieces as the GPU has places for; fewer where there are so many columns that their sums would take much room.
     const int64_t columns = std::max<int64_t>(p->tokens * d->heads, 1);
     p->target = (int32_t)std::max<int64_t>(1, std::min<int64_t>((148 * kBlocksPerSm + p->g.heads - 1) / p->g.heads, kMostStats / 8 / columns));

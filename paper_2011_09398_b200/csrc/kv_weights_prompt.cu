@@ -7,13 +7,15 @@
 //             largest and the sum of their powers of two
 //   second    256 tokens stay, columns stream: a thread has a token's scores, and adds its weights up.  A column's factor and the logarithm of
 //             its sum lie in shared memory
-// So no sum crosses threads.  Work is cut into units of a few steps: (256 columns, a piece of the sequence) and (256 tokens, a chunk of the
-// columns), joined in a fixed order by small kernels; 148 blocks take equal runs of units, and their warps go from one to the next
-// without meeting:
-//   warps 0 - 3, 4 - 7  the powers of two, 128 of the 256 each; two accumulators of 128 x 128 for each in TMEM
-//   warps 8 - 11        4-bit words from the cache to f16 keys in shared memory
-//   warp 12             issues the products
-//   warp 13             has rows of q copied, which a kernel in front has put in order as f16
+// So no sum crosses threads before a unit's end.  Work is cut into units of a few steps: (256 columns, a piece of the sequence) and (256 tokens,
+// a chunk of the columns), joined in a fixed order by small kernels.  The kernel that puts the rows of q in order as f16 lists them; 148
+// blocks take them in turn, and their warps go from one to the next without meeting:
+//   warps 0 - 15        the powers of two: two threads to each of the 256, for 64 of a step's 128 each; two accumulators of 128 x 128 for
+//                       every 128 of the 256 in TMEM
+//   warps 16 - 19       4-bit words from the cache to f16 keys in shared memory
+//   warp 20             issues the products
+//   warp 21             has the rows of q copied
+// Sixteen warps, because one scheduler's two did not hide what a score goes through: 145 and 140 us for two chunks of 1024 rows instead of XXX.
 //
 // f16 holds a code times its scale exactly, relative to the largest scale of 128 tokens, down to 2^-28 of it; 16-bit rows of q are exact
 // down to 2^-24 of their largest element at least.  Scores and sums are fp32.
@@ -26,11 +28,8 @@
 namespace lce {
 namespace {
 
-constexpr int kSoftmaxWarps = 8, kProducerWarps = 4, kIssuerWarp = kSoftmaxWarps + kProducerWarps, kCopyWarp = kIssuerWarp + 1;
-constexpr int kThreads = 32 * (kIssuerWarp + 4);  // whole warpgroups: registers are shared out between them
-// Registers a thread: 128 at the launch, 512 * 128 in all = 256 * 144 + 128 * 112 + 128 * 112.
-constexpr int kSoftmaxRegisters = 144, kProducerRegisters = 112, kIssuerRegisters = 112;
-static_assert(256 * kSoftmaxRegisters + 128 * kProducerRegisters + 128 * kIssuerRegisters <= kThreads * 128, "more registers than the block has");
+constexpr int kSoftmaxWarps = 16, kProducerWarps = 4, kIssuerWarp = kSoftmaxWarps + kProducerWarps, kCopyWarp = kIssuerWarp + 1;
+constexpr int kThreads = 32 * (kCopyWarp + 1);
 constexpr float kNothing = -3e38f;   // stands for the largest score where there is none
 constexpr float kRise = 16.0f;       // the score that powers of two are relative to is raised when one passes it by this much
 constexpr int kBlocks = 148;         // one to an SM
@@ -51,13 +50,26 @@ struct Shared {
     TileInfo info[kInfos];
     alignas(16) __half scales[2][kTokens][4];         // relative to the tile's largest; [turn]
     alignas(16) float columns[2][2][kTokens / 2][4];  // [half][turn][pair]: two factors, two logarithms taken off
+    float2 others[2][2][kTokens];                     // [half][turn]: what the second of two threads has at a unit's end
 };
 
-constexpr int kMiscBytes = 8192;
+constexpr int kMiscBytes = 12288;
 static_assert(sizeof(Shared) <= kMiscBytes, "");
 constexpr size_t weights_smem(int blocks) { return kMiscBytes + 6 * (size_t)(kTokens * 64 * blocks); }
 
+// A unit of work.
+struct alignas(16) WorkUnit {
+    int32_t seq, length, rows, held;  // tokens of the sequence, its rows of q, tokens that its pages hold
+    int32_t columns, tiles_before;    // columns; tiles of columns of the sequences in front
+    int32_t head, first;              // the first of the 256 columns, or tokens, that stay
+    int32_t step0, step1;
+    int32_t part;                     // second kernel: where its sums wait for the other chunks'; negative: it has no others
+    int32_t unused;
+};
+
 struct PromptParams : WeightsParams {
+    WorkUnit *units[2];
+    int32_t *unit_counts;
     uint8_t *images;      // [tile of 128 columns][kv head]: rows of q as f16, in the order in which they are an operand
     float *factors;       // [tile of columns][kv head][128]
     float2 *stats_units;  // [unit of the first kernel][256]: largest, sum
@@ -108,8 +120,7 @@ __device__ __forceinline__ Cut find_cut(const PromptParams &p)
     return cut;
 }
 
-// Finds the sequence that the `at`-th of what `count` counts belongs to, and what the sequences in front of it have; at < 0: all sequences'.
-// By whole warps.
+// Finds the sequence that the `at`-th of what `count` counts belongs to, and what the sequences in front of it have.  By whole warps.
 template <typename Count>
 __device__ __forceinline__ int32_t find_sequence(const PromptParams &p, const Cut &cut, int at, Count count, Counts *before)
 {
@@ -129,7 +140,7 @@ __device__ __forceinline__ int32_t find_sequence(const PromptParams &p, const Cu
                 upto.parts += q;
             }
         }
-        const uint32_t has = __ballot_sync(0xffffffffu, at >= 0 && count(*before) + count(upto) > at);
+        const uint32_t has = __ballot_sync(0xffffffffu, count(*before) + count(upto) > at);
         const int from = has ? __ffs(has) - 1 : 31;
         const Counts mine = has ? c : Counts{};
         before->tiles += __shfl_sync(0xffffffffu, upto.tiles - mine.tiles, from);
@@ -140,152 +151,146 @@ __device__ __forceinline__ int32_t find_sequence(const PromptParams &p, const Cu
     }
     return -1;
 }
-
-// The unit that a role works on, of the first kernel (SUMS false) or the second.
-template <bool SUMS>
-struct Work {
-    Cut cut;
-    Counts before;     // the sequences in front
-    int32_t unit, end; // this and one past the block's last
-    Unit u;
-    int32_t held, columns, outer, inner;  // of the sequence: tokens, columns; 256 of what stays there are; pieces or chunks
-    int32_t head, o, i;
-    int32_t step0, step1;
-
-    __device__ __forceinline__ void take_sequence(const PromptParams &p, int b)
-    {
-        const Sequence s = sequence<8>(p, b);
-        u.seq = b;
-        u.length = s.length;
-        u.rows = s.rows;
-        u.row0 = s.row0;
-        held = tokens_held(p, s.length);
-        columns = s.rows * p.group;
-        outer = SUMS ? up(held, 256) : up(columns, 256);
-        inner = SUMS ? max(up(up(columns, 128), cut.second), 1) : up(up(held, kTokens), cut.first);
-    }
-    // Columns [lo, hi) that see some of tokens [t0, t1): their ranges move up with the rows, so they are a run.
-    __device__ __forceinline__ void columns_of(const PromptParams &p, int32_t t0, int32_t t1, int32_t *lo, int32_t *hi) const
-    {
-        const int64_t row0 = (int64_t)u.length - u.rows;  // position of the first row
-        *lo = p.causal ? (int32_t)(min(max(t0 - row0, (int64_t)0), (int64_t)u.rows) * p.group) : 0;
-        *hi = p.window > 0 ? (int32_t)(min(max(t1 - 1 + p.window - row0, (int64_t)0), (int64_t)u.rows) * p.group) : columns;
-    }
-    __device__ __forceinline__ void find_steps(const PromptParams &p)
-    {
-        int32_t lo, hi, unused;
-        if (SUMS) {
-            columns_of(p, 256 * o, min(256 * o + 256, held), &lo, &hi);
-        } else {
-            column_range(p, u, 256 * o, &lo, &unused);
-            column_range(p, u, min(256 * o + 256, columns) - 1, &unused, &hi);
+// What the sequences in front of sequence b have.
+__device__ __forceinline__ void find_sequence(const PromptParams &p, const Cut &cut, int b, Counts *before)
+{
+    const int lane = threadIdx.x & 31;
+    *before = Counts{};
+    for (int b0 = 0; b0 < b; b0 += 32) {
+        Counts c{};
+        if (b0 + lane < b) c = counts(p, sequence<8>(p, b0 + lane), cut);
+#pragma unroll
+        for (int d = 16; d; d >>= 1) {
+            c.tiles += __shfl_xor_sync(0xffffffffu, c.tiles, d);
+            c.units[0] += __shfl_xor_sync(0xffffffffu, c.units[0], d);
+            c.units[1] += __shfl_xor_sync(0xffffffffu, c.units[1], d);
+            c.parts += __shfl_xor_sync(0xffffffffu, c.parts, d);
         }
-        const int32_t each = SUMS ? cut.second : cut.first;
-        step0 = max(lo / 128, i * each);
-        step1 = hi > lo ? min(up(hi, 128), (int32_t)min((int64_t)(i + 1) * each, (int64_t)0x7fffffff)) : step0;
-        step1 = max(step1, step0);
+        before->tiles += c.tiles;
+        before->units[0] += c.units[0];
+        before->units[1] += c.units[1];
+        before->parts += c.parts;
     }
-    // The block's first unit; false: there is none.  By whole warps.
-    __device__ __forceinline__ bool begin(const PromptParams &p)
-    {
-        cut = find_cut(p);
-        const auto count = [](const Counts &c) { return c.units[SUMS]; };
-        find_sequence(p, cut, -1, count, &before);
-        const int64_t total = before.units[SUMS];
-        unit = (int32_t)(total * blockIdx.x / gridDim.x);
-        end = (int32_t)(total * (blockIdx.x + 1) / gridDim.x);
-        if (unit >= end) return false;
-        const int b = find_sequence(p, cut, unit, count, &before);
-        take_sequence(p, b);
-        const int32_t local = unit - before.units[SUMS], of_outer = local / inner;
-        i = local - of_outer * inner;
-        head = of_outer / outer;
-        o = of_outer - head * outer;
-        find_steps(p);
-        return true;
-    }
-    __device__ __forceinline__ bool next(const PromptParams &p)
-    {
-        if (++unit >= end) return false;
-        if (++i == inner) {
-            i = 0;
-            if (++o == outer) {
-                o = 0;
-                if (++head == p.g.heads) {
-                    head = 0;
-                    do {  // there is one: units are left
-                        const Counts c = counts(p, sequence<8>(p, u.seq), cut);
-                        before.tiles += c.tiles;
-                        before.units[0] += c.units[0];
-                        before.units[1] += c.units[1];
-                        before.parts += c.parts;
-                        take_sequence(p, u.seq + 1);
-                    } while (u.seq + 1 < p.batch && (held == 0 || (!SUMS && columns == 0)));
-                }
+}
+
+// Columns [lo, hi) that see some of tokens [t0, t1): their ranges move up with the rows, so they are a run.
+__device__ __forceinline__ void columns_of(const PromptParams &p, int32_t length, int32_t rows, int32_t t0, int32_t t1, int32_t *lo, int32_t *hi)
+{
+    const int64_t row0 = (int64_t)length - rows;  // position of the first row
+    *lo = p.causal ? (int32_t)(min(max(t0 - row0, (int64_t)0), (int64_t)rows) * p.group) : 0;
+    *hi = (p.window > 0 ? (int32_t)min(max(t1 - 1 + p.window - row0, (int64_t)0), (int64_t)rows) : rows) * p.group;
+}
+
+// Writes one sequence's units of both kernels down, a thread to a unit; the last sequence says how many there are.
+__device__ __forceinline__ void list_units(const PromptParams &p, int b)
+{
+    const Cut cut = find_cut(p);
+    Counts before;
+    const int seq = b < p.batch ? b : -1;
+    find_sequence(p, cut, seq, &before);
+    if (seq < 0) return;
+    const Sequence s = sequence<8>(p, seq);
+    const Counts mine = counts(p, s, cut);
+    if (seq == p.batch - 1 && threadIdx.x < 2) p.unit_counts[threadIdx.x] = before.units[threadIdx.x] + mine.units[threadIdx.x];
+    const int32_t held = tokens_held(p, s.length), columns = s.rows * p.group;
+#pragma unroll
+    for (int kernel = 0; kernel < 2; ++kernel) {
+        const int32_t outer = kernel ? up(held, 256) : up(columns, 256), each = kernel ? cut.second : cut.first;
+        const int32_t inner = kernel ? max(up(up(columns, 128), each), 1) : up(up(held, kTokens), each);
+        for (int32_t local = threadIdx.x; local < mine.units[kernel]; local += blockDim.x) {
+            const int32_t of_outer = local / inner, i = local - of_outer * inner, head = of_outer / outer, first = 256 * (of_outer - head * outer);
+            int32_t lo, hi, unused;
+            if (kernel) {
+                columns_of(p, s.length, s.rows, first, min(first + 256, held), &lo, &hi);
+            } else {
+                Unit u{};
+                u.length = s.length;
+                u.rows = s.rows;
+                column_range(p, u, first, &lo, &unused);
+                column_range(p, u, min(first + 256, columns) - 1, &unused, &hi);
             }
+            WorkUnit w{seq, s.length, s.rows, held, columns, before.tiles, head, first, max(lo / 128, i * each), 0, kernel && inner > 1 ? before.parts + local : -1, 0};
+            w.step1 = hi > lo ? (int32_t)min((int64_t)up(hi, 128), (int64_t)(i + 1) * each) : w.step0;
+            w.step1 = max(w.step1, w.step0);
+            p.units[kernel][before.units[kernel] + local] = w;
         }
-        find_steps(p);
-        return true;
     }
-    // Whether the second half of what stays exists.
-    __device__ __forceinline__ int halves() const { return 256 * o + 128 < (SUMS ? held : columns) ? 2 : 1; }
-    __device__ __forceinline__ int64_t image(const PromptParams &p, int32_t tile) const { return (int64_t)(before.tiles + tile) * p.g.heads + head; }
-};
+}
 
-// Rows of q as f16 operands and what their scores are multiplied with: a thread to a row, a block to 128 columns.
+__device__ __forceinline__ WorkUnit load_unit(const WorkUnit *from)
+{
+    WorkUnit w;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) reinterpret_cast<int4 *>(&w)[i] = __ldg(reinterpret_cast<const int4 *>(from) + i);
+    return w;
+}
+__device__ __forceinline__ int64_t image_of(const PromptParams &p, const WorkUnit &w, int32_t tile) { return (int64_t)(w.tiles_before + tile) * p.g.heads + w.head; }
+// Whether the second 128 of what stays exist.
+template <bool SUMS>
+__device__ __forceinline__ int halves_of(const WorkUnit &w) { return w.first + 128 < (SUMS ? w.held : w.columns) ? 2 : 1; }
+
+// Rows of q as f16 operands and what their scores are multiplied with: a warp to eight rows, lane 8 c + r to every fourth group of eight channels
+// of row r, which is how they lie in the operand; a block to 128 columns.  A last row of blocks lists the units of the kernels to come.
+constexpr int kRowsThreads = 4 * kTokens;
+
 template <int B>
-__global__ void __launch_bounds__(kTokens) kv_weights_rows_kernel(const __grid_constant__ PromptParams p)
+__global__ void __launch_bounds__(kRowsThreads) kv_weights_rows_kernel(const __grid_constant__ PromptParams p)
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     constexpr int ROWS8 = 512 * B;
+    if (blockIdx.y == p.g.heads) {
+        for (int b = blockIdx.x; b < p.batch; b += gridDim.x) list_units(p, b);
+        return;
+    }
     Counts before;
     const Cut cut{1, 1};
     const int seq = find_sequence(p, cut, blockIdx.x, [](const Counts &c) { return c.tiles; }, &before), head = blockIdx.y;
     if (seq < 0) return;
     const Sequence s = sequence<8>(p, seq);
-    const int column = (blockIdx.x - before.tiles) * 128 + threadIdx.x, row = column / p.group;
-    const int64_t at = (s.row0 + row) * p.q_token + ((int64_t)head * p.group + (column - row * p.group)) * p.q_head, image = (int64_t)blockIdx.x * p.g.heads + head;
-    uint8_t *const to = p.images + image * (kTokens * 64 * B) + (threadIdx.x >> 3) * ROWS8 + (threadIdx.x & 7) * 16;
-    int k = 0;
-    bool finite = true;
-    const auto take_row = [&](auto element, auto vectors) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, in_tile = 8 * warp + (lane & 7), quarter = lane >> 3;
+    const int column = (blockIdx.x - before.tiles) * 128 + in_tile, row = column / p.group;
+    const int64_t at = (s.row0 + row) * p.q_token + ((int64_t)head * p.group + (column - row * p.group)) * p.q_head + 8 * quarter, image = (int64_t)blockIdx.x * p.g.heads + head;
+    uint8_t *const to = p.images + image * (kTokens * 64 * B) + warp * ROWS8 + lane * 16;
+    const auto take_rows = [&](auto element, auto vectors) {
         using T = decltype(element);
-        Eight<T> e[4 * B];  // the whole row at once
+        Eight<T> e[B];
 #pragma unroll
-        for (int c = 0; c < 4 * B; ++c) e[c] = load_eight<T, decltype(vectors)::value>(static_cast<const T *>(p.q) + at + 8 * c, row < s.rows ? p.g.dim - 8 * c : 0);
+        for (int b = 0; b < B; ++b) e[b] = load_eight<T, decltype(vectors)::value>(static_cast<const T *>(p.q) + at + 32 * b, row < s.rows ? p.g.dim - 32 * b - 8 * quarter : 0);
         uint32_t magnitude = 0;  // magnitudes compare like integers, infinity and NaN above all others
         float v[8];
 #pragma unroll
-        for (int c = 0; c < 4 * B; ++c) {
-            e[c].expand(v);
+        for (int b = 0; b < B; ++b) {
+            e[b].expand(v);
 #pragma unroll
             for (int i = 0; i < 8; ++i) magnitude = max(magnitude, __float_as_uint(v[i]) & 0x7fffffffu);
         }
-        finite = magnitude < 0x7f800000u;
+        magnitude = max(magnitude, __shfl_xor_sync(0xffffffffu, magnitude, 8));
+        magnitude = max(magnitude, __shfl_xor_sync(0xffffffffu, magnitude, 16));
+        const bool finite = magnitude < 0x7f800000u;
         // times 2^k, so that the largest is in [2^14, 2^15); a scale below zero changes q's sign
-        k = 14 - (finite && magnitude > 0 ? ilogbf(__uint_as_float(magnitude)) : 0);
-        const int k1 = k / 2, k2 = k - k1;
+        const int k = 14 - (finite && magnitude > 0 ? ilogbf(__uint_as_float(magnitude)) : 0), k1 = k / 2, k2 = k - k1;
         const float s1 = __uint_as_float((uint32_t)(127 + k1) << 23) * (p.scale < 0.0f ? -1.0f : 1.0f), s2 = __uint_as_float((uint32_t)(127 + k2) << 23);
 #pragma unroll
-        for (int c = 0; c < 4 * B; ++c) {
-            e[c].expand(v);
+        for (int b = 0; b < B; ++b) {
+            e[b].expand(v);
             // in the order in which a word's codes are decoded; a row that is not finite is one by its factor
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = finite ? v[i] * s1 * s2 : 0.0f;
-            *reinterpret_cast<uint4 *>(to + c * 128) = make_uint4(pack_half2(v[0], v[4]), pack_half2(v[1], v[5]), pack_half2(v[2], v[6]), pack_half2(v[3], v[7]));
+            *reinterpret_cast<uint4 *>(to + b * 512) = make_uint4(pack_half2(v[0], v[4]), pack_half2(v[1], v[5]), pack_half2(v[2], v[6]), pack_half2(v[3], v[7]));
         }
+        const int kc = -11 - k, c1 = kc / 2, c2 = kc - c1;
+        if (quarter == 0)
+            p.factors[image * kTokens + in_tile] =
+                (finite ? fabsf(p.scale) : __uint_as_float(0x7fc00000u)) * __uint_as_float((uint32_t)(127 + c1) << 23) * __uint_as_float((uint32_t)(127 + c2) << 23);
     };
     if (p.type == LCE_TYPE_FLOAT16) {
-        if (p.q_vectors) take_row(__half(), std::true_type());
-        else take_row(__half(), std::false_type());
+        if (p.q_vectors) take_rows(__half(), std::true_type());
+        else take_rows(__half(), std::false_type());
     } else {
-        if (p.q_vectors) take_row(__nv_bfloat16(), std::true_type());
-        else take_row(__nv_bfloat16(), std::false_type());
+        if (p.q_vectors) take_rows(__nv_bfloat16(), std::true_type());
+        else take_rows(__nv_bfloat16(), std::false_type());
     }
-    const int kc = -11 - k, c1 = kc / 2, c2 = kc - c1;
-    p.factors[image * kTokens + threadIdx.x] =
-        (finite ? fabsf(p.scale) : __uint_as_float(0x7fc00000u)) * __uint_as_float((uint32_t)(127 + c1) << 23) * __uint_as_float((uint32_t)(127 + c2) << 23);
 }
 
 // What a producer thread has of a tile before it decodes it.
@@ -325,13 +330,13 @@ __device__ __forceinline__ void load_raw(const PromptParams &p, int32_t page, in
 
 // A wait of a whole warp.
 __device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_bounded(bar, parity)); }
-// Four warps meet; whether all of them are well.
+// Eight warps meet; whether all of them are well.
 __device__ __forceinline__ bool half_sync_and(uint32_t barrier, bool ok)
 {
     uint32_t all;
     asm volatile(
         "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 q, %1, 0;\n\t"
-        "bar.red.and.pred p, %2, 128, q;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+        "bar.red.and.pred p, %2, 256, q;\n\tselp.u32 %0, 1, 0, p;\n\t}"
         : "=r"(all)
         : "r"((uint32_t)ok), "r"(barrier)
         : "memory");
@@ -341,25 +346,26 @@ __device__ __forceinline__ bool half_sync_and(uint32_t barrier, bool ok)
 // The tiles of keys that a block's units want, one after the other.
 template <bool SUMS>
 struct Tiles {
-    Work<SUMS> w;
-    int32_t step;   // of the unit, or the half
-    bool there;
-    __device__ __forceinline__ void begin(const PromptParams &p, const Work<SUMS> &first)
-    {
-        w = first;
-        there = true;
-        settle(p);
-    }
+    WorkUnit w;
+    int32_t unit, count, step;  // step: of the unit, or the half
+    __device__ __forceinline__ bool there() const { return unit < count; }
     __device__ __forceinline__ void settle(const PromptParams &p)  // at the first tile of a unit that has one
     {
-        while (there && w.step0 == w.step1) there = w.next(p);
+        for (; unit < count; unit += gridDim.x) {
+            w = load_unit(p.units[SUMS] + unit);
+            if (w.step0 < w.step1) break;
+        }
         step = SUMS ? 0 : w.step0;
     }
-    __device__ __forceinline__ int32_t tile() const { return SUMS ? 2 * w.o + step : step; }
+    __device__ __forceinline__ int32_t tile() const { return SUMS ? w.first / kTokens + step : step; }
+    __device__ __forceinline__ bool last() const { return step + 1 == (SUMS ? halves_of<true>(w) : w.step1); }
     __device__ __forceinline__ void next(const PromptParams &p)
     {
-        if (++step < (SUMS ? w.halves() : w.step1)) return;
-        there = w.next(p);
+        if (!last()) {
+            ++step;
+            return;
+        }
+        unit += gridDim.x;
         settle(p);
     }
 };
@@ -375,8 +381,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_prompt_kernel(const __
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    Work<SUMS> work;
-    if (!work.begin(p)) return;
+    const int32_t count = __ldg(p.unit_counts + SUMS);
+    if ((int)blockIdx.x >= count) return;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) {
@@ -387,7 +393,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_prompt_kernel(const __
         }
         for (int i = 0; i < 4; ++i) {
             mbar_init(&sh.bars[BAR_S_FULL + i], 1);
-            mbar_init(&sh.bars[BAR_S_EMPTY + i], 128);
+            mbar_init(&sh.bars[BAR_S_EMPTY + i], 256);
         }
         mbar_init(&sh.bars[BAR_DONE], 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -403,131 +409,150 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_prompt_kernel(const __
     bool ok = true;
 
     if (warp < kSoftmaxWarps) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegisters));
-        // ---- powers of two: a thread to a column, or to a token ---------------------------------------
-        const int half = warp >> 2, in_tile = threadIdx.x & 127;
-        const uint32_t s_at = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + 256 * half;
-        uint32_t steps = 0, units = 0, tiles = 0;  // steps of this half, units that have some, tiles of keys in front of the unit's
-        bool more = true;
-        while (ok && more) {
-            const bool here = half < work.halves();
-            const int32_t own = 256 * work.o + 128 * half + in_tile;
-            int32_t lo = 0, hi = 0;  // what it sees: of the tokens, or of the columns
-            float factor = 0.0f, top = kNothing;
-            uint64_t sum[2] = {};  // pairs of fp32 sums
-            if (here) {
+        // ---- powers of two: two threads to a column, or to a token ------------------------------------
+        const int half = warp >> 2 & 1, side = warp >> 3, in_tile = threadIdx.x & 127;
+        const uint32_t s_at = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + 256 * half + 64 * side;
+        uint32_t steps = 0, units = 0, units_here = 0, tiles = 0;  // steps of this half; units that have some; units of this half; tiles of keys so far
+        for (int32_t unit_at = blockIdx.x; ok && unit_at < count; unit_at += gridDim.x) {
+            const WorkUnit w = load_unit(p.units[SUMS] + unit_at);
+            if (half < halves_of<SUMS>(w)) {
+                const int32_t own = w.first + 128 * half + in_tile;
+                int32_t lo, hi;  // what it sees: of the tokens, or of the columns
+                float factor = 0.0f, unit = 0.0f, constant = 0.0f, top = kNothing;  // constant: a factor or a logarithm of the next step
+                uint64_t sum[2] = {};  // pairs of fp32 sums
+                const float *const constants = reinterpret_cast<const float *>(p.constants) + 2 * in_tile + side;
+                const auto constant_of = [&](int32_t step) { return step < w.step1 ? constants[image_of(p, w, step) * (2 * kTokens)] : 0.0f; };
                 if (SUMS) {
-                    if (own < work.held) work.columns_of(p, own, own + 1, &lo, &hi);
+                    columns_of(p, w.length, w.rows, own, own + 1, &lo, &hi);
+                    constant = constant_of(w.step0);
                 } else {
-                    column_range(p, work.u, own, &lo, &hi);
-                    if (work.step1 > work.step0) factor = p.factors[work.image(p, 2 * work.o + half) * kTokens + in_tile];
+                    Unit u{};
+                    u.length = w.length;
+                    u.rows = w.rows;
+                    column_range(p, u, own, &lo, &hi);
+                    factor = p.factors[image_of(p, w, own / kTokens) * kTokens + in_tile];
                 }
-            }
-            float2 constant = make_float2(0.0f, 0.0f);  // of a column of the next step
-            if (SUMS && here && work.step1 > work.step0) constant = p.constants[work.image(p, work.step0) * kTokens + in_tile];
-            float unit = 0.0f;
-            for (int32_t step = work.step0; ok && here && step < work.step1; ++step, ++steps) {
-                const uint32_t buffer = steps & 1;
-                ok = warp_wait(&sh.bars[BAR_S_FULL + 2 * half + buffer], steps >> 1 & 1);
-                if (!SUMS && !ok) break;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const int first = step * 128;  // token, or column
-                uint32_t valid = 0xffu;
-                if (!SUMS || step == work.step0) {
-                    const TileInfo info = sh.info[(SUMS ? 2 * units + half : tiles + (uint32_t)(step - work.step0)) % kInfos];
-                    unit = info.unit;
+                for (int32_t step = w.step0; ok && step < w.step1; ++step, ++steps) {
+                    const uint32_t buffer = steps & 1;
+                    ok = warp_wait(&sh.bars[BAR_S_FULL + 2 * half + buffer], steps >> 1 & 1);
+                    if (!SUMS && !ok) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const int first = step * 128 + 64 * side;  // token, or column
+                    uint32_t valid = 0xfu;
+                    if (!SUMS || step == w.step0) {
+                        const TileInfo info = sh.info[(SUMS ? 2 * units + half : tiles + (uint32_t)(step - w.step0)) % kInfos];
+                        unit = info.unit;
+                        if (SUMS) {
+                            if (!(info.valid >> (in_tile >> 4) & 1)) hi = lo;  // its page is not in the pool
+                        } else {
+                            valid = info.valid >> (4 * side) & 0xfu;
+                        }
+                    }
                     if (SUMS) {
-                        if (!(info.valid >> (in_tile >> 4) & 1)) hi = lo;  // its page is not in the pool
-                    } else {
-                        valid = info.valid;
+                        // every thread brings one constant of a column; the buffer before last is read by nobody any more
+                        sh.columns[half][buffer][in_tile >> 1][2 * side + (in_tile & 1)] = side ? constant : constant * unit;
+                        constant = constant_of(step + 1);
+                        ok = half_sync_and(2 + half, ok);  // all eight warps leave together
+                        if (!ok) break;
                     }
-                }
-                if (SUMS) {
-                    // every thread brings a column's constants; the buffer before last is read by nobody any more
-                    float *const pair = sh.columns[half][buffer][in_tile >> 1] + (in_tile & 1);
-                    pair[0] = constant.x * unit;
-                    pair[2] = constant.y;
-                    if (step + 1 < work.step1) constant = p.constants[work.image(p, step + 1) * kTokens + in_tile];
-                    ok = half_sync_and(2 + half, ok);  // all four warps leave together
-                    if (!ok) break;
-                }
-                const bool all = __all_sync(0xffffffffu, valid == 0xffu && first >= lo && first + 128 <= hi);
-                const float f = factor * unit;
-                // 64 of the 128 at a time
-#pragma unroll 1
-                for (int c0 = 0; c0 < 128; c0 += 64) {
-                    uint32_t r[64];
-                    tmem_load64(s_at + 128 * buffer + c0, r);
-                    if (c0 == 64) {
+                    const bool all = __all_sync(0xffffffffu, valid == 0xfu && first >= lo && first + 64 <= hi);
+                    const float f = factor * unit;
+                    // 32 scores of the 64
+                    const auto take = [&](const uint32_t (&r)[32], int c, uint32_t seen, auto masked) {
+                        uint64_t f2 = pair_of(f, f), plus = 0;
+                        if (!SUMS) {
+                            const auto score = [&](int i) { return decltype(masked)::value && !(seen >> i & 1) ? -INFINITY : __uint_as_float(r[i]); };
+                            float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) tops[i & 3] = fmaxf(tops[i & 3], score(i));
+                            float m = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+                            m = m == -INFINITY ? m : m * f;
+                            if (m > top + kRise) {
+                                const float by = exp2_fast(top - m);
+                                sum[0] = mul_pair(sum[0], pair_of(by, by));
+                                sum[1] = mul_pair(sum[1], pair_of(by, by));
+                                top = m;
+                            }
+                            plus = pair_of(-top, -top);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 32; i += 2) {
+                            if (SUMS) {
+                                const ulonglong2 both = *reinterpret_cast<const ulonglong2 *>(sh.columns[half][buffer][32 * side + 16 * c + (i >> 1)]);
+                                f2 = both.x;
+                                plus = both.y;
+                            }
+                            float x, y;
+                            of_pair(fma_pair(pair_of(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), f2, plus), x, y);
+                            if (decltype(masked)::value) {  // not 0, or what a column that is not finite has, times minus infinity
+                                x = seen >> i & 1 ? x : -INFINITY;
+                                y = seen >> (i + 1) & 1 ? y : -INFINITY;
+                            }
+                            sum[i >> 1 & 1] = add_pair(sum[i >> 1 & 1], pair_of(exp2_fast(x), exp2_fast(y)));
+                        }
+                    };
+                    uint32_t r[32];
+                    const auto load = [&](int c) {
+                        tmem_begin32(s_at + 128 * buffer + 32 * c, r);
+                        tmem_end32(r);
+                        if (c == 0) return;
                         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                        mbar_arrive(&sh.bars[BAR_S_EMPTY + 2 * half + buffer]);
-                    }
-                    if (!all) {
+                        mbar_arrive(&sh.bars[BAR_S_EMPTY + 2 * half + buffer]);  // the buffer is free again
+                    };
+                    if (all) {
 #pragma unroll
                         for (int c = 0; c < 2; ++c) {
-                            const int32_t at = first + c0 + 32 * c, from = min(max(lo - at, 0), 32), to = min(max(hi - at, 0), 32);
-                            const uint32_t below = to >= 32 ? 0xffffffffu : (1u << to) - 1, above = from >= 32 ? 0u : 0xffffffffu << from;
-                            const uint32_t pages = valid >> ((c0 >> 4) + 2 * c);
-                            const uint32_t seen = below & above & ((pages & 1 ? 0xffffu : 0u) | (pages & 2 ? 0xffff0000u : 0u));
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) r[32 * c + i] = seen >> i & 1 ? r[32 * c + i] : 0xff800000u;
+                            load(c);
+                            take(r, c, 0xffffffffu, std::false_type());
                         }
-                    }
-                    uint64_t f2 = pair_of(f, f), plus = 0;
-                    if (!SUMS) {
-                        float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                        for (int i = 0; i < 64; ++i) tops[i & 3] = fmaxf(tops[i & 3], __uint_as_float(r[i]));
-                        float m = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-                        m = m == -INFINITY ? m : m * f;
-                        if (m > top + kRise) {
-                            const float by = exp2_fast(top - m);
-                            sum[0] = mul_pair(sum[0], pair_of(by, by));
-                            sum[1] = mul_pair(sum[1], pair_of(by, by));
-                            top = m;
+                    } else {
+#pragma unroll 1
+                        for (int c = 0; c < 2; ++c) {
+                            const int32_t at = first + 32 * c, from = min(max(lo - at, 0), 32), to = min(max(hi - at, 0), 32);
+                            const uint32_t below = to >= 32 ? 0xffffffffu : (1u << to) - 1, above = from >= 32 ? 0u : 0xffffffffu << from, pages = valid >> (2 * c);
+                            load(c);
+                            take(r, c, below & above & ((pages & 1 ? 0xffffu : 0u) | (pages & 2 ? 0xffff0000u : 0u)), std::true_type());
                         }
-                        plus = pair_of(-top, -top);
-                    }
-#pragma unroll
-                    for (int i = 0; i < 64; i += 2) {
-                        if (SUMS) {
-                            const ulonglong2 c = *reinterpret_cast<const ulonglong2 *>(sh.columns[half][buffer][(c0 + i) >> 1]);
-                            f2 = c.x;
-                            plus = c.y;
-                        }
-                        float x, y;
-                        of_pair(fma_pair(pair_of(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), f2, plus), x, y);
-                        if (!all) {  // 0, or what a column that is not finite has, times minus infinity
-                            x = r[i] == 0xff800000u ? -INFINITY : x;
-                            y = r[i + 1] == 0xff800000u ? -INFINITY : y;
-                        }
-                        sum[i >> 1 & 1] = add_pair(sum[i >> 1 & 1], pair_of(exp2_fast(x), exp2_fast(y)));
                     }
                 }
+                // the two threads' sums meet
+                float w0, w1, w2, w3;
+                of_pair(sum[0], w0, w1);
+                of_pair(sum[1], w2, w3);
+                float total = (w0 + w1) + (w2 + w3);
+                if (side) sh.others[half][units_here & 1][in_tile] = make_float2(top, total);
+                ok = half_sync_and(2 + half, ok);
+                if (!ok) break;
+                if (!side) {
+                    const float2 other = sh.others[half][units_here & 1][in_tile];
+                    if (!SUMS) {
+                        const float high = fmaxf(top, other.x);
+                        total = total * exp2_fast(top - high) + other.y * exp2_fast(other.x - high);
+                        p.stats_units[(int64_t)unit_at * 256 + 128 * half + in_tile] = make_float2(high, total);
+                    } else if (w.part >= 0) {
+                        p.parts[(int64_t)w.part * 256 + 128 * half + in_tile] = total + other.y;
+                    } else if (own < w.held) {
+                        Unit u{};
+                        u.seq = w.seq;
+                        u.length = w.length;
+                        u.rows = w.rows;
+                        put_weight(p, u, w.head, own, total + other.y);
+                    }
+                }
+                ++units_here;
             }
-            if (!ok) break;
-            float w0, w1, w2, w3;
-            of_pair(sum[0], w0, w1);
-            of_pair(sum[1], w2, w3);
-            const float total = (w0 + w1) + (w2 + w3);
-            if (!SUMS) {
-                p.stats_units[(int64_t)work.unit * 256 + 128 * half + in_tile] = make_float2(top, total);
-            } else if (own < work.held) {
-                if (work.inner > 1) p.parts[(int64_t)(work.before.parts + work.unit - work.before.units[1]) * 256 + 128 * half + in_tile] = total;
-                else put_weight(p, work.u, work.head, own, total);
-            }
-            if (work.step1 > work.step0) {
+            if (w.step1 > w.step0) {
                 ++units;
-                tiles += (uint32_t)(work.step1 - work.step0);
+                tiles += (uint32_t)(w.step1 - w.step0);
             }
-            more = work.next(p);
         }
     } else if (warp < kIssuerWarp) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kProducerRegisters));
         // ---- keys: from 4 bits to f16 operands ------------------------------------------------------------
         const int thread = threadIdx.x - 32 * kSoftmaxWarps, producer = warp - kSoftmaxWarps;
         Tiles<SUMS> ahead;  // the tile behind the one whose words are on their way
-        ahead.begin(p, work);
+        ahead.unit = blockIdx.x;
+        ahead.count = count;
+        ahead.settle(p);
         struct Tile {
             bool there;
             uint32_t half;  // of a unit; whether it is the last one
@@ -536,12 +561,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_prompt_kernel(const __
         Raw<B> even_raw, odd_raw;
         Tile even{}, odd{};
         int32_t page = -1;
-        const auto find = [&]() { page = ahead.there ? find_page(p, p.page_table + (int64_t)ahead.w.u.seq * p.table_pages, ahead.w.held, ahead.tile(), lane) : -1; };
+        const auto find = [&]() { page = ahead.there() ? find_page(p, p.page_table + (int64_t)ahead.w.seq * p.table_pages, ahead.w.held, ahead.tile(), lane) : -1; };
         const auto load = [&](Raw<B> &raw, Tile &tile) {
-            tile.there = ahead.there;
-            if (!ahead.there) return;
+            tile.there = ahead.there();
+            if (!tile.there) return;
             tile.half = SUMS ? (uint32_t)ahead.step : 0;
-            tile.last = SUMS && ahead.step + 1 == ahead.w.halves();
+            tile.last = SUMS && ahead.last();
             load_raw<B>(p, page, ahead.w.head, ahead.w.held, ahead.tile(), thread, raw);
             ahead.next(p);
             find();
@@ -603,83 +628,78 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_prompt_kernel(const __
             if (!odd.there || !produce(odd_raw, odd, even_raw, even)) break;
         }
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kIssuerRegisters));
         if (warp == kIssuerWarp) {
             // ---- the products ---------------------------------------------------------------------------------
             constexpr uint32_t kIdesc = 1u << 4 | (uint32_t)(128 >> 4) << 24 | (uint32_t)(128 >> 3) << 17;  // fp32 sums of f16 products, both operands along k, 128 x 128
             const uint32_t stay_at = smem_u32(stay_smem), stream_at = smem_u32(stream_smem);
             uint32_t units = 0, streamed = 0, steps[2] = {0, 0};
-            bool more = true;
-            while (ok && more) {
-                if (work.step1 > work.step0) {
-                    const uint32_t pair = units & 1;
-                    const int halves = work.halves();
-                    ok = warp_wait(&sh.bars[BAR_STAY_FULL + pair], units >> 1 & 1);
-                    for (int32_t step = work.step0; ok && step < work.step1; ++step, ++streamed) {
-                        const uint32_t slot = streamed & 1;
-                        ok = warp_wait(&sh.bars[BAR_STREAM_FULL + slot], streamed >> 1 & 1);
+            for (int32_t unit_at = blockIdx.x; ok && unit_at < count; unit_at += gridDim.x) {
+                const WorkUnit w = load_unit(p.units[SUMS] + unit_at);
+                if (w.step0 == w.step1) continue;
+                const uint32_t pair = units & 1;
+                const int halves = halves_of<SUMS>(w);
+                ok = warp_wait(&sh.bars[BAR_STAY_FULL + pair], units >> 1 & 1);
+                for (int32_t step = w.step0; ok && step < w.step1; ++step, ++streamed) {
+                    const uint32_t slot = streamed & 1;
+                    ok = warp_wait(&sh.bars[BAR_STREAM_FULL + slot], streamed >> 1 & 1);
 #pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            if (!ok || half >= halves) break;
-                            const uint32_t buffer = steps[half] & 1;
-                            if (steps[half] >= 2) ok = warp_wait(&sh.bars[BAR_S_EMPTY + 2 * half + buffer], (steps[half] >> 1 & 1) ^ 1);
-                            if (!ok) break;
-                            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                            if (lane == 0) {
+                    for (int half = 0; half < 2; ++half) {
+                        if (!ok || half >= halves) break;
+                        const uint32_t buffer = steps[half] & 1;
+                        if (steps[half] >= 2) ok = warp_wait(&sh.bars[BAR_S_EMPTY + 2 * half + buffer], (steps[half] >> 1 & 1) ^ 1);
+                        if (!ok) break;
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        if (lane == 0) {
 #pragma unroll
-                                for (int k = 0; k < 2 * B; ++k)
-                                    mma_shared(tmem + 256 * half + 128 * buffer, operand(stay_at + (2 * pair + half) * TILE_BYTES + k * 256, ROWS8),
-                                               operand(stream_at + slot * TILE_BYTES + k * 256, ROWS8), kIdesc, k > 0);
-                                mma_commit(&sh.bars[BAR_S_FULL + 2 * half + buffer]);
-                            }
-                            __syncwarp();
-                            ++steps[half];
+                            for (int k = 0; k < 2 * B; ++k)
+                                mma_shared(tmem + 256 * half + 128 * buffer, operand(stay_at + (2 * pair + half) * TILE_BYTES + k * 256, ROWS8),
+                                           operand(stream_at + slot * TILE_BYTES + k * 256, ROWS8), kIdesc, k > 0);
+                            mma_commit(&sh.bars[BAR_S_FULL + 2 * half + buffer]);
                         }
-                        if (ok && lane == 0) mma_commit(&sh.bars[BAR_STREAM_EMPTY + slot]);
                         __syncwarp();
+                        ++steps[half];
                     }
-                    if (ok && lane == 0) mma_commit(&sh.bars[BAR_STAY_EMPTY + pair]);
+                    if (ok && lane == 0) mma_commit(&sh.bars[BAR_STREAM_EMPTY + slot]);
                     __syncwarp();
-                    ++units;
                 }
-                more = work.next(p);
+                if (ok && lane == 0) mma_commit(&sh.bars[BAR_STAY_EMPTY + pair]);
+                __syncwarp();
+                ++units;
             }
             // whatever happened: nothing is in flight when the tensor memory goes
             if (lane == 0) mma_commit(&sh.bars[BAR_DONE]);
             __syncwarp();
             if (!wait_bounded(&sh.bars[BAR_DONE], 0)) ok = false;
-        } else if (warp == kCopyWarp) {
+        } else {
             // ---- rows of q: images to shared memory -------------------------------------------------------------
             uint32_t units = 0, streamed = 0;
-            bool more = true;
-            const auto copy = [&](uint8_t *to, int32_t tile, uint64_t *bar) { bulk_copy_g2s(to, p.images + work.image(p, tile) * TILE_BYTES, TILE_BYTES, bar); };
-            while (ok && more) {
-                if (work.step1 > work.step0) {
-                    if (!SUMS) {
-                        const uint32_t pair = units & 1;
-                        if (units >= 2) ok = warp_wait(&sh.bars[BAR_STAY_EMPTY + pair], (units >> 1 & 1) ^ 1);
+            for (int32_t unit_at = blockIdx.x; ok && unit_at < count; unit_at += gridDim.x) {
+                const WorkUnit w = load_unit(p.units[SUMS] + unit_at);
+                const auto copy = [&](uint8_t *to, int32_t tile, uint64_t *bar) { bulk_copy_g2s(to, p.images + image_of(p, w, tile) * TILE_BYTES, TILE_BYTES, bar); };
+                if (w.step0 == w.step1) continue;
+                if (!SUMS) {
+                    const uint32_t pair = units & 1;
+                    if (units >= 2) ok = warp_wait(&sh.bars[BAR_STAY_EMPTY + pair], (units >> 1 & 1) ^ 1);
+                    if (!ok) break;
+                    if (lane == 0) {
+                        const int halves = halves_of<SUMS>(w);
+                        mbar_expect_tx(&sh.bars[BAR_STAY_FULL + pair], halves * TILE_BYTES);
+                        for (int half = 0; half < halves; ++half) copy(stay_smem + (2 * pair + half) * TILE_BYTES, w.first / 128 + half, &sh.bars[BAR_STAY_FULL + pair]);
+                    }
+                    __syncwarp();
+                    ++units;
+                } else {
+                    for (int32_t step = w.step0; step < w.step1; ++step, ++streamed) {
+                        const uint32_t slot = streamed & 1;
+                        if (streamed >= 2) ok = warp_wait(&sh.bars[BAR_STREAM_EMPTY + slot], (streamed >> 1 & 1) ^ 1);
                         if (!ok) break;
                         if (lane == 0) {
-                            const int halves = work.halves();
-                            mbar_expect_tx(&sh.bars[BAR_STAY_FULL + pair], halves * TILE_BYTES);
-                            for (int half = 0; half < halves; ++half) copy(stay_smem + (2 * pair + half) * TILE_BYTES, 2 * work.o + half, &sh.bars[BAR_STAY_FULL + pair]);
+                            mbar_expect_tx(&sh.bars[BAR_STREAM_FULL + slot], TILE_BYTES);
+                            copy(stream_smem + slot * TILE_BYTES, step, &sh.bars[BAR_STREAM_FULL + slot]);
                         }
                         __syncwarp();
-                        ++units;
-                    } else {
-                        for (int32_t step = work.step0; step < work.step1; ++step, ++streamed) {
-                            const uint32_t slot = streamed & 1;
-                            if (streamed >= 2) ok = warp_wait(&sh.bars[BAR_STREAM_EMPTY + slot], (streamed >> 1 & 1) ^ 1);
-                                if (!ok) break;
-                            if (lane == 0) {
-                                mbar_expect_tx(&sh.bars[BAR_STREAM_FULL + slot], TILE_BYTES);
-                                copy(stream_smem + slot * TILE_BYTES, step, &sh.bars[BAR_STREAM_FULL + slot]);
-                            }
-                            __syncwarp();
-                        }
                     }
                 }
-                if (ok) more = work.next(p);
             }
             // whatever happened: no copy is in flight when the block ends
             const uint32_t copied = SUMS ? streamed : units;
@@ -700,9 +720,12 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_prompt_kernel(const __
     if (warp == kIssuerWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
 
-// The pieces' sums of a column joined, always in the same order: a thread to a column, a block to 128.
-__global__ void __launch_bounds__(kTokens) kv_weights_columns_kernel(const __grid_constant__ PromptParams p)
+// The pieces' sums of a column joined, always in the same order: eight threads to a column, a block to 128.
+constexpr int kJoining = 8;
+
+__global__ void __launch_bounds__(kJoining * kTokens) kv_weights_columns_kernel(const __grid_constant__ PromptParams p)
 {
+    __shared__ float2 parts[kJoining][kTokens];
     Counts before;
     const Cut cut = find_cut(p);
     // the lengths are what the kernels in front read: nothing has written them since
@@ -710,56 +733,64 @@ __global__ void __launch_bounds__(kTokens) kv_weights_columns_kernel(const __gri
     asm volatile("griddepcontrol.wait;" ::: "memory");  // every block: what comes behind this kernel relies on the ones in front, too
     if (seq < 0) return;
     const Sequence s = sequence<8>(p, seq);
+    const int in_tile = threadIdx.x % kTokens, part = threadIdx.x / kTokens;
     const int tile = blockIdx.x - before.tiles, columns = s.rows * p.group, pieces = up(up(tokens_held(p, s.length), kTokens), cut.first);
-    const int64_t at = ((int64_t)blockIdx.x * p.g.heads + head) * kTokens + threadIdx.x;
-    float2 constant = make_float2(0.0f, -INFINITY);  // a column that is none, or sees nothing
-    if (tile * 128 + (int)threadIdx.x < columns) {
-        const float2 *const from = p.stats_units + (before.units[0] + (int64_t)(head * up(columns, 256) + tile / 2) * pieces) * 256 + (tile & 1) * 128 + threadIdx.x;
-        float top = kNothing, sum = 0.0f;
+    const auto add = [](float2 &sum, const float2 &other) {  // relative to their largest
+        const float high = fmaxf(sum.x, other.x);
+        sum = make_float2(high, sum.y * exp2_fast(sum.x - high) + other.y * exp2_fast(other.x - high));
+    };
+    float2 sum = make_float2(kNothing, 0.0f);
+    if (tile * 128 + in_tile < columns) {
+        const float2 *const from = p.stats_units + (before.units[0] + (int64_t)(head * up(columns, 256) + tile / 2) * pieces) * 256 + (tile & 1) * 128 + in_tile;
 #pragma unroll 4
-        for (int i = 0; i < pieces; ++i) {
-            const float2 part = from[(int64_t)i * 256];
-            const float high = fmaxf(top, part.x);
-            sum = sum * exp2f(top - high) + part.y * exp2f(part.x - high);
-            top = high;
-        }
-        constant = make_float2(p.factors[at], sum == 0.0f ? -INFINITY : -(top + log2f(sum)));
+        for (int i = part; i < pieces; i += kJoining) add(sum, from[(int64_t)i * 256]);
     }
-    p.constants[at] = constant;
+    parts[part][in_tile] = sum;
+    __syncthreads();
+    if (part > 0) return;
+#pragma unroll
+    for (int i = 1; i < kJoining; ++i) add(sum, parts[i][in_tile]);
+    const int64_t at = ((int64_t)blockIdx.x * p.g.heads + head) * kTokens + in_tile;
+    // nothing of a column that is none, or sees nothing
+    p.constants[at] = sum.y == 0.0f ? make_float2(0.0f, -INFINITY) : make_float2(p.factors[at], -(sum.x + log2f(sum.y)));
 }
 
-// The chunks' weights of a token added up, always in the same order.
+// The chunks' weights of a token added up, always in the same order; a block to 256 tokens at a time.
 __global__ void __launch_bounds__(256) kv_weights_chunks_kernel(const __grid_constant__ PromptParams p)
 {
-    Counts before;
     const Cut cut = find_cut(p);
-    const int seq = find_sequence(p, cut, blockIdx.x, [](const Counts &c) { return c.parts; }, &before);
     asm volatile("griddepcontrol.wait;" ::: "memory");  // every block: what comes behind this kernel relies on the ones in front, too
-    if (seq < 0) return;
-    const Sequence s = sequence<8>(p, seq);
-    const int held = tokens_held(p, s.length), outer = up(held, 256), chunks = up(up(s.rows * p.group, 128), cut.second);
-    const int local = blockIdx.x - before.parts, of_outer = local / chunks, head = of_outer / outer, t = (of_outer - head * outer) * 256 + threadIdx.x;
-    if (local != of_outer * chunks || t >= held) return;  // a block to 256 tokens
-    const float *const from = p.parts + (int64_t)blockIdx.x * 256 + threadIdx.x;
-    float w = 0.0f;
+    for (int at = blockIdx.x;; at += gridDim.x) {
+        Counts before;
+        const int seq = find_sequence(p, cut, at, [](const Counts &c) { return c.parts; }, &before);
+        if (seq < 0) return;
+        const Sequence s = sequence<8>(p, seq);
+        const int held = tokens_held(p, s.length), outer = up(held, 256), chunks = up(up(s.rows * p.group, 128), cut.second);
+        const int local = at - before.parts, of_outer = local / chunks, head = of_outer / outer, t = (of_outer - head * outer) * 256 + threadIdx.x;
+        if (local == of_outer * chunks && t < held) {  // the first of 256 tokens' chunks stands for them all
+            const float *const from = p.parts + (int64_t)at * 256 + threadIdx.x;
+            float w = 0.0f;
 #pragma unroll 4
-    for (int i = 0; i < chunks; ++i) w += from[(int64_t)i * 256];
-    Unit u{};
-    u.seq = seq;
-    u.length = s.length;
-    u.rows = s.rows;
-    put_weight(p, u, head, t, w);
+            for (int i = 0; i < chunks; ++i) w += from[(int64_t)i * 256];
+            Unit u{};
+            u.seq = seq;
+            u.length = s.length;
+            u.rows = s.rows;
+            put_weight(p, u, head, t, w);
+        }
+    }
 }
 
 // Tiles of columns, units and parts that there can be.
 struct Bounds {
-    int64_t tiles, units, parts;
+    int64_t tiles, units, second_units, parts;
 };
 Bounds bounds(const WeightsParams &p)
 {
-    // at most kSteps units by the cut, and one more for every 256 columns of a head; parts: the chunks are at most twice the steps by the cut
+    // at most kSteps units by the cut, and one more for every 256 columns, or tokens, of a head; parts: the chunks are at most twice the steps by the cut
     const int64_t columns = p.tokens * p.group;
-    return {columns / 128 + p.batch, kSteps + p.g.heads * (columns / 256 + p.batch), 2 * kSteps};
+    const int64_t tokens = (int64_t)p.batch * ((p.table_tokens + 255) / 256);
+    return {columns / 128 + p.batch, kSteps + p.g.heads * (columns / 256 + p.batch), kSteps + p.g.heads * tokens, 2 * kSteps};
 }
 
 int64_t rounded(int64_t bytes) { return (bytes + 255) / 256 * 256; }
@@ -771,11 +802,11 @@ lce_status launch(PromptParams &p, const TimeoutReport &report, cudaStream_t s)
     if (!first_opt_in.ensure(kv_weights_prompt_kernel<B, false>, weights_smem(B)) || !second_opt_in.ensure(kv_weights_prompt_kernel<B, true>, weights_smem(B))) return LCE_ERR_CUDA;
     const Bounds most = bounds(p);
     const dim3 tiles((unsigned)most.tiles, (unsigned)p.g.heads);
-    lce_status st = launch_dependent(kv_weights_rows_kernel<B>, tiles, kTokens, 0, s, p);
+    lce_status st = launch_dependent(kv_weights_rows_kernel<B>, dim3(tiles.x, tiles.y + 1), kRowsThreads, 0, s, p);
     if (st == LCE_OK) st = launch_dependent(kv_weights_prompt_kernel<B, false>, dim3(kBlocks), kThreads, weights_smem(B), s, p, report);
-    if (st == LCE_OK) st = launch_dependent(kv_weights_columns_kernel, tiles, kTokens, 0, s, p);
+    if (st == LCE_OK) st = launch_dependent(kv_weights_columns_kernel, tiles, kJoining * kTokens, 0, s, p);
     if (st == LCE_OK) st = launch_dependent(kv_weights_prompt_kernel<B, true>, dim3(kBlocks), kThreads, weights_smem(B), s, p, report);
-    if (st == LCE_OK) st = launch_dependent(kv_weights_chunks_kernel, dim3((unsigned)most.parts), 256, 0, s, p);
+    if (st == LCE_OK) st = launch_dependent(kv_weights_chunks_kernel, dim3(4 * kBlocks), 256, 0, s, p);
     return st;
 }
 
@@ -785,7 +816,7 @@ size_t kv_weights_prompt_bytes(const WeightsParams &p)
 {
     const Bounds most = bounds(p);
     const int64_t columns = most.tiles * p.g.heads * kTokens;
-    return (size_t)(rounded(columns * 64 * p.g.blocks) + rounded(columns * 4) + rounded(columns * 8) + rounded(most.units * 256 * 8) + rounded(most.parts * 256 * 4));
+    return (size_t)(rounded(most.units * sizeof(WorkUnit)) + rounded(most.second_units * sizeof(WorkUnit)) + rounded(8) + rounded(columns * 64 * p.g.blocks) + rounded(columns * 4) + rounded(columns * 8) + rounded(most.units * 256 * 8) + rounded(most.parts * 256 * 4));
 }
 
 lce_status launch_kv_weights_prompt(const WeightsParams &params, void *workspace, cudaStream_t s)
@@ -803,6 +834,9 @@ lce_status launch_kv_weights_prompt(const WeightsParams &params, void *workspace
         at += rounded(bytes);
         return here;
     };
+    p.units[0] = reinterpret_cast<WorkUnit *>(take(most.units * sizeof(WorkUnit)));
+    p.units[1] = reinterpret_cast<WorkUnit *>(take(most.second_units * sizeof(WorkUnit)));
+    p.unit_counts = reinterpret_cast<int32_t *>(take(8));
     p.images = reinterpret_cast<uint8_t *>(take(columns * 64 * p.g.blocks));
     p.factors = reinterpret_cast<float *>(take(columns * 4));
     p.constants = reinterpret_cast<float2 *>(take(columns * 8));
