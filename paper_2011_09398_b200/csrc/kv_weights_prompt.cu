@@ -34,6 +34,7 @@ constexpr float kNothing = -3e38f;   // stands for the largest score where there
 constexpr float kRise = 16.0f;       // the score that powers of two are relative to is raised when one passes it by this much
 constexpr int kBlocks = 148;         // one to an SM
 constexpr int kSteps = kBlocks * 8;  // units are cut so that there are about as many
+constexpr int kHeldUnits = 32;       // of a block, in shared memory
 constexpr int kInfos = 8;            // tiles of keys; the producers are less than four units, of two tiles, ahead of the softmax
 
 enum { BAR_STAY_FULL = 0, BAR_STAY_EMPTY = BAR_STAY_FULL + 2, BAR_STREAM_FULL = BAR_STAY_EMPTY + 2, BAR_STREAM_EMPTY = BAR_STREAM_FULL + 2,
@@ -44,19 +45,6 @@ struct TileInfo {
     uint32_t valid;  // bit per 16 tokens: their page is in the pool
 };
 
-struct Shared {
-    uint64_t bars[BAR_COUNT];
-    uint32_t tmem, largest[2][kProducerWarps];
-    TileInfo info[kInfos];
-    alignas(16) __half scales[2][kTokens][4];         // relative to the tile's largest; [turn]
-    alignas(16) float columns[2][2][kTokens / 2][4];  // [half][turn][pair]: two factors, two logarithms taken off
-    float2 others[2][2][kTokens];                     // [half][turn]: what the second of two threads has at a unit's end
-};
-
-constexpr int kMiscBytes = 12288;
-static_assert(sizeof(Shared) <= kMiscBytes, "");
-constexpr size_t weights_smem(int blocks) { return kMiscBytes + 6 * (size_t)(kTokens * 64 * blocks); }
-
 // A unit of work.
 struct alignas(16) WorkUnit {
     int32_t seq, length, rows, held;  // tokens of the sequence, its rows of q, tokens that its pages hold
@@ -66,6 +54,20 @@ struct alignas(16) WorkUnit {
     int32_t part;                     // second kernel: where its sums wait for the other chunks'; negative: it has no others
     int32_t unused;
 };
+
+struct Shared {
+    uint64_t bars[BAR_COUNT];
+    uint32_t tmem, largest[2][kProducerWarps];
+    TileInfo info[kInfos];
+    alignas(16) __half scales[2][kTokens][4];         // relative to the tile's largest; [turn]
+    alignas(16) float columns[2][2][kTokens / 2][4];  // [half][turn][pair]: two factors, two logarithms taken off
+    float2 others[2][2][kTokens];                     // [half][turn]: what the second of two threads has at a unit's end
+    WorkUnit units[kHeldUnits];                       // the block's first ones
+};
+
+constexpr int kMiscBytes = 12288;
+static_assert(sizeof(Shared) <= kMiscBytes, "");
+constexpr size_t weights_smem(int blocks) { return kMiscBytes + 6 * (size_t)(kTokens * 64 * blocks); }
 
 struct PromptParams : WeightsParams {
     WorkUnit *units[2];
@@ -209,20 +211,20 @@ __device__ __forceinline__ void list_units(const PromptParams &p, int b)
                 column_range(p, u, first, &lo, &unused);
                 column_range(p, u, min(first + 256, columns) - 1, &unused, &hi);
             }
-            WorkUnit w{seq, s.length, s.rows, held, columns, before.tiles, head, first, max(lo / 128, i * each), 0, kernel && inner > 1 ? before.parts + local : -1, 0};
-            w.step1 = hi > lo ? (int32_t)min((int64_t)up(hi, 128), (int64_t)(i + 1) * each) : w.step0;
-            w.step1 = max(w.step1, w.step0);
+            // equal shares of what is seen
+            const int32_t seen0 = lo / 128, seen = hi > lo ? up(hi, 128) - seen0 : 0;
+            const WorkUnit w{seq, s.length, s.rows, held, columns, before.tiles, head, first, seen0 + (int32_t)((int64_t)seen * i / inner),
+                             seen0 + (int32_t)((int64_t)seen * (i + 1) / inner), kernel && inner > 1 ? before.parts + local : -1, 0};
             p.units[kernel][before.units[kernel] + local] = w;
         }
     }
 }
 
-__device__ __forceinline__ WorkUnit load_unit(const WorkUnit *from)
+// The block's k-th unit, which is unit `at`.
+template <bool SUMS>
+__device__ __forceinline__ WorkUnit load_unit(const PromptParams &p, const Shared &sh, int32_t k, int32_t at)
 {
-    WorkUnit w;
-#pragma unroll
-    for (int i = 0; i < 3; ++i) reinterpret_cast<int4 *>(&w)[i] = __ldg(reinterpret_cast<const int4 *>(from) + i);
-    return w;
+    return k < kHeldUnits ? sh.units[k] : p.units[SUMS][at];
 }
 __device__ __forceinline__ int64_t image_of(const PromptParams &p, const WorkUnit &w, int32_t tile) { return (int64_t)(w.tiles_before + tile) * p.g.heads + w.head; }
 // Whether the second 128 of what stays exist.
@@ -347,26 +349,27 @@ __device__ __forceinline__ bool half_sync_and(uint32_t barrier, bool ok)
 template <bool SUMS>
 struct Tiles {
     WorkUnit w;
-    int32_t unit, count, step;  // step: of the unit, or the half
+    int32_t k, unit, count, step;  // step: of the unit, or the half
     __device__ __forceinline__ bool there() const { return unit < count; }
-    __device__ __forceinline__ void settle(const PromptParams &p)  // at the first tile of a unit that has one
+    __device__ __forceinline__ void settle(const PromptParams &p, const Shared &sh)  // at the first tile of a unit that has one
     {
-        for (; unit < count; unit += gridDim.x) {
-            w = load_unit(p.units[SUMS] + unit);
+        for (; unit < count; unit += gridDim.x, ++k) {
+            w = load_unit<SUMS>(p, sh, k, unit);
             if (w.step0 < w.step1) break;
         }
         step = SUMS ? 0 : w.step0;
     }
     __device__ __forceinline__ int32_t tile() const { return SUMS ? w.first / kTokens + step : step; }
     __device__ __forceinline__ bool last() const { return step + 1 == (SUMS ? halves_of<true>(w) : w.step1); }
-    __device__ __forceinline__ void next(const PromptParams &p)
+    __device__ __forceinline__ void next(const PromptParams &p, const Shared &sh)
     {
         if (!last()) {
             ++step;
             return;
         }
         unit += gridDim.x;
-        settle(p);
+        ++k;
+        settle(p, sh);
     }
 };
 
@@ -383,6 +386,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_prompt_kernel(const __
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int32_t count = __ldg(p.unit_counts + SUMS);
     if ((int)blockIdx.x >= count) return;
+    for (int i = threadIdx.x; i < 3 * kHeldUnits; i += kThreads) {
+        const int32_t at = blockIdx.x + i / 3 * gridDim.x;
+        if (at < count) reinterpret_cast<int4 *>(sh.units)[i] = reinterpret_cast<const int4 *>(p.units[SUMS] + at)[i % 3];
+    }
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) {
@@ -413,14 +420,15 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_prompt_kernel(const __
         const int half = warp >> 2 & 1, side = warp >> 3, in_tile = threadIdx.x & 127;
         const uint32_t s_at = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + 256 * half + 64 * side;
         uint32_t steps = 0, units = 0, units_here = 0, tiles = 0;  // steps of this half; units that have some; units of this half; tiles of keys so far
-        for (int32_t unit_at = blockIdx.x; ok && unit_at < count; unit_at += gridDim.x) {
-            const WorkUnit w = load_unit(p.units[SUMS] + unit_at);
+        float constant = 0.0f;  // a factor or a logarithm of a column of the next step
+        const float *const constants = reinterpret_cast<const float *>(p.constants) + 2 * in_tile + side;
+        for (int32_t unit_at = blockIdx.x, k = 0; ok && unit_at < count; unit_at += gridDim.x, ++k) {
+            const WorkUnit w = load_unit<SUMS>(p, sh, k, unit_at);
             if (half < halves_of<SUMS>(w)) {
                 const int32_t own = w.first + 128 * half + in_tile;
                 int32_t lo, hi;  // what it sees: of the tokens, or of the columns
-                float factor = 0.0f, unit = 0.0f, constant = 0.0f, top = kNothing;  // constant: a factor or a logarithm of the next step
+                float factor = 0.0f, unit = 0.0f, top = kNothing;
                 uint64_t sum[2] = {};  // pairs of fp32 sums
-                const float *const constants = reinterpret_cast<const float *>(p.constants) + 2 * in_tile + side;
                 const auto constant_of = [&](int32_t step) { return step < w.step1 ? constants[image_of(p, w, step) * (2 * kTokens)] : 0.0f; };
                 if (SUMS) {
                     columns_of(p, w.length, w.rows, own, own + 1, &lo, &hi);
@@ -550,9 +558,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_prompt_kernel(const __
         // ---- keys: from 4 bits to f16 operands ------------------------------------------------------------
         const int thread = threadIdx.x - 32 * kSoftmaxWarps, producer = warp - kSoftmaxWarps;
         Tiles<SUMS> ahead;  // the tile behind the one whose words are on their way
+        ahead.k = 0;
         ahead.unit = blockIdx.x;
         ahead.count = count;
-        ahead.settle(p);
+        ahead.settle(p, sh);
         struct Tile {
             bool there;
             uint32_t half;  // of a unit; whether it is the last one
@@ -568,7 +577,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_prompt_kernel(const __
             tile.half = SUMS ? (uint32_t)ahead.step : 0;
             tile.last = SUMS && ahead.last();
             load_raw<B>(p, page, ahead.w.head, ahead.w.held, ahead.tile(), thread, raw);
-            ahead.next(p);
+            ahead.next(p, sh);
             find();
         };
         find();
@@ -633,8 +642,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_prompt_kernel(const __
             constexpr uint32_t kIdesc = 1u << 4 | (uint32_t)(128 >> 4) << 24 | (uint32_t)(128 >> 3) << 17;  // fp32 sums of f16 products, both operands along k, 128 x 128
             const uint32_t stay_at = smem_u32(stay_smem), stream_at = smem_u32(stream_smem);
             uint32_t units = 0, streamed = 0, steps[2] = {0, 0};
-            for (int32_t unit_at = blockIdx.x; ok && unit_at < count; unit_at += gridDim.x) {
-                const WorkUnit w = load_unit(p.units[SUMS] + unit_at);
+            for (int32_t unit_at = blockIdx.x, k = 0; ok && unit_at < count; unit_at += gridDim.x, ++k) {
+                const WorkUnit w = load_unit<SUMS>(p, sh, k, unit_at);
                 if (w.step0 == w.step1) continue;
                 const uint32_t pair = units & 1;
                 const int halves = halves_of<SUMS>(w);
@@ -673,8 +682,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_prompt_kernel(const __
         } else {
             // ---- rows of q: images to shared memory -------------------------------------------------------------
             uint32_t units = 0, streamed = 0;
-            for (int32_t unit_at = blockIdx.x; ok && unit_at < count; unit_at += gridDim.x) {
-                const WorkUnit w = load_unit(p.units[SUMS] + unit_at);
+            for (int32_t unit_at = blockIdx.x, k = 0; ok && unit_at < count; unit_at += gridDim.x, ++k) {
+                const WorkUnit w = load_unit<SUMS>(p, sh, k, unit_at);
                 const auto copy = [&](uint8_t *to, int32_t tile, uint64_t *bar) { bulk_copy_g2s(to, p.images + image_of(p, w, tile) * TILE_BYTES, TILE_BYTES, bar); };
                 if (w.step0 == w.step1) continue;
                 if (!SUMS) {
