@@ -12,9 +12,9 @@
 // blocks take them in turn, and their warps go from one to the next without meeting:
 //   warps 0 - 15        the powers of two: two threads to each of the 256, for 64 of a step's 128 each; two accumulators of 128 x 128 for
 //                       every 128 of the 256 in TMEM
-//   warps 16 - 19       4-bit words from the cache to f16 keys in shared memory
-//   warp 20             issues the products
-//   warp 21             has the rows of q copied
+//   warps 16 - 23       4-bit words from the cache to f16 keys in shared memory
+//   warp 24             issues the products
+//   warp 25             has the rows of q copied
 // Sixteen warps, because one scheduler's two did not hide what a score goes through: 145 and 140 us for two chunks of 1024 rows instead of XXX.
 //
 // f16 holds a code times its scale exactly, relative to the largest scale of 128 tokens, down to 2^-28 of it; 16-bit rows of q are exact
@@ -28,7 +28,7 @@
 namespace lce {
 namespace {
 
-constexpr int kSoftmaxWarps = 16, kProducerWarps = 4, kIssuerWarp = kSoftmaxWarps + kProducerWarps, kCopyWarp = kIssuerWarp + 1;
+constexpr int kSoftmaxWarps = 16, kProducerWarps = 8, kIssuerWarp = kSoftmaxWarps + kProducerWarps, kCopyWarp = kIssuerWarp + 1;
 constexpr int kThreads = 32 * (kCopyWarp + 1);
 constexpr float kNothing = -3e38f;   // stands for the largest score where there is none
 constexpr float kRise = 16.0f;       // the score that powers of two are relative to is raised when one passes it by this much
@@ -295,11 +295,13 @@ __global__ void __launch_bounds__(kRowsThreads) kv_weights_rows_kernel(const __g
     }
 }
 
-// What a producer thread has of a tile before it decodes it.
+// What a producer thread has of a tile before it decodes it: eight tokens to a warp at a time, lane 8 q + t to channels 8 q .. of each block of
+// token t.
+constexpr int kKeyGroups = kTokens / 8 / kProducerWarps;
 template <int B>
 struct Raw {
-    uint32_t scales[B];  // of its token
-    uint32_t keys[4][B];
+    uint32_t scales[B];  // of its token, for the first 128 threads
+    uint32_t keys[kKeyGroups][B];
     uint32_t valid;
 };
 
@@ -317,12 +319,12 @@ __device__ __forceinline__ void load_raw(const PromptParams &p, int32_t page, in
 #pragma unroll
     for (int b = 0; b < B; ++b) r.scales[b] = 0;
     {
-        const uint32_t *const at = tile_at(thread >> 4);
-        if (at && tile * kTokens + thread < held) load_planes<B, 16>(at + 128 * B, thread & 15, r.scales);
+        const uint32_t *const at = tile_at(thread >> 4 & 7);
+        if (at && thread < kTokens && tile * kTokens + thread < held) load_planes<B, 16>(at + 128 * B, thread & 15, r.scales);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int half = i * 4 + warp;
+    for (int i = 0; i < kKeyGroups; ++i) {
+        const int half = i * kProducerWarps + warp;
         const uint32_t *const at = tile_at(half >> 1);
 #pragma unroll
         for (int b = 0; b < B; ++b) r.keys[i][b] = 0;
@@ -595,14 +597,15 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_prompt_kernel(const __
             }
             top = __reduce_max_sync(0xffffffffu, top);
             if (lane == 0) sh.largest[turn][producer] = top;
-            ok = producers_sync_and(ok);
+            ok = half_sync_and(1, ok);
             if (!ok) return false;
 #pragma unroll
-            for (int i = 0; i < kProducerWarps; ++i) top = max(top, sh.largest[turn][i]);
+            for (int i = 0; i < kTokens / 32; ++i) top = max(top, sh.largest[turn][i]);
             const int exponent = max((int)(top >> 23) - 127, -100);
             const float by = __uint_as_float((uint32_t)(127 + 11 - exponent) << 23);  // relative scales, below 2^12: 7 of them fit
 #pragma unroll
-            for (int b = 0; b < B; ++b) sh.scales[turn][thread][b] = __float2half_rn(__uint_as_float(key_scale(raw.scales[b])) * by);
+            for (int b = 0; b < B; ++b)
+                if (thread < kTokens) sh.scales[turn][thread][b] = __float2half_rn(__uint_as_float(key_scale(raw.scales[b])) * by);
             // second kernel: a unit's tile i is its half i, whether there is a second one or not
             const uint32_t slot = SUMS ? 2 * (units & 1) + tile.half : n & 1;
             uint8_t *const to_tile = (SUMS ? stay_smem : stream_smem) + slot * TILE_BYTES;
@@ -612,10 +615,10 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_prompt_kernel(const __
                 ok = wait_bounded(&sh.bars[BAR_STREAM_EMPTY + slot], (n >> 1 & 1) ^ 1);
             }
             if (thread == 0) sh.info[(SUMS ? 2 * units + tile.half : n) % kInfos] = TileInfo{__uint_as_float((uint32_t)(127 + exponent) << 23), raw.valid};
-            producers_sync();
+            asm volatile("bar.sync 1, 256;" ::: "memory");
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int eight = i * 4 + producer, token = eight * 8 + (lane & 7), quarter = lane >> 3;
+            for (int i = 0; i < kKeyGroups; ++i) {
+                const int eight = i * kProducerWarps + producer, token = eight * 8 + (lane & 7), quarter = lane >> 3;
                 uint8_t *const to = to_tile + eight * ROWS8 + quarter * 128 + (lane & 7) * 16;
                 const uint2 scales = *reinterpret_cast<const uint2 *>(sh.scales[turn][token]);
 #pragma unroll
