@@ -12,9 +12,11 @@
 // blocks take them in turn, and their warps go from one to the next without meeting:
 //   warps 0 - 15        the powers of two: two threads to each of the 256, for 64 of a step's 128 each; two accumulators of 128 x 128 for
 //                       every 128 of the 256 in TMEM
-//   warps 16 - 23       4-bit words from the cache to f16 keys in shared memory
+//   warps 16 - 23       4-bit words to f16 keys, both in shared memory
 //   warp 24             issues the products
 //   warp 25             has the rows of q copied
+//   warp 26             has the keys' words copied from the cache (loads of the warps that decode them do not stay in flight over the fence in
+//                       front of the products: 143 instead of XXX us)
 // Sixteen warps, because one scheduler's two did not hide what a score goes through: 145 and 140 us for two chunks of 1024 rows instead of XXX.
 //
 // f16 holds a code times its scale exactly, relative to the largest scale of 128 tokens, down to 2^-28 of it; 16-bit rows of q are exact
@@ -28,8 +30,8 @@
 namespace lce {
 namespace {
 
-constexpr int kSoftmaxWarps = 16, kProducerWarps = 8, kIssuerWarp = kSoftmaxWarps + kProducerWarps, kCopyWarp = kIssuerWarp + 1;
-constexpr int kThreads = 32 * (kCopyWarp + 1);
+constexpr int kSoftmaxWarps = 16, kProducerWarps = 8, kIssuerWarp = kSoftmaxWarps + kProducerWarps, kCopyWarp = kIssuerWarp + 1, kWordsWarp = kCopyWarp + 1;
+constexpr int kThreads = 32 * (kWordsWarp + 1);
 constexpr float kNothing = -3e38f;   // stands for the largest score where there is none
 constexpr float kRise = 16.0f;       // the score that powers of two are relative to is raised when one passes it by this much
 constexpr int kBlocks = 148;         // one to an SM
@@ -38,7 +40,7 @@ constexpr int kHeldUnits = 32;       // of a block, in shared memory
 constexpr int kInfos = 8;            // tiles of keys; the producers are less than four units, of two tiles, ahead of the softmax
 
 enum { BAR_STAY_FULL = 0, BAR_STAY_EMPTY = BAR_STAY_FULL + 2, BAR_STREAM_FULL = BAR_STAY_EMPTY + 2, BAR_STREAM_EMPTY = BAR_STREAM_FULL + 2,
-       BAR_S_FULL = BAR_STREAM_EMPTY + 2, BAR_S_EMPTY = BAR_S_FULL + 4, BAR_DONE = BAR_S_EMPTY + 4, BAR_COUNT };
+       BAR_WORDS_FULL = BAR_STREAM_EMPTY + 2, BAR_WORDS_EMPTY = BAR_WORDS_FULL + 2, BAR_S_FULL = BAR_WORDS_EMPTY + 2, BAR_S_EMPTY = BAR_S_FULL + 4, BAR_DONE = BAR_S_EMPTY + 4, BAR_COUNT };
 
 struct TileInfo {
     float unit;      // 2^e: scores count in it
@@ -57,7 +59,7 @@ struct alignas(16) WorkUnit {
 
 struct Shared {
     uint64_t bars[BAR_COUNT];
-    uint32_t tmem, largest[2][kProducerWarps];
+    uint32_t tmem, largest[2][kProducerWarps], valid[2];  // valid: of a tile's words, as in TileInfo
     TileInfo info[kInfos];
     alignas(16) __half scales[2][kTokens][4];         // relative to the tile's largest; [turn]
     alignas(16) float columns[2][2][kTokens / 2][4];  // [half][turn][pair]: two factors, two logarithms taken off
@@ -67,7 +69,9 @@ struct Shared {
 
 constexpr int kMiscBytes = 12288;
 static_assert(sizeof(Shared) <= kMiscBytes, "");
-constexpr size_t weights_smem(int blocks) { return kMiscBytes + 6 * (size_t)(kTokens * 64 * blocks); }
+// Words of 128 tokens: the keys of eight tiles of the cache, then their scales.
+__host__ __device__ constexpr int words_bytes(int blocks) { return kTokens / kKvTile * 320 * blocks; }
+constexpr size_t weights_smem(int blocks) { return kMiscBytes + 6 * (size_t)(kTokens * 64 * blocks) + 2 * words_bytes(blocks); }
 
 struct PromptParams : WeightsParams {
     WorkUnit *units[2];
@@ -295,40 +299,22 @@ __global__ void __launch_bounds__(kRowsThreads) kv_weights_rows_kernel(const __g
     }
 }
 
-// What a producer thread has of a tile before it decodes it: eight tokens to a warp at a time, lane 8 q + t to channels 8 q .. of each block of
-// token t.
+// Eight tokens to a producer warp at a time, lane 8 q + t to channels 8 q .. of each block of token t.
 constexpr int kKeyGroups = kTokens / 8 / kProducerWarps;
-template <int B>
-struct Raw {
-    uint32_t scales[B];  // of its token, for the first 128 threads
-    uint32_t keys[kKeyGroups][B];
-    uint32_t valid;
-};
 
-template <int B>
-__device__ __forceinline__ void load_raw(const PromptParams &p, int32_t page, int head, int held, int tile, int thread, Raw<B> &r)
+// The B words of a place (a lane's of 64 places, a token's of 16) in shared memory, plane by plane.
+template <int B, int ROWS>
+__device__ __forceinline__ void shared_planes(const uint32_t *base, int place, uint32_t (&w)[B])
 {
-    constexpr int TILE = kv_tile_words(B);
-    const int lane = thread & 31, warp = thread >> 5, tiles_per_page = p.g.page_size / kKvTile;
-    const int32_t place = page >= 0 && page < p.g.pages ? (page * p.g.heads + head) * tiles_per_page + (tile * 8 + lane) % tiles_per_page : -1;
-    r.valid = __ballot_sync(0xffffffffu, place >= 0);
-    const auto tile_at = [&](int t) -> const uint32_t * {
-        const int32_t at = __shfl_sync(0xffffffffu, place, t);
-        return at >= 0 ? p.cache + (int64_t)at * TILE : nullptr;
-    };
-#pragma unroll
-    for (int b = 0; b < B; ++b) r.scales[b] = 0;
-    {
-        const uint32_t *const at = tile_at(thread >> 4 & 7);
-        if (at && thread < kTokens && tile * kTokens + thread < held) load_planes<B, 16>(at + 128 * B, thread & 15, r.scales);
-    }
-#pragma unroll
-    for (int i = 0; i < kKeyGroups; ++i) {
-        const int half = i * kProducerWarps + warp;
-        const uint32_t *const at = tile_at(half >> 1);
-#pragma unroll
-        for (int b = 0; b < B; ++b) r.keys[i][b] = 0;
-        if (at) load_planes<B, 64>(at, (half & 1) * 32 + (lane & 7) * 4 + (lane >> 3), r.keys[i]);
+    if (B == 4) {
+        const uint4 v = reinterpret_cast<const uint4 *>(base)[place];
+        w[0] = v.x; w[B > 1 ? 1 : 0] = v.y; w[B > 2 ? 2 : 0] = v.z; w[B > 3 ? 3 : 0] = v.w;
+    } else {
+        if (B & 2) {
+            const uint2 v = reinterpret_cast<const uint2 *>(base)[place];
+            w[0] = v.x; w[B > 1 ? 1 : 0] = v.y;
+        }
+        if (B & 1) w[B - 1] = base[ROWS * (B - 1) + place];
     }
 }
 
@@ -352,6 +338,13 @@ template <bool SUMS>
 struct Tiles {
     WorkUnit w;
     int32_t k, unit, count, step;  // step: of the unit, or the half
+    __device__ __forceinline__ void begin(const PromptParams &p, const Shared &sh, int32_t units)
+    {
+        k = 0;
+        unit = blockIdx.x;
+        count = units;
+        settle(p, sh);
+    }
     __device__ __forceinline__ bool there() const { return unit < count; }
     __device__ __forceinline__ void settle(const PromptParams &p, const Shared &sh)  // at the first tile of a unit that has one
     {
@@ -383,6 +376,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_prompt_kernel(const __
     extern __shared__ __align__(1024) uint8_t smem[];
     Shared &sh = *reinterpret_cast<Shared *>(smem);
     uint8_t *const stay_smem = smem + kMiscBytes, *const stream_smem = stay_smem + 4 * TILE_BYTES;  // two pairs of tiles; two tiles
+    uint8_t *const words_smem = stream_smem + 2 * TILE_BYTES;
+    constexpr uint32_t WORDS_BYTES = words_bytes(B), SCALES_AT = kTokens / kKvTile * 256 * B;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -399,6 +394,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_prompt_kernel(const __
             mbar_init(&sh.bars[BAR_STAY_EMPTY + i], 1);
             mbar_init(&sh.bars[BAR_STREAM_FULL + i], SUMS ? 1 : 32 * kProducerWarps);
             mbar_init(&sh.bars[BAR_STREAM_EMPTY + i], 1);
+            mbar_init(&sh.bars[BAR_WORDS_FULL + i], 1);
+            mbar_init(&sh.bars[BAR_WORDS_EMPTY + i], 32 * kProducerWarps);
         }
         for (int i = 0; i < 4; ++i) {
             mbar_init(&sh.bars[BAR_S_FULL + i], 1);
@@ -559,85 +556,68 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_prompt_kernel(const __
     } else if (warp < kIssuerWarp) {
         // ---- keys: from 4 bits to f16 operands ------------------------------------------------------------
         const int thread = threadIdx.x - 32 * kSoftmaxWarps, producer = warp - kSoftmaxWarps;
-        Tiles<SUMS> ahead;  // the tile behind the one whose words are on their way
-        ahead.k = 0;
-        ahead.unit = blockIdx.x;
-        ahead.count = count;
-        ahead.settle(p, sh);
-        struct Tile {
-            bool there;
-            uint32_t half;  // of a unit; whether it is the last one
-            bool last;
-        };
-        Raw<B> even_raw, odd_raw;
-        Tile even{}, odd{};
-        int32_t page = -1;
-        const auto find = [&]() { page = ahead.there() ? find_page(p, p.page_table + (int64_t)ahead.w.seq * p.table_pages, ahead.w.held, ahead.tile(), lane) : -1; };
-        const auto load = [&](Raw<B> &raw, Tile &tile) {
-            tile.there = ahead.there();
-            if (!tile.there) return;
-            tile.half = SUMS ? (uint32_t)ahead.step : 0;
-            tile.last = SUMS && ahead.last();
-            load_raw<B>(p, page, ahead.w.head, ahead.w.held, ahead.tile(), thread, raw);
-            ahead.next(p, sh);
-            find();
-        };
-        find();
-        load(even_raw, even);
-        uint32_t n = 0, units = 0;
-        const auto produce = [&](const Raw<B> &raw, const Tile &tile, Raw<B> &next_raw, Tile &next) -> bool {
-            load(next_raw, next);
+        Tiles<SUMS> tile;
+        tile.begin(p, sh, count);
+        for (uint32_t n = 0, units = 0; tile.there(); ++n) {
+            const uint32_t turn = n & 1;
+            uint32_t scales[B], keys[kKeyGroups][B];
+            ok = wait_bounded(&sh.bars[BAR_WORDS_FULL + turn], n >> 1 & 1);
+            const uint32_t *const words = reinterpret_cast<const uint32_t *>(words_smem + turn * WORDS_BYTES);
+            const uint32_t valid = sh.valid[turn];
+            // a token that is none, or not in the pool, has keys of 0
+            shared_planes<B, 16>(words + SCALES_AT / 4 + (thread >> 4 & 7) * 16 * B, thread & 15, scales);
+            const bool there = (valid >> (thread >> 4 & 7) & 1) && tile.tile() * kTokens + (thread & 127) < tile.w.held;
+#pragma unroll
+            for (int b = 0; b < B; ++b) scales[b] = there ? key_scale(scales[b]) : 0;
+#pragma unroll
+            for (int i = 0; i < kKeyGroups; ++i) {
+                const int eight = i * kProducerWarps + producer;
+                shared_planes<B, 64>(words + (eight >> 1) * 64 * B, (eight & 1) * 32 + (lane & 7) * 4 + (lane >> 3), keys[i]);
+            }
+            mbar_arrive(&sh.bars[BAR_WORDS_EMPTY + turn]);
             // the largest scale of the tile (bits of bf16 numbers compare like integers; a NaN does not count)
-            const int turn = n & 1;
             uint32_t top = 0;
 #pragma unroll
-            for (int b = 0; b < B; ++b) {
-                const uint32_t s = key_scale(raw.scales[b]);
-                if (s < 0x7f800000u) top = max(top, s);
-            }
+            for (int b = 0; b < B; ++b)
+                if (scales[b] < 0x7f800000u) top = max(top, scales[b]);
             top = __reduce_max_sync(0xffffffffu, top);
             if (lane == 0) sh.largest[turn][producer] = top;
             ok = half_sync_and(1, ok);
-            if (!ok) return false;
+            if (!ok) break;
 #pragma unroll
             for (int i = 0; i < kTokens / 32; ++i) top = max(top, sh.largest[turn][i]);
             const int exponent = max((int)(top >> 23) - 127, -100);
             const float by = __uint_as_float((uint32_t)(127 + 11 - exponent) << 23);  // relative scales, below 2^12: 7 of them fit
 #pragma unroll
             for (int b = 0; b < B; ++b)
-                if (thread < kTokens) sh.scales[turn][thread][b] = __float2half_rn(__uint_as_float(key_scale(raw.scales[b])) * by);
+                if (thread < kTokens) sh.scales[turn][thread][b] = __float2half_rn(__uint_as_float(scales[b]) * by);
             // second kernel: a unit's tile i is its half i, whether there is a second one or not
-            const uint32_t slot = SUMS ? 2 * (units & 1) + tile.half : n & 1;
+            const uint32_t half = SUMS ? (uint32_t)tile.step : 0, slot = SUMS ? 2 * (units & 1) + half : n & 1;
             uint8_t *const to_tile = (SUMS ? stay_smem : stream_smem) + slot * TILE_BYTES;
             if (SUMS) {
-                if (units >= 2 && tile.half == 0) ok = wait_bounded(&sh.bars[BAR_STAY_EMPTY + (units & 1)], (units >> 1 & 1) ^ 1);
+                if (units >= 2 && half == 0) ok = wait_bounded(&sh.bars[BAR_STAY_EMPTY + (units & 1)], (units >> 1 & 1) ^ 1);
             } else if (n >= 2) {
                 ok = wait_bounded(&sh.bars[BAR_STREAM_EMPTY + slot], (n >> 1 & 1) ^ 1);
             }
-            if (thread == 0) sh.info[(SUMS ? 2 * units + tile.half : n) % kInfos] = TileInfo{__uint_as_float((uint32_t)(127 + exponent) << 23), raw.valid};
+            if (thread == 0) sh.info[(SUMS ? 2 * units + half : n) % kInfos] = TileInfo{__uint_as_float((uint32_t)(127 + exponent) << 23), valid};
             asm volatile("bar.sync 1, 256;" ::: "memory");
 #pragma unroll
             for (int i = 0; i < kKeyGroups; ++i) {
                 const int eight = i * kProducerWarps + producer, token = eight * 8 + (lane & 7), quarter = lane >> 3;
                 uint8_t *const to = to_tile + eight * ROWS8 + quarter * 128 + (lane & 7) * 16;
-                const uint2 scales = *reinterpret_cast<const uint2 *>(sh.scales[turn][token]);
+                const uint2 by_block = *reinterpret_cast<const uint2 *>(sh.scales[turn][token]);
 #pragma unroll
                 for (int b = 0; b < B; ++b)
-                    *reinterpret_cast<uint4 *>(to + b * 512) = decode(raw.keys[i][b], as_half2(__byte_perm(b & 2 ? scales.y : scales.x, 0, b & 1 ? 0x3232 : 0x1010)));
+                    *reinterpret_cast<uint4 *>(to + b * 512) = decode(keys[i][b], as_half2(__byte_perm(b & 2 ? by_block.y : by_block.x, 0, b & 1 ? 0x3232 : 0x1010)));
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             if (!SUMS) {
                 mbar_arrive(&sh.bars[BAR_STREAM_FULL + slot]);
-            } else if (tile.last) {
+            } else if (tile.last()) {
                 mbar_arrive(&sh.bars[BAR_STAY_FULL + (units & 1)]);
                 ++units;
             }
-            ++n;
-            return true;
-        };
-        while (even.there) {
-            if (!produce(even_raw, even, odd_raw, odd)) break;
-            if (!odd.there || !produce(odd_raw, odd, even_raw, even)) break;
+            tile.next(p, sh);
         }
     } else {
         if (warp == kIssuerWarp) {
@@ -682,6 +662,38 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_prompt_kernel(const __
             if (lane == 0) mma_commit(&sh.bars[BAR_DONE]);
             __syncwarp();
             if (!wait_bounded(&sh.bars[BAR_DONE], 0)) ok = false;
+        } else if (warp == kWordsWarp) {
+            // ---- the keys' words to shared memory: a lane to a tile of the cache -------------------------------
+            Tiles<SUMS> tile;
+            tile.begin(p, sh, count);
+            const int32_t tiles_per_page = p.g.page_size / kKvTile;
+            const auto find = [&]() { return tile.there() ? find_page(p, p.page_table + (int64_t)tile.w.seq * p.table_pages, tile.w.held, tile.tile(), lane) : -1; };
+            int32_t page = find();  // a tile ahead
+            uint32_t n = 0;
+            for (; tile.there(); ++n) {
+                const uint32_t slot = n & 1;
+                const int32_t place = page >= 0 && page < p.g.pages ? (page * p.g.heads + tile.w.head) * tiles_per_page + (tile.tile() * 8 + lane) % tiles_per_page : -1;
+                tile.next(p, sh);
+                page = find();
+                if (n >= 2) ok = warp_wait(&sh.bars[BAR_WORDS_EMPTY + slot], (n >> 1 & 1) ^ 1);
+                if (!ok) break;
+                const uint32_t valid = __ballot_sync(0xffffffffu, place >= 0);
+                uint64_t *const bar = &sh.bars[BAR_WORDS_FULL + slot];
+                if (lane == 0) {
+                    sh.valid[slot] = valid;
+                    mbar_expect_tx(bar, __popc(valid) * 320 * B);
+                }
+                __syncwarp();
+                if (place >= 0) {
+                    uint8_t *const to = words_smem + slot * WORDS_BYTES;
+                    const uint32_t *const from = p.cache + (int64_t)place * kv_tile_words(B);
+                    bulk_copy_g2s(to + lane * 256 * B, from, 256 * B, bar);
+                    bulk_copy_g2s(to + SCALES_AT + lane * 64 * B, from + 128 * B, 64 * B, bar);
+                }
+            }
+            // whatever happened: no copy is in flight when the block ends
+            for (uint32_t i = n < 2 ? 0 : n - 2; i < n; ++i)
+                if (!wait_bounded(&sh.bars[BAR_WORDS_FULL + (i & 1)], i >> 1 & 1)) ok = false;
         } else {
             // ---- rows of q: images to shared memory -------------------------------------------------------------
             uint32_t units = 0, streamed = 0;
