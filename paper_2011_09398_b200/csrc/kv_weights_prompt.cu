@@ -62,7 +62,7 @@ struct Shared {
     uint32_t tmem, largest[2][kProducerWarps], valid[2];  // valid: of a tile's words, as in TileInfo
     TileInfo info[kInfos];
     alignas(16) __half scales[2][kTokens][4];         // relative to the tile's largest; [turn]
-    alignas(16) float columns[2][2][kTokens / 2][4];  // [half][turn][pair]: two factors, two logarithms taken off
+    alignas(16) float columns[2][2][kTokens];         // [half][turn]: the logarithms of columns' sums, taken off
     float2 others[2][2][kTokens];                     // [half][turn]: what the second of two threads has at a unit's end
     WorkUnit units[kHeldUnits];                       // the block's first ones
 };
@@ -79,7 +79,8 @@ struct PromptParams : WeightsParams {
     uint8_t *images;      // [tile of 128 columns][kv head]: rows of q as f16, in the order in which they are an operand
     float *factors;       // [tile of columns][kv head][128]
     float2 *stats_units;  // [unit of the first kernel][256]: largest, sum
-    float2 *constants;    // [tile of columns][kv head][128]: factor, less the logarithm of the sum
+    float *tile_factors;  // [tile of columns][kv head]: the factor of all its rows that are finite
+    float *constants;     // [tile of columns][kv head][128]: less the logarithm of the sum
     float *parts;         // [unit of the second kernel of sequences whose columns are cut][256]
 };
 
@@ -245,6 +246,7 @@ __global__ void __launch_bounds__(kRowsThreads) kv_weights_rows_kernel(const __g
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     constexpr int ROWS8 = 512 * B;
+    __shared__ uint32_t largest[kRowsThreads / 32];
     if (blockIdx.y == p.g.heads) {
         for (int b = blockIdx.x; b < p.batch; b += gridDim.x) list_units(p, b);
         return;
@@ -274,8 +276,12 @@ __global__ void __launch_bounds__(kRowsThreads) kv_weights_rows_kernel(const __g
         magnitude = max(magnitude, __shfl_xor_sync(0xffffffffu, magnitude, 8));
         magnitude = max(magnitude, __shfl_xor_sync(0xffffffffu, magnitude, 16));
         const bool finite = magnitude < 0x7f800000u;
-        // times 2^k, so that the largest is in [2^14, 2^15); a scale below zero changes q's sign
-        const int k = 14 - (finite && magnitude > 0 ? ilogbf(__uint_as_float(magnitude)) : 0), k1 = k / 2, k2 = k - k1;
+        // all 128 rows times 2^k, so that the largest is in [2^14, 2^15); a scale below zero changes q's sign
+        const uint32_t of_warp = __reduce_max_sync(0xffffffffu, finite ? magnitude : 0);
+        if (lane == 0) largest[warp] = of_warp;
+        __syncthreads();
+        const uint32_t top = __reduce_max_sync(0xffffffffu, largest[lane % (kRowsThreads / 32)]);
+        const int k = 14 - (top > 0 ? ilogbf(__uint_as_float(top)) : 0), k1 = k / 2, k2 = k - k1;
         const float s1 = __uint_as_float((uint32_t)(127 + k1) << 23) * (p.scale < 0.0f ? -1.0f : 1.0f), s2 = __uint_as_float((uint32_t)(127 + k2) << 23);
 #pragma unroll
         for (int b = 0; b < B; ++b) {
@@ -286,9 +292,9 @@ __global__ void __launch_bounds__(kRowsThreads) kv_weights_rows_kernel(const __g
             *reinterpret_cast<uint4 *>(to + b * 512) = make_uint4(pack_half2(v[0], v[4]), pack_half2(v[1], v[5]), pack_half2(v[2], v[6]), pack_half2(v[3], v[7]));
         }
         const int kc = -11 - k, c1 = kc / 2, c2 = kc - c1;
-        if (quarter == 0)
-            p.factors[image * kTokens + in_tile] =
-                (finite ? fabsf(p.scale) : __uint_as_float(0x7fc00000u)) * __uint_as_float((uint32_t)(127 + c1) << 23) * __uint_as_float((uint32_t)(127 + c2) << 23);
+        const float factor = fabsf(p.scale) * __uint_as_float((uint32_t)(127 + c1) << 23) * __uint_as_float((uint32_t)(127 + c2) << 23);
+        if (quarter == 0) p.factors[image * kTokens + in_tile] = finite ? factor : __uint_as_float(0x7fc00000u);
+        if (threadIdx.x == 0) p.tile_factors[image] = factor;
     };
     if (p.type == LCE_TYPE_FLOAT16) {
         if (p.q_vectors) take_rows(__half(), std::true_type());
@@ -419,8 +425,15 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_prompt_kernel(const __
         const int half = warp >> 2 & 1, side = warp >> 3, in_tile = threadIdx.x & 127;
         const uint32_t s_at = tmem + ((uint32_t)(32 * (warp & 3)) << 16) + 256 * half + 64 * side;
         uint32_t steps = 0, units = 0, units_here = 0, tiles = 0;  // steps of this half; units that have some; units of this half; tiles of keys so far
-        float constant = 0.0f;  // a factor or a logarithm of a column of the next step
-        const float *const constants = reinterpret_cast<const float *>(p.constants) + 2 * in_tile + side;
+        // Brought ahead, also from one unit to the next: second kernel, of the next step's tile of columns its factor and what is taken off column
+        // in_tile; first kernel, the factor of the next unit's column.
+        float next_factor = 0.0f, next_constant = 0.0f;
+        bool ahead = false;
+        const auto bring = [&](const WorkUnit &w, int32_t step) {
+            const int64_t image = image_of(p, w, SUMS ? step : w.first / kTokens + half);
+            next_factor = SUMS ? p.tile_factors[image] : p.factors[image * kTokens + in_tile];
+            if (SUMS && !side) next_constant = p.constants[image * kTokens + in_tile];
+        };
         for (int32_t unit_at = blockIdx.x, k = 0; ok && unit_at < count; unit_at += gridDim.x, ++k) {
             const WorkUnit w = load_unit<SUMS>(p, sh, k, unit_at);
             if (half < halves_of<SUMS>(w)) {
@@ -428,16 +441,25 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_prompt_kernel(const __
                 int32_t lo, hi;  // what it sees: of the tokens, or of the columns
                 float factor = 0.0f, unit = 0.0f, top = kNothing;
                 uint64_t sum[2] = {};  // pairs of fp32 sums
-                const auto constant_of = [&](int32_t step) { return step < w.step1 ? constants[image_of(p, w, step) * (2 * kTokens)] : 0.0f; };
+                const bool some = w.step0 < w.step1;
                 if (SUMS) {
                     columns_of(p, w.length, w.rows, own, own + 1, &lo, &hi);
-                    constant = constant_of(w.step0);
                 } else {
                     Unit u{};
                     u.length = w.length;
                     u.rows = w.rows;
                     column_range(p, u, own, &lo, &hi);
-                    factor = p.factors[image_of(p, w, own / kTokens) * kTokens + in_tile];
+                }
+                if (some) {
+                    if (!ahead) bring(w, w.step0);
+                    factor = next_factor;
+                    // the unit behind: if it is one without this half, or without steps, nobody uses what is brought for it
+                    ahead = k + 1 < kHeldUnits && unit_at + (int32_t)gridDim.x < count;
+                    if (!SUMS && ahead) {
+                        const WorkUnit &behind = sh.units[k + 1];
+                        ahead = behind.step0 < behind.step1 && half < halves_of<SUMS>(behind);
+                        if (ahead) bring(behind, 0);
+                    }
                 }
                 for (int32_t step = w.step0; ok && step < w.step1; ++step, ++steps) {
                     const uint32_t buffer = steps & 1;
@@ -456,9 +478,16 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_prompt_kernel(const __
                         }
                     }
                     if (SUMS) {
-                        // every thread brings one constant of a column; the buffer before last is read by nobody any more
-                        sh.columns[half][buffer][in_tile >> 1][2 * side + (in_tile & 1)] = side ? constant : constant * unit;
-                        constant = constant_of(step + 1);
+                        // the buffer before last is read by nobody any more
+                        if (!side) sh.columns[half][buffer][in_tile] = next_constant;
+                        factor = next_factor;
+                        if (step + 1 < w.step1) {
+                            bring(w, step + 1);
+                        } else if (ahead) {
+                            const WorkUnit &behind = sh.units[k + 1];
+                            ahead = behind.step0 < behind.step1 && half < halves_of<SUMS>(behind);
+                            if (ahead) bring(behind, behind.step0);
+                        }
                         ok = half_sync_and(2 + half, ok);  // all eight warps leave together
                         if (!ok) break;
                     }
@@ -466,7 +495,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_prompt_kernel(const __
                     const float f = factor * unit;
                     // 32 scores of the 64
                     const auto take = [&](const uint32_t (&r)[32], int c, uint32_t seen, auto masked) {
-                        uint64_t f2 = pair_of(f, f), plus = 0;
+                        const uint64_t f2 = pair_of(f, f);
+                        uint64_t plus = 0;
                         if (!SUMS) {
                             const auto score = [&](int i) { return decltype(masked)::value && !(seen >> i & 1) ? -INFINITY : __uint_as_float(r[i]); };
                             float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
@@ -484,11 +514,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_prompt_kernel(const __
                         }
 #pragma unroll
                         for (int i = 0; i < 32; i += 2) {
-                            if (SUMS) {
-                                const ulonglong2 both = *reinterpret_cast<const ulonglong2 *>(sh.columns[half][buffer][32 * side + 16 * c + (i >> 1)]);
-                                f2 = both.x;
-                                plus = both.y;
-                            }
+                            if (SUMS) plus = *reinterpret_cast<const uint64_t *>(&sh.columns[half][buffer][64 * side + 32 * c + i]);
                             float x, y;
                             of_pair(fma_pair(pair_of(__uint_as_float(r[i]), __uint_as_float(r[i + 1])), f2, plus), x, y);
                             if (decltype(masked)::value) {  // not 0, or what a column that is not finite has, times minus infinity
@@ -547,6 +573,8 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_prompt_kernel(const __
                     }
                 }
                 ++units_here;
+            } else {
+                ahead = false;
             }
             if (w.step1 > w.step0) {
                 ++units;
@@ -776,7 +804,7 @@ __global__ void __launch_bounds__(kJoining * kTokens) kv_weights_columns_kernel(
     for (int i = 1; i < kJoining; ++i) add(sum, parts[i][in_tile]);
     const int64_t at = ((int64_t)blockIdx.x * p.g.heads + head) * kTokens + in_tile;
     // nothing of a column that is none, or sees nothing
-    p.constants[at] = sum.y == 0.0f ? make_float2(0.0f, -INFINITY) : make_float2(p.factors[at], -(sum.x + log2f(sum.y)));
+    p.constants[at] = sum.y == 0.0f ? -INFINITY : -(sum.x + log2f(sum.y));
 }
 
 // The chunks' weights of a token added up, always in the same order; a block to 256 tokens at a time.
@@ -840,7 +868,7 @@ size_t kv_weights_prompt_bytes(const WeightsParams &p)
 {
     const Bounds most = bounds(p);
     const int64_t columns = most.tiles * p.g.heads * kTokens;
-    return (size_t)(rounded(most.units * sizeof(WorkUnit)) + rounded(most.second_units * sizeof(WorkUnit)) + rounded(8) + rounded(columns * 64 * p.g.blocks) + rounded(columns * 4) + rounded(columns * 8) + rounded(most.units * 256 * 8) + rounded(most.parts * 256 * 4));
+    return (size_t)(rounded(most.units * sizeof(WorkUnit)) + rounded(most.second_units * sizeof(WorkUnit)) + rounded(8) + rounded(columns * 64 * p.g.blocks) + rounded(columns * 4) + rounded(columns / kTokens * 4) + rounded(columns * 4) + rounded(most.units * 256 * 8) + rounded(most.parts * 256 * 4));
 }
 
 lce_status launch_kv_weights_prompt(const WeightsParams &params, void *workspace, cudaStream_t s)
@@ -863,7 +891,8 @@ lce_status launch_kv_weights_prompt(const WeightsParams &params, void *workspace
     p.unit_counts = reinterpret_cast<int32_t *>(take(8));
     p.images = reinterpret_cast<uint8_t *>(take(columns * 64 * p.g.blocks));
     p.factors = reinterpret_cast<float *>(take(columns * 4));
-    p.constants = reinterpret_cast<float2 *>(take(columns * 8));
+    p.tile_factors = reinterpret_cast<float *>(take(columns / kTokens * 4));
+    p.constants = reinterpret_cast<float *>(take(columns * 4));
     p.stats_units = reinterpret_cast<float2 *>(take(most.units * 256 * 8));
     p.parts = reinterpret_cast<float *>(take(most.parts * 256 * 4));
     switch (p.g.blocks) {
