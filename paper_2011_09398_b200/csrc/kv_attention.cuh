@@ -194,10 +194,6 @@ __device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t mask, uint32_t w
 }
 // Bytes exchanged in either half.
 __device__ __forceinline__ uint32_t swap_bytes(uint32_t w) { return __byte_perm(w, 0, 0x2301); }
-// Lets the join, which this call launches behind, take its place while this kernel runs.  It waits for all of it, and nothing
-// that a caller launches can start before the join is done.
-__device__ __forceinline__ void release_join() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-
 // Prompts: kv_prompt.cu.  16-bit rows of up to 128 channels; `units` column tiles of kPromptColumns.
 constexpr int kPromptColumns = 256;
 lce_status launch_kv_prompt(const AttnParams &p, cudaStream_t s);

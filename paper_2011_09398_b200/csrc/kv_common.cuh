@@ -73,6 +73,10 @@ __host__ __device__ __forceinline__ int kv_scale_word(int blocks, int token, int
     return 128 * blocks + 16 * first + token * width + (b - first);
 }
 
+// Lets the kernel that the same call launches behind this one (the join of pieces, the next step) take its place while this one runs.  It waits
+// for all of it, and nothing that a caller launches can start before that one is done.
+__device__ __forceinline__ void release_join() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // --- clusters of blocks ---------------------------------------------------------------------------
 
 __device__ __forceinline__ void cluster_sync()

@@ -68,7 +68,7 @@ __global__ void __launch_bounds__(kThreads) kv_evict_select_kernel(const __grid_
     const int row = blockIdx.x / p.cluster, rank = blockIdx.x - row * p.cluster, seq = row / p.g.heads, head = row - seq * p.g.heads;
     for (int i = threadIdx.x; i < kDigits * kBins / 4; i += kThreads) reinterpret_cast<uint4 *>(&sh.bins[0][0])[i] = make_uint4(0, 0, 0, 0);
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the moving takes its place; it waits for all of this kernel
+    release_join();
     const int32_t length = max(__ldg(p.lengths + seq), 0), held = min(length, p.table_tokens);
     const int32_t *const table = p.page_table + (int64_t)seq * p.table_pages;
     const float *const scores = p.scores + seq * p.scores_seq + head * p.scores_head;

@@ -228,7 +228,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(B, NT, SPLIT)) kv_weig
     extern __shared__ __align__(16) uint32_t smem[];
     __shared__ float tops[kWarps][COLUMNS], sums[kWarps][COLUMNS];
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the second kernel takes its place; it waits for all of this one
+    release_join();
     Piece piece;
     if (!find_piece(p, blockIdx.x, &piece)) return;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, head = blockIdx.y;

@@ -244,7 +244,7 @@ template <int B>
 __global__ void __launch_bounds__(kRowsThreads) kv_weights_rows_kernel(const __grid_constant__ PromptParams p)
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    release_join();
     constexpr int ROWS8 = 512 * B;
     __shared__ uint32_t largest[kRowsThreads / 32];
     if (blockIdx.y == p.g.heads) {
@@ -386,7 +386,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_prompt_kernel(const __
     constexpr uint32_t WORDS_BYTES = words_bytes(B), SCALES_AT = kTokens / kKvTile * 256 * B;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    release_join();
     const int32_t count = __ldg(p.unit_counts + SUMS);
     if ((int)blockIdx.x >= count) return;
     for (int i = threadIdx.x; i < 3 * kHeldUnits; i += kThreads) {
