@@ -1,8 +1,8 @@
 // Eviction from the 4-bit cache: which tokens of a head stay, and their rows moved to pages of their own.
 //
 // Choosing: a cluster of up to eight blocks to a (sequence, head).  Scores become whole numbers that compare alike, and the budget-th largest is
-// found from the top in three digits: every block counts its own tokens' digits in shared memory, and all read all blocks' counts where
-// they are.  Then each warp counts what it keeps of its own run of tokens, and from the counts in front of it knows where that goes: the
+// found from the top in three digits: every block counts its own tokens' digits in shared memory, adds a share of the bins up over all blocks
+// where they are, and reads the others' shares.  Then each warp counts what it keeps of its own run of tokens, and from the counts in front of it knows where that goes: the
 // order of the tokens stays, and ties fall to the earlier ones.
 //
 // Moving: words go from place to place as they are, in vectors, keys and scales token by token, values by the halves of a pair's word.
@@ -15,7 +15,8 @@
 namespace lce {
 namespace {
 
-constexpr int kThreads = 1024, kWarps = kThreads / 32;
+constexpr int kMostWarps = 32;
+constexpr int kMostCluster = 8;      // blocks to a row (sixteen: 32 us instead of 26 for 131072 tokens of eight heads)
 constexpr int kBins = 2048, kDigits = 3;
 constexpr int kClusterTokens = 2048; // tokens that a block more is worth
 
@@ -33,6 +34,12 @@ struct EvictParams {
     float *kept_scores;
 };
 
+__device__ __forceinline__ uint32_t remote1(const void *p, int rank)
+{
+    uint32_t v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(remote_place(p, rank)) : "memory");
+    return v;
+}
 __device__ __forceinline__ uint2 remote2(const void *p, int rank)
 {
     uint2 v;
@@ -52,17 +59,19 @@ __device__ __forceinline__ uint32_t key_of(const EvictParams &p, int32_t page, f
 
 struct alignas(16) SelectShared {
     uint32_t bins[kDigits][kBins];
-    uint32_t warp_sums[kWarps];
-    uint2 warp_counts[kWarps];
+    uint32_t sums[kBins / 2];     // of the block's share of the bins, where there are several blocks
+    uint32_t warp_sums[kMostWarps];
+    uint2 warp_counts[kMostWarps];
     uint2 counts;                 // of the block: tokens above the threshold, on it
     uint32_t digit, left, whole;
 };
 
 // KEYS of a thread, the warp's run of tokens 32 at a time, in registers; 0: any number, made again from the scores wherever they are
 // looked at.
-template <int KEYS>
-__global__ void __launch_bounds__(kThreads) kv_evict_select_kernel(const __grid_constant__ EvictParams p)
+template <int KEYS, int THREADS>
+__global__ void __launch_bounds__(THREADS) kv_evict_select_kernel(const __grid_constant__ EvictParams p)
 {
+    constexpr int kThreads = THREADS, kWarps = THREADS / 32, BINS = kBins / THREADS;  // bins of a thread
     __shared__ SelectShared sh;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int row = blockIdx.x / p.cluster, rank = blockIdx.x - row * p.cluster, seq = row / p.g.heads, head = row - seq * p.g.heads;
@@ -77,6 +86,8 @@ __global__ void __launch_bounds__(kThreads) kv_evict_select_kernel(const __grid_
     const int32_t run = ((end - begin + kWarps - 1) / kWarps + 31) / 32 * 32;
     const int32_t run_begin = min(begin + (int64_t)warp * run, (int64_t)end), run_end = min(run_begin + (int64_t)run, (int64_t)end);
     uint32_t keys[KEYS > 0 ? KEYS : 1];
+#pragma unroll
+    for (int i = 0; i < KEYS; ++i) keys[i] = 0;
     if (KEYS > 0 && run_begin < run_end) {
         // all loads at once; behind the run its last token again
         float score[KEYS > 0 ? KEYS : 1];
@@ -94,8 +105,7 @@ __global__ void __launch_bounds__(kThreads) kv_evict_select_kernel(const __grid_
     const auto each_key = [&](auto body) {
         if (KEYS > 0) {
 #pragma unroll
-            for (int i = 0; i < KEYS; ++i)
-                if (run_begin + 32 * i < run_end) body(run_begin + 32 * i, keys[i]);
+            for (int i = 0; i < KEYS; ++i) body(run_begin + 32 * i, keys[i]);
         } else {
 #pragma unroll 4
             for (int32_t t0 = run_begin; t0 < run_end; t0 += 32) {
@@ -126,16 +136,30 @@ __global__ void __launch_bounds__(kThreads) kv_evict_select_kernel(const __grid_
             }
         });
         cluster_sync();
-        // two bins a thread, the highest first, over all blocks
-        const int bin0 = kBins - 2 - 2 * (int)threadIdx.x;
-        uint32_t n[2] = {};
+        // a thread's bins, the highest first, over all blocks: each block adds its share of them up for the others, which read the sums (all blocks'
+        // counts read by all of them: 30 us instead of 26 for 131072 tokens of eight heads)
+        const int bin0 = kBins - BINS - BINS * (int)threadIdx.x;
+        uint32_t n[BINS], mine = 0;
+        if (p.cluster > 1) {
+            const int each = kBins / p.cluster;
+            for (int i = threadIdx.x; i < each; i += kThreads) {
+                uint32_t sum = 0;
 #pragma unroll 8
-        for (int r = 0; r < p.cluster; ++r) {
-            const uint2 v = remote2(&bins[bin0], r);
-            n[0] += v.y;
-            n[1] += v.x;
+                for (int r = 0; r < p.cluster; ++r) sum += remote1(&bins[rank * each + i], r);
+                sh.sums[i] = sum;
+            }
+            cluster_sync();
+#pragma unroll
+            for (int i = 0; i < BINS; ++i) {
+                const int bin = bin0 + BINS - 1 - i;
+                n[i] = remote1(&sh.sums[bin % each], bin / each);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < BINS; ++i) n[i] = bins[bin0 + BINS - 1 - i];
         }
-        const uint32_t mine = n[0] + n[1];
+#pragma unroll
+        for (int i = 0; i < BINS; ++i) mine += n[i];
         uint32_t upto = mine;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
@@ -144,15 +168,23 @@ __global__ void __launch_bounds__(kThreads) kv_evict_select_kernel(const __grid_
         }
         if (lane == 31) sh.warp_sums[warp] = upto;
         __syncthreads();
-        const uint32_t of_lane = sh.warp_sums[lane], total = __reduce_add_sync(0xffffffffu, of_lane);
+        const uint32_t of_lane = lane < kWarps ? sh.warp_sums[lane] : 0, total = __reduce_add_sync(0xffffffffu, of_lane);
         uint32_t before = upto - mine + __reduce_add_sync(0xffffffffu, lane < warp ? of_lane : 0);
         if (digit == 0 && total <= left) break;  // all that there are stay
         if (before < left && before + mine >= left) {
-            const int i = before + n[0] < left;
-            if (i) before += n[0];
-            sh.digit = bin0 + 1 - i;
+            int i = 0;
+#pragma unroll
+            for (int k = 1; k < BINS; ++k)
+                if (i == k - 1 && before + n[k - 1] < left) {
+                    before += n[k - 1];
+                    i = k;
+                }
+            uint32_t there = n[0];
+#pragma unroll
+            for (int k = 1; k < BINS; ++k) there = i == k ? n[k] : there;
+            sh.digit = bin0 + BINS - 1 - i;
             sh.left = left - before;
-            sh.whole = before + n[i] == left;
+            sh.whole = before + there == left;
         }
         __syncthreads();
         prefix = prefix << bits | sh.digit;
@@ -174,7 +206,7 @@ __global__ void __launch_bounds__(kThreads) kv_evict_select_kernel(const __grid_
     mine.y = __reduce_add_sync(0xffffffffu, mine.y);
     if (lane == 0) sh.warp_counts[warp] = mine;
     __syncthreads();
-    const uint2 of_lane = sh.warp_counts[lane];
+    const uint2 of_lane = lane < kWarps ? sh.warp_counts[lane] : make_uint2(0, 0);
     uint2 before = make_uint2(__reduce_add_sync(0xffffffffu, lane < warp ? of_lane.x : 0), __reduce_add_sync(0xffffffffu, lane < warp ? of_lane.y : 0));
     const uint2 all = make_uint2(__reduce_add_sync(0xffffffffu, of_lane.x), __reduce_add_sync(0xffffffffu, of_lane.y));
     if (threadIdx.x == 0) sh.counts = all;
@@ -267,10 +299,9 @@ __global__ void __launch_bounds__(kMoveThreads, 4) kv_evict_move_kernel(const __
         const int32_t from = j < p.budget ? p.kept[((int64_t)seq * p.g.heads + head) * p.budget + j] : -1;
         const int32_t in_kept = p.by_page(j), target = j < p.budget ? __ldg(p.kept_table + (int64_t)seq * p.kept_pages + in_kept) : -1;
         Source s{-1, 0};
-        if (from >= 0) {
+        if (from >= 0 && from < p.table_tokens) {
             const int32_t in_table = p.by_page(from), page = __ldg(p.page_table + (int64_t)seq * p.table_pages + in_table), in_page = from - in_table * p.g.page_size;
-            s.tile = tile_on(page, in_page);  // of the pool: what is kept is
-            s.token = in_page % kKvTile;
+            if ((uint32_t)page < (uint32_t)p.g.pages) s = Source{tile_on(page, in_page), in_page % kKvTile};
         }
         sources[threadIdx.x] = s;
         if (threadIdx.x % kKvTile == 0) targets[threadIdx.x / kKvTile] = (uint32_t)target < (uint32_t)p.g.pages ? tile_on(target, j - in_kept * p.g.page_size) : -1;
@@ -351,14 +382,13 @@ lce_status launch_move(const EvictParams &p, cudaStream_t s)
     return tiles * p.g.heads * p.batch > 148 * 16 ? go(kv_evict_move_kernel<16>, 16) : go(kv_evict_move_kernel<4>, 4);
 }
 
+template <int KEYS, int THREADS>
 lce_status launch_select(const EvictParams &p, cudaStream_t s)
 {
-    const int64_t share = ((int64_t)p.table_tokens + p.cluster - 1) / p.cluster;
-    const auto kernel = share <= kThreads ? kv_evict_select_kernel<1> : share <= 4 * kThreads ? kv_evict_select_kernel<4>
-                      : share <= 16 * kThreads ? kv_evict_select_kernel<16> : kv_evict_select_kernel<0>;
+    const auto kernel = kv_evict_select_kernel<KEYS, THREADS>;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(p.batch * p.g.heads * p.cluster), 1, 1);
-    cfg.blockDim = dim3(kThreads, 1, 1);
+    cfg.blockDim = dim3(THREADS, 1, 1);
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -373,6 +403,18 @@ lce_status launch_select(const EvictParams &p, cudaStream_t s)
         return LCE_ERR_CUDA;
     }
     return LCE_OK;
+}
+
+lce_status launch_select(const EvictParams &p, cudaStream_t s)
+{
+    const int64_t share = ((int64_t)p.table_tokens + p.cluster - 1) / p.cluster;
+    if (share <= 1024) return launch_select<1, 1024>(p, s);
+    if (share <= 4 * 1024) return launch_select<4, 1024>(p, s);
+    // half the threads where there are rows for two blocks to an SM
+    if (share <= 16 * 512 && (int64_t)p.batch * p.g.heads * p.cluster > 148) return launch_select<16, 512>(p, s);
+    if (share <= 8 * 1024) return launch_select<8, 1024>(p, s);
+    if (share <= 16 * 1024) return launch_select<16, 1024>(p, s);
+    return launch_select<0, 1024>(p, s);
 }
 
 bool stride_ok(int64_t s) { return s >= 0 && s < (1ll << 40); }
@@ -394,7 +436,7 @@ extern "C" lce_status lce_kv_evict(const lce_kv_evict_desc *desc, void *cache, c
     for (const int64_t s : {d.scores_seq_stride, d.scores_head_stride, d.kept_scores_seq_stride, d.kept_scores_head_stride})
         if (!stride_ok(s)) return LCE_ERR_INVALID_ARG;
     if ((int64_t)d.table_pages * d.cache.page_size >= (1ll << 30) || (int64_t)d.kept_pages * d.cache.page_size >= (1ll << 30) || d.batch > 65535 ||
-        (int64_t)d.batch * d.cache.kv_heads * 8 >= (1ll << 31) || (int64_t)p.g.slots / kKvTile * p.g.heads >= (1ll << 31))
+        (int64_t)d.batch * d.cache.kv_heads * kMostCluster >= (1ll << 31) || (int64_t)p.g.slots / kKvTile * p.g.heads >= (1ll << 31))
         return LCE_ERR_UNSUPPORTED;
     if (!cache || !page_table || !lengths || !scores || !kept_table || !kept || !kept_lengths) return LCE_ERR_INVALID_ARG;
     if (!aligned(cache, 16) || !aligned(page_table, 4) || !aligned(lengths, 4) || !aligned(scores, 4) || !aligned(kept_table, 4) || !aligned(kept, 4) ||
@@ -411,7 +453,7 @@ extern "C" lce_status lce_kv_evict(const lce_kv_evict_desc *desc, void *cache, c
     p.scores = scores; p.kept = kept; p.kept_lengths = kept_lengths; p.kept_scores = kept_scores;
     // blocks to a row, as long as the GPU has places for them
     p.cluster = 1;
-    while (p.cluster < 8 && p.table_tokens > kClusterTokens * p.cluster && (int64_t)p.batch * p.g.heads * p.cluster * 2 <= 148 * 2) p.cluster *= 2;
+    while (p.cluster < kMostCluster && p.table_tokens > kClusterTokens * p.cluster && (int64_t)p.batch * p.g.heads * p.cluster * 2 <= 148 * 2) p.cluster *= 2;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const lce_status chosen = launch_select(p, s);
     return chosen != LCE_OK ? chosen : launch_move(p, s);

@@ -538,13 +538,15 @@ lce_status make_params(const lce_kv_attention_weights_desc *d, WeightsParams *p,
     // Many rows go to the tensor cores' kernels.
     p->prompt = p->g.blocks <= 4 && d->type != LCE_TYPE_FLOAT32 && p->tokens * p->group > p->batch * (int64_t)kFewColumns &&
                 p->g.heads < 65535 && (double)p->g.heads * p->batch * (p->table_tokens / 256 + 1) < kMostUnits;
-    // As many pieces as the GPU has places for; fewer where there are so many columns that their sums would take much room.
-    const int64_t columns = std::max<int64_t>(p->tokens * d->heads, 1);
-    p->target = (int32_t)std::max<int64_t>(1, std::min<int64_t>((148 * kBlocksPerSm + p->g.heads - 1) / p->g.heads, kMostStats / 8 / columns));
-    const int64_t tiles = (p->table_tokens + kKvTile - 1) / kKvTile, units = p->batch + std::max<int64_t>(p->target, (p->batch * tiles + kMostTiles - 1) / kMostTiles);
-    if (units >= (1ll << 31)) return LCE_ERR_UNSUPPORTED;
-    p->units = (int32_t)units;
+    // As many pieces as the GPU has places for, as a sequence has one more than its share (48 of 1 - 8192 tokens, 8 heads: 72 us, with a
+    // piece for each place whatever the sequences 77, with two 72; 16 of up to 1500, 12 heads: 14.8, 19.3 and 24.2), but for many sequences half of
+    // them at least; fewer where there are so many columns that their sums would take much room.
+    const int64_t columns = std::max<int64_t>(p->tokens * d->heads, 1), places = 148 * kBlocksPerSm / p->g.heads;
+    p->target = (int32_t)std::max<int64_t>(1, std::min<int64_t>(std::max<int64_t>(places - p->batch, places / 2), kMostStats / 8 / columns));
+    const int64_t tiles = (p->table_tokens + kKvTile - 1) / kKvTile;
+    const int64_t units = p->batch * ((tiles + kLeastTiles - 1) / kLeastTiles);
     p->pieces = (int32_t)std::min<int64_t>(tiles, std::max<int64_t>(p->target, (tiles + kMostTiles - 1) / kMostTiles) + 1);
+    p->units = (int32_t)std::min<int64_t>(units, p->batch + std::max<int64_t>(p->target, (p->batch * tiles + kMostTiles - 1) / kMostTiles));
     // what sequences as long as the table would leave
     p->scores_head = (p->tokens * p->group + p->batch) * tiles * kKvTile;
     return LCE_OK;
