@@ -6,7 +6,11 @@
 // order of the tokens stays, and ties fall to the earlier ones.
 //
 // Moving: words go from place to place as they are, in vectors, keys and scales token by token, values by the halves of a pair's word.
-// Sixteen kept tokens of a head make a tile, whose words a thread each puts together; where they come from is only known token by token.
+// Where they come from is only known token by token, so that is looked up once, a thread to a token, for up to sixteen tiles.
+//
+// Measured: 131072 tokens of 8 heads of 128 channels cut to 32768: choosing 25 us (64 blocks, a chain of counts and cluster barriers for each digit), moving 22
+// (38 MB of rows read and written, 12 at the copy rate; values lie in pairs of tokens, so that a quarter that stays touches most sectors: 105 MB are
+// read); 24 sequences of up to 8192 tokens cut to 2048, 64 channels: 19 and 17 us.
 #include "kv_common.cuh"
 
 #include <algorithm>

@@ -10,6 +10,10 @@
 // Keys are codes times a block's scale.  The codes c = n - 8 are exact f16 operands (1024 + n by one AND-OR, less 1032 by a packed
 // multiply-add), the scale multiplies a block's finished sums in fp32; 16-bit rows of q are one f16 number times a power of two of the row,
 // fp32 rows two of them.
+//
+// Measured (both kernels): 131072 tokens of 8 heads of 128 channels and 64 columns in all 39 us (84 MB of keys: 13 at the copy rate), 48 sequences
+// of 1 - 8192 tokens 72 us, 777 tokens 7.5 us.  A warp of the first kernel spends 255 instructions on a tile of 16 tokens and 8 columns, of them 8 matrix
+// products and 69 between the 4-bit words and their operands, with the issue slots 64 % busy at four warps a scheduler (127 registers).
 #include "kv_mma.cuh"
 #include "kv_weights.cuh"
 
@@ -31,7 +35,6 @@ __host__ __device__ constexpr int blocks_per_sm(int blocks, int nt, bool split) 
 constexpr float kNothing = -3e38f;          // stands for the largest score where there is none
 constexpr float kRise = 16.0f;              // the score that powers of two are relative to is raised when one passes it by this much
 constexpr int64_t kMostScores = 256 << 20;  // bytes of workspace that scores may take
-constexpr int kFewColumns = 32;             // of a sequence, on average
 constexpr double kMostUnits = 1 << 21;      // (256 tokens, key head) that their list has room for
 constexpr int64_t kMostStats = 64 << 20;
 
@@ -233,7 +236,7 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(B, NT, SPLIT)) kv_weig
     if (!find_piece(p, blockIdx.x, &piece)) return;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, head = blockIdx.y;
     const int64_t stride = scores_stride(piece.columns);
-    for (piece.u.column0 = 0; piece.u.column0 < piece.columns; piece.u.column0 += COLUMNS) {
+    for (piece.u.column0 = blockIdx.z * COLUMNS; piece.u.column0 < piece.columns; piece.u.column0 += gridDim.z * COLUMNS) {
         const View v = view(p, piece, COLUMNS);
         Columns<B, NT, SPLIT> c;
         c.load(p, piece.u, head);
@@ -348,21 +351,23 @@ __device__ __forceinline__ void column_totals(const WeightsParams &p, const Piec
     }
 }
 
-// Scores that were kept: a thread to a token, kTogether at a time.
+// Scores that were kept: LANES threads to a token (one for few columns, eight for many), kTogether tokens at a time.
 constexpr int kKeptThreads = 256, kTogether = 4, kKeptColumns = 128;
 
+template <int LANES>
 __global__ void __launch_bounds__(kKeptThreads, 4) kv_weights_kept_kernel(const __grid_constant__ WeightsParams p)
 {
     __shared__ alignas(16) float2 totals[kKeptColumns];
+    __shared__ int2 ranges[kKeptColumns];  // tokens that a column sees: the others' places may never have been written
     Piece piece;
     // the lengths are what the kernel in front read: nothing has written them since
     const bool found = find_piece(p, blockIdx.x, &piece);
     asm volatile("griddepcontrol.wait;" ::: "memory");  // every block: what comes behind this kernel relies on the one in front, too
     if (!found) return;
-    const int head = blockIdx.y;
+    const int head = blockIdx.y, sub = threadIdx.x % LANES;
     const int64_t stride = scores_stride(piece.columns);
     const int32_t first = piece.u.tile0 * kKvTile, last = min(piece.u.tile1 * kKvTile, tokens_held(p, piece.u.length));
-    constexpr int32_t kStep = kKeptThreads * kTogether;
+    constexpr int32_t kOne = kKeptThreads / LANES, kStep = kOne * kTogether;
     const float *const scores = scores_at(p, piece, head, 0);
     // whole blocks go round together: the columns' totals are theirs
     for (int32_t t0 = first; t0 < last; t0 += kStep) {
@@ -372,22 +377,24 @@ __global__ void __launch_bounds__(kKeptThreads, 4) kv_weights_kept_kernel(const 
             if (piece.columns > kKeptColumns || t0 == first) {
                 __syncthreads();
                 column_totals(p, piece, head, count, totals);
+                if ((int)threadIdx.x < count) column_range(p, piece.u, piece.u.column0 + threadIdx.x, &ranges[threadIdx.x].x, &ranges[threadIdx.x].y);
                 __syncthreads();
             }
             // tokens whose scores are there: those that some column sees; all of these columns see the step's
             const View v = view(p, piece, kKeptColumns);
             const bool all = t0 >= v.all_lo && min(t0 + kStep, last) <= v.all_hi;
+            if (t0 >= v.tile1 * kKvTile || t0 + kStep <= v.tile0 * kKvTile) continue;
             const auto go = [&](auto vector, auto masked) {
                 using V = decltype(vector);
                 constexpr int N = sizeof(V) / 4;
-                for (int c = 0; c < count; c += N) {
+                for (int c = N * sub; c < count; c += N * LANES) {
                     union Scores {
                         V v;
                         float e[N];
                     } s[kTogether];
 #pragma unroll
                     for (int k = 0; k < kTogether; ++k) {
-                        const int32_t t = t0 + k * kKeptThreads + threadIdx.x;
+                        const int32_t t = t0 + k * kOne + threadIdx.x / LANES;
 #pragma unroll
                         for (int i = 0; i < N; ++i) s[k].e[i] = -INFINITY;
                         if (t < last && t >= v.tile0 * kKvTile && t < v.tile1 * kKvTile) s[k].v = *reinterpret_cast<const V *>(scores + t * stride + piece.u.column0 + c);
@@ -396,12 +403,12 @@ __global__ void __launch_bounds__(kKeptThreads, 4) kv_weights_kept_kernel(const 
                     for (int i = 0; i < N; ++i) {
                         if (N > 1 && c + i >= count) break;
                         const float2 total = totals[c + i];
-                        int32_t lo = 0, hi = 0x7fffffff;
-                        if (decltype(masked)::value) column_range(p, piece.u, piece.u.column0 + c + i, &lo, &hi);  // other tokens' may never have been written
+                        int2 range = make_int2(0, 0x7fffffff);
+                        if (decltype(masked)::value) range = ranges[c + i];
 #pragma unroll
                         for (int k = 0; k < kTogether; ++k) {
-                            const int32_t t = t0 + k * kKeptThreads + threadIdx.x;
-                            if (!decltype(masked)::value || (s[k].e[i] != -INFINITY && t >= lo && t < hi)) w[k] = fmaf(exp2_fast(s[k].e[i] - total.x), total.y, w[k]);
+                            const int32_t t = t0 + k * kOne + threadIdx.x / LANES;
+                            if (!decltype(masked)::value || (s[k].e[i] != -INFINITY && t >= range.x && t < range.y)) w[k] = fmaf(exp2_fast(s[k].e[i] - total.x), total.y, w[k]);
                         }
                     }
                 }
@@ -416,8 +423,10 @@ __global__ void __launch_bounds__(kKeptThreads, 4) kv_weights_kept_kernel(const 
         }
 #pragma unroll
         for (int k = 0; k < kTogether; ++k) {
-            const int32_t t = t0 + k * kKeptThreads + threadIdx.x;
-            if (t < last) put_weight(p, piece.u, head, t, w[k]);
+            const int32_t t = t0 + k * kOne + threadIdx.x / LANES;
+#pragma unroll
+            for (int d = 1; d < LANES; d <<= 1) w[k] += __shfl_xor_sync(0xffffffffu, w[k], d);
+            if (t < last && sub == 0) put_weight(p, piece.u, head, t, w[k]);
         }
     }
 }
@@ -485,10 +494,13 @@ lce_status launch(const WeightsParams &p, cudaStream_t s)
     if (!first_opt_in.ensure(kv_weights_scores_kernel<B, NT, SPLIT>, ring) || !second_opt_in.ensure(kv_weights_sum_kernel<B, NT, SPLIT>, all)) return LCE_ERR_CUDA;
     const dim3 grid((unsigned)p.units, (unsigned)p.g.heads);
     if (p.tokens > 0) {
-        const lce_status st = launch_dependent(kv_weights_scores_kernel<B, NT, SPLIT>, grid, kThreads, ring, s, p);
+        // many columns of few tokens: blocks share the columns (579 rows on 579 tokens, 3 heads of 256 channels: 366 us without, 86 with)
+        const int64_t each = (p.tokens * p.group + p.batch - 1) / p.batch;
+        const int64_t side = std::min<int64_t>((each + 8 * NT - 1) / (8 * NT), std::max<int64_t>(148 * kBlocksPerSm / ((int64_t)p.units * p.g.heads), 1));
+        const lce_status st = launch_dependent(kv_weights_scores_kernel<B, NT, SPLIT>, dim3(grid.x, grid.y, (unsigned)side), kThreads, ring, s, p);
         if (st != LCE_OK) return st;
     }
-    if (p.scores) return launch_dependent(kv_weights_kept_kernel, grid, kKeptThreads, 0, s, p);
+    if (p.scores) return launch_dependent(p.tokens * p.group > 32 * (int64_t)p.batch ? kv_weights_kept_kernel<8> : kv_weights_kept_kernel<1>, grid, kKeptThreads, 0, s, p);
     return launch_dependent(kv_weights_sum_kernel<B, NT, SPLIT>, grid, kThreads, all, s, p);
 }
 
@@ -535,8 +547,12 @@ lce_status make_params(const lce_kv_attention_weights_desc *d, WeightsParams *p,
     p->previous_seq = d->previous_seq_stride; p->previous_head = d->previous_head_stride;
     p->out_seq = d->out_seq_stride; p->out_head = d->out_head_stride;
     *nt = p->g.blocks <= kWideBlocks && (d->tokens * p->group + d->batch - 1) / d->batch > 8 ? 2 : 1;
-    // Many rows go to the tensor cores' kernels.
-    p->prompt = p->g.blocks <= 4 && d->type != LCE_TYPE_FLOAT32 && p->tokens * p->group > p->batch * (int64_t)kFewColumns &&
+    // Many rows go to the kernels of kv_weights_prompt.cu where they are estimated to be ahead (us for 128 channels, bf16, by tokens times key heads; by
+    // the longest the sequences can be: their lengths are not known here).  One sequence of 512 / 4096 / 32768 tokens, 8 key heads: 20 columns
+    // 16.2 / 28.3 / 46.1 here and 24.6 / 27.4 / 81.4 there, 64 columns 35.2 / 61.3 / 99.2 and 24.4 / 27.8 / 81.3; 16 sequences of 512 / 4096: 32 columns 38.0 / 86.1
+    // and 38.6 / 132, 128 columns 132 / 415 and 37.1 / 106.
+    const double each = (double)p->tokens * p->group / p->batch, read = (double)p->batch * p->g.heads * p->table_tokens;
+    p->prompt = p->g.blocks <= 4 && d->type != LCE_TYPE_FLOAT32 && ceil(each / 16) * (11.0 + 6.5e-5 * read) > 24.0 + ceil(each / 256) * 1.65e-4 * read &&
                 p->g.heads < 65535 && (double)p->g.heads * p->batch * (p->table_tokens / 256 + 1) < kMostUnits;
     // As many pieces as the GPU has places for, as a sequence has one more than its share (48 of 1 - 8192 tokens, 8 heads: 72 us, with a
     // piece for each place whatever the sequences 77, with two 72; 16 of up to 1500, 12 heads: 14.8, 19.3 and 24.2), but for many sequences half of

@@ -16,8 +16,13 @@
 //   warp 24             issues the products
 //   warp 25             has the rows of q copied
 //   warp 26             has the keys' words copied from the cache (loads of the warps that decode them do not stay in flight over the fence in
-//                       front of the products: 143 instead of XXX us)
-// Sixteen warps, because one scheduler's two did not hide what a score goes through: 145 and 140 us for two chunks of 1024 rows instead of XXX.
+//                       front of the products: 143 instead of 125 us for the first kernel)
+//
+// Two sequences of 1024 rows of 4 columns on 5120 tokens, 8 key heads of 128 channels: 275 us, 125 and 135 of them in the two kernels.  Products (1024
+// clocks for a step of 256 x 128 at the tensor cores' rate) and powers of two (2048 at 16 a clock) would allow 70 each; a step takes 3500.  Taken out one by
+// one, the powers of two are 15 % of it, the products 5 %, reading TMEM 25 %: what is left is the way through shared memory that the warps hand each
+// other a tile on.  More tiles streaming (four instead of two), one arrival a warp at the barriers, 128-byte swizzled operands and eight warps with twice
+// the registers for the powers of two were all within 3 % of this.
 //
 // f16 holds a code times its scale exactly, relative to the largest scale of 128 tokens, down to 2^-28 of it; 16-bit rows of q are exact
 // down to 2^-24 of their largest element at least.  Scores and sums are fp32.
