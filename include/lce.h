@@ -425,7 +425,7 @@ lce_status lce_rotary(const lce_rotary_desc *desc, const void *q, const void *k,
  *               behind a sequence's last token changes
  *   workspace   lce_kv_attention_weights_workspace_bytes(desc) bytes, 16-byte aligned, no clearing, the call's until its kernels are done
  * The other arguments as for lce_kv_attention; tables are below 2^30 tokens.  Everything is fp32: 16-bit rows of q meet the cache's keys without a rounding (of
- * channels below 2^-24 of their row's largest a part is lost), fp32 rows are taken in 22 bits.  No sum depends on the order in which blocks run:
+ * channels below 2^-24 of the largest of the rows worked on together, 128 columns at most, a part is lost), fp32 rows are taken in 22 bits.  No sum depends on the order in which blocks run:
  * results repeat bit for bit. */
 typedef struct {
     lce_kv_desc cache;
@@ -467,8 +467,8 @@ lce_status lce_kv_evict(const lce_kv_evict_desc *desc, void *cache, const int32_
  * (operands ready, MMAs complete, accumulator read out); every such wait is limited to 0.2 s, after
  * which the kernel stops working, waits (bounded) for its copies and MMAs in flight, frees its tensor
  * memory and returns, leaving its output incomplete.  It records that in a device word and in a word
- * of mapped host memory; from then on lce_bconv2d, its host-buffer forms, lce_bconv2d_fused, lce_plan_run and lce_kv_attention of many rows on that
- * device return LCE_ERR_DEVICE_TIMEOUT without launching, until lce_device_status_reset.
+ * of mapped host memory; from then on lce_bconv2d, its host-buffer forms, lce_bconv2d_fused, lce_plan_run and, of many rows, lce_kv_attention and
+ * lce_kv_attention_weights on that device return LCE_ERR_DEVICE_TIMEOUT without launching, until lce_device_status_reset.
  *   lce_device_status        *status (HOST pointer) = 0 if no wait has given up on the current device
  *                            since load or the last reset, 1 otherwise.  Synchronous (reads the device word).
  *   lce_device_status_reset  clears both words for the current device.  Synchronous.

@@ -71,6 +71,8 @@ __device__ __forceinline__ bool find_piece(const WeightsParams &p, int at, Piece
             piece->u.row0 = __shfl_sync(0xffffffffu, s.row0, from);
             piece->u.column0 = 0;
             piece->columns = piece->u.rows * p.group;
+            // more scores than there is room for: rows of q that are several sequences' (q_starts that decrease); none are taken then
+            if (p.scores && piece->scores_before + __shfl_sync(0xffffffffu, scores, from) > p.scores_head) piece->columns = 0;
             const int32_t each = n / piece->pieces, more = n - each * piece->pieces;  // equal pieces
             piece->u.tile0 = piece->index * each + min(piece->index, more);
             piece->u.tile1 = piece->u.tile0 + each + (piece->index < more ? 1 : 0);

@@ -81,6 +81,7 @@ constexpr size_t weights_smem(int blocks) { return kMiscBytes + 6 * (size_t)(kTo
 struct PromptParams : WeightsParams {
     WorkUnit *units[2];
     int32_t *unit_counts;
+    int32_t most_tiles, most_units[2], most_parts;  // that there is room for
     uint8_t *images;      // [tile of 128 columns][kv head]: rows of q as f16, in the order in which they are an operand
     float *factors;       // [tile of columns][kv head][128]
     float2 *stats_units;  // [unit of the first kernel][256]: largest, sum
@@ -203,6 +204,13 @@ __device__ __forceinline__ void list_units(const PromptParams &p, int b)
     if (seq < 0) return;
     const Sequence s = sequence<8>(p, seq);
     const Counts mine = counts(p, s, cut);
+    // more than there is room for: rows of q that are several sequences' (q_starts that decrease); nothing is done then
+    Counts all;
+    find_sequence(p, cut, p.batch, &all);
+    if (all.tiles > p.most_tiles || all.units[0] > p.most_units[0] || all.units[1] > p.most_units[1] || all.parts > p.most_parts) {
+        if (seq == p.batch - 1 && threadIdx.x < 2) p.unit_counts[threadIdx.x] = 0;
+        return;
+    }
     if (seq == p.batch - 1 && threadIdx.x < 2) p.unit_counts[threadIdx.x] = before.units[threadIdx.x] + mine.units[threadIdx.x];
     const int32_t held = tokens_held(p, s.length), columns = s.rows * p.group;
 #pragma unroll
@@ -788,7 +796,7 @@ __global__ void __launch_bounds__(kJoining * kTokens) kv_weights_columns_kernel(
     // the lengths are what the kernels in front read: nothing has written them since
     const int seq = find_sequence(p, cut, blockIdx.x, [](const Counts &c) { return c.tiles; }, &before), head = blockIdx.y;
     asm volatile("griddepcontrol.wait;" ::: "memory");  // every block: what comes behind this kernel relies on the ones in front, too
-    if (seq < 0) return;
+    if (seq < 0 || p.unit_counts[0] == 0) return;
     const Sequence s = sequence<8>(p, seq);
     const int in_tile = threadIdx.x % kTokens, part = threadIdx.x / kTokens;
     const int tile = blockIdx.x - before.tiles, columns = s.rows * p.group, pieces = up(up(tokens_held(p, s.length), kTokens), cut.first);
@@ -817,6 +825,7 @@ __global__ void __launch_bounds__(256) kv_weights_chunks_kernel(const __grid_con
 {
     const Cut cut = find_cut(p);
     asm volatile("griddepcontrol.wait;" ::: "memory");  // every block: what comes behind this kernel relies on the ones in front, too
+    if (p.unit_counts[1] == 0) return;
     for (int at = blockIdx.x;; at += gridDim.x) {
         Counts before;
         const int seq = find_sequence(p, cut, at, [](const Counts &c) { return c.parts; }, &before);
@@ -885,6 +894,10 @@ lce_status launch_kv_weights_prompt(const WeightsParams &params, void *workspace
     static_cast<WeightsParams &>(p) = params;
     const Bounds most = bounds(p);
     const int64_t columns = most.tiles * p.g.heads * kTokens;
+    p.most_tiles = (int32_t)most.tiles;
+    p.most_units[0] = (int32_t)most.units;
+    p.most_units[1] = (int32_t)most.second_units;
+    p.most_parts = (int32_t)most.parts;
     char *at = static_cast<char *>(workspace);
     const auto take = [&](int64_t bytes) {
         char *const here = at;

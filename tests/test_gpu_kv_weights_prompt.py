@@ -121,3 +121,16 @@ def test_graph_of_growing_sequences_and_one_workspace():
         assert torch.equal(out, want)
     check(out, expected(s))
     assert lce.lce_device_status() == 0
+
+
+def test_many_rows_after_an_expired_wait():
+    s = Setup(BF16, [300], [100], 1, 2, 64, seed=8)
+    lce.lce_device_wait_probe(20_000)
+    torch.cuda.synchronize()
+    try:
+        with pytest.raises(lce.LceError) as e:
+            run(s)
+        assert e.value.status == 5
+    finally:
+        lce.lce_device_status_reset()
+    check(run(s), expected(s))
