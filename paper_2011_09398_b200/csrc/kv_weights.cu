@@ -4,8 +4,8 @@
 // the largest score and the sum of a whole column before the first weight is known.  So there are two kernels over pieces of the
 // sequences: the first makes the scores, S = K Q^T with the 4-bit keys on the 16-row side of m16n8k16 products and 8 or 16 columns on the other,
 // and each piece's largest and sum of every column; the second joins the pieces' (always in the same order) and adds a token's weights up
-// over the columns.  Where a sequence's columns fit one tile of them, as in a decode step, the second kernel reads the scores that the first
-// one left, 4 bytes each, next to which the keys were 80 bytes for 128 channels; otherwise it makes them again.
+// over the columns.  Where there is room for them the second kernel reads the scores that the first one left, 4 bytes each, next to which the
+// keys were 80 bytes for 128 channels; otherwise it makes them again.
 //
 // Keys are codes times a block's scale.  The codes c = n - 8 are exact f16 operands (1024 + n by one AND-OR, less 1032 by a packed
 // multiply-add), the scale multiplies a block's finished sums in fp32; 16-bit rows of q are one f16 number times a power of two of the row,

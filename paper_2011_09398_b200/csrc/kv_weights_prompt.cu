@@ -1,12 +1,12 @@
 // Attention weights by token of many rows (a prompt, or its last rows), on the 5th-generation tensor cores.
 //
 // The softmax needs a column's largest score and sum before its first weight is known, so the scores are made twice, by two kernels of one
-// shape: 256 rows of one operand stay in shared memory, tiles of 128 rows of the other one stream past them, and every thread of eight warps
-// has one of the 256 in TMEM, with its 128 products a step.
-//   first     256 columns (rows of q that share a key/value head) stay, keys stream: a thread has a column's scores, and keeps their
+// shape: 256 rows of one operand stay in shared memory, tiles of 128 rows of the other one stream past them, and two threads
+// have one of the 256 in TMEM, 64 of its 128 products a step each.
+//   first     256 columns (rows of q that share a key/value head) stay, keys stream: threads have a column's scores, and keep their
 //             largest and the sum of their powers of two
-//   second    256 tokens stay, columns stream: a thread has a token's scores, and adds its weights up.  A column's factor and the logarithm of
-//             its sum lie in shared memory
+//   second    256 tokens stay, columns stream: threads have a token's scores, and add its weights up.  The logarithms of the columns' sums
+//             lie in shared memory
 // So no sum crosses threads before a unit's end.  Work is cut into units of a few steps: (256 columns, a piece of the sequence) and (256 tokens,
 // a chunk of the columns), joined in a fixed order by small kernels.  The kernel that puts the rows of q in order as f16 lists them; 148
 // blocks take them in turn, and their warps go from one to the next without meeting:
@@ -24,8 +24,9 @@
 // other a tile on.  More tiles streaming (four instead of two), one arrival a warp at the barriers, 128-byte swizzled operands and eight warps with twice
 // the registers for the powers of two were all within 3 % of this.
 //
-// f16 holds a code times its scale exactly, relative to the largest scale of 128 tokens, down to 2^-28 of it; 16-bit rows of q are exact
-// down to 2^-24 of their largest element at least.  Scores and sums are fp32.
+// f16 holds a code times its scale exactly, relative to the largest scale of 128 tokens, down to 2^-28 of it; 16-bit rows of q,
+// 128 of them times one power of two, are exact down to 2^-24 of their largest element at least, and what is lost of smaller ones is below 2^-39 of it.
+// Scores and sums are fp32.
 #include "kv_tensor.cuh"
 #include "kv_weights.cuh"
 
