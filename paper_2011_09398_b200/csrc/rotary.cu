@@ -5,7 +5,7 @@
 // vectors, of either half of the head or next to one another.  An angle is the product of position and step in 64 bits, whose upper half is
 // a part of a turn: no reduction, and nothing is lost far out.
 //
-// Measured: 16384 tokens of 32 and 8 heads of 128 channels in bf16 (336 MB) 61 us, 5.4 TB/s; 1777 tokens of 20 and 5 heads of 80 in fp32, 32
+// Measured: 16384 tokens of 32 and 8 heads of 128 channels in bf16 (336 MB) 55 us, 6.1 TB/s; 1777 tokens of 20 and 5 heads of 80 in fp32, 32
 // channels turned (28 MB), 6.5 us; one token 5 us, launch and call.
 #include "kv_common.cuh"
 
@@ -53,9 +53,9 @@ __device__ __forceinline__ void turn_of(uint32_t part, float amplitude, float &c
     if (quarter & 2) s = -s;
 }
 
-// kTogether heads' loads are on their way at once.
+// kTogether heads' loads are on their way at once: four heads of 16 bits by three blocks an SM (two blocks: 61 us for 16384 tokens, two heads 58).
 template <typename T, bool PAIRS, int kTogether>
-__global__ void __launch_bounds__(kThreads, kTogether * sizeof(T) <= 4 ? 3 : 2) rotary_kernel(const __grid_constant__ RotaryParams p)
+__global__ void __launch_bounds__(kThreads, 3) rotary_kernel(const __grid_constant__ RotaryParams p)
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int64_t item = (int64_t)blockIdx.x * kThreads + threadIdx.x;
