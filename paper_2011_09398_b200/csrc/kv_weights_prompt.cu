@@ -192,7 +192,7 @@ __device__ __forceinline__ void columns_of(const PromptParams &p, int32_t length
 {
     const int64_t row0 = (int64_t)length - rows;  // position of the first row
     *lo = p.causal ? (int32_t)(min(max(t0 - row0, (int64_t)0), (int64_t)rows) * p.group) : 0;
-    *hi = (p.window > 0 ? (int32_t)min(max(t1 - 1 + p.window - row0, (int64_t)0), (int64_t)rows) : rows) * p.group;
+    *hi = (p.window > 0 ? (int32_t)min(max((int64_t)t1 - 1 + p.window - row0, (int64_t)0), (int64_t)rows) : rows) * p.group;
 }
 
 // Writes one sequence's units of both kernels down, a thread to a unit; the last sequence says how many there are.

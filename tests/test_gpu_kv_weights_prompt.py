@@ -134,3 +134,10 @@ def test_many_rows_after_an_expired_wait():
     finally:
         lce.lce_device_status_reset()
     check(run(s), expected(s))
+
+
+@pytest.mark.parametrize("rows", [1, 90])
+@pytest.mark.parametrize("causal", [True, False])
+def test_the_widest_window(rows, causal):
+    s = Setup(F16, [300], [rows], 1, 2, 64, seed=9)
+    check(run(s, window=2 ** 31 - 1, causal=causal), expected(s, causal=causal))
