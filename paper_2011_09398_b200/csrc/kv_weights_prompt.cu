@@ -641,8 +641,9 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_prompt_kernel(const __
             } else if (n >= 2) {
                 ok = wait_bounded(&sh.bars[BAR_STREAM_EMPTY + slot], (n >> 1 & 1) ^ 1);
             }
+            ok = half_sync_and(1, ok);  // where the place did not get free for one of them, all leave: nothing is written there, and nobody told so
+            if (!ok) break;
             if (thread == 0) sh.info[(SUMS ? 2 * units + half : n) % kInfos] = TileInfo{__uint_as_float((uint32_t)(127 + exponent) << 23), valid};
-            asm volatile("bar.sync 1, 256;" ::: "memory");
 #pragma unroll
             for (int i = 0; i < kKeyGroups; ++i) {
                 const int eight = i * kProducerWarps + producer, token = eight * 8 + (lane & 7), quarter = lane >> 3;
