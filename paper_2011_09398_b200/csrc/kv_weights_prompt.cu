@@ -29,6 +29,7 @@
 // Scores and sums are fp32.
 #include "kv_tensor.cuh"
 #include "kv_weights.cuh"
+#include "kv_weights_rings.cuh"
 
 #include <algorithm>
 #include <type_traits>
@@ -43,7 +44,6 @@ constexpr float kRise = 16.0f;       // the score that powers of two are relativ
 constexpr int kBlocks = 148;         // one to an SM
 constexpr int kSteps = kBlocks * 8;  // units are cut so that there are about as many
 constexpr int kHeldUnits = 32;       // of a block, in shared memory
-constexpr int kInfos = 8;            // tiles of keys; the producers are less than four units, of two tiles, ahead of the softmax
 
 enum { BAR_STAY_FULL = 0, BAR_STAY_EMPTY = BAR_STAY_FULL + 2, BAR_STREAM_FULL = BAR_STAY_EMPTY + 2, BAR_STREAM_EMPTY = BAR_STREAM_FULL + 2,
        BAR_WORDS_FULL = BAR_STREAM_EMPTY + 2, BAR_WORDS_EMPTY = BAR_WORDS_FULL + 2, BAR_S_FULL = BAR_WORDS_EMPTY + 2, BAR_S_EMPTY = BAR_S_FULL + 4, BAR_DONE = BAR_S_EMPTY + 4, BAR_COUNT };
@@ -476,14 +476,14 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_prompt_kernel(const __
                     }
                 }
                 for (int32_t step = w.step0; ok && step < w.step1; ++step, ++steps) {
-                    const uint32_t buffer = steps & 1;
-                    ok = warp_wait(&sh.bars[BAR_S_FULL + 2 * half + buffer], steps >> 1 & 1);
+                    const uint32_t buffer = step_buffer(steps);
+                    ok = warp_wait(&sh.bars[BAR_S_FULL + 2 * half + buffer], step_parity(steps));
                     if (!SUMS && !ok) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const int first = step * 128 + 64 * side;  // token, or column
                     uint32_t valid = 0xfu;
                     if (!SUMS || step == w.step0) {
-                        const TileInfo info = sh.info[(SUMS ? 2 * units + half : tiles + (uint32_t)(step - w.step0)) % kInfos];
+                        const TileInfo info = sh.info[info_place(SUMS, tiles + (uint32_t)(step - w.step0), units, half)];
                         unit = info.unit;
                         if (SUMS) {
                             if (!(info.valid >> (in_tile >> 4) & 1)) hi = lo;  // its page is not in the pool
@@ -643,7 +643,7 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_prompt_kernel(const __
             }
             ok = half_sync_and(1, ok);  // where the place did not get free for one of them, all leave: nothing is written there, and nobody told so
             if (!ok) break;
-            if (thread == 0) sh.info[(SUMS ? 2 * units + half : n) % kInfos] = TileInfo{__uint_as_float((uint32_t)(127 + exponent) << 23), valid};
+            if (thread == 0) sh.info[info_place(SUMS, n, units, half)] = TileInfo{__uint_as_float((uint32_t)(127 + exponent) << 23), valid};
 #pragma unroll
             for (int i = 0; i < kKeyGroups; ++i) {
                 const int eight = i * kProducerWarps + producer, token = eight * 8 + (lane & 7), quarter = lane >> 3;
@@ -668,20 +668,21 @@ __global__ void __launch_bounds__(kThreads, 1) kv_weights_prompt_kernel(const __
             constexpr uint32_t kIdesc = 1u << 4 | (uint32_t)(128 >> 4) << 24 | (uint32_t)(128 >> 3) << 17;  // fp32 sums of f16 products, both operands along k, 128 x 128
             const uint32_t stay_at = smem_u32(stay_smem), stream_at = smem_u32(stream_smem);
             uint32_t units = 0, streamed = 0, steps[2] = {0, 0};
+            const auto read_out = [&](int half, uint32_t step) { return warp_wait(&sh.bars[BAR_S_EMPTY + 2 * half + step_buffer(step)], step_parity(step)); };
             for (int32_t unit_at = blockIdx.x, k = 0; ok && unit_at < count; unit_at += gridDim.x, ++k) {
                 const WorkUnit w = load_unit<SUMS>(p, sh, k, unit_at);
                 if (w.step0 == w.step1) continue;
                 const uint32_t pair = units & 1;
                 const int halves = halves_of<SUMS>(w);
-                ok = warp_wait(&sh.bars[BAR_STAY_FULL + pair], units >> 1 & 1);
+                ok = before_unit(halves, steps, read_out) && warp_wait(&sh.bars[BAR_STAY_FULL + pair], units >> 1 & 1);
                 for (int32_t step = w.step0; ok && step < w.step1; ++step, ++streamed) {
                     const uint32_t slot = streamed & 1;
                     ok = warp_wait(&sh.bars[BAR_STREAM_FULL + slot], streamed >> 1 & 1);
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         if (!ok || half >= halves) break;
-                        const uint32_t buffer = steps[half] & 1;
-                        if (steps[half] >= 2) ok = warp_wait(&sh.bars[BAR_S_EMPTY + 2 * half + buffer], (steps[half] >> 1 & 1) ^ 1);
+                        const uint32_t buffer = step_buffer(steps[half]);
+                        ok = before_step(half, steps, read_out);
                         if (!ok) break;
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                         if (lane == 0) {
