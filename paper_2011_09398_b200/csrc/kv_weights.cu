@@ -439,7 +439,9 @@ __global__ void __launch_bounds__(kThreads, blocks_per_sm(B, NT, SPLIT)) kv_weig
     __shared__ float2 totals[COLUMNS];
     float *const weights = reinterpret_cast<float *>(smem) + kWarps * kStages * key_words(B);  // of the piece's tokens
     Piece piece;
-    // the lengths are what the kernel in front read: nothing has written them since
+    // The lengths are what the kernel in front read, nothing has written them since; of a call without rows there is none in front, and who
+    // has written them may still be at it.
+    if (p.tokens == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
     const bool found = find_piece(p, blockIdx.x, &piece);
     asm volatile("griddepcontrol.wait;" ::: "memory");  // every block: what comes behind this kernel relies on the one in front, too
     if (!found) return;

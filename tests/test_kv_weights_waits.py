@@ -19,3 +19,18 @@ def test_producers_of_keys_publish_nothing_behind_a_wait_that_gave_up():
         assert not (pending and kind == "publish"), kinds
         pending = kind == "wait" or (pending and kind != "meet")
     assert not pending, kinds
+
+
+def test_lengths_are_read_ahead_only_behind_a_kernel_of_the_same_call():
+    """Kernels that work out their piece from the lengths before they wait: one of the same call is in front, which has read them, or they wait."""
+    text = (CSRC / "kv_weights.cu").read_text()
+    kernels = text.split("__global__")[1:]
+    ahead = [k for k in kernels if 0 <= k.find("find_piece(") < k.index('asm volatile("griddepcontrol.wait;"')]
+    alone = [k for k in kernels if "kv_weights_sum_kernel(" in k.split("{")[0]]  # which a call without rows launches by itself
+    assert len(kernels) == 3 and len(alone) == 1
+    for k in ahead:
+        assert "kv_weights_kept_kernel(" in k.split("{")[0]
+    assert 0 < alone[0].index('if (p.tokens == 0) asm volatile("griddepcontrol.wait;"') < alone[0].index("find_piece(")
+    launches = text[text.index("lce_status launch(const WeightsParams"):]
+    # kept scores are only there where there were rows
+    assert "p.tokens > 0 && bytes <= kMostScores" in text and launches.index("if (p.tokens > 0)") < launches.index("kv_weights_kept_kernel<")
