@@ -53,7 +53,7 @@ def is_stale() -> bool:
 
 def _host_is_stale() -> bool:
     return not HOST_MODULE.exists() or HOST_MODULE.stat().st_mtime < max(
-        f.stat().st_mtime for f in (HOST_SRC, INCLUDE / "lce.h"))
+        f.stat().st_mtime for f in (HOST_SRC, CSRC / "row_overlap.cuh", INCLUDE / "lce.h"))
 
 
 def _build_host() -> None:

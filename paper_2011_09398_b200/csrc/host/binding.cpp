@@ -20,6 +20,7 @@
 
 #include <string>
 
+#include "../row_overlap.cuh"
 #include "lce.h"
 
 namespace {
@@ -661,6 +662,10 @@ PyObject *kv_evict(PyObject *const *a)
         d.kept_scores_head_stride = made[2].stride(1);
     } else {
         pks = token_rows(a[11], d.batch, heads, d.budget, &d.kept_scores_seq_stride, &d.kept_scores_head_stride, "kept_scores");
+        const lce::RowSet kept_rows{pks, d.batch, heads, d.kept_scores_seq_stride, d.kept_scores_head_stride, d.budget, 4};
+        if (!lce::rows_apart(kept_rows)) value_error("kept_scores must have rows apart from one another");
+        if (lce::rows_meet({ps, d.batch, heads, d.scores_seq_stride, d.scores_head_stride, (int64_t)d.table_pages * d.cache.page_size, 4}, kept_rows))
+            value_error("kept_scores must not be memory of scores");
     }
     void *pc = device_pointer(cache, at::kByte, "cache"), *s = current_stream();
     if (d.batch > 0) check(without_gil([&] { return lce_kv_evict(&d, pc, pt, pl, ps, pk, whole[0], whole[1], pks, s); }), "lce_kv_evict");

@@ -12,6 +12,7 @@
 // (38 MB of rows read and written, 12 at the copy rate; values lie in pairs of tokens, so that a quarter that stays touches most sectors: 105 MB are
 // read); 24 sequences of up to 8192 tokens cut to 2048, 64 channels: 19 and 17 us.
 #include "kv_common.cuh"
+#include "row_overlap.cuh"
 
 #include <algorithm>
 #include <type_traits>
@@ -446,6 +447,10 @@ extern "C" lce_status lce_kv_evict(const lce_kv_evict_desc *desc, void *cache, c
     if (!aligned(cache, 16) || !aligned(page_table, 4) || !aligned(lengths, 4) || !aligned(scores, 4) || !aligned(kept_table, 4) || !aligned(kept, 4) ||
         !aligned(kept_lengths, 4) || !aligned(kept_scores, 4))
         return LCE_ERR_ALIGNMENT;
+    // Scores are read again where they are written to their new places, by other warps and blocks, too.  How long rows of scores are follows from the
+    // lengths, on the device: here every row is looked at by its first element.
+    const RowSet new_scores{kept_scores, d.batch, p.g.heads, d.kept_scores_seq_stride, d.kept_scores_head_stride, d.budget, 4};
+    if (kept_scores && (!rows_apart(new_scores) || rows_meet({scores, d.batch, p.g.heads, d.scores_seq_stride, d.scores_head_stride, 1, 4}, new_scores))) return LCE_ERR_INVALID_ARG;
     p.batch = d.batch; p.table_pages = d.table_pages; p.kept_pages = d.kept_pages;
     p.table_tokens = d.table_pages * d.cache.page_size;
     p.budget = d.budget; p.first = d.first; p.recent = d.recent;

@@ -1,0 +1,55 @@
+"""Buffers that a call would write while it still reads them are refused before anything is launched; those side by side are not."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2011_09398_b200 as lce
+from paper_2011_09398_b200 import build as lce_build
+from test_bounded_cache_abi import INVALID, evict_desc
+
+at = ctypes.c_void_p  # places that are never touched: there is no GPU, or the call is refused first
+
+
+@pytest.fixture(scope="module")
+def lib():
+    lce_build.build()
+    return lce.library()
+
+
+def accepted(status):
+    """Passed all checks: here, without a GPU, the launch is what fails."""
+    return status not in (1, 2, 3, 6)
+
+
+def evict(lib, scores, kept_scores, **change):
+    d = evict_desc(**change)
+    return lib.lce_kv_evict(ctypes.byref(d), at(1 << 20), at(2 << 20), at(3 << 20), at(scores), at(4 << 20), at(5 << 20), at(6 << 20), at(kept_scores) if kept_scores else None, None)
+
+
+def test_scores_and_kept_scores(lib):
+    # 2 sequences, 2 heads: scores of 48 in rows of 48, kept scores of 20 in rows of 20
+    here = 7 << 20
+    same = dict(kept_scores_seq_stride=96, kept_scores_head_stride=48)
+    for there in (here, here + 4 * 96, here - 4 * 19, here + 4 * 48 - 4 * 19):
+        assert evict(lib, here, there) == INVALID, there
+        assert evict(lib, here, there, **same) == INVALID, there
+    one_row = dict(batch=1, cache=(8, 16, 1, 64))
+    assert evict(lib, here, here, **one_row) == INVALID
+    assert evict(lib, here, here, scores_head_stride=0) == INVALID  # one row of scores for all heads
+    # rows of kept scores apart from one another
+    other = 8 << 20
+    for bad in (dict(kept_scores_head_stride=0), dict(kept_scores_head_stride=19), dict(kept_scores_seq_stride=0), dict(kept_scores_seq_stride=39), dict(kept_scores_seq_stride=20, kept_scores_head_stride=20)):
+        assert evict(lib, here, other, **bad) == INVALID, bad
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="calls that are accepted would be launched")
+def test_scores_and_kept_scores_beside_one_another(lib):
+    here, other = 7 << 20, 8 << 20
+    for good in (dict(), dict(scores_head_stride=0), dict(kept_scores_seq_stride=20, kept_scores_head_stride=40), dict(batch=1, kept_scores_seq_stride=0),
+                 dict(cache=(8, 16, 1, 64), kept_scores_head_stride=0)):
+        assert accepted(evict(lib, here, other, **good)), good
+    assert accepted(evict(lib, here, None))
+    # in the same rows, behind the scores
+    assert accepted(evict(lib, here, here + 4 * 48, scores_seq_stride=136, scores_head_stride=68, kept_scores_seq_stride=136, kept_scores_head_stride=68))
+    assert accepted(evict(lib, here, here + 4 * 192)) and accepted(evict(lib, here + 4 * 80, here))

@@ -1,0 +1,40 @@
+"""Buffers of the bounded cache's calls that share memory: refused where a call would write what it still reads, taken where they lie side by side."""
+import pytest
+import torch
+
+from gpu_util import DEV
+from test_gpu_kv_evict import Pool
+
+pytestmark = pytest.mark.gpu
+
+
+def test_scores_and_kept_scores_of_one_buffer():
+    p = Pool([200, 90], 33, kv_heads=3, dim=32, seed=1)
+    capacity = p.table.shape[1] * p.page
+    want = [t.clone() for t in p.run(recent=4)]
+    buffer = torch.zeros(2, 3, capacity + 33, device=DEV)
+    scores = buffer[:, :, :capacity]
+    scores.copy_(torch.from_numpy(p.scores))
+    before, cache = buffer.clone(), p.cache.clone()
+    for kept_scores in (scores, buffer, buffer[:, :, 5:], buffer[:, :, capacity - 1:]):
+        with pytest.raises(ValueError, match="kept_scores must not be memory of scores"):
+            p.run(scores, recent=4, kept_scores=kept_scores)
+    one = scores[:, :1].expand(-1, 3, -1)
+    with pytest.raises(ValueError, match="kept_scores must not be memory of scores"):
+        p.run(one, recent=4, kept_scores=scores)
+    for kept_scores in (torch.zeros(2, 1, 33, device=DEV).expand(-1, 3, -1), torch.zeros(1, 3, 33, device=DEV).expand(2, -1, -1), torch.zeros(200, device=DEV).as_strided((2, 3, 33), (90, 30, 1))):
+        with pytest.raises(ValueError, match="apart"):
+            p.run(scores, recent=4, kept_scores=kept_scores)
+    assert torch.equal(buffer, before) and torch.equal(p.cache, cache)
+    got = p.run(scores, recent=4, kept_scores=buffer[:, :, capacity:])
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and torch.equal(scores, before[:, :, :capacity])
+
+
+def test_sums_carried_in_two_buffers_in_turn():
+    p = Pool([300, 120], 64, kv_heads=2, dim=32, seed=2)
+    capacity = p.table.shape[1] * p.page
+    turns = [torch.from_numpy(p.scores).to(DEV), torch.full((2, 2, capacity), 9.0, device=DEV)]
+    want = [t.clone() for t in p.run(first=2, recent=8)]
+    kept, lengths, kept_scores = p.run(turns[0], first=2, recent=8, kept_scores=turns[1])
+    assert kept_scores is turns[1] and torch.equal(kept, want[0]) and torch.equal(lengths, want[1]) and torch.equal(turns[1][:, :, :64], want[2])
+    assert bool((turns[1][:, :, 64:] == 9).all())
