@@ -451,7 +451,7 @@ lce_status lce_kv_attention_weights(const lce_kv_attention_weights_desc *desc, c
  * of a page outside the pool are not written; what else such a page holds stays).
  *   scores        fp32 [batch][kv_heads][..], strides in elements; a head stride of 0 makes all heads keep the same tokens
  *   kept          int32 [batch][kv_heads][budget]: the places that each kept token came from, ascending, -1 behind the last
- *   kept_lengths  int32 [batch]: how many there are
+ *   kept_lengths  int32 [batch]: how many there are; may be `lengths`
  *   kept_scores   fp32 [batch][kv_heads][..] with strides of its own, or NULL: their scores in `budget` places, 0 behind the last.  Rows apart
  *                 from one another and from `scores` (LCE_ERR_INVALID_ARG where the strides and pointers show that they are not): sums that
  *                 are carried from call to call need two buffers in turn

@@ -441,7 +441,7 @@ def lce_kv_evict(desc: KvDesc, cache: torch.Tensor, page_table: torch.Tensor, le
     """Every head of a sequence keeps `budget` tokens: the `first` first, the `recent` last, and those with the highest scores (fp32
     [sequences, kv_heads, page_table.shape[1] * page_size or more]; expanded over the heads all of them keep the same).  Their rows move, in order, to
     the pages of kept_table (int32 [sequences, pages]), none of which may be one that is read.  Returns kept (int32 [sequences,
-    kv_heads, budget]: where each came from, -1 behind the last), kept_lengths and kept_scores [sequences, kv_heads, budget or more], which must not
+    kv_heads, budget]: where each came from, -1 behind the last), kept_lengths (which may be lengths) and kept_scores [sequences, kv_heads, budget or more], which must not
     be memory of scores."""
     return _native.kv_evict(desc, cache, page_table, lengths, scores, kept_table, budget, first, recent, kept, kept_lengths, kept_scores)
 

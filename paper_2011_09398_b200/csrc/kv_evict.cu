@@ -248,7 +248,6 @@ __global__ void __launch_bounds__(THREADS) kv_evict_select_kernel(const __grid_c
         kept[i] = -1;
         if (kept_scores) kept_scores[i] = 0.0f;
     }
-    if (head == 0 && rank == 0 && threadIdx.x == 0) p.kept_lengths[seq] = (int32_t)count;
     cluster_sync();  // nobody leaves while its counts are read
 }
 
@@ -301,7 +300,11 @@ __global__ void __launch_bounds__(kMoveThreads, 4) kv_evict_move_kernel(const __
     const auto tile_on = [&](int32_t page, int32_t in_page) { return (page * p.g.heads + head) * tiles_per_page + in_page / kKvTile; };
     if (threadIdx.x < TILES * kKvTile) {
         const int32_t j = first + threadIdx.x;
-        const int32_t from = j < p.budget ? p.kept[((int64_t)seq * p.g.heads + head) * p.budget + j] : -1;
+        const int32_t *const kept = p.kept + ((int64_t)seq * p.g.heads + head) * p.budget;
+        const int32_t from = j < p.budget ? kept[j] : -1;
+        // Every head has as many.  Here and not in the kernel in front, which reads the lengths: they may be the same memory.
+        if (head == 0 && j < p.budget && from >= 0 && (j + 1 == p.budget || kept[j + 1] < 0)) p.kept_lengths[seq] = j + 1;
+        if (head == 0 && j == 0 && from < 0) p.kept_lengths[seq] = 0;
         const int32_t in_kept = p.by_page(j), target = j < p.budget ? __ldg(p.kept_table + (int64_t)seq * p.kept_pages + in_kept) : -1;
         Source s{-1, 0};
         if (from >= 0 && from < p.table_tokens) {

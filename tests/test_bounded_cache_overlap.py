@@ -1,5 +1,6 @@
 """Buffers that a call would write while it still reads them are refused before anything is launched; those side by side are not."""
 import ctypes
+from pathlib import Path
 
 import pytest
 import torch
@@ -53,3 +54,12 @@ def test_scores_and_kept_scores_beside_one_another(lib):
     # in the same rows, behind the scores
     assert accepted(evict(lib, here, here + 4 * 48, scores_seq_stride=136, scores_head_stride=68, kept_scores_seq_stride=136, kept_scores_head_stride=68))
     assert accepted(evict(lib, here, here + 4 * 192)) and accepted(evict(lib, here + 4 * 80, here))
+
+
+def test_kept_lengths_are_written_by_no_kernel_that_reads_the_lengths():
+    """They may be the same memory: blocks of the kernel that chooses can begin after others of it are done."""
+    text = (Path(lce.__file__).parent / "csrc" / "kv_evict.cu").read_text()
+    kernels = text.split("__global__")[1:]
+    kernels[-1] = kernels[-1][:kernels[-1].index("\nlce_status ")]
+    reads, writes = (["kv_evict_select" in k.split("{")[0] for k in kernels if what in k] for what in ("p.lengths", "p.kept_lengths"))
+    assert reads == [True] and writes == [False]

@@ -1,7 +1,9 @@
 """Buffers of the bounded cache's calls that share memory: refused where a call would write what it still reads, taken where they lie side by side."""
+import numpy as np
 import pytest
 import torch
 
+import paper_2011_09398_b200 as lce
 from gpu_util import DEV
 from test_gpu_kv_evict import Pool
 
@@ -38,3 +40,24 @@ def test_sums_carried_in_two_buffers_in_turn():
     kept, lengths, kept_scores = p.run(turns[0], first=2, recent=8, kept_scores=turns[1])
     assert kept_scores is turns[1] and torch.equal(kept, want[0]) and torch.equal(lengths, want[1]) and torch.equal(turns[1][:, :, :64], want[2])
     assert bool((turns[1][:, :, 64:] == 9).all())
+
+
+@pytest.mark.parametrize("sequences, kv_heads, length, budget", [(1, 1, 100, 40), (3, 4, 500, 40), (90, 16, 200, 40), (4, 8, 40000, 1000)])
+def test_lengths_in_place(sequences, kv_heads, length, budget):
+    """More blocks than the GPU takes at once: those of a sequence's later heads begin when the first head's are done."""
+    lengths = [0, length, budget, budget - 1, 1][:sequences] + [length - 7 * i % 97 for i in range(max(sequences - 5, 0))]
+    lengths[-1] = length
+    p = Pool(lengths, budget, kv_heads=kv_heads, dim=32, page=64 if length > 1000 else 16, seed=sequences)
+    want = [t.clone() for t in p.run(first=3, recent=9)]
+    cache = p.cache.clone()
+    assert want[1].tolist() == [min(n, budget) for n in lengths]
+    i32 = lambda a: torch.from_numpy(np.ascontiguousarray(a, np.int32)).to(DEV)
+    carried, scores = i32(p.lengths), torch.from_numpy(p.scores).to(DEV)
+    for start in (lengths, lengths[::-1][:sequences]):
+        carried.copy_(torch.tensor(start, dtype=torch.int32))
+        same = torch.equal(carried.cpu(), torch.tensor(lengths, dtype=torch.int32))
+        wanted = want if same else [t.clone() for t in lce.lce_kv_evict(p.desc, p.cache, i32(p.table), carried.clone(), scores, i32(p.kept_table), budget, first=3, recent=9)]
+        got = lce.lce_kv_evict(p.desc, p.cache, i32(p.table), carried, scores, i32(p.kept_table), budget, first=3, recent=9, kept_lengths=carried)
+        assert got[1] is carried and all(torch.equal(a, b) for a, b in zip(got, wanted))
+        if same:
+            assert torch.equal(p.cache, cache)
