@@ -420,9 +420,10 @@ lce_status lce_rotary(const lce_rotary_desc *desc, const void *q, const void *k,
  * last n of the sequence, are new: what `previous` holds for them does not count.  So a buffer that carries the sums from call to call
  * needs no clearing as sequences grow.  A row that sees no token adds nothing; one that is not finite, or sees a key that is not, makes
  * the weights of all tokens that it sees NaN.  A sequence without rows is only decayed.
- *   previous    fp32, or NULL (zeros); may be `out` with its strides.  With decay 0 it is not read
- *   out         fp32 [batch][kv_heads][table_pages * page_size], strides in elements between sequences and between heads; nothing
- *               behind a sequence's last token changes
+ *   previous    fp32, or NULL (zeros); may be `out` with its strides, and no other memory of it (LCE_ERR_INVALID_ARG where the strides and
+ *               pointers show that it is).  With decay 0 it is not read
+ *   out         fp32 [batch][kv_heads][table_pages * page_size], strides in elements between sequences and between heads, rows apart from
+ *               one another (LCE_ERR_INVALID_ARG where two begin at one place); nothing behind a sequence's last token changes
  *   workspace   lce_kv_attention_weights_workspace_bytes(desc) bytes, 16-byte aligned, no clearing, the call's until its kernels are done
  * The other arguments as for lce_kv_attention; tables are below 2^30 tokens.  Everything is fp32: 16-bit rows of q meet the cache's keys without a rounding (of
  * channels below 2^-24 of the largest of the rows worked on together, 128 columns at most, a part is lost), fp32 rows are taken in 22 bits.  No sum depends on the order in which blocks run:

@@ -429,7 +429,7 @@ def lce_kv_attention_weights(desc: KvDesc, q: torch.Tensor, cache: torch.Tensor,
                              workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """out[sequence, kv head, token] = decay * previous + the attention weights that lce_kv_attention's rows of q give the token, added
     up over the rows and the head's query heads.  previous and out: fp32 [sequences, kv_heads, page_table.shape[1] * page_size or more], out may
-    be previous; the tokens that the rows stand at have no previous weight.  Nothing behind a sequence's last token is written
+    be previous (with its strides) or other memory; the tokens that the rows stand at have no previous weight.  Nothing behind a sequence's last token is written
     (arbitrary where out is not given).  The other arguments as for lce_kv_attention."""
     return _native.kv_attention_weights(desc, q, cache, page_table, lengths, q_starts, previous, out, desc.head_dim ** -0.5 if scale is None else scale,
                                         causal, window, decay, workspace)

@@ -613,6 +613,11 @@ PyObject *kv_attention_weights(PyObject *const *a)
     d.causal = causal;
     d.window = window;
     if (d.batch == 0 || room_for == 0) return returned(a[7], made);
+    const lce::RowSet out_rows{out, d.batch, d.cache.kv_heads, d.out_seq_stride, d.out_head_stride, room_for, 4};
+    if (!lce::rows_apart(out_rows)) value_error("out must have rows apart from one another");
+    if (previous && previous != out && d.decay != 0.0f &&
+        lce::rows_meet({previous, d.batch, d.cache.kv_heads, d.previous_seq_stride, d.previous_head_stride, room_for, 4}, out_rows))
+        value_error("out must be previous itself, with its strides, or other memory");
     if (a[12] == Py_None) room = empty_like_device({(int64_t)lce_kv_attention_weights_workspace_bytes(&d)}, at::kByte, tq);
     const at::Tensor &ws = a[12] == Py_None ? room : tensor(a[12], "workspace");
     on_current_device(ws, "workspace");

@@ -16,6 +16,7 @@
 // products and 69 between the 4-bit words and their operands, with the issue slots 64 % busy at four warps a scheduler (127 registers).
 #include "kv_mma.cuh"
 #include "kv_weights.cuh"
+#include "row_overlap.cuh"
 
 #include <math.h>
 
@@ -611,6 +612,15 @@ extern "C" lce_status lce_kv_attention_weights(const lce_kv_attention_weights_de
         !aligned(out, 4) || !aligned(workspace, 16))
         return LCE_ERR_ALIGNMENT;
     if (workspace_size < workspace_bytes(p)) return LCE_ERR_WORKSPACE;
+    // A weight is written by the thread that reads the previous one, so only in place may they be the same memory.  How long rows are follows from
+    // the lengths, on the device: here every row is looked at by its first element.
+    const RowSet new_sums{out, p.batch, p.g.heads, p.out_seq, p.out_head, 1, 4}, old_sums{previous, p.batch, p.g.heads, p.previous_seq, p.previous_head, 1, 4};
+    if (!rows_apart(new_sums)) return LCE_ERR_INVALID_ARG;
+    if (previous == out) {
+        if (desc->decay != 0.0f && ((p.batch > 1 && p.previous_seq != p.out_seq) || (p.g.heads > 1 && p.previous_head != p.out_head))) return LCE_ERR_INVALID_ARG;
+    } else if (previous && desc->decay != 0.0f && rows_meet(old_sums, new_sums)) {
+        return LCE_ERR_INVALID_ARG;
+    }
     p.q_vectors = p.g.dim % 8 == 0 && aligned(q, 8 * element) && p.q_token % 8 == 0 && p.q_head % 8 == 0;
     p.q = q; p.cache = static_cast<const uint32_t *>(cache); p.page_table = page_table; p.lengths = lengths; p.q_starts = q_starts;
     p.previous = desc->decay != 0.0f ? previous : nullptr;

@@ -7,7 +7,7 @@ import torch
 
 import paper_2011_09398_b200 as lce
 from paper_2011_09398_b200 import build as lce_build
-from test_bounded_cache_abi import INVALID, evict_desc
+from test_bounded_cache_abi import INVALID, evict_desc, weights_desc
 
 at = ctypes.c_void_p  # places that are never touched: there is no GPU, or the call is refused first
 
@@ -63,3 +63,32 @@ def test_kept_lengths_are_written_by_no_kernel_that_reads_the_lengths():
     kernels[-1] = kernels[-1][:kernels[-1].index("\nlce_status ")]
     reads, writes = (["kv_evict_select" in k.split("{")[0] for k in kernels if what in k] for what in ("p.lengths", "p.kept_lengths"))
     assert reads == [True] and writes == [False]
+
+
+def weigh(lib, previous, out, **change):
+    d = weights_desc(**change)
+    return lib.lce_kv_attention_weights(ctypes.byref(d), at(1 << 20), at(2 << 20), at(3 << 20), at(4 << 20), None, at(previous) if previous else None, at(out), at(5 << 20), 1 << 40, None)
+
+
+def test_previous_weights_and_out(lib):
+    # 2 sequences, 2 heads, rows of 48
+    here, other = 7 << 20, 8 << 20
+    for there in (here + 4 * 48, here - 4 * 96):
+        assert weigh(lib, there, here) == INVALID, there
+    for bad in (dict(previous_head_stride=0), dict(previous_seq_stride=192), dict(out_seq_stride=48, out_head_stride=96)):
+        assert weigh(lib, here, here, **bad) == INVALID, bad
+    assert weigh(lib, here + 4 * 48, here, previous_head_stride=0) == INVALID  # one row for all heads, where one of them writes
+    for bad in (dict(out_head_stride=0), dict(out_seq_stride=0), dict(out_seq_stride=48)):
+        assert weigh(lib, None, other, **bad) == INVALID, bad
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="calls that are accepted would be launched")
+def test_previous_weights_and_out_beside_one_another(lib):
+    here, other = 7 << 20, 8 << 20
+    assert accepted(weigh(lib, None, here)) and accepted(weigh(lib, here, here)) and accepted(weigh(lib, other, here))
+    assert accepted(weigh(lib, other, here, previous_head_stride=0)) and accepted(weigh(lib, other, here, previous_head_stride=0, previous_seq_stride=0))
+    assert accepted(weigh(lib, here + 4 * 48, here, decay=0.0))  # not read
+    # by turns in one buffer, and strides that lead nowhere
+    assert accepted(weigh(lib, here + 4 * 48, here, previous_seq_stride=192, previous_head_stride=96, out_seq_stride=192, out_head_stride=96))
+    one = dict(batch=1, tokens=1, cache=(8, 16, 1, 64))
+    assert accepted(weigh(lib, here, here, out_seq_stride=0, out_head_stride=0, **one)) and accepted(weigh(lib, None, here, out_seq_stride=0, out_head_stride=0, **one))

@@ -5,6 +5,7 @@ import torch
 
 import paper_2011_09398_b200 as lce
 from gpu_util import DEV
+from test_gpu_kv_attention import Setup
 from test_gpu_kv_evict import Pool
 
 pytestmark = pytest.mark.gpu
@@ -61,3 +62,29 @@ def test_lengths_in_place(sequences, kv_heads, length, budget):
         assert got[1] is carried and all(torch.equal(a, b) for a, b in zip(got, wanted))
         if same:
             assert torch.equal(p.cache, cache)
+
+
+@pytest.mark.parametrize("dtype, lengths, news", [(torch.float32, [100, 60], [1, 1]), (torch.bfloat16, [400, 300], [150, 140])])
+def test_previous_weights_and_out_of_one_buffer(dtype, lengths, news):
+    s = Setup(dtype, lengths, news, 2, 2, 64, seed=3)
+    capacity = s.table.shape[1] * s.page
+    start = torch.rand(2, 2, capacity, device=DEV)
+    call = lambda previous, out, **more: lce.lce_kv_attention_weights(*s.arguments(), previous=previous, out=out, decay=0.5, **more)
+    want = call(start, torch.zeros_like(start))
+    # rows by turns: the sums before and the new ones
+    buffer = torch.zeros(2, 2, 2, capacity + 1, device=DEV)
+    buffer[:, :, 0, :capacity] = start
+    old, new = buffer[:, :, 0], buffer[:, :, 1]
+    before = buffer.clone()
+    for previous, out in ((old, old[:, :, 1:]), (old[:, :, 1:], old), (old, buffer[:, 0]), (old[:, :1].expand(-1, 2, -1), old), (old, buffer.view(-1).as_strided(old.shape, (2 * capacity + 2, capacity + 1, 1)))):
+        with pytest.raises(ValueError, match="previous"):
+            call(previous, out)
+    for out in (torch.zeros(2, 1, capacity, device=DEV).expand(-1, 2, -1), torch.zeros(4 * capacity, device=DEV).as_strided(start.shape, (capacity, capacity - 1, 1))):
+        with pytest.raises(ValueError, match="apart"):
+            call(None, out)
+    assert torch.equal(buffer, before)
+    assert call(old, new) is new and torch.equal(new[:, :, :capacity], want) and torch.equal(old, before[:, :, 0])
+    # one row of sums for all heads, as it is read
+    one = old[:, :1].expand(-1, 2, -1)
+    assert torch.equal(call(one, torch.zeros_like(start)), call(one.contiguous(), torch.zeros_like(start)))
+    assert call(old, old) is old and torch.equal(old[:, :, :capacity], torch.where(want == 0, before[:, :, 0, :capacity], want))
