@@ -399,7 +399,8 @@ lce_status lce_rotary_steps(int32_t rotary_dim, int32_t scaling, double base, do
 /*   q, k        [tokens][q_heads or k_heads][head_dim] of `type`, channels next to one another; strides in elements between tokens and
  *               between heads, not negative.  head_dim 1 .. 256, rotary_dim even, 0 .. head_dim.  k_heads 0: no k
  *   positions   int32[tokens], any sign
- *   q_out, k_out  likewise; q_out may be q with q's strides, k_out k with k's.  Rows of an output must be apart from one another
+ *   q_out, k_out  likewise; q_out may be q with q's strides, k_out k with k's.  Otherwise rows of an output are apart from one another and
+ *               from all other rows (LCE_ERR_INVALID_ARG)
  * Angles are exact to 2^-32 of a turn, sines and cosines to 2^-23, products and sums fp32, rounded to `type` once.  tokens == 0 is a no-op. */
 typedef struct {
     int32_t head_dim, rotary_dim;

@@ -412,7 +412,8 @@ def lce_rotary_steps(rotary_dim: int, base: float = 10000.0, scaling: int = ROTA
 def lce_rotary(desc: RotaryDesc, q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, steps: torch.Tensor,
                q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
     """Turns q [tokens, heads, head_dim] and k [tokens, kv heads, head_dim] (fp32, fp16 or bf16; views with strides are fine; k may be
-    None) by their positions (int32 [tokens]) and steps (lce_rotary_steps on the device).  q_out may be q, k_out k."""
+    None) by their positions (int32 [tokens]) and steps (lce_rotary_steps on the device).  q_out may be q, k_out k; other memory of the
+    inputs, or of one another, is refused."""
     return _native.rotary(desc, q, k, positions, steps, q_out, k_out)
 
 

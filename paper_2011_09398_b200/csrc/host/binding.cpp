@@ -546,7 +546,7 @@ PyObject *rotary(PyObject *const *a)
         const at::Tensor &t = a[5 + i] == Py_None ? made[i] : tensor(a[5 + i], names[i]);
         out[i] = rows(t, heads, d.head_dim, names[i]);
         if (out[i].tokens != d.tokens || t.scalar_type() != tq.scalar_type()) value_error(std::string(names[i]) + " must be like what it is made from");
-        if (out[i].data == in[i].data && d.tokens > 1 && (out[i].token_stride != in[i].token_stride || (heads > 1 && out[i].head_stride != in[i].head_stride)))
+        if (out[i].data == in[i].data && d.tokens > 0 && ((d.tokens > 1 && out[i].token_stride != in[i].token_stride) || (heads > 1 && out[i].head_stride != in[i].head_stride)))
             value_error(std::string(names[i]) + " in place must have the strides of what it is made from");
     }
     d.q_token_stride = in[0].token_stride; d.q_head_stride = in[0].head_stride;

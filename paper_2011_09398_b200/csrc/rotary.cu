@@ -8,6 +8,7 @@
 // Measured: 16384 tokens of 32 and 8 heads of 128 channels in bf16 (336 MB) 55 us, 6.1 TB/s; 1777 tokens of 20 and 5 heads of 80 in fp32, 32
 // channels turned (28 MB), 6.5 us; one token 5 us, launch and call.
 #include "kv_common.cuh"
+#include "row_overlap.cuh"
 
 #include <math.h>
 
@@ -255,6 +256,17 @@ extern "C" lce_status lce_rotary(const lce_rotary_desc *desc, const void *q, con
     const size_t size = type_size(d.type);
     if (!aligned(q, size) || !aligned(q_out, size) || !aligned(positions, 4) || !aligned(steps, 8)) return LCE_ERR_ALIGNMENT;
     if (d.k_heads > 0 && (!aligned(k, size) || !aligned(k_out, size))) return LCE_ERR_ALIGNMENT;
+    // Threads read some heads and write them while others are at other heads: in place, but over no other row that is read or written.
+    const auto row_set = [&](const void *data, int32_t heads, int64_t token_stride, int64_t head_stride) {
+        return RowSet{data, d.tokens, heads, token_stride, head_stride, d.head_dim, (int64_t)size};
+    };
+    const RowSet in[2] = {row_set(q, d.q_heads, d.q_token_stride, d.q_head_stride), row_set(k, d.k_heads, d.k_token_stride, d.k_head_stride)};
+    const RowSet out[2] = {row_set(q_out, d.q_heads, d.q_out_token_stride, d.q_out_head_stride), row_set(k_out, d.k_heads, d.k_out_token_stride, d.k_out_head_stride)};
+    for (int i = 0; i < 2; ++i) {
+        const bool in_place = in[i].data == out[i].data && (d.tokens == 1 || in[i].outer_stride == out[i].outer_stride) && (in[i].inner <= 1 || in[i].inner_stride == out[i].inner_stride);
+        if (!rows_apart(out[i]) || (!in_place && rows_meet(in[i], out[i])) || rows_meet(in[1 - i], out[i])) return LCE_ERR_INVALID_ARG;
+    }
+    if (rows_meet(out[0], out[1])) return LCE_ERR_INVALID_ARG;
     p.tokens = d.tokens;
     p.items = d.tokens * p.units;
     p.dim = d.head_dim; p.rotary_dim = d.rotary_dim; p.q_heads = d.q_heads; p.heads = d.q_heads + d.k_heads;

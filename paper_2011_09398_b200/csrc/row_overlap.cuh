@@ -23,7 +23,7 @@ inline int64_t floor_div(int64_t a, int64_t b) { return a / b - (a % b != 0 && (
 inline bool some_between(int64_t at, int64_t stride, int64_t from, int64_t to, int64_t below, int64_t above)
 {
     if (from > to) return false;
-    if (stride == 0) return -below < at && at < above;
+    if (stride == 0 || (from == 0 && to == 0)) return -below < at && at < above;
     const int64_t lowest = floor_div(-below - at, stride) + 1, highest = -floor_div(at - above, stride) - 1;
     return std::max(lowest, from) <= std::min(highest, to);
 }
@@ -61,6 +61,8 @@ inline bool rows_meet(RowSet a, RowSet b)
     if (!inner_alike && inner_pairs == most) a.inner = b.inner = 1;
     const int64_t apart = (int64_t)(reinterpret_cast<uintptr_t>(b.data) - reinterpret_cast<uintptr_t>(a.data)), a_length = a.length * a.size, b_length = b.length * b.size;
     const int64_t a_outer = a.outer_stride * a.size, b_outer = b.outer_stride * b.size, a_inner = a.inner_stride * a.size, b_inner = b.inner_stride * b.size;
+    // all inner rows of one outer row as one long one: views side by side in the rows of one buffer are told apart by this
+    if (outer_alike && !some_between(apart, b_outer, -(a.outer - 1), b.outer - 1, (b.inner - 1) * b_inner + b_length, (a.inner - 1) * a_inner + a_length)) return false;
     const auto meet = [&](int64_t at) {
         if (outer_alike) return some_between(at, b_outer, -(a.outer - 1), b.outer - 1, b_length, a_length);
         for (int64_t i = 0; i < a.outer; ++i)

@@ -7,7 +7,7 @@ import torch
 
 import paper_2011_09398_b200 as lce
 from paper_2011_09398_b200 import build as lce_build
-from test_bounded_cache_abi import INVALID, evict_desc, weights_desc
+from test_bounded_cache_abi import INVALID, evict_desc, rotary_desc, weights_desc
 
 at = ctypes.c_void_p  # places that are never touched: there is no GPU, or the call is refused first
 
@@ -92,3 +92,37 @@ def test_previous_weights_and_out_beside_one_another(lib):
     assert accepted(weigh(lib, here + 4 * 48, here, previous_seq_stride=192, previous_head_stride=96, out_seq_stride=192, out_head_stride=96))
     one = dict(batch=1, tokens=1, cache=(8, 16, 1, 64))
     assert accepted(weigh(lib, here, here, out_seq_stride=0, out_head_stride=0, **one)) and accepted(weigh(lib, None, here, out_seq_stride=0, out_head_stride=0, **one))
+
+
+def turn(lib, q, k, q_out, k_out, **change):
+    d = rotary_desc(**change)
+    return lib.lce_rotary(ctypes.byref(d), at(q), at(k) if k else None, at(1 << 20), at(2 << 20), at(q_out), at(k_out) if k_out else None, None)
+
+
+# queries and keys beside one another in rows of one buffer, as a projection writes them: 4 and 2 heads of 64, 3 tokens
+SIDE_BY_SIDE = dict(q_token_stride=384, k_token_stride=384, q_out_token_stride=384, k_out_token_stride=384)
+BUFFER, SIZE = 7 << 20, 4 * 384 * 3
+
+
+def test_rotary_over_other_rows(lib):
+    q, k, other = BUFFER, BUFFER + 4 * 256, BUFFER + SIZE
+    for q_out, k_out in ((k, k), (q, q), (k, q), (q + 4 * 64, k), (q, k - 4 * 64), (other, other), (other, other + 4 * 255), (q, k + 4 * 384), (q + 32, k), (other, q)):
+        assert turn(lib, q, k, q_out, k_out, **SIDE_BY_SIDE) == INVALID, (q_out, k_out)
+    # in place, but with other strides
+    for bad in (dict(q_out_token_stride=256), dict(q_out_head_stride=128), dict(k_out_token_stride=768)):
+        assert turn(lib, q, k, q, k, **{**SIDE_BY_SIDE, **bad}) == INVALID, bad
+    assert turn(lib, q, None, q, None, tokens=1, k_heads=0, q_out_head_stride=65) == INVALID
+    # rows of an output that meet
+    for bad in (dict(q_out_head_stride=0), dict(q_out_head_stride=63), dict(q_out_token_stride=0), dict(k_out_token_stride=64), dict(k_out_head_stride=0)):
+        assert turn(lib, q, k, other, other + SIZE, **{**SIDE_BY_SIDE, **bad}) == INVALID, bad
+    assert turn(lib, q, k, q, k, **{**SIDE_BY_SIDE, "k_head_stride": 0, "k_out_head_stride": 0}) == INVALID  # one row of k for all heads, in place
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="calls that are accepted would be launched")
+def test_rotary_beside_other_rows(lib):
+    q, k, other = BUFFER, BUFFER + 4 * 256, BUFFER + SIZE
+    for q_out, k_out in ((q, k), (other, k), (q, other), (other, other + 4 * 256), (other + 4 * 128, other)):
+        assert accepted(turn(lib, q, k, q_out, k_out, **SIDE_BY_SIDE)), (q_out, k_out)
+    assert accepted(turn(lib, q, None, q, None, k_heads=0)) and accepted(turn(lib, q, None, q, None, tokens=1, k_heads=0, q_out_token_stride=7))
+    assert accepted(turn(lib, q, k, other, other + SIZE, q_token_stride=0, q_head_stride=0, k_head_stride=0))  # one row read again and again
+    assert accepted(turn(lib, q, k, other, other + SIZE, q_out_token_stride=64, q_out_head_stride=192, k_out_token_stride=64, k_out_head_stride=192))  # heads in front of tokens

@@ -88,3 +88,24 @@ def test_previous_weights_and_out_of_one_buffer(dtype, lengths, news):
     one = old[:, :1].expand(-1, 2, -1)
     assert torch.equal(call(one, torch.zeros_like(start)), call(one.contiguous(), torch.zeros_like(start)))
     assert call(old, old) is old and torch.equal(old[:, :, :capacity], torch.where(want == 0, before[:, :, 0, :capacity], want))
+
+
+@pytest.mark.parametrize("tokens", [1, 5])
+def test_rotary_over_other_rows(tokens):
+    wide = torch.rand(tokens, 8 * 64, device=DEV)
+    before = wide.clone()
+    view = lambda first, heads: wide.as_strided((tokens, heads, 64), (8 * 64, 64, 1), 64 * first)
+    q, k = view(0, 4), view(4, 2)
+    desc, positions, steps = lce.make_rotary_desc(64), torch.arange(tokens, dtype=torch.int32, device=DEV) + 3, lce.lce_rotary_steps(64).to(DEV)
+    call = lambda **outs: lce.lce_rotary(desc, q, k, positions, steps, **outs)
+    for outs in (dict(q_out=view(2, 4)), dict(q_out=view(4, 4)), dict(k_out=view(0, 2)), dict(q_out=q, k_out=view(3, 2)), dict(q_out=torch.empty(tokens, 1, 64, device=DEV).expand(-1, 4, -1))):
+        with pytest.raises(lce.LceError) as e:
+            call(**outs)
+        assert e.value.status == 1
+    with pytest.raises(ValueError, match="strides"):
+        call(q_out=wide.as_strided((tokens, 4, 64), (8 * 64, 128, 1)))
+    assert torch.equal(wide, before)
+    want = call()
+    # keys to where the values were, queries in place
+    got = call(q_out=q, k_out=view(6, 2))
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and torch.equal(k, before.as_strided(k.shape, k.stride(), 64 * 4))
