@@ -426,9 +426,13 @@ lce_status lce_rotary(const lce_rotary_desc *desc, const void *q, const void *k,
  *   out         fp32 [batch][kv_heads][table_pages * page_size], strides in elements between sequences and between heads, rows apart from
  *               one another (LCE_ERR_INVALID_ARG where two begin at one place); nothing behind a sequence's last token changes
  *   workspace   lce_kv_attention_weights_workspace_bytes(desc) bytes, 16-byte aligned, no clearing, the call's until its kernels are done
- * The other arguments as for lce_kv_attention; tables are below 2^30 tokens.  Everything is fp32: 16-bit rows of q meet the cache's keys without a rounding (of
- * channels below 2^-24 of the largest of the rows worked on together, 128 columns at most, a part is lost), fp32 rows are taken in 22 bits.  No sum depends on the order in which blocks run:
- * results repeat bit for bit. */
+ * The other arguments as for lce_kv_attention; tables are below 2^30 tokens.  Scores, powers and sums are fp32.  16-bit rows of q meet the cache's
+ * keys without a rounding, fp32 rows are taken in 22 bits.  Many 16-bit rows of up to 128 channels are worked on by 128 columns (a row of q is one for
+ * each query head of the key/value head) and 128 tokens: there a part is lost of q's channels below 2^-24 of the largest of the columns, and of
+ * keys whose scale is below 2^-28 of the largest of the tokens, a channel at most 2^-32 of that largest scale.  No sum depends on the
+ * order in which blocks run: results repeat bit for bit.
+ * A window counts places of the cache.  Once lce_kv_evict has moved a sequence's tokens they are no longer positions, and the heads' tokens at a
+ * place differ: a window then means the newest places of each head, here and in lce_kv_attention. */
 typedef struct {
     lce_kv_desc cache;
     int32_t batch, heads, table_pages;

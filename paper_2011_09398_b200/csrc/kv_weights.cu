@@ -550,8 +550,9 @@ lce_status make_params(const lce_kv_attention_weights_desc *d, WeightsParams *p,
     p->previous_seq = d->previous_seq_stride; p->previous_head = d->previous_head_stride;
     p->out_seq = d->out_seq_stride; p->out_head = d->out_head_stride;
     *nt = p->g.blocks <= kWideBlocks && (d->tokens * p->group + d->batch - 1) / d->batch > 8 ? 2 : 1;
-    // Many rows go to the kernels of kv_weights_prompt.cu where they are estimated to be ahead (us for 128 channels, bf16, by tokens times key heads; by
-    // the longest the sequences can be: their lengths are not known here).  One sequence of 512 / 4096 / 32768 tokens, 8 key heads: 20 columns
+    // Many rows go to the kernels of kv_weights_prompt.cu where they are estimated to be ahead (us, by tokens times key heads; by the longest the
+    // sequences can be: their lengths are not known here).  Measured with 128 channels in bf16 and used for fewer, too: those kernels' time hardly depends on
+    // the channels (two chunks of 1024 rows on 5120 tokens: 32 channels 268 us, 64 279, 96 283, 128 291), that of the others falls with them.  One sequence of 512 / 4096 / 32768 tokens, 8 key heads: 20 columns
     // 16.2 / 28.3 / 46.1 here and 24.6 / 27.4 / 81.4 there, 64 columns 35.2 / 61.3 / 99.2 and 24.4 / 27.8 / 81.3; 16 sequences of 512 / 4096: 32 columns 38.0 / 86.1
     // and 38.6 / 132, 128 columns 132 / 415 and 37.1 / 106.
     const double each = (double)p->tokens * p->group / p->batch, read = (double)p->batch * p->g.heads * p->table_tokens;
