@@ -279,6 +279,9 @@ def prepare(case, seed):
         s["desc"] = lce.make_kv_desc(s["pages"], case["page"], case["kv_heads"], case["dim"])
         s["cache"] = torch.zeros(lce.lce_kv_cache_bytes(s["desc"]), dtype=torch.uint8, device=DEVICE)
         lce.lce_kv_quantize(s["desc"], s["k"], s["v"], s["slots"], s["cache"])
+        if case["kind"] == "evict":  # the call wants a table as wide as the budget, also where no sequence has that many tokens
+            missing = -(-case["budget"] // case["page"]) - s["kept_table"].shape[1]
+            s["kept_table"] = torch.nn.functional.pad(s["kept_table"], (0, max(missing, 0)), value=-1)
     else:
         rows, blocks = s["pages"] * case["page"], (case["dim"] + BLOCK - 1) // BLOCK
         s["cache"] = {name: (torch.zeros(rows, case["kv_heads"], blocks * BLOCK // 2, dtype=torch.uint8, device=DEVICE),
