@@ -18,7 +18,7 @@
 //   warp 26             has the keys' words copied from the cache (loads of the warps that decode them do not stay in flight over the fence in
 //                       front of the products: 143 instead of 125 us for the first kernel)
 //
-// Two sequences of 1024 rows of 4 columns on 5120 tokens, 8 key heads of 128 channels: 275 us, 125 and 135 of them in the two kernels.  Products (1024
+// Two sequences of 1024 rows of 4 columns on 5120 tokens, 8 key heads of 128 channels: 278 us, 125 and 135 of them in the two kernels.  Products (1024
 // clocks for a step of 256 x 128 at the tensor cores' rate) and powers of two (2048 at 16 a clock) would allow 70 each; a step takes 3500.  Taken out one by
 // one, the powers of two are 15 % of it, the products 5 %, reading TMEM 25 %: what is left is the way through shared memory that the warps hand each
 // other a tile on.  More tiles streaming (four instead of two), one arrival a warp at the barriers, 128-byte swizzled operands and eight warps with twice

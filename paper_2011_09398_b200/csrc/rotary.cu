@@ -5,7 +5,7 @@
 // vectors, of either half of the head or next to one another.  An angle is the product of position and step in 64 bits, whose upper half is
 // a part of a turn: no reduction, and nothing is lost far out.
 //
-// Measured: 16384 tokens of 32 and 8 heads of 128 channels in bf16 (336 MB) 55 us, 6.1 TB/s; 1777 tokens of 20 and 5 heads of 80 in fp32, 32
+// Measured: 16384 tokens of 32 and 8 heads of 128 channels in bf16 (336 MB) 56 us, 6.0 TB/s; 1777 tokens of 20 and 5 heads of 80 in fp32, 32
 // channels turned (28 MB), 6.5 us; one token 5 us, launch and call.
 #include "kv_common.cuh"
 #include "row_overlap.cuh"
